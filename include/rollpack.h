@@ -546,6 +546,110 @@ rp_status rp_step_trace_enable(rp_engine* eng, int32_t cap);
  * capacity are not recorded). */
 rp_status rp_step_trace_read(rp_engine* eng, rp_step_record* out, int32_t cap, int32_t* n_out);
 
+/* ---- A KV cache held in 4 bits -------------------------------------------------
+ *
+ * The KV cache is the memory that long responses fill (section 4.2), and reading
+ * it is what bounds decode attention (section 2.2).  These calls keep it in 4.25
+ * bits per element: K and V of a token and KV head in blocks of 32 consecutive
+ * dimensions, each one scale, a power of two, and 32 codes of four bits, a sign and
+ * one of 0, 0.5, 1, 1.5, 2, 3, 4, 6.  The scale s is the least power of two with
+ * amax <= 7 s (2^-125 <= s <= 2^125), a code the nearest value (ties to the even
+ * mantissa, at most 6 s).  A block that holds an infinity or a NaN reads as NaN.
+ *
+ * The calls need no engine.  They launch kernels on hip_stream and return; they
+ * allocate nothing, never wait, and can be captured into a graph, whose replays
+ * read the contexts, offsets and page ids that the batch's arrays then hold.  Host
+ * structures are read only during the call.  The current device must be the one
+ * that the buffers (and the stream, when not NULL) belong to. */
+
+/* The cache of one layer: caller-owned device memory of rp_kvq_cache_bytes bytes,
+ * 256-byte aligned.  It need not be cleared: only positions below a sequence's
+ * context are used.  Pages hold 64 tokens; the bytes of a page have an order of their own
+ * (rp_kvq_append writes them, rp_kvq_read gives values back). */
+typedef struct rp_kvq_cache {
+  void* blocks;
+  int64_t n_pages;      /* 1 .. 2^24 */
+  int32_t n_kv_heads;   /* 1 .. 1024 */
+  int32_t head_dim;     /* 64 or 128 */
+} rp_kvq_cache;
+
+/* Which rows (tokens) of a call belong to which sequence.  The arrays are device
+ * memory, read when the kernels run.
+ *   n_seqs         sequences, 0 .. 2^20
+ *   n_rows         rows of the call's tensors, 0 .. 2^24; rows behind the last
+ *                  sequence's are neither read nor written (a padded batch)
+ *   row_offsets    [n_seqs + 1] ascending: sequence b has rows [off[b], off[b+1]);
+ *                  NULL: sequence b has row b (a decode step)
+ *   contexts       [n_seqs] tokens of sequence b, its rows of this call among them:
+ *                  they are the last ones, row i of n at position context - n + i
+ *   page_table     [n_seqs] rows of table_stride entries: the page of positions
+ *                  64 p .. 64 p + 63.  Entries past a sequence's context are not read
+ *   max_rows       most rows of any sequence (without row_offsets not used)
+ *   max_context    largest context; at most 64 * table_stride
+ * A sequence with a context below 0 or above max_context, with more than max_rows rows
+ * or with a page id outside the cache is not followed there: nothing is appended for such a
+ * row, and reading or attending gives it NaN (rows past max_rows are left alone).
+ * Positions below 0 (more rows than tokens) hold no key: such rows are not appended and
+ * give zeros. */
+typedef struct rp_kvq_batch {
+  int32_t n_seqs;
+  int32_t n_rows;
+  int32_t max_rows;
+  int32_t max_context;
+  const int32_t* row_offsets;
+  const int32_t* contexts;
+  const int32_t* page_table;
+  int64_t table_stride;
+} rp_kvq_batch;
+
+/* A device tensor [n_rows, heads, head_dim] of dtype (rp_dtype) F32 or BF16; strides
+ * in elements, the head_dim elements contiguous.  Any alignment of the element type
+ * serves; 16-byte aligned rows and heads are faster.  Rows of a tensor that is written may not
+ * overlap. */
+typedef struct rp_kvq_tensor {
+  void* data;
+  int64_t row_stride;
+  int64_t head_stride;
+  int32_t dtype;
+} rp_kvq_tensor;
+
+/* Bytes of a cache of n_pages pages (the KV footprint of section 4.4, in pages). */
+rp_status rp_kvq_cache_bytes(int64_t n_pages, int32_t n_kv_heads, int32_t head_dim, size_t* bytes);
+
+/* Quantise the batch's K and V rows into the cache at their positions: what the
+ * memory-bound decode steps of section 2.2 then read.  k and v are [n_rows,
+ * n_kv_heads, head_dim] of one dtype.  No two sequences may have the same page where rows are
+ * written (each byte would hold either's).  Errors: RP_ERR_INVALID_ARG, RP_ERR_HIP. */
+rp_status rp_kvq_append(const rp_kvq_cache* cache, const rp_kvq_batch* batch, const rp_kvq_tensor* k,
+                        const rp_kvq_tensor* v, void* hip_stream);
+
+/* The values that the cache holds of the batch's rows, into k and v (as
+ * rp_kvq_append; fp32 and bf16 both hold every value exactly): what a request takes along
+ * when it moves to another replica (the migration of section 5 recomputes it instead). */
+rp_status rp_kvq_read(const rp_kvq_cache* cache, const rp_kvq_batch* batch, const rp_kvq_tensor* k,
+                      const rp_kvq_tensor* v, void* hip_stream);
+
+/* Bytes of the workspace of rp_kvq_attend for this batch's n_seqs, n_rows, max_rows, max_context and
+ * whether it has row_offsets (section 2.2's split of few long contexts over the whole GPU leaves
+ * partial results there).  Its arrays are not read. */
+rp_status rp_kvq_attend_workspace(const rp_kvq_cache* cache, const rp_kvq_batch* batch, int32_t n_q_heads,
+                                  size_t* bytes);
+
+/* Causal attention of the batch's rows over their sequences' cached keys, the
+ * attention of a decode step (one row per sequence, section 2.2) or of a prefill
+ * (section 2.1): for row r of a sequence, at position p, and query head h
+ *   out[r, h] = sum_t softmax_t(scale q[r, h] . k[t, h / G]) v[t, h / G],  t = 0 .. p,
+ * G = n_q_heads / n_kv_heads.  The rows' own keys must be in the cache (rp_kvq_append
+ * before this call on the same stream).  Scores, softmax and sums are fp32.
+ *   n_q_heads  a multiple of n_kv_heads
+ *   scale      positive and finite (1 / sqrt(head_dim))
+ *   q, out     [n_rows, n_q_heads, head_dim] of one dtype; out may not overlap q
+ *   workspace  device, 256-byte aligned, of rp_kvq_attend_workspace bytes (NULL when that is 0);
+ *              not shared by calls that may run at the same time */
+rp_status rp_kvq_attend(const rp_kvq_cache* cache, const rp_kvq_batch* batch, int32_t n_q_heads, float scale,
+                        const rp_kvq_tensor* q, const rp_kvq_tensor* out, void* workspace, size_t workspace_bytes,
+                        void* hip_stream);
+
 /* Message of the last failed call on this thread ("" if none). */
 const char* rp_last_error(void);
 

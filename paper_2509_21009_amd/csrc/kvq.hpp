@@ -1,0 +1,198 @@
+// The KV cache held in 4 bits: its format, the batch that its calls take, and the plan that cuts attention
+// into work items.  Host code and device code share what is here.
+//
+// Format.  The hd dimensions of one token and KV head are cut into blocks of 32.  A block is one scale
+// byte b, the power of two s = 2^(b - 127), and 32 codes of four bits, the sign over an index into
+// 0, 0.5, 1, 1.5, 2, 3, 4, 6 (e2m1): the value is s times the code's.  These are the operands of gfx950's
+// v_cvt_scalef32_pk_bf16_fp4, which turns two codes and a scale into two bf16 in one instruction; bf16 holds
+// every such value exactly.  4.25 bits per element: a token takes 17/64 of its bf16 size.
+//   s is the least power of two with amax <= 7 s: up to 7 s the code 6 is at most s off, which is also the half
+//   step of the codes below it, so a larger scale would lose more in the small elements than it gains in the largest.
+//   2^-125 <= s <= 2^125 keeps every value a normal bf16 number (or zero); amax above 7 * 2^125 saturates at 6 * 2^125.
+//   A block that holds an infinity or a NaN gets b = 255 and reads as NaN.
+//   A code is the nearest one, ties to the one with the even mantissa (v_cvt_scalef32_pk_fp4_f32's rounding).
+//
+// Layout.  Pages of 64 tokens, [page][KV head]: one block of 68 hd bytes
+//   K codes [64 tokens x hd], V codes [64 tokens x hd], K scales [2 hd], V scales [2 hd]
+// in the order in which the lanes of a wave hold them as operands of v_mfma_f32_16x16x32_bf16 (lane 16g + c), so that
+// every load of a page is 16 bytes per lane and 1 KB per instruction without a gap:
+//   K: MFMA row c of tile u is token 16u + c, and lane group g has dimensions hd/4 g .. hd/4 (g + 1) of it, for head
+//      dimension 128 one scale block.  K scales: byte u of the lane's word is tile u's.
+//   V: MFMA row c has dimensions hd/16 c .. hd/16 (c + 1) (one tile for each), and lane group g has tokens
+//      16u + 4g .. 16u + 4g + 3 of tile u: those whose scores the lane gets from the K product, so that the
+//      probabilities are the other operand without an exchange.  V scales: byte r of word u is token 16u + 4g + r's.
+// A token's bytes are its own, so that appending never reads.
+#pragma once
+
+#include <cstddef>
+#include <cstdint>
+
+#ifndef __HIPCC__
+#define RP_HD inline
+#else
+#include <hip/hip_runtime.h>
+#define RP_HD __host__ __device__ __forceinline__
+#endif
+
+namespace rollpack {
+
+constexpr int kKvqPage = 64;    // tokens of a page
+constexpr int kKvqBlock = 32;   // dimensions that share a scale
+
+RP_HD size_t kvq_block_bytes(int hd) { return static_cast<size_t>(68) * hd; }  // of one (page, KV head)
+
+// Byte offsets in a (page, head) block.  Codes: of the byte that holds dimension d of token t, low half first.
+RP_HD int kvq_k_code(int t, int d, int hd) {
+  const int u = t >> 4, c = t & 15, g = d / (hd / 4), e = d % (hd / 4);
+  return hd == 128 ? u * 1024 + (g * 16 + c) * 16 + e / 2 : (u >> 1) * 1024 + (g * 16 + c) * 16 + (u & 1) * 8 + e / 2;
+}
+RP_HD int kvq_v_code(int t, int d, int hd) {
+  const int u = t >> 4, g = (t >> 2) & 3, r = t & 3, c = d / (hd / 16), e = d % (hd / 16);
+  return 32 * hd + (hd == 128 ? u * 1024 + (g * 16 + c) * 16 + r * 4 + e / 2
+                              : (u >> 1) * 1024 + (g * 16 + c) * 16 + ((u & 1) * 4 + r) * 2 + e / 2);
+}
+// Scales: of block i (dimensions 32i .. 32i + 31) of token t.
+RP_HD int kvq_k_scale(int t, int i, int hd) { return 64 * hd + (i * 16 + (t & 15)) * 4 + (t >> 4); }
+RP_HD int kvq_v_scale(int t, int i, int hd) {
+  return 66 * hd + (i * 4 + ((t >> 2) & 3)) * 16 + (t >> 4) * 4 + (t & 3);
+}
+
+// The scale byte of a block whose largest magnitude has these fp32 bits (sign clear).
+RP_HD uint32_t kvq_scale_byte(uint32_t amax_bits) {
+  if (amax_bits >= 0x7f800000u) return 255;
+  // amax = m 2^e, 1 <= m < 2: the scale's exponent is e - 2 for m <= 1.75 and e - 1 above; the carry tells them apart
+  const int b = static_cast<int>((amax_bits + 0x1fffffu) >> 23) - 2;
+  return static_cast<uint32_t>(b < 2 ? 2 : b > 252 ? 252 : b);
+}
+
+// Which rows of a call belong to which sequence; pointers are device memory.
+struct KvqBatch {
+  int n_seqs = 0, n_rows = 0, max_rows = 1, max_context = 0;
+  const int32_t* row_off = nullptr;    // [n_seqs + 1], or null: sequence b is row b
+  const int32_t* context = nullptr;    // [n_seqs] with the call's rows
+  const int32_t* page_table = nullptr; int64_t table_stride = 0;
+  const int32_t* table_row = nullptr;  // [n_seqs] the sequence's row of the page table, or null: b
+};
+
+struct KvqCache {
+  char* blocks = nullptr;
+  int n_pages = 0, n_kv = 0, hd = 0;
+};
+
+// A strided [rows, heads, hd] tensor, hd contiguous; strides in elements.
+struct KvqTensor {
+  void* p = nullptr;
+  int64_t row_stride = 0, head_stride = 0;
+  int bf16 = 1;
+  int vec = 0;  // pointer and strides allow accesses of 16 bytes (set by kvq_vec)
+};
+inline int kvq_vec(const KvqTensor& t) {
+  const int64_t per = t.bf16 ? 8 : 4;
+  return reinterpret_cast<uintptr_t>(t.p) % 16 == 0 && t.row_stride % per == 0 && t.head_stride % per == 0;
+}
+
+RP_HD bool kvq_page_ok(const KvqCache& c, int id) { return id >= 0 && id < c.n_pages; }
+
+// A sequence of the batch: its rows of the call (max_rows at most), its context, and whether both are within the call's
+// bounds.  Offsets outside the call's rows are taken as its ends, so that no row outside them is touched.
+struct KvqSeq {
+  int r0, n, ctx;
+  bool ok;
+};
+RP_HD int kvq_clamp(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
+RP_HD int kvq_max_rows(const KvqBatch& bt) { return bt.row_off ? bt.max_rows : 1; }
+RP_HD KvqSeq kvq_seq(const KvqBatch& bt, int b) {
+  KvqSeq s;
+  if (bt.row_off) {
+    s.r0 = kvq_clamp(bt.row_off[b], 0, bt.n_rows);
+    s.n = kvq_clamp(bt.row_off[b + 1], s.r0, bt.n_rows) - s.r0;
+  } else {
+    s.r0 = b < bt.n_rows ? b : bt.n_rows;
+    s.n = b < bt.n_rows ? 1 : 0;
+  }
+  s.ctx = bt.context[b];
+  s.ok = s.ctx >= 0 && s.ctx <= bt.max_context && s.n <= kvq_max_rows(bt);
+  if (s.n > kvq_max_rows(bt)) s.n = kvq_max_rows(bt);
+  return s;
+}
+
+// ---- the plan of attention -----------------------------------------------------------
+//
+// Work is counted in tiles: `cols` consecutive columns of a sequence and KV head, a column being one query
+// head of one row.  A tile's pages are cut into items of `ppi` pages, which blocks take; more than one item per tile
+// leaves partial outputs, which a second kernel joins.  Contexts are in device memory, so every block computes the plan
+// from them by itself (the lanes of a wave price 64 sizes at once), and a captured graph follows the contexts
+// that it finds at its replay.
+
+constexpr int kKvqTileItems = 64;  // items of one tile at most: the join holds one per lane
+// Items beyond one per tile, for all KV heads together: bounds the workspace.  ppi >= pages / this keeps to it.
+constexpr int kKvqExtraItems = 2048;
+
+struct KvqPlanInput {
+  int64_t tile_pages = 0;  // sum over tiles of their pages, one KV head
+  int tiles = 0;           // of one KV head
+  int max_pages = 0;       // of any tile
+};
+
+// Price of items of ppi pages, in us.  A block's waves take a page in page_us between them, and its ends (plan, first
+// loads, combining its waves) take ends_us; joining is a second launch.
+RP_HD float kvq_price(const KvqPlanInput& in, int n_kv, int ppi, float page_us, float ends_us, float join_us) {
+  const bool join = ppi < in.max_pages;
+  const float pages = static_cast<float>(in.tile_pages);
+  const float items = (join ? pages / ppi + 0.5f * in.tiles : static_cast<float>(in.tiles)) * n_kv;
+  const float one = (ppi < in.max_pages ? ppi : in.max_pages) * page_us + ends_us;
+  const float all = (pages * n_kv * page_us + items * ends_us) * (1.f / 256.f);
+  const float even = all + 0.5f * one;  // past a block per CU the CUs even out to half an item
+  return (items <= 256.f ? one : (one > even ? one : even)) + (join ? join_us : 0.f);
+}
+
+// The least size allowed, and candidate i of 64 (a geometric ladder from there to whole tiles).
+RP_HD int kvq_least_ppi(const KvqPlanInput& in, int n_kv) {
+  const int64_t extra = kKvqExtraItems / n_kv > 1 ? kKvqExtraItems / n_kv : 1;
+  const int64_t a = (in.tile_pages + extra - 1) / extra, b = (in.max_pages + kKvqTileItems - 1) / kKvqTileItems;
+  const int64_t l = a > b ? a : b;
+  return l < 1 ? 1 : l > in.max_pages ? (in.max_pages > 1 ? in.max_pages : 1) : static_cast<int>(l);
+}
+
+// Pages of the keys that a sequence's rows see, its tiles, and the items of one tile.
+RP_HD int kvq_pages(const KvqSeq& s) { return s.ok ? (s.ctx + kKvqPage - 1) / kKvqPage : 0; }
+RP_HD int kvq_tiles(const KvqSeq& s, int group, int cols) { return (s.n * group + cols - 1) / cols; }
+RP_HD int kvq_items(int pages, int ppi) { return pages <= ppi ? 1 : (pages + ppi - 1) / ppi; }
+
+struct KvqAttendArgs {
+  KvqCache cache;
+  KvqBatch batch;
+  KvqTensor q, out;
+  int n_q = 0;
+  float scale = 1.f;
+  // workspace: per item and KV head [tile_cols, hd] partial outputs, [2, tile_cols] maxima and sums
+  int64_t items = 0;  // that it holds, and that are launched
+  float* part_o = nullptr;
+  float* part_ml = nullptr;
+};
+
+// Tiles that a batch has at most (of one KV head), for tiles of `cols` columns.
+inline int64_t kvq_tile_bound(const KvqBatch& b, int group, int cols) {
+  const int64_t rows = b.row_off ? b.n_rows : (b.n_rows < b.n_seqs ? b.n_rows : b.n_seqs);
+  const int64_t per_seq = (static_cast<int64_t>(kvq_max_rows(b)) * group + cols - 1) / cols;
+  const int64_t by_rows = rows * group / cols + b.n_seqs, by_seqs = per_seq * b.n_seqs;
+  return by_rows < by_seqs ? by_rows : by_seqs;
+}
+inline int64_t kvq_item_bound(const KvqBatch& b, int n_kv, int group, int cols) {
+  const int64_t tiles = kvq_tile_bound(b, group, cols);
+  const int64_t pages = (static_cast<int64_t>(b.max_context) + kKvqPage - 1) / kKvqPage;
+  const int64_t extra = kKvqExtraItems / n_kv > 1 ? kKvqExtraItems / n_kv : 1;
+  const int64_t most = tiles * (pages > 1 ? pages : 1);
+  return tiles + extra < most ? tiles + extra : most;
+}
+// Bytes of the workspace of launch_kvq_attend.
+size_t kvq_attend_bytes(const KvqCache& c, const KvqBatch& b, int n_q);
+
+#ifdef __HIPCC__
+hipError_t launch_kvq_append(const KvqCache& c, const KvqBatch& b, const KvqTensor& k, const KvqTensor& v, hipStream_t s);
+hipError_t launch_kvq_read(const KvqCache& c, const KvqBatch& b, const KvqTensor& k, const KvqTensor& v, hipStream_t s);
+// a.part_o and a.part_ml are set from `ws`, of kvq_attend_bytes bytes.
+hipError_t launch_kvq_attend(KvqAttendArgs a, void* ws, hipStream_t s);
+#endif
+
+}  // namespace rollpack

@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "engine.hpp"
+#include "kvq.hpp"
 #include "static_ws.hpp"
 #include "tail_batch.hpp"
 
@@ -91,6 +92,118 @@ int32_t run_one_shot(rollpack::Engine& e, int32_t n, const int64_t* seq_ids, con
     default:
       throw RpError(RP_ERR_INVALID_ARG, "unknown schedule mode");
   }
+}
+
+// ---- the 4-bit cache: arguments to the kernels' form ----------------------------------
+
+void kvq_require(bool ok, const char* what) {
+  if (!ok) throw rollpack::RpError(RP_ERR_INVALID_ARG, std::string("4-bit cache: ") + what);
+}
+
+rollpack::KvqCache kvq_cache(const rp_kvq_cache* c, bool need_memory) {
+  kvq_require(c, "null cache");
+  kvq_require(c->head_dim == 64 || c->head_dim == 128, "head_dim must be 64 or 128");
+  kvq_require(c->n_kv_heads >= 1 && c->n_kv_heads <= 1024, "1 <= n_kv_heads <= 1024");
+  kvq_require(c->n_pages >= 1 && c->n_pages <= (int64_t{1} << 24), "1 <= n_pages <= 2^24");
+  if (need_memory) {
+    kvq_require(c->blocks && reinterpret_cast<uintptr_t>(c->blocks) % 256 == 0, "blocks must be 256-byte aligned device memory");
+  }
+  rollpack::KvqCache k;
+  k.blocks = static_cast<char*>(c->blocks);
+  k.n_pages = static_cast<int>(c->n_pages);
+  k.n_kv = c->n_kv_heads;
+  k.hd = c->head_dim;
+  return k;
+}
+
+rollpack::KvqBatch kvq_batch(const rp_kvq_batch* b, bool need_memory) {
+  kvq_require(b, "null batch");
+  kvq_require(b->n_seqs >= 0 && b->n_seqs <= (1 << 20), "0 <= n_seqs <= 2^20");
+  kvq_require(b->n_rows >= 0 && b->n_rows <= (1 << 24), "0 <= n_rows <= 2^24");
+  kvq_require(!b->row_offsets || (b->max_rows >= 0 && b->max_rows <= b->n_rows), "0 <= max_rows <= n_rows");
+  kvq_require(b->max_context >= 0 && b->max_context <= (1 << 30), "0 <= max_context <= 2^30");
+  kvq_require(b->row_offsets || b->n_rows >= b->n_seqs, "without row_offsets every sequence has a row");
+  if (need_memory && b->n_seqs > 0) {
+    kvq_require(b->contexts, "null contexts");
+    kvq_require(b->page_table, "null page_table");
+    kvq_require(b->table_stride >= 1 && b->table_stride <= (int64_t{1} << 32), "1 <= table_stride <= 2^32");
+    kvq_require(b->max_context <= b->table_stride * rollpack::kKvqPage, "max_context is past the page table's rows");
+  }
+  rollpack::KvqBatch k;
+  k.n_seqs = b->n_seqs;
+  k.n_rows = b->n_rows;
+  k.max_rows = b->max_rows;
+  k.max_context = b->max_context;
+  k.row_off = b->row_offsets;
+  k.context = b->contexts;
+  k.page_table = b->page_table;
+  k.table_stride = b->table_stride;
+  return k;
+}
+
+rollpack::KvqTensor kvq_tensor(const rp_kvq_tensor* t, int64_t rows, int64_t heads, int64_t hd, bool written) {
+  kvq_require(t, "null tensor");
+  kvq_require(t->data, "null tensor data");
+  kvq_require(t->dtype == RP_DTYPE_F32 || t->dtype == RP_DTYPE_BF16, "tensors are F32 or BF16");
+  kvq_require(reinterpret_cast<uintptr_t>(t->data) % (t->dtype == RP_DTYPE_F32 ? 4 : 2) == 0, "misaligned tensor");
+  constexpr int64_t most = int64_t{1} << 38;  // keeps every offset of 2^24 rows within 64 bits
+  kvq_require(t->row_stride >= 0 && t->head_stride >= 0 && t->row_stride <= most && t->head_stride <= most,
+              "strides must be 0 .. 2^38");
+  if (written) {  // one of the two is the outer dimension
+    const bool rows_outer = (heads == 1 || t->head_stride >= hd) && (rows == 1 || t->row_stride >= (heads - 1) * t->head_stride + hd);
+    const bool heads_outer = (rows == 1 || t->row_stride >= hd) && (heads == 1 || t->head_stride >= (rows - 1) * t->row_stride + hd);
+    kvq_require(rows_outer || heads_outer, "rows of a written tensor overlap");
+  }
+  rollpack::KvqTensor k;
+  k.p = t->data;
+  k.row_stride = t->row_stride;
+  k.head_stride = t->head_stride;
+  k.bf16 = t->dtype == RP_DTYPE_BF16;
+  k.vec = rollpack::kvq_vec(k);
+  return k;
+}
+
+hipStream_t kvq_stream(void* hip_stream) {
+  const hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  if (s) {
+    int dev = -1;
+    hipDevice_t sdev = -1;
+    hipError_t e = hipGetDevice(&dev);
+    if (e == hipSuccess) e = hipStreamGetDevice(s, &sdev);
+    if (e != hipSuccess) throw rollpack::RpError(RP_ERR_HIP, std::string("4-bit cache: stream: ") + hipGetErrorString(e));
+    kvq_require(sdev == dev, "the stream belongs to another device than the current one");
+  }
+  return s;
+}
+
+void kvq_launched(hipError_t e, const char* what) {
+  if (e != hipSuccess) throw rollpack::RpError(RP_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
+}
+
+// Append and read: the same arguments.
+template <typename F>
+rp_status kvq_rows_call(const rp_kvq_cache* cache, const rp_kvq_batch* batch, const rp_kvq_tensor* k, const rp_kvq_tensor* v,
+                        bool written, void* hip_stream, F launch) {
+  return guarded([&] {
+    const rollpack::KvqCache c = kvq_cache(cache, true);
+    const rollpack::KvqBatch b = kvq_batch(batch, true);
+    if (b.n_seqs == 0 || b.n_rows == 0) return;
+    const rollpack::KvqTensor kt = kvq_tensor(k, b.n_rows, c.n_kv, c.hd, written);
+    const rollpack::KvqTensor vt = kvq_tensor(v, b.n_rows, c.n_kv, c.hd, written);
+    kvq_require(kt.bf16 == vt.bf16, "k and v must have one dtype");
+    kvq_require(!written || kt.p != vt.p, "k and v are the same memory");
+    launch(c, b, kt, vt, kvq_stream(hip_stream));
+  });
+}
+
+// The batch of an attention call, and the bytes of its workspace.
+size_t kvq_attend_size(const rollpack::KvqCache& c, const rollpack::KvqBatch& b, int32_t n_q) {
+  kvq_require(n_q >= 1 && n_q <= 65536 && n_q % c.n_kv == 0, "n_q_heads must be a multiple of n_kv_heads");
+  const int64_t group = n_q / c.n_kv;
+  kvq_require(static_cast<int64_t>(b.row_off ? b.max_rows : 1) * group < (int64_t{1} << 30) &&
+                  rollpack::kvq_item_bound(b, c.n_kv, static_cast<int>(group), 16) * c.n_kv < (int64_t{1} << 31),
+              "too many rows and heads for one call");
+  return rollpack::kvq_attend_bytes(c, b, n_q);
 }
 
 }  // namespace
@@ -390,6 +503,55 @@ rp_status rp_stream_read_gbs(const void* dev_buf, size_t bytes, int32_t reps, vo
     (void)hipEventDestroy(e1);
     check(err, "stream read");
     *gbs_out = static_cast<double>(bytes / 16 * 16) / (best * 1e-3) / 1e9;
+  });
+}
+
+rp_status rp_kvq_cache_bytes(int64_t n_pages, int32_t n_kv_heads, int32_t head_dim, size_t* bytes) {
+  return guarded([&] {
+    kvq_require(bytes, "null argument");
+    const rp_kvq_cache c{nullptr, n_pages, n_kv_heads, head_dim};
+    kvq_cache(&c, false);
+    *bytes = static_cast<size_t>(n_pages) * n_kv_heads * rollpack::kvq_block_bytes(head_dim);
+  });
+}
+
+rp_status rp_kvq_append(const rp_kvq_cache* cache, const rp_kvq_batch* batch, const rp_kvq_tensor* k,
+                        const rp_kvq_tensor* v, void* hip_stream) {
+  return kvq_rows_call(cache, batch, k, v, false, hip_stream, [](auto&&... a) { kvq_launched(rollpack::launch_kvq_append(a...), "rp_kvq_append"); });
+}
+
+rp_status rp_kvq_read(const rp_kvq_cache* cache, const rp_kvq_batch* batch, const rp_kvq_tensor* k,
+                      const rp_kvq_tensor* v, void* hip_stream) {
+  return kvq_rows_call(cache, batch, k, v, true, hip_stream, [](auto&&... a) { kvq_launched(rollpack::launch_kvq_read(a...), "rp_kvq_read"); });
+}
+
+rp_status rp_kvq_attend_workspace(const rp_kvq_cache* cache, const rp_kvq_batch* batch, int32_t n_q_heads,
+                                  size_t* bytes) {
+  return guarded([&] {
+    kvq_require(bytes, "null argument");
+    *bytes = kvq_attend_size(kvq_cache(cache, false), kvq_batch(batch, false), n_q_heads);
+  });
+}
+
+rp_status rp_kvq_attend(const rp_kvq_cache* cache, const rp_kvq_batch* batch, int32_t n_q_heads, float scale,
+                        const rp_kvq_tensor* q, const rp_kvq_tensor* out, void* workspace, size_t workspace_bytes,
+                        void* hip_stream) {
+  return guarded([&] {
+    rollpack::KvqAttendArgs a;
+    a.cache = kvq_cache(cache, true);
+    a.batch = kvq_batch(batch, true);
+    const size_t need = kvq_attend_size(a.cache, a.batch, n_q_heads);
+    kvq_require(scale > 0.f && std::isfinite(scale), "scale must be positive and finite");
+    if (a.batch.n_seqs == 0 || a.batch.n_rows == 0) return;
+    a.q = kvq_tensor(q, a.batch.n_rows, n_q_heads, a.cache.hd, false);
+    a.out = kvq_tensor(out, a.batch.n_rows, n_q_heads, a.cache.hd, true);
+    kvq_require(a.q.bf16 == a.out.bf16, "q and out must have one dtype");
+    kvq_require(a.q.p != a.out.p, "out is q's memory");
+    kvq_require(need == 0 || (workspace && reinterpret_cast<uintptr_t>(workspace) % 256 == 0), "workspace must be 256-byte aligned device memory");
+    kvq_require(workspace_bytes >= need, "workspace smaller than rp_kvq_attend_workspace");
+    a.n_q = n_q_heads;
+    a.scale = scale;
+    kvq_launched(rollpack::launch_kvq_attend(a, workspace, kvq_stream(hip_stream)), "rp_kvq_attend");
   });
 }
 

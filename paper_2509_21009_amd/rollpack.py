@@ -84,6 +84,22 @@ class RpStepRecord(ctypes.Structure):
                 ("end_ms", ctypes.c_double)]
 
 
+class RpKvqCache(ctypes.Structure):
+    _fields_ = [("blocks", ctypes.c_void_p), ("n_pages", ctypes.c_int64), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
+
+
+class RpKvqBatch(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("max_rows", ctypes.c_int32),
+                ("max_context", ctypes.c_int32), ("row_offsets", ctypes.c_void_p), ("contexts", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p), ("table_stride", ctypes.c_int64)]
+
+
+class RpKvqTensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("dtype", ctypes.c_int32)]
+
+
 class RollpackError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"{STATUS.get(status, status)}: {msg}")
@@ -95,6 +111,7 @@ _I32P = ctypes.POINTER(ctypes.c_int32)
 _I64P = ctypes.POINTER(ctypes.c_int64)
 _F32P = ctypes.POINTER(ctypes.c_float)
 _SZP = ctypes.POINTER(ctypes.c_size_t)
+_KC, _KB, _KT = ctypes.POINTER(RpKvqCache), ctypes.POINTER(RpKvqBatch), ctypes.POINTER(RpKvqTensor)
 
 # name -> (restype, argtypes), in the order of include/rollpack.h
 SIGNATURES = {
@@ -142,6 +159,11 @@ SIGNATURES = {
     "rp_profile_every": (ctypes.c_int, [_P, ctypes.c_int32]),
     "rp_profile_read": (ctypes.c_int, [_P, ctypes.POINTER(RpKernelStats), ctypes.c_int32, _I32P]),
     "rp_stream_read_gbs": (ctypes.c_int, [_P, ctypes.c_size_t, ctypes.c_int32, _P, ctypes.POINTER(ctypes.c_double)]),
+    "rp_kvq_cache_bytes": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, _SZP]),
+    "rp_kvq_append": (ctypes.c_int, [_KC, _KB, _KT, _KT, _P]),
+    "rp_kvq_read": (ctypes.c_int, [_KC, _KB, _KT, _KT, _P]),
+    "rp_kvq_attend_workspace": (ctypes.c_int, [_KC, _KB, ctypes.c_int32, _SZP]),
+    "rp_kvq_attend": (ctypes.c_int, [_KC, _KB, ctypes.c_int32, ctypes.c_float, _KT, _KT, _P, ctypes.c_size_t, _P]),
     "rp_last_error": (ctypes.c_char_p, []),
 }
 
@@ -472,6 +494,32 @@ def rp_stream_read_gbs(buf, reps: int = 5) -> float:
     return gbs.value
 
 
+def rp_kvq_cache_bytes(n_pages: int, n_kv_heads: int, head_dim: int) -> int:
+    b = ctypes.c_size_t()
+    _check(load_library().rp_kvq_cache_bytes(n_pages, n_kv_heads, head_dim, ctypes.byref(b)))
+    return b.value
+
+
+def rp_kvq_append(cache: RpKvqCache, batch: RpKvqBatch, k: RpKvqTensor, v: RpKvqTensor, stream_ptr: int) -> None:
+    _check(load_library().rp_kvq_append(cache, batch, k, v, stream_ptr))
+
+
+def rp_kvq_read(cache: RpKvqCache, batch: RpKvqBatch, k: RpKvqTensor, v: RpKvqTensor, stream_ptr: int) -> None:
+    _check(load_library().rp_kvq_read(cache, batch, k, v, stream_ptr))
+
+
+def rp_kvq_attend_workspace(cache: RpKvqCache, batch: RpKvqBatch, n_q_heads: int) -> int:
+    b = ctypes.c_size_t()
+    _check(load_library().rp_kvq_attend_workspace(cache, batch, n_q_heads, ctypes.byref(b)))
+    return b.value
+
+
+def rp_kvq_attend(cache: RpKvqCache, batch: RpKvqBatch, n_q_heads: int, scale: float, q: RpKvqTensor,
+                  out: RpKvqTensor, workspace_ptr: Optional[int], workspace_bytes: int, stream_ptr: int) -> None:
+    _check(load_library().rp_kvq_attend(cache, batch, n_q_heads, scale, q, out, workspace_ptr, workspace_bytes,
+                                        stream_ptr))
+
+
 def rp_last_error() -> str:
     return load_library().rp_last_error().decode()
 
@@ -591,6 +639,120 @@ class Engine:
                              P0: int, R0: int, eta: float, eta_r: Optional[float] = None):
         return rp_rollout_tail_batched(self.handle, seq_ids, prompt_tokens, prompt_offsets, max_new_tokens, seed,
                                        temperature, P0, R0, eta, eta_r)
+
+
+class KvqBatch:
+    """The batch of a KvqCache call (rp_kvq_batch): its device arrays, kept alive, and their bounds."""
+
+    def __init__(self, struct: RpKvqBatch, tensors):
+        self.struct, self.tensors = struct, tensors
+
+
+class KvqCache:
+    """A KV cache of one layer held in 4 bits (rp_kvq_*), over torch-allocated memory.
+
+    Calls run on torch's current stream of the cache's device, with every tensor on that device.
+    They allocate their results (unless `out` is given) and can be captured into a graph; the
+    batch's arrays are then read at each replay.
+    """
+
+    def __init__(self, n_pages: int, n_kv_heads: int, head_dim: int, device="cuda"):
+        import torch
+        self.torch = torch
+        self.n_pages, self.n_kv_heads, self.head_dim = n_pages, n_kv_heads, head_dim
+        self.blocks = torch.zeros(rp_kvq_cache_bytes(n_pages, n_kv_heads, head_dim), dtype=torch.uint8, device=device)
+        self.device = self.blocks.device
+        if self.device.type != "cuda":
+            raise ValueError("the 4-bit cache lives in GPU memory")
+        self.struct = RpKvqCache(self.blocks.data_ptr(), n_pages, n_kv_heads, head_dim)
+        self._types = {torch.float32: RP_DTYPE_F32, torch.bfloat16: RP_DTYPE_BF16}
+
+    def batch(self, contexts, page_table, row_offsets=None, n_rows: Optional[int] = None,
+              max_rows: Optional[int] = None, max_context: Optional[int] = None) -> KvqBatch:
+        """contexts [n_seqs], page_table [n_seqs, pages] (its rows may be strided) and row_offsets
+        [n_seqs + 1]: int32 tensors on the device.  Without row_offsets every sequence has one row.
+        n_rows: rows of the call's tensors (by default n_seqs; with row_offsets it must be given),
+        max_rows: most of one sequence (by default n_rows), max_context: the largest context (by default what
+        the page table's rows hold)."""
+        for t, dims in ((contexts, 1), (page_table, 2), (row_offsets, 1)):
+            if t is None:
+                continue
+            if t.dtype != self.torch.int32 or t.device != self.device or t.dim() != dims or \
+                    (t.numel() > 1 and t.stride(-1) != 1):
+                raise ValueError("batch arrays are int32 tensors on the cache's device, contiguous along their last dimension")
+        n = contexts.shape[0]
+        if page_table.shape[0] != n or (row_offsets is not None and row_offsets.shape[0] != n + 1):
+            raise ValueError("contexts [n], page_table [n, pages] and row_offsets [n + 1] must agree")
+        if n_rows is None:
+            if row_offsets is not None:
+                raise ValueError("row_offsets need n_rows")
+            n_rows = n
+        held = page_table.shape[1] * 64
+        if max_context is None:
+            max_context = min(held, 1 << 30)
+        if max_context > held:
+            raise ValueError("max_context is past the page table's rows")
+        stride = page_table.stride(0) if n > 1 else page_table.shape[1]
+        b = RpKvqBatch(n, n_rows, n_rows if max_rows is None else max_rows, max_context,
+                       None if row_offsets is None else row_offsets.data_ptr(), contexts.data_ptr(),
+                       page_table.data_ptr(), stride)
+        return KvqBatch(b, (contexts, page_table, row_offsets))
+
+    def _tensor(self, t, rows: int, heads: int) -> RpKvqTensor:
+        if t.device != self.device or tuple(t.shape) != (rows, heads, self.head_dim):
+            raise ValueError(f"expected [{rows}, {heads}, {self.head_dim}] on {self.device}, got {tuple(t.shape)} on {t.device}")
+        dt = self._types.get(t.dtype)
+        if dt is None or (t.stride(2) != 1 and t.numel() > 0):
+            raise ValueError("tensors are float32 or bfloat16 with contiguous head dimensions")
+        return RpKvqTensor(t.data_ptr(), t.stride(0), t.stride(1), dt)
+
+    def _call(self, fn, *args):
+        """fn(cache, *args, stream) with the cache's device current."""
+        cuda = self.torch.cuda
+        stream = cuda.current_stream(self.device).cuda_stream
+        if cuda.current_device() == self.device.index:
+            fn(self.struct, *args, stream)
+        else:
+            with cuda.device(self.device):
+                fn(self.struct, *args, stream)
+
+    def append(self, batch: KvqBatch, k, v) -> None:
+        """Quantise k and v [n_rows, n_kv_heads, head_dim] into the cache at the rows' positions."""
+        n = batch.struct.n_rows
+        self._call(rp_kvq_append, batch.struct, self._tensor(k, n, self.n_kv_heads), self._tensor(v, n, self.n_kv_heads))
+
+    def read(self, batch: KvqBatch, dtype=None, out=None):
+        """(k, v) that the cache holds of the batch's rows, in dtype (bfloat16) or into the tensors `out`."""
+        torch, n = self.torch, batch.struct.n_rows
+        if out is None:
+            dims = (n, self.n_kv_heads, self.head_dim)
+            dtype = torch.bfloat16 if dtype is None else dtype
+            out = (torch.empty(dims, dtype=dtype, device=self.device), torch.empty(dims, dtype=dtype, device=self.device))
+        k, v = out
+        self._call(rp_kvq_read, batch.struct, self._tensor(k, n, self.n_kv_heads), self._tensor(v, n, self.n_kv_heads))
+        return k, v
+
+    def attend_workspace(self, batch: KvqBatch, n_q_heads: int):
+        """A workspace for attend with this batch's bounds, for callers who keep one (one per call in flight)."""
+        n = rp_kvq_attend_workspace(self.struct, batch.struct, n_q_heads)
+        return self.torch.empty(n, dtype=self.torch.uint8, device=self.device)
+
+    def attend(self, batch: KvqBatch, q, scale: Optional[float] = None, out=None, workspace=None):
+        """Causal attention of q [n_rows, n_q_heads, head_dim] over the cached keys; scale 1 / sqrt(head_dim) by default."""
+        torch, n = self.torch, batch.struct.n_rows
+        if q.dim() != 3:
+            raise ValueError("q is [n_rows, n_q_heads, head_dim]")
+        heads = q.shape[1]
+        if out is None:
+            out = torch.empty(tuple(q.shape), dtype=q.dtype, device=self.device)
+        if workspace is None:
+            workspace = self.attend_workspace(batch, heads)
+        elif workspace.device != self.device or not workspace.is_contiguous():
+            raise ValueError("the workspace is a contiguous tensor on the cache's device")
+        self._call(rp_kvq_attend, batch.struct, heads, self.head_dim ** -0.5 if scale is None else scale,
+                   self._tensor(q, n, heads), self._tensor(out, n, heads), workspace.data_ptr(),
+                   workspace.numel() * workspace.element_size())
+        return out
 
 
 def weights_struct(shape, weights: dict):
