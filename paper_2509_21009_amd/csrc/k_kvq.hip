@@ -1,6 +1,6 @@
 // The KV cache held in 4 bits (kvq.hpp has its format): quantising rows into it, reading them back, and
 // causal GQA attention over it.
-#include <type_traits>
+#include <algorithm>
 
 #include "device_common.hpp"
 #include "kernels.hpp"
@@ -87,9 +87,10 @@ __device__ __forceinline__ RowPlace row_place(const KvqCache& c, const KvqBatch&
   return p;
 }
 
+template <bool BF16>
 __device__ __forceinline__ void load8(const KvqTensor& x, int row, int head, int d, float (&f)[8]) {
   const int64_t at = row * x.row_stride + head * x.head_stride + d;
-  if (x.bf16) {
+  if constexpr (BF16) {
     const bf16_t* p = static_cast<const bf16_t*>(x.p) + at;
     if (x.vec) {
       const u32x4 w = *reinterpret_cast<const u32x4*>(p);
@@ -112,9 +113,10 @@ __device__ __forceinline__ void load8(const KvqTensor& x, int row, int head, int
   }
 }
 
+template <bool BF16>
 __device__ __forceinline__ void store8(const KvqTensor& x, int row, int head, int d, const float (&f)[8]) {
   const int64_t at = row * x.row_stride + head * x.head_stride + d;
-  if (x.bf16) {
+  if constexpr (BF16) {
     bf16_t* p = static_cast<bf16_t*>(x.p) + at;
     if (x.vec) {
       u32x4 w;
@@ -171,13 +173,13 @@ __device__ __forceinline__ void dequantise8(uint32_t w, uint32_t byte, float (&f
 }
 
 // Eight consecutive dimensions d.. of token t, as they lie in a block: one word at hd 128; for V at hd 64 two halves of one.
-template <int HD>
+template <int HD, bool BF16>
 __global__ __launch_bounds__(256) void k_kvq_append(KvqCache c, KvqBatch bt, KvqTensor k, KvqTensor v) {
   const RowPlace p = row_place<HD>(c, bt);
   float kf[8] = {}, vf[8] = {};
   if (p.state == 1) {
-    load8(k, p.row, p.kh, p.d, kf);
-    load8(v, p.row, p.kh, p.d, vf);
+    load8<BF16>(k, p.row, p.kh, p.d, kf);
+    load8<BF16>(v, p.row, p.kh, p.d, vf);
   }
   uint32_t kb, vb;
   const uint32_t kw = quantise8(kf, kb), vw = quantise8(vf, vb);  // every lane: the maxima cross lanes
@@ -195,7 +197,7 @@ __global__ __launch_bounds__(256) void k_kvq_append(KvqCache c, KvqBatch bt, Kvq
   }
 }
 
-template <int HD>
+template <int HD, bool BF16>
 __global__ __launch_bounds__(256) void k_kvq_read(KvqCache c, KvqBatch bt, KvqTensor k, KvqTensor v) {
   const RowPlace p = row_place<HD>(c, bt);
   if (p.state == 0) return;
@@ -217,101 +219,48 @@ __global__ __launch_bounds__(256) void k_kvq_read(KvqCache c, KvqBatch bt, KvqTe
 #pragma unroll
     for (int i = 0; i < 8; ++i) kf[i] = vf[i] = x;
   }
-  store8(k, p.row, p.kh, p.d, kf);
-  store8(v, p.row, p.kh, p.d, vf);
+  store8<BF16>(k, p.row, p.kh, p.d, kf);
+  store8<BF16>(v, p.row, p.kh, p.d, vf);
 }
 
-// ---- the plan, computed by every wave for itself ---------------------------------------
-
-struct PlanShape {
-  int cols;                           // columns of a tile
-  float page_us, ends_us, join_us;    // kvq_price
+// How a launch cuts its tiles.
+struct Cut {
+  int find;   // tiles are found by their sequences' rows (0: tile b is sequence b's only one)
+  int items;  // of a tile at most
+  int least;  // pages of an item, unless it is its tile's only one
 };
 
-// Where an index falls: the sequence, the tiles and items before it (of one KV head), and what is left of the index.
-struct Found {
-  int b, tile0, item0, rest, ppi;
-  KvqSeq s;
-};
+// ---- which tile a block has ------------------------------------------------------------
 
-// Finds item `index` (by_tile: tile `index`) of the batch; b = -1 past the last.  Lanes take 64 sequences at a time.
-__device__ Found plan_find(const KvqBatch& bt, int n_kv, int group, const PlanShape& sh, int index, bool by_tile) {
+// Sums over the wave's lanes up to each lane, in six additions across lanes.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // one lane up within 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // lane 15 of a row of 16 to the next
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to the upper half
+  return x;
+}
+
+// Tile `index` of the batch: its sequence (-1 past the last) and which of the sequence's.  Each wave finds it for itself;
+// lane l counts the sequences l per .. (l + 1) per - 1.
+__device__ __forceinline__ int find_tile(const KvqBatch& bt, int group, int index, int& tile) {
   const int lane = threadIdx.x & 63;
-  KvqPlanInput in;
-  int64_t tp = 0;
-  int tiles = 0, mp = 0;
-  for (int o = 0; o < bt.n_seqs; o += 64) {
-    if (o + lane < bt.n_seqs) {
-      const KvqSeq s = kvq_seq(bt, o + lane);
-      const int t = kvq_tiles(s, group, sh.cols), p = t ? kvq_pages(s) : 0;
-      tp += static_cast<int64_t>(t) * p;
-      tiles += t;
-      mp = max(mp, p);
-    }
+  const int per = (bt.n_seqs + 63) >> 6, b0 = lane * per, b1 = min(b0 + per, bt.n_seqs);
+  int mine = 0;
+#pragma unroll 4
+  for (int b = b0; b < b1; ++b) mine += kvq_tiles(kvq_rows(bt, b), group);
+  const int scan = wave_scan(mine);
+  const uint64_t past = __ballot(scan > index);
+  if (!past) return -1;
+  const int w = __ffsll(static_cast<unsigned long long>(past)) - 1;
+  tile = index - __builtin_amdgcn_readlane(scan - mine, w);
+  for (int b = w * per;; ++b) {  // within that lane's sequences
+    const int t = kvq_tiles(kvq_rows(bt, b), group);
+    if (tile < t) return b;
+    tile -= t;
   }
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) {
-    tp += __shfl_xor(static_cast<long long>(tp), m, 64);
-    tiles += __shfl_xor(tiles, m, 64);
-    mp = max(mp, __shfl_xor(mp, m, 64));
-  }
-  in.tile_pages = tp;
-  in.tiles = tiles;
-  in.max_pages = mp;
-  const int least = kvq_least_ppi(in, n_kv), most = max(1, mp);
-  int ppi = most;
-  if (least < most) {
-    const float l2 = log2f(static_cast<float>(most) / least);
-    int cand = min(most, static_cast<int>(least * exp2f(l2 * lane * (1.f / 63.f)) + 0.5f));
-    if (lane == 63) cand = most;
-    const float us = kvq_price(in, n_kv, cand, sh.page_us, sh.ends_us, sh.join_us);
-    float best = us;
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) best = fminf(best, __shfl_xor(best, m, 64));
-    const int who = 63 - __clzll(__ballot(us == best));  // the largest of the cheapest
-    ppi = __builtin_amdgcn_readlane(cand, who);
-  }
-  Found f;
-  f.b = -1;
-  f.ppi = ppi;
-  f.tile0 = f.item0 = f.rest = 0;
-  f.s = KvqSeq{0, 0, 0, false};
-  int tile_base = 0, item_base = 0;
-  for (int o = 0; o < bt.n_seqs; o += 64) {
-    KvqSeq s{0, 0, 0, false};
-    int t = 0, it = 0;
-    if (o + lane < bt.n_seqs) {
-      s = kvq_seq(bt, o + lane);
-      t = kvq_tiles(s, group, sh.cols);
-      it = t * kvq_items(kvq_pages(s), ppi);
-    }
-    int ts = t, is = it;  // inclusive sums
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-      const int a = __shfl_up(ts, m, 64), c = __shfl_up(is, m, 64);
-      if (lane >= m) {
-        ts += a;
-        is += c;
-      }
-    }
-    const int mine = by_tile ? tile_base + ts : item_base + is;
-    const uint64_t past = __ballot(mine > index);
-    if (past) {
-      const int w = __ffsll(static_cast<unsigned long long>(past)) - 1;
-      f.b = o + w;
-      f.tile0 = tile_base + __builtin_amdgcn_readlane(ts - t, w);
-      f.item0 = item_base + __builtin_amdgcn_readlane(is - it, w);
-      f.rest = index - (by_tile ? f.tile0 : f.item0);
-      f.s.r0 = __builtin_amdgcn_readlane(s.r0, w);
-      f.s.n = __builtin_amdgcn_readlane(s.n, w);
-      f.s.ctx = __builtin_amdgcn_readlane(s.ctx, w);
-      f.s.ok = __builtin_amdgcn_readlane(static_cast<int>(s.ok), w);
-      return f;
-    }
-    tile_base += __builtin_amdgcn_readlane(ts, 63);
-    item_base += __builtin_amdgcn_readlane(is, 63);
-  }
-  return f;
 }
 
 // ---- attention, 16 columns a block ------------------------------------------------------
@@ -341,81 +290,106 @@ __device__ __forceinline__ void split8(float (&x)[8], bf16x8_t (&out)[N]) {
 
 // A page of one head as a lane holds it.
 template <int HD>
-struct PageRegs {
-  u32x4 k[HD / 32], v[HD / 32], vs;
-  uint32_t ks;
+struct PageK {
+  u32x4 k[HD / 32];
+  uint32_t s;
   __device__ __forceinline__ void load(const char* block) {
-    const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+    const int lane = threadIdx.x & 63;
     const u32x4* p = reinterpret_cast<const u32x4*>(block) + lane;
 #pragma unroll
     for (int i = 0; i < HD / 32; ++i) k[i] = __builtin_nontemporal_load(p + 64 * i);
-    ks = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(block + 64 * HD) + (g * HD / 128) * 16 + c);
+    s = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(block + 64 * HD) + ((lane >> 4) * HD / 128) * 16 + (lane & 15));
+  }
+};
+template <int HD>
+struct PageV {
+  u32x4 v[HD / 32], s;
+  __device__ __forceinline__ void load(const char* block) {
+    const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+    const u32x4* p = reinterpret_cast<const u32x4*>(block + 32 * HD) + lane;
 #pragma unroll
-    for (int i = 0; i < HD / 32; ++i) v[i] = __builtin_nontemporal_load(p + 2 * HD + 64 * i);
-    vs = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(block + 66 * HD) + (c * HD / 512) * 4 + g);
+    for (int i = 0; i < HD / 32; ++i) v[i] = __builtin_nontemporal_load(p + 64 * i);
+    s = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(block + 66 * HD) + (c * HD / 512) * 4 + g);
   }
 };
 
-__device__ __forceinline__ float scale_of(uint32_t word, int byte) {
-  return __uint_as_float(((word >> (8 * byte)) & 255u) << 23);
+// Byte `i` of a word as the scale of a four-bit conversion, which reads a float's exponent field and nothing else of it.
+__device__ __forceinline__ float scale_of(uint32_t word, int i) {
+  return __uint_as_float(i == 3 ? word >> 1 : word << (23 - 8 * i));
 }
 
-// S^T of tile u: rows are the tile's tokens, columns the 16 columns; NQ pieces of the query.
+// The queries of the 16 columns, and S^T = K Q^T of a page's tile u: rows are the tile's tokens, columns the queries.
+// Queries are NQ pieces of bf16, one, or three (24 bits) of fp32; K unpacked to bf16 is exact.
+// (v_mfma_scale_f32_16x16x128_f8f6f4 would take K's codes as they are, with queries as two e4m3 pieces, but its sum keeps
+// only about 11 bits below its largest product; scores are sums in fp32.)
 template <int HD, int NQ>
-__device__ __forceinline__ f32x4_t tile_scores(const PageRegs<HD>& pg, int u, const bf16x8_t (&qf)[HD / 32][NQ]) {
-  f32x4_t acc{0.f, 0.f, 0.f, 0.f};
-  const float s = scale_of(pg.ks, u);
+struct Query {
+  bf16x8_t q[HD / 32][NQ];
+  __device__ __forceinline__ void load(const KvqTensor& t, int row, int head) {
+    const int g = (threadIdx.x & 63) >> 4;
+    float x[HD / 32][8];
 #pragma unroll
-  for (int j = 0; j < HD / 32; ++j) {
-    const uint32_t w = HD == 128 ? pg.k[u][j] : pg.k[u >> 1][2 * (u & 1) + j];
-    const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, u32x4{code_pair<0>(w, s), code_pair<1>(w, s), code_pair<2>(w, s), code_pair<3>(w, s)});
+    for (int j = 0; j < HD / 32; ++j) load8<NQ == 1>(t, row, head, g * (HD / 4) + 8 * j, x[j]);
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) acc = mfma16x16x32(kf, qf[j][n], acc);
+    for (int j = 0; j < HD / 32; ++j) split8<NQ>(x[j], q[j]);
   }
-  return acc;
-}
+  __device__ __forceinline__ f32x4_t scores(const PageK<HD>& pg, int u) const {
+    f32x4_t acc{0.f, 0.f, 0.f, 0.f};
+    const float s = scale_of(pg.s, u);
+#pragma unroll
+    for (int j = 0; j < HD / 32; ++j) {
+      const uint32_t w = HD == 128 ? pg.k[u][j] : pg.k[u >> 1][2 * (u & 1) + j];
+      const u32x4 k{code_pair<0>(w, s), code_pair<1>(w, s), code_pair<2>(w, s), code_pair<3>(w, s)};
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) acc = mfma16x16x32(__builtin_bit_cast(bf16x8_t, k), q[j][n], acc);
+    }
+    return acc;
+  }
+};
 
 // O^T += V^T P^T over tokens 32h .. 32h + 31 of the page: accumulator i's rows are dimensions hd/16 c + i.
 template <int HD, int NP>
-__device__ __forceinline__ void half_values(const PageRegs<HD>& pg, int h, const bf16x8_t (&pf)[NP], f32x4_t (&o)[HD / 16]) {
-  uint32_t x[HD / 32][8];  // [dimension pair][token]: two dimensions of a token
+__device__ __forceinline__ void half_values(const PageV<HD>& pg, int h, const bf16x8_t (&pf)[NP], f32x4_t (&o)[HD / 16]) {
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const float s = scale_of(pg.vs[2 * h + (k >> 2)], k & 3);
-    if constexpr (HD == 128) {
-      const uint32_t w = pg.v[2 * h + (k >> 2)][k & 3];
-      x[0][k] = code_pair<0>(w, s);
-      x[1][k] = code_pair<1>(w, s);
-      x[2][k] = code_pair<2>(w, s);
-      x[3][k] = code_pair<3>(w, s);
-    } else {
-      const uint32_t w = pg.v[h][k >> 1];
-      x[0][k] = k & 1 ? code_pair<2>(w, s) : code_pair<0>(w, s);
-      x[1][k] = k & 1 ? code_pair<3>(w, s) : code_pair<1>(w, s);
+  for (int j = 0; j < HD / 32; ++j) {  // a pair of dimensions
+    uint32_t x[8];                     // of eight tokens
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float s = scale_of(pg.s[2 * h + (k >> 2)], k & 3);
+      const uint32_t w = HD == 128 ? pg.v[2 * h + (k >> 2)][k & 3] : pg.v[h][k >> 1];
+      const int byte = HD == 128 ? j : 2 * (k & 1) + j;
+      x[k] = byte == 0 ? code_pair<0>(w, s) : byte == 1 ? code_pair<1>(w, s) : byte == 2 ? code_pair<2>(w, s) : code_pair<3>(w, s);
     }
-  }
 #pragma unroll
-  for (int i = 0; i < HD / 16; ++i) {  // eight tokens of one dimension: the low or high halves of neighbouring tokens' pairs
-    u32x4 w;
+    for (int i = 0; i < 2; ++i) {  // its two dimensions: the low or high halves of neighbouring tokens' pairs
+      u32x4 w;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      w[e] = __builtin_amdgcn_perm(x[i / 2][2 * e + 1], x[i / 2][2 * e], i & 1 ? 0x07060302u : 0x05040100u);
+      for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], i ? 0x07060302u : 0x05040100u);
 #pragma unroll
-    for (int n = 0; n < NP; ++n) o[i] = mfma16x16x32(__builtin_bit_cast(bf16x8_t, w), pf[n], o[i]);
+      for (int n = 0; n < NP; ++n) o[2 * j + i] = mfma16x16x32(__builtin_bit_cast(bf16x8_t, w), pf[n], o[2 * j + i]);
+    }
   }
 }
 
-// A page that holds a NaN value block (or, past the context, anything): the blocks' scales become 2^-127, which a zero
-// probability clears, and the lane's outputs turn NaN if its column sees the token.  A lane's outputs all lie in one
-// block of 32 dimensions.
+// Whether any value block of the page may hold NaN: a scale byte of 192 or more (2^65), which is 255 or next to never met.
+__device__ __forceinline__ bool may_be_nan(const u32x4& s) {
+  uint32_t t = 0;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) t |= s[u] & (s[u] << 1);
+  return t & 0x80808080u;
+}
+
+// Such a page: the scales of NaN blocks become 2^-127, which the zero probability of a key out of sight clears (as NaN it
+// would not), and the lane's outputs turn NaN if its column sees the token.  A lane's outputs all lie in one block of 32
+// dimensions.
 template <int HD>
-__device__ __forceinline__ void nan_values(PageRegs<HD>& pg, const char* block, int tok0, int lim, f32x4_t (&o)[HD / 16]) {
+__device__ __forceinline__ void nan_values(PageV<HD>& pg, const char* block, int tok0, int lim, f32x4_t (&o)[HD / 16]) {
   const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
   for (int u = 0; u < 4; ++u)
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-      if (((pg.vs[u] >> (8 * r)) & 255u) == 255u) pg.vs[u] &= ~(255u << (8 * r));
+      if (((pg.s[u] >> (8 * r)) & 255u) == 255u) pg.s[u] &= ~(255u << (8 * r));
   bool bad = false;
   for (int t = 0; t < kKvqPage; ++t)
     bad |= tok0 + t <= lim && static_cast<unsigned char>(block[kvq_v_scale(t, g * HD / 128, HD)]) == 255;
@@ -425,101 +399,94 @@ __device__ __forceinline__ void nan_values(PageRegs<HD>& pg, const char* block, 
   }
 }
 
-__device__ __forceinline__ bool has_nan_scale(const u32x4& vs) {
-  float top = 0.f;  // scales are positive: of valid blocks at most 2^125, of NaN blocks infinity
-#pragma unroll
-  for (int u = 0; u < 4; ++u)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) top = fmaxf(top, scale_of(vs[u], r));
-  return top > 8.5e37f;
-}
-
 // One block of NW waves takes an item: 16 columns of a sequence and KV head (a column is a query head of a row, the
 // G heads of a row side by side) over a range of pages, which the waves take in turn.  Per page a wave forms
 // S^T = K Q^T, an online softmax in the log2 domain and O^T += V^T P^T with MFMA, straight from registers: no
-// value of the cache is used by more than one wave, so nothing passes through LDS but the waves' results.
-//   Q and P are operands in bf16.  fp32 queries are three bf16 pieces (24 bits), and so are their probabilities; of
-// bf16 queries the probabilities are two pieces, so that the output's own rounding is the only one that counts.
+// value of the cache is used by more than one wave, so nothing passes through LDS but the waves' results.  The next
+// page's K is loaded when the scores are formed, its V when the outputs are.
+//   P is an operand in bf16: two pieces of it (16 bits), so that the output's own rounding is the only one that
+// counts; three for fp32.
 //   The running maximum moves only when a score passes it by more than 2^8: probabilities up to 256 lose nothing in
-// fp32 or bf16, and the outputs need rescaling a few times per item instead of every page.
-template <int HD, int NQ, int NP, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void k_kvq_attend(KvqAttendArgs a, PlanShape sh) {
-  constexpr int NT = HD / 16, OLD = HD + 4;
+// fp32 or bf16, the outputs need rescaling a few times per item instead of every page, and no page waits for a maximum
+// over lanes.
+template <int HD, bool F32, int NW>
+__global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendArgs a, Cut sh) {
+  constexpr int NT = HD / 16, OLD = HD + 4, NP = F32 ? 3 : 2;
   __shared__ __attribute__((aligned(16))) float so[NW][16 * OLD];
   __shared__ float sm[NW][16], sl[NW][16];
   const KvqBatch& bt = a.batch;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
-  const int item = blockIdx.x / n_kv, kh = blockIdx.x - item * n_kv;
-  const Found f = plan_find(bt, n_kv, G, sh, item, false);
-  if (f.b < 0) return;
-  const int n_pages = kvq_pages(f.s), splits = kvq_items(n_pages, f.ppi);
-  const int tile = f.rest / splits, split = f.rest - tile * splits;
-  const int j0 = tile * 16, n_cols = min(16, f.s.n * G - j0);
-  const int first = f.s.ctx - f.s.n;  // position of the sequence's first row
-  const int end = f.s.ok ? max(0, first + (j0 + n_cols - 1) / G + 1) : 0;  // keys that the tile sees
-  const int p0 = split * f.ppi, p1 = min(p0 + f.ppi, (end + kKvqPage - 1) / kKvqPage);
-  const int np = max(0, p1 - p0);
+  const int kh = blockIdx.y, split = blockIdx.z;
+  int tile = 0;
+  const int b = sh.find ? find_tile(bt, G, blockIdx.x, tile) : static_cast<int>(blockIdx.x);
+  if (b < 0) return;
+  const KvqSeq sq = kvq_seq(bt, b);
+  const KvqTile tl = kvq_tile(sq, G, tile);
+  const int j0 = tile * kKvqCols, n_cols = tl.cols, first = tl.first;
+  const int pages = kvq_pages(tl.end), items = kvq_items(pages, sh.items, sh.least);
+  if (n_cols <= 0 || split >= items) return;
+  const int per_item = kvq_item_pages(pages, items), p0 = split * per_item;
+  const int np = max(0, min(per_item, pages - p0));
   const int nw = np > wave ? (np - wave + NW - 1) / NW : 0;  // this wave's pages: wave, wave + NW, ...
   const int open = first + j0 / G + 1;  // keys that every column sees
 
   // The column: its query, and the last key that it sees.
   const int cc = min(c, n_cols - 1), row = (j0 + cc) / G, head = kh * G + (j0 + cc) - row * G;
-  const int lim = f.s.ok ? first + row : -1;
+  const int lim = sq.ok ? first + row : -1;
   const float scale_log2 = a.scale * kLog2e;
 
-  const int32_t* pt = table_of(bt, f.b);
-  const int ptv = lane < np ? pt[p0 + lane] : 0;  // lane i has page i of the item, the first 64
-  const size_t bytes = kvq_block_bytes(HD);
-  PageRegs<HD> pg[2];
-  const char* at[2];
-  bool lost[2];
-  auto load = [&](int sl, int i) {
-    const int q = min(wave + NW * i, max(np - 1, 0));  // past the last page: the last again
-    int id = q < 64 ? __builtin_amdgcn_readlane(ptv, q) : pt[p0 + q];
-    lost[sl] = !kvq_page_ok(a.cache, id);
-    id = lost[sl] ? 0 : id;
-    at[sl] = a.cache.blocks + (static_cast<size_t>(id) * n_kv + kh) * bytes;
-    pg[sl].load(at[sl]);
-  };
   f32x4_t o[NT];
 #pragma unroll
   for (int i = 0; i < NT; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   float m_run = -INFINITY, l_run = 0.f;
   if (nw > 0) {
-    bf16x8_t qf[HD / 32][NQ];
-    {
-      float x[HD / 32][8];
-#pragma unroll
-      for (int j = 0; j < HD / 32; ++j) load8(a.q, f.s.r0 + row, head, g * (HD / 4) + 8 * j, x[j]);
-      load(0, 0);
-      load(1, 1);
-#pragma unroll
-      for (int j = 0; j < HD / 32; ++j) split8<NQ>(x[j], qf[j]);
-    }
-    auto step = [&](int sl, int i) {
+    const int32_t* pt = table_of(bt, b) + p0;
+    const int ptv = lane < np ? pt[lane] : 0;  // lane i has page i of the item, the first 64
+    const size_t bytes = kvq_block_bytes(HD);
+    const char* base = a.cache.blocks + kh * bytes;
+    bool lost = false, lost_next = false;  // the page's id is outside the cache: page 0 stands in, and its scores are NaN
+    auto block_of = [&](int i) {
+      const int q = min(wave + NW * i, np - 1);  // past the last page: the last again
+      const int id = q < 64 ? __builtin_amdgcn_readlane(ptv, q) : pt[q];
+      lost_next = !kvq_page_ok(a.cache, id);
+      return base + static_cast<size_t>(lost_next ? 0 : id) * n_kv * bytes;
+    };
+    Query<HD, F32 ? 3 : 1> qf;
+    PageK<HD> pk;
+    PageV<HD> pv;
+    const char* at = block_of(0);
+    lost = lost_next;
+    pk.load(at);
+    qf.load(a.q, sq.r0 + row, head);
+    pv.load(at);
+    for (int i = 0; i < nw; ++i) {
       const int tok0 = (p0 + wave + NW * i) * kKvqPage;
-      float sv[16];
-      float pmax = -INFINITY;
-      const bool masked = tok0 + kKvqPage > open;
+      f32x4_t s[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const f32x4_t s = tile_scores<HD, NQ>(pg[sl], u, qf);
+      for (int u = 0; u < 4; ++u) s[u] = qf.scores(pk, u);
+      const char* next = block_of(i + 1);
+      pk.load(next);
+      if (lost || tok0 + kKvqPage > open) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float v = s[e];
-          if (lost[sl]) v = __builtin_nanf("");
-          if (masked && tok0 + 16 * u + 4 * g + e > lim) v = -INFINITY;
-          sv[4 * u + e] = v;
-          pmax = fmaxf(pmax, v);
-        }
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float v = lost ? __builtin_nanf("") : s[u][e];
+            s[u][e] = tok0 + 16 * u + 4 * g + e > lim ? -INFINITY : v;
+          }
       }
-      pmax = fmaxf(pmax, __shfl_xor(pmax, 16, 64));
-      pmax = fmaxf(pmax, __shfl_xor(pmax, 32, 64));
-      pmax *= scale_log2;
-      if (__any(pmax > m_run + 8.f)) {
-        const float m_new = pmax > m_run + 8.f ? pmax : m_run;
+      float top = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, s[u][e]);
+      top *= scale_log2;
+      if (__any(top > m_run + 8.f)) {
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float m_new = top > m_run + 8.f ? top : m_run;
         const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
         l_run *= alpha;
         m_run = m_new;
@@ -527,37 +494,32 @@ __global__ __launch_bounds__(64 * NW, 2) void k_kvq_attend(KvqAttendArgs a, Plan
         for (int t = 0; t < NT; ++t) o[t] *= alpha;
       }
       const float shift = m_run == -INFINITY ? 0.f : m_run;
-      float sum = 0.f;
 #pragma unroll
-      for (int k = 0; k < 16; ++k) {
-        sv[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[k], scale_log2, -shift));
-        sum += sv[k];
-      }
-      l_run += sum;  // of this lane's tokens; the lanes of a column add up at the end
-      if (__any(has_nan_scale(pg[sl].vs))) nan_values<HD>(pg[sl], at[sl], tok0, lim, o);
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s[u][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e], scale_log2, -shift));
+          l_run += s[u][e];  // of this lane's tokens; the lanes of a column add up at the end
+        }
+      if (__any(may_be_nan(pv.s))) nan_values<HD>(pv, at, tok0, lim, o);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         float x[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = sv[8 * h + k];
+        for (int k = 0; k < 8; ++k) x[k] = s[2 * h + (k >> 2)][k & 3];
         bf16x8_t pf[NP];
         split8<NP>(x, pf);
-        half_values<HD, NP>(pg[sl], h, pf, o);
+        half_values<HD, NP>(pv, h, pf, o);
       }
-    };
-    for (int i = 0; i < nw; i += 2) {
-      step(0, i);
-      load(0, i + 2);
-      if (i + 1 < nw) {
-        step(1, i + 1);
-        load(1, i + 3);
-      }
+      at = next;
+      lost = lost_next;
+      pv.load(at);
     }
     l_run += __shfl_xor(l_run, 16, 64);
     l_run += __shfl_xor(l_run, 32, 64);
   }
 
-  // Join the waves: one without a page has m = -inf, l = 0, o = 0.
+  // Combine the waves: one without a page has m = -inf, l = 0, o = 0.
   if (g == 0) {
     sm[wave][c] = m_run;
     sl[wave][c] = l_run;
@@ -567,14 +529,16 @@ __global__ __launch_bounds__(64 * NW, 2) void k_kvq_attend(KvqAttendArgs a, Plan
 #pragma unroll
   for (int w = 1; w < NW; ++w) mx = fmaxf(mx, sm[w][c]);
   const float fac = m_run == -INFINITY ? (l_run == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m_run - mx);
+  if (c < n_cols) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
+    for (int e = 0; e < 4; ++e)
 #pragma unroll
-    for (int i = 0; i < NT; i += 4)  // dimensions hd/16 (4g + e) + i ..
-      *reinterpret_cast<f32x4_t*>(&so[wave][c * OLD + (4 * g + e) * NT + i]) =
-          f32x4_t{o[i][e], o[i + 1][e], o[i + 2][e], o[i + 3][e]} * fac;
+      for (int i = 0; i < NT; i += 4)  // dimensions hd/16 (4g + e) + i ..
+        *reinterpret_cast<f32x4_t*>(&so[wave][c * OLD + (4 * g + e) * NT + i]) =
+            f32x4_t{o[i][e], o[i + 1][e], o[i + 2][e], o[i + 3][e]} * fac;
+  }
   __syncthreads();
-  const int64_t part = static_cast<int64_t>(f.item0 + f.rest) * n_kv + kh;
+  const int64_t part = (static_cast<int64_t>(blockIdx.x) * sh.items + split) * n_kv + kh;
   for (int q = tid; q < n_cols * (HD / 8); q += 64 * NW) {
     const int col = q / (HD / 8), d = q % (HD / 8) * 8;
     float m4 = sm[0][col], den = 0.f, x[8];
@@ -583,23 +547,23 @@ __global__ __launch_bounds__(64 * NW, 2) void k_kvq_attend(KvqAttendArgs a, Plan
 #pragma unroll
     for (int w = 0; w < NW; ++w)
       den += sm[w][col] == -INFINITY ? sl[w][col] : sl[w][col] * __builtin_amdgcn_exp2f(sm[w][col] - m4);
+    f32x4_t y[2]{};
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      x[k] = so[0][col * OLD + d + k];
-#pragma unroll
-      for (int w = 1; w < NW; ++w) x[k] += so[w][col * OLD + d + k];
+    for (int w = 0; w < NW; ++w) {
+      y[0] += *reinterpret_cast<const f32x4_t*>(&so[w][col * OLD + d]);
+      y[1] += *reinterpret_cast<const f32x4_t*>(&so[w][col * OLD + d + 4]);
     }
-    if (splits == 1) {
+    if (items == 1) {
       const int r = (j0 + col) / G, h = kh * G + (j0 + col) - r * G;
       // a row before the sequence's first token sees no key: zeros; a sequence out of bounds: NaN
-      const float inv = !f.s.ok ? __builtin_nanf("") : first + r < 0 ? 0.f : 1.f / den;
+      const float inv = !sq.ok ? __builtin_nanf("") : first + r < 0 ? 0.f : 1.f / den;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] *= inv;
-      store8(a.out, f.s.r0 + r, h, d, x);
+      for (int k = 0; k < 8; ++k) x[k] = y[k >> 2][k & 3] * inv;
+      store8<!F32>(a.out, sq.r0 + r, h, d, x);
     } else {
       float* po = a.part_o + (part * 16 + col) * HD + d;
-      *reinterpret_cast<f32x4_t*>(po) = f32x4_t{x[0], x[1], x[2], x[3]};
-      *reinterpret_cast<f32x4_t*>(po + 4) = f32x4_t{x[4], x[5], x[6], x[7]};
+      *reinterpret_cast<f32x4_t*>(po) = y[0];
+      *reinterpret_cast<f32x4_t*>(po + 4) = y[1];
       if (d == 0) {
         a.part_ml[part * 32 + col] = m4;
         a.part_ml[part * 32 + 16 + col] = den;
@@ -608,59 +572,100 @@ __global__ __launch_bounds__(64 * NW, 2) void k_kvq_attend(KvqAttendArgs a, Plan
   }
 }
 
-// Joins the items of a tile: one block per (tile, KV head), a thread per column and eight dimensions.
-template <int HD>
-__global__ __launch_bounds__(16 * HD / 8) void k_kvq_join(KvqAttendArgs a, PlanShape sh) {
-  constexpr int NTH = 16 * HD / 8;
-  __shared__ float sw[16][kKvqTileItems];
-  __shared__ float sden[16];
+// Joins the items of a tile: one block per (tile, KV head, column).  Four dimensions to a thread, the items dealt out to
+// groups of threads whose loads are all in flight at once.
+template <int HD, bool F32>
+__global__ __launch_bounds__(256) void k_kvq_join(KvqAttendArgs a, Cut sh) {
+  constexpr int LPC = HD / 4, NG = 256 / LPC, PER = kKvqTileItems / NG;
+  __shared__ float sw[kKvqTileItems];
+  __shared__ __attribute__((aligned(16))) f32x4_t sx[NG][LPC];
   const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
-  const int ti = blockIdx.x / n_kv, kh = blockIdx.x - ti * n_kv;
-  const Found f = plan_find(a.batch, n_kv, G, sh, ti, true);
-  if (f.b < 0) return;
-  const int n = kvq_items(kvq_pages(f.s), f.ppi);
-  if (n <= 1) return;  // written by its only item
-  const int tile = f.rest, j0 = tile * 16, n_cols = min(16, f.s.n * G - j0);
-  if (static_cast<int64_t>(f.item0) + (tile + 1) * n > a.items) return;  // offsets that do not ascend
-  const int64_t part = (static_cast<int64_t>(f.item0) + tile * n) * n_kv + kh;  // of split 0; n_kv between splits
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int col = wave; col < n_cols; col += NTH / 64) {
+  const int kh = blockIdx.y, col = blockIdx.z;
+  int tile = 0;
+  const int b = sh.find ? find_tile(a.batch, G, blockIdx.x, tile) : static_cast<int>(blockIdx.x);
+  if (b < 0) return;
+  const KvqSeq sq = kvq_seq(a.batch, b);
+  const KvqTile tl = kvq_tile(sq, G, tile);
+  const int n = kvq_items(kvq_pages(tl.end), sh.items, sh.least);
+  if (n == 1 || col >= tl.cols) return;  // one item has written the output itself
+  const int j0 = tile * kKvqCols;
+  const int64_t part = static_cast<int64_t>(blockIdx.x) * sh.items * n_kv + kh;  // of item 0; n_kv between items
+  const int grp = threadIdx.x / LPC, d = threadIdx.x % LPC * 4;
+  const float* po = a.part_o + (part * 16 + col) * HD + d;
+  const int64_t step = static_cast<int64_t>(n_kv) * 16 * HD;
+  f32x4_t x[PER];
+#pragma unroll
+  for (int k = 0; k < PER; ++k) x[k] = *reinterpret_cast<const f32x4_t*>(po + min(grp + NG * k, n - 1) * step);
+  float den = 0.f;
+  if (threadIdx.x < 64) {
+    const int lane = threadIdx.x;
     const float* ml = a.part_ml + (part + static_cast<int64_t>(min(lane, n - 1)) * n_kv) * 32 + col;
     const float m = lane < n ? ml[0] : -INFINITY, l = lane < n ? ml[16] : 0.f;
     const float mx = wave_max(m);
     const float w = m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - mx);
-    sw[col][lane] = w;
-    const float den = wave_sum(w * l);
-    if (lane == 0) sden[col] = den;
+    sw[lane] = w;
+    den = wave_sum(w * l);
   }
   __syncthreads();
-  const int col = threadIdx.x / (HD / 8), d = threadIdx.x % (HD / 8) * 8;
-  if (col >= n_cols) return;
-  const float* po = a.part_o + (part * 16 + col) * HD + d;
-  const int64_t step = static_cast<int64_t>(n_kv) * 16 * HD;
-  f32x4_t x0{0.f, 0.f, 0.f, 0.f}, x1 = x0;
-#pragma unroll 8
-  for (int s = 0; s < n; ++s) {
-    x0 += *reinterpret_cast<const f32x4_t*>(po + s * step) * sw[col][s];
-    x1 += *reinterpret_cast<const f32x4_t*>(po + s * step + 4) * sw[col][s];
-  }
-  const int r = (j0 + col) / G, h = kh * G + (j0 + col) - r * G;
-  const float inv = !f.s.ok ? __builtin_nanf("") : f.s.ctx - f.s.n + r < 0 ? 0.f : 1.f / sden[col];
-  float x[8];
+  f32x4_t sum{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int k = 0; k < 8; ++k) x[k] = (k < 4 ? x0[k] : x1[k - 4]) * inv;
-  store8(a.out, f.s.r0 + r, h, d, x);
+  for (int k = 0; k < PER; ++k)
+    if (grp + NG * k < n) sum += x[k] * sw[grp + NG * k];
+  sx[grp][threadIdx.x % LPC] = sum;
+  __syncthreads();
+  if (threadIdx.x < HD / 8) {
+    const int r = (j0 + col) / G, h = kh * G + (j0 + col) - r * G;
+    const float inv = tl.first + r < 0 ? 0.f : 1.f / den;
+    f32x4_t y[2]{};
+#pragma unroll
+    for (int k = 0; k < NG; ++k) {
+      y[0] += sx[k][2 * threadIdx.x];
+      y[1] += sx[k][2 * threadIdx.x + 1];
+    }
+    float out[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) out[k] = y[k >> 2][k & 3] * inv;
+    store8<!F32>(a.out, sq.r0 + r, h, threadIdx.x * 8, out);
+  }
 }
 
-constexpr PlanShape kWalk{16, 0.4f, 2.5f, 4.5f};
+// What a launch of attention does, from the bounds of the call alone.
+struct AttendPlan {
+  Cut cut;
+  int waves;      // of a block
+  int64_t tiles;  // at most
+};
 
-template <int HD>
-hipError_t attend_hd(const KvqAttendArgs& a, int64_t tiles, int64_t items, hipStream_t s) {
+AttendPlan attend_plan(const KvqCache& c, const KvqBatch& b, int n_q) {
+  const int G = n_q / c.n_kv;
+  AttendPlan p;
+  p.tiles = kvq_tile_bound(b, G);
+  const int64_t blocks = std::max<int64_t>(1, p.tiles * c.n_kv);
+  const int pages = std::max(1, kvq_pages(b.max_context));
+  p.cut = Cut{!kvq_one_tile(b, G), 1, 4};
+  if (blocks < 256) p.cut.items = static_cast<int>(std::min<int64_t>(kvq_items(pages, kKvqTileItems, p.cut.least), (384 + blocks - 1) / blocks));
+  if (pages <= 16) p.cut.items = 1;
+  const int64_t all = blocks * p.cut.items;
+  const int per = kvq_item_pages(pages, p.cut.items);
+  p.waves = all >= 2048 && per <= 4 ? 1 : all <= 384 && per > 16 ? 8 : 4;
+  return p;
+}
+
+template <int HD, bool F32>
+hipError_t attend_launch(const KvqAttendArgs& a, const AttendPlan& p, hipStream_t s) {
   const int n_kv = a.cache.n_kv;
-  const dim3 grid(static_cast<uint32_t>(items * n_kv));
-  if (a.q.bf16) launch_kernel((k_kvq_attend<HD, 1, 2, 4>), grid, dim3(256), 0, s, a, kWalk);
-  else launch_kernel((k_kvq_attend<HD, 3, 3, 4>), grid, dim3(256), 0, s, a, kWalk);
-  if (items > tiles) launch_kernel(k_kvq_join<HD>, dim3(static_cast<uint32_t>(tiles * n_kv)), dim3(16 * HD / 8), 0, s, a, kWalk);
+  const dim3 grid(static_cast<uint32_t>(p.tiles), n_kv, p.cut.items);
+  switch (p.waves) {
+    case 1: launch_kernel((k_kvq_attend<HD, F32, 1>), grid, dim3(64), 0, s, a, p.cut); break;
+    case 2: launch_kernel((k_kvq_attend<HD, F32, 2>), grid, dim3(128), 0, s, a, p.cut); break;
+    case 4: launch_kernel((k_kvq_attend<HD, F32, 4>), grid, dim3(256), 0, s, a, p.cut); break;
+    case 8: launch_kernel((k_kvq_attend<HD, F32, 8>), grid, dim3(512), 0, s, a, p.cut); break;
+    default: return hipErrorInvalidValue;
+  }
+  if (p.cut.items > 1) {
+    const int cols = static_cast<int>(std::min<int64_t>(kKvqCols, static_cast<int64_t>(kvq_max_rows(a.batch)) * (a.n_q / n_kv)));
+    launch_kernel((k_kvq_join<HD, F32>), dim3(static_cast<uint32_t>(p.tiles), n_kv, cols), dim3(256), 0, s, a, p.cut);
+  }
   return hipGetLastError();
 }
 
@@ -672,31 +677,35 @@ dim3 row_grid(const KvqCache& c, int n_rows) {
 }  // namespace
 
 size_t kvq_attend_bytes(const KvqCache& c, const KvqBatch& b, int n_q) {
-  const int G = n_q / c.n_kv;
-  const int64_t tiles = kvq_tile_bound(b, G, 16), items = kvq_item_bound(b, c.n_kv, G, 16);
-  if (items <= tiles) return 0;
-  return static_cast<size_t>(items) * c.n_kv * (16 * c.hd + 32) * 4;
+  const AttendPlan p = attend_plan(c, b, n_q);
+  if (p.cut.items == 1) return 0;
+  return static_cast<size_t>(p.tiles) * p.cut.items * c.n_kv * kKvqCols * (c.hd + 2) * 4;
 }
 
 hipError_t launch_kvq_append(const KvqCache& c, const KvqBatch& b, const KvqTensor& k, const KvqTensor& v, hipStream_t s) {
-  if (c.hd == 128) launch_kernel(k_kvq_append<128>, row_grid(c, b.n_rows), dim3(256), 0, s, c, b, k, v);
-  else launch_kernel(k_kvq_append<64>, row_grid(c, b.n_rows), dim3(256), 0, s, c, b, k, v);
+  const dim3 grid = row_grid(c, b.n_rows), block(256);
+  if (c.hd == 128 && k.bf16) launch_kernel((k_kvq_append<128, true>), grid, block, 0, s, c, b, k, v);
+  else if (c.hd == 128) launch_kernel((k_kvq_append<128, false>), grid, block, 0, s, c, b, k, v);
+  else if (k.bf16) launch_kernel((k_kvq_append<64, true>), grid, block, 0, s, c, b, k, v);
+  else launch_kernel((k_kvq_append<64, false>), grid, block, 0, s, c, b, k, v);
   return hipGetLastError();
 }
 
 hipError_t launch_kvq_read(const KvqCache& c, const KvqBatch& b, const KvqTensor& k, const KvqTensor& v, hipStream_t s) {
-  if (c.hd == 128) launch_kernel(k_kvq_read<128>, row_grid(c, b.n_rows), dim3(256), 0, s, c, b, k, v);
-  else launch_kernel(k_kvq_read<64>, row_grid(c, b.n_rows), dim3(256), 0, s, c, b, k, v);
+  const dim3 grid = row_grid(c, b.n_rows), block(256);
+  if (c.hd == 128 && k.bf16) launch_kernel((k_kvq_read<128, true>), grid, block, 0, s, c, b, k, v);
+  else if (c.hd == 128) launch_kernel((k_kvq_read<128, false>), grid, block, 0, s, c, b, k, v);
+  else if (k.bf16) launch_kernel((k_kvq_read<64, true>), grid, block, 0, s, c, b, k, v);
+  else launch_kernel((k_kvq_read<64, false>), grid, block, 0, s, c, b, k, v);
   return hipGetLastError();
 }
 
 hipError_t launch_kvq_attend(KvqAttendArgs a, void* ws, hipStream_t s) {
-  const int G = a.n_q / a.cache.n_kv;
-  const int64_t tiles = kvq_tile_bound(a.batch, G, 16), items = kvq_item_bound(a.batch, a.cache.n_kv, G, 16);
-  a.items = items;
+  const AttendPlan p = attend_plan(a.cache, a.batch, a.n_q);
   a.part_o = static_cast<float*>(ws);
-  a.part_ml = a.part_o ? a.part_o + items * a.cache.n_kv * 16 * a.cache.hd : nullptr;
-  return a.cache.hd == 128 ? attend_hd<128>(a, tiles, items, s) : attend_hd<64>(a, tiles, items, s);
+  a.part_ml = a.part_o ? a.part_o + p.tiles * p.cut.items * a.cache.n_kv * kKvqCols * a.cache.hd : nullptr;
+  if (a.q.bf16) return a.cache.hd == 128 ? attend_launch<128, false>(a, p, s) : attend_launch<64, false>(a, p, s);
+  return a.cache.hd == 128 ? attend_launch<128, true>(a, p, s) : attend_launch<64, true>(a, p, s);
 }
 
 }  // namespace rollpack

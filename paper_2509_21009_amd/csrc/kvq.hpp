@@ -14,8 +14,8 @@
 //
 // Layout.  Pages of 64 tokens, [page][KV head]: one block of 68 hd bytes
 //   K codes [64 tokens x hd], V codes [64 tokens x hd], K scales [2 hd], V scales [2 hd]
-// in the order in which the lanes of a wave hold them as operands of v_mfma_f32_16x16x32_bf16 (lane 16g + c), so that
-// every load of a page is 16 bytes per lane and 1 KB per instruction without a gap:
+// in the order in which the lanes of a wave (lane 16g + c) hold them as operands of v_mfma_f32_16x16x32_bf16, so that every load of codes is
+// 16 bytes per lane and 1 KB per instruction without a gap:
 //   K: MFMA row c of tile u is token 16u + c, and lane group g has dimensions hd/4 g .. hd/4 (g + 1) of it, for head
 //      dimension 128 one scale block.  K scales: byte u of the lane's word is tile u's.
 //   V: MFMA row c has dimensions hd/16 c .. hd/16 (c + 1) (one tile for each), and lane group g has tokens
@@ -101,7 +101,7 @@ struct KvqSeq {
 };
 RP_HD int kvq_clamp(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
 RP_HD int kvq_max_rows(const KvqBatch& bt) { return bt.row_off ? bt.max_rows : 1; }
-RP_HD KvqSeq kvq_seq(const KvqBatch& bt, int b) {
+RP_HD KvqSeq kvq_rows(const KvqBatch& bt, int b) {  // the rows alone
   KvqSeq s;
   if (bt.row_off) {
     s.r0 = kvq_clamp(bt.row_off[b], 0, bt.n_rows);
@@ -110,54 +110,52 @@ RP_HD KvqSeq kvq_seq(const KvqBatch& bt, int b) {
     s.r0 = b < bt.n_rows ? b : bt.n_rows;
     s.n = b < bt.n_rows ? 1 : 0;
   }
+  s.ctx = 0;
+  s.ok = s.n <= kvq_max_rows(bt);
+  if (!s.ok) s.n = kvq_max_rows(bt);
+  return s;
+}
+RP_HD KvqSeq kvq_seq(const KvqBatch& bt, int b) {
+  KvqSeq s = kvq_rows(bt, b);
   s.ctx = bt.context[b];
-  s.ok = s.ctx >= 0 && s.ctx <= bt.max_context && s.n <= kvq_max_rows(bt);
-  if (s.n > kvq_max_rows(bt)) s.n = kvq_max_rows(bt);
+  s.ok = s.ok && s.ctx >= 0 && s.ctx <= bt.max_context;
   return s;
 }
 
-// ---- the plan of attention -----------------------------------------------------------
+// ---- how attention is cut --------------------------------------------------------------
 //
-// Work is counted in tiles: `cols` consecutive columns of a sequence and KV head, a column being one query
-// head of one row.  A tile's pages are cut into items of `ppi` pages, which blocks take; more than one item per tile
-// leaves partial outputs, which a second kernel joins.  Contexts are in device memory, so every block computes the plan
-// from them by itself (the lanes of a wave price 64 sizes at once), and a captured graph follows the contexts
-// that it finds at its replay.
+// Work is counted in tiles: 16 columns of a sequence and KV head, a column being one query head of one row (the G
+// heads of a row side by side).  A tile's pages are cut into items, which blocks take; more than one item leaves partial
+// outputs, which a second kernel joins.  Contexts are in device memory: the host bounds the items of a tile from the
+// call's bounds, and a block counts its tile's from the context it finds, so that a captured graph follows them.
 
+constexpr int kKvqCols = 16;
 constexpr int kKvqTileItems = 64;  // items of one tile at most: the join holds one per lane
-// Items beyond one per tile, for all KV heads together: bounds the workspace.  ppi >= pages / this keeps to it.
-constexpr int kKvqExtraItems = 2048;
 
-struct KvqPlanInput {
-  int64_t tile_pages = 0;  // sum over tiles of their pages, one KV head
-  int tiles = 0;           // of one KV head
-  int max_pages = 0;       // of any tile
+// Pages of `keys` keys; the items of a tile of so many pages, at most `most` of them and none below `least` pages unless
+// it is the only one; the pages of an item.
+RP_HD int kvq_pages(int keys) { return (keys + kKvqPage - 1) / kKvqPage; }
+RP_HD int kvq_items(int pages, int most, int least) {
+  const int n = (pages + least - 1) / least;
+  return n < 1 ? 1 : n < most ? n : most;
+}
+RP_HD int kvq_item_pages(int pages, int items) { return items == 1 ? pages : (pages + items - 1) / items; }
+
+RP_HD int kvq_tiles(const KvqSeq& s, int group) { return (s.n * group + kKvqCols - 1) / kKvqCols; }
+
+// A tile of a sequence: its columns, the position of the sequence's first row, and the keys that some column sees.
+struct KvqTile {
+  int cols, first, end;
 };
-
-// Price of items of ppi pages, in us.  A block's waves take a page in page_us between them, and its ends (plan, first
-// loads, combining its waves) take ends_us; joining is a second launch.
-RP_HD float kvq_price(const KvqPlanInput& in, int n_kv, int ppi, float page_us, float ends_us, float join_us) {
-  const bool join = ppi < in.max_pages;
-  const float pages = static_cast<float>(in.tile_pages);
-  const float items = (join ? pages / ppi + 0.5f * in.tiles : static_cast<float>(in.tiles)) * n_kv;
-  const float one = (ppi < in.max_pages ? ppi : in.max_pages) * page_us + ends_us;
-  const float all = (pages * n_kv * page_us + items * ends_us) * (1.f / 256.f);
-  const float even = all + 0.5f * one;  // past a block per CU the CUs even out to half an item
-  return (items <= 256.f ? one : (one > even ? one : even)) + (join ? join_us : 0.f);
+RP_HD KvqTile kvq_tile(const KvqSeq& s, int group, int tile) {
+  KvqTile t;
+  const int j0 = tile * kKvqCols, left = s.n * group - j0;
+  t.cols = left < kKvqCols ? left : kKvqCols;
+  t.first = s.ctx - s.n;
+  const int end = t.first + (j0 + t.cols - 1) / group + 1;
+  t.end = s.ok && end > 0 ? end : 0;
+  return t;
 }
-
-// The least size allowed, and candidate i of 64 (a geometric ladder from there to whole tiles).
-RP_HD int kvq_least_ppi(const KvqPlanInput& in, int n_kv) {
-  const int64_t extra = kKvqExtraItems / n_kv > 1 ? kKvqExtraItems / n_kv : 1;
-  const int64_t a = (in.tile_pages + extra - 1) / extra, b = (in.max_pages + kKvqTileItems - 1) / kKvqTileItems;
-  const int64_t l = a > b ? a : b;
-  return l < 1 ? 1 : l > in.max_pages ? (in.max_pages > 1 ? in.max_pages : 1) : static_cast<int>(l);
-}
-
-// Pages of the keys that a sequence's rows see, its tiles, and the items of one tile.
-RP_HD int kvq_pages(const KvqSeq& s) { return s.ok ? (s.ctx + kKvqPage - 1) / kKvqPage : 0; }
-RP_HD int kvq_tiles(const KvqSeq& s, int group, int cols) { return (s.n * group + cols - 1) / cols; }
-RP_HD int kvq_items(int pages, int ppi) { return pages <= ppi ? 1 : (pages + ppi - 1) / ppi; }
 
 struct KvqAttendArgs {
   KvqCache cache;
@@ -165,25 +163,18 @@ struct KvqAttendArgs {
   KvqTensor q, out;
   int n_q = 0;
   float scale = 1.f;
-  // workspace: per item and KV head [tile_cols, hd] partial outputs, [2, tile_cols] maxima and sums
-  int64_t items = 0;  // that it holds, and that are launched
+  // workspace: per item and KV head [16, hd] partial outputs, [2, 16] maxima and sums
   float* part_o = nullptr;
   float* part_ml = nullptr;
 };
 
-// Tiles that a batch has at most (of one KV head), for tiles of `cols` columns.
-inline int64_t kvq_tile_bound(const KvqBatch& b, int group, int cols) {
-  const int64_t rows = b.row_off ? b.n_rows : (b.n_rows < b.n_seqs ? b.n_rows : b.n_seqs);
-  const int64_t per_seq = (static_cast<int64_t>(kvq_max_rows(b)) * group + cols - 1) / cols;
-  const int64_t by_rows = rows * group / cols + b.n_seqs, by_seqs = per_seq * b.n_seqs;
+// Tiles that a batch has at most (of one KV head).  Up to 16 columns a sequence: one each.
+inline bool kvq_one_tile(const KvqBatch& b, int group) { return static_cast<int64_t>(kvq_max_rows(b)) * group <= kKvqCols; }
+inline int64_t kvq_tile_bound(const KvqBatch& b, int group) {
+  if (kvq_one_tile(b, group)) return b.n_seqs;
+  const int64_t per_seq = (static_cast<int64_t>(kvq_max_rows(b)) * group + kKvqCols - 1) / kKvqCols;
+  const int64_t by_rows = static_cast<int64_t>(b.n_rows) * group / kKvqCols + b.n_seqs, by_seqs = per_seq * b.n_seqs;
   return by_rows < by_seqs ? by_rows : by_seqs;
-}
-inline int64_t kvq_item_bound(const KvqBatch& b, int n_kv, int group, int cols) {
-  const int64_t tiles = kvq_tile_bound(b, group, cols);
-  const int64_t pages = (static_cast<int64_t>(b.max_context) + kKvqPage - 1) / kKvqPage;
-  const int64_t extra = kKvqExtraItems / n_kv > 1 ? kKvqExtraItems / n_kv : 1;
-  const int64_t most = tiles * (pages > 1 ? pages : 1);
-  return tiles + extra < most ? tiles + extra : most;
 }
 // Bytes of the workspace of launch_kvq_attend.
 size_t kvq_attend_bytes(const KvqCache& c, const KvqBatch& b, int n_q);

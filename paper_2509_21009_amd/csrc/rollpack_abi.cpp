@@ -188,6 +188,7 @@ rp_status kvq_rows_call(const rp_kvq_cache* cache, const rp_kvq_batch* batch, co
     const rollpack::KvqCache c = kvq_cache(cache, true);
     const rollpack::KvqBatch b = kvq_batch(batch, true);
     if (b.n_seqs == 0 || b.n_rows == 0) return;
+    kvq_require(static_cast<int64_t>(b.n_rows) * c.n_kv <= (int64_t{1} << 26), "too many rows and heads for one call");
     const rollpack::KvqTensor kt = kvq_tensor(k, b.n_rows, c.n_kv, c.hd, written);
     const rollpack::KvqTensor vt = kvq_tensor(v, b.n_rows, c.n_kv, c.hd, written);
     kvq_require(kt.bf16 == vt.bf16, "k and v must have one dtype");
@@ -201,7 +202,7 @@ size_t kvq_attend_size(const rollpack::KvqCache& c, const rollpack::KvqBatch& b,
   kvq_require(n_q >= 1 && n_q <= 65536 && n_q % c.n_kv == 0, "n_q_heads must be a multiple of n_kv_heads");
   const int64_t group = n_q / c.n_kv;
   kvq_require(static_cast<int64_t>(b.row_off ? b.max_rows : 1) * group < (int64_t{1} << 30) &&
-                  rollpack::kvq_item_bound(b, c.n_kv, static_cast<int>(group), 16) * c.n_kv < (int64_t{1} << 31),
+                  rollpack::kvq_tile_bound(b, static_cast<int>(group)) < (int64_t{1} << 22),
               "too many rows and heads for one call");
   return rollpack::kvq_attend_bytes(c, b, n_q);
 }

@@ -61,8 +61,8 @@ static void scales() {
   assert(kvq_scale_byte(0) == 2 && kvq_scale_byte(0x7f800000u) == 255 && kvq_scale_byte(0x7fc00000u) == 255);
 }
 
-// Device values out of bounds are neither followed nor counted; the items of every size that the plan may choose fit the
-// bound that the launch and the workspace are made for.
+// Device values out of bounds are not followed; tiles fit the bound that the launch and the workspace are made for, and
+// a tile's items have each of its pages once.
 static void batches() {
   std::mt19937 rng(11);
   auto pick = [&](int lo, int hi) { return lo + static_cast<int>(rng() % static_cast<uint32_t>(hi - lo + 1)); };
@@ -70,7 +70,7 @@ static void batches() {
   c.n_pages = 10;
   assert(!kvq_page_ok(c, -1) && kvq_page_ok(c, 0) && kvq_page_ok(c, 9) && !kvq_page_ok(c, 10) && !kvq_page_ok(c, 0x7fffffff));
   for (int round = 0; round < 4000; ++round) {
-    const int n = pick(1, round % 3 ? 12 : 300), group = pick(1, 40), n_kv = pick(1, 9) * (round % 7 ? 1 : 100);
+    const int n = pick(1, round % 3 ? 12 : 300), group = pick(1, 40);
     const bool wild = round % 5 == 0;
     std::vector<int32_t> off(n + 1), ctx(n);
     KvqBatch b;
@@ -92,37 +92,28 @@ static void batches() {
     b.context = ctx.data();
     bool ascending = true;
     for (int i = 0; i < n; ++i) ascending = ascending && off[i] >= 0 && off[i + 1] >= off[i] && off[i + 1] <= b.n_rows;
-    KvqPlanInput in;
-    std::vector<int> pages(n), tiles(n);
+    int64_t tiles = 0;
+    const int most = pick(1, kKvqTileItems), least = pick(1, 20);
     for (int i = 0; i < n; ++i) {
       const KvqSeq s = kvq_seq(b, i);
       assert(s.r0 >= 0 && s.n >= 0 && s.r0 + s.n <= b.n_rows);
       assert(s.n <= kvq_max_rows(b) && (!s.ok || (s.ctx >= 0 && s.ctx <= b.max_context)));
-      pages[i] = kvq_pages(s);
-      assert(pages[i] >= 0 && static_cast<int64_t>(pages[i]) * kKvqPage < b.max_context + int64_t{kKvqPage});
-      tiles[i] = kvq_tiles(s, group, 16);
-      if (!tiles[i]) pages[i] = 0;
-      in.tile_pages += static_cast<int64_t>(tiles[i]) * pages[i];
-      in.tiles += tiles[i];
-      in.max_pages = std::max(in.max_pages, pages[i]);
-    }
-    const int64_t items = kvq_item_bound(b, n_kv, group, 16), most_tiles = kvq_tile_bound(b, group, 16);
-    assert(items >= most_tiles || b.max_context <= kKvqPage);
-    if (!ascending && b.row_off) continue;
-    assert(in.tiles <= most_tiles);
-    const int least = kvq_least_ppi(in, n_kv), most = std::max(1, in.max_pages);
-    assert(least >= 1 && least <= most);
-    for (int ppi = least;; ppi += std::max(1, (most - least) / 20)) {
-      ppi = std::min(ppi, most);
-      int64_t sum = 0;
-      for (int i = 0; i < n; ++i) {
-        const int k = kvq_items(pages[i], ppi);
-        assert(k >= 1 && k <= kKvqTileItems && (pages[i] <= ppi) == (k == 1));
-        sum += static_cast<int64_t>(tiles[i]) * k;
+      const int nt = kvq_tiles(s, group);
+      assert(!kvq_one_tile(b, group) || nt <= 1);
+      for (int t = 0; t < nt; ++t) {
+        const KvqTile tl = kvq_tile(s, group, t);
+        assert(tl.cols >= 1 && tl.cols <= kKvqCols && t * kKvqCols + tl.cols <= s.n * group);
+        assert(tl.end >= 0 && tl.end <= b.max_context && (s.ok || tl.end == 0) && (!s.ok || tl.end <= s.ctx));
+        if (t + 1 == nt && s.ok) assert(tl.end == s.ctx);
+        const int pages = kvq_pages(tl.end), items = kvq_items(pages, most, least), per = kvq_item_pages(pages, items);
+        assert(items >= 1 && items <= most && (items == 1 || pages > least));
+        int sum = 0;
+        for (int k = 0; k < items; ++k) sum += std::max(0, std::min(per, pages - k * per));
+        assert(sum == pages);
       }
-      assert(sum <= items);
-      if (ppi == most) break;
+      tiles += nt;
     }
+    if (ascending || !b.row_off) assert(tiles <= kvq_tile_bound(b, group));
   }
 }
 

@@ -92,7 +92,7 @@ def test_read_refuses_overlapping_outputs(lib):
 
 def test_attend_refuses_bad_arguments(lib):
     big = 1 << 40
-    ok = dict(cache=_cache(), batch=_batch(), n_q=6, scale=0.1, q=_tensor(6), out=_tensor(6, data=2 * PTR), ws=4 * PTR, n=big)
+    ok = dict(cache=_cache(), batch=_batch(max_context=1 << 13, table_stride=1 << 7), n_q=6, scale=0.1, q=_tensor(6), out=_tensor(6, data=2 * PTR), ws=4 * PTR, n=big)
 
     def call(**kw):
         a = {**ok, **kw}
@@ -102,7 +102,7 @@ def test_attend_refuses_bad_arguments(lib):
     cases += [dict(q=_tensor(6, **b)) for b in BAD_TENSORS]
     cases += [dict(out=_tensor(6, **{**dict(data=2 * PTR), **b})) for b in BAD_TENSORS + OVERLAPS]
     cases += [dict(n_q=n) for n in (0, -2, 7, 65538)] + [dict(scale=s) for s in (0.0, -0.1, float("nan"), float("inf"))]
-    need = rp.rp_kvq_attend_workspace(_cache(), _batch(), 6)
+    need = rp.rp_kvq_attend_workspace(_cache(), ok["batch"], 6)
     assert need > 0
     cases += [dict(out=_tensor(6)), dict(out=_tensor(6, data=2 * PTR, dtype=0)), dict(ws=0), dict(ws=4 * PTR + 16), dict(n=need - 1),
               dict(cache=None), dict(batch=None), dict(q=None), dict(out=None)]
@@ -111,8 +111,9 @@ def test_attend_refuses_bad_arguments(lib):
     for kw in (dict(batch=_batch(max_rows=-1)), dict(n_q=7), dict(cache=_cache(head_dim=80))):
         a = {**ok, **kw}
         _refused(rp.rp_kvq_attend_workspace, a["cache"], a["batch"], a["n_q"])
-    # more work items than a launch can have
-    _refused(rp.rp_kvq_attend_workspace, _cache(n_kv_heads=1024), _batch(n_rows=1 << 24, n_seqs=1 << 20, max_rows=1 << 24, max_context=256), 65536)
+    # more blocks than a launch can have
+    _refused(rp.rp_kvq_append, _cache(n_kv_heads=1024), _batch(n_rows=(1 << 16) + 1), _tensor(1024), _tensor(1024, data=2 * PTR), 0)
+    _refused(rp.rp_kvq_attend_workspace, _cache(n_kv_heads=1024), _batch(n_rows=1 << 24, n_seqs=1 << 20, max_rows=1 << 24, max_context=256), 1 << 16)
 
 
 def test_empty_batches_do_nothing(lib):
@@ -126,8 +127,8 @@ def test_empty_batches_do_nothing(lib):
 def test_workspace_is_bounded(lib):
     """Long contexts do not grow it without end, and a context of a page needs none."""
     c = _cache(n_kv_heads=4)
-    one = rp.rp_kvq_attend_workspace(c, _batch(n_seqs=1, n_rows=1, row_offsets=0, max_context=1 << 20), 28)
-    assert one <= (512 + 1) * 4 * (16 * 128 + 32) * 4
+    one = rp.rp_kvq_attend_workspace(c, _batch(n_seqs=1, n_rows=1, row_offsets=0, max_context=1 << 20, table_stride=1 << 14), 28)
+    assert 0 < one <= 64 * 4 * (16 * 128 + 32) * 4
     assert rp.rp_kvq_attend_workspace(c, _batch(n_seqs=64, n_rows=64, row_offsets=0, max_context=64), 28) == 0
 
 
