@@ -1,6 +1,7 @@
 // The KV cache held in 4 bits (kvq.hpp has its format): quantising rows into it, reading them back, and
 // causal GQA attention over it.
 #include <algorithm>
+#include <type_traits>
 
 #include "device_common.hpp"
 #include "kernels.hpp"
@@ -15,6 +16,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // ---- the batch -----------------------------------------------------------------------
 
@@ -347,39 +350,66 @@ struct Query {
   }
 };
 
-// O^T += V^T P^T over tokens 32h .. 32h + 31 of the page: accumulator i's rows are dimensions hd/16 c + i.
-template <int HD, int NP>
-__device__ __forceinline__ void half_values(const PageV<HD>& pg, int h, const bf16x8_t (&pf)[NP], f32x4_t (&o)[HD / 16]) {
+// The two values of byte `i` of a word of codes, packed as the type's operand.
+template <bool HALF>
+__device__ __forceinline__ uint32_t value_pair(uint32_t w, float s, int i) {
+  if constexpr (HALF) {
+    return __builtin_bit_cast(uint32_t, i == 0   ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 0)
+                                        : i == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 1)
+                                        : i == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 2)
+                                                 : __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 3));
+  } else {
+    return i == 0 ? code_pair<0>(w, s) : i == 1 ? code_pair<1>(w, s) : i == 2 ? code_pair<2>(w, s) : code_pair<3>(w, s);
+  }
+}
+
+// O^T += V^T P^T over tokens 32h .. 32h + 31 of the page: accumulator i's rows are dimensions hd/16 c + i.  x: the
+// lane's eight probabilities.  HALF: V and P in fp16, P rounded to it; else V in bf16 and P as NP pieces of it.
+template <int HD, bool HALF, int NP>
+__device__ __forceinline__ void half_values(const PageV<HD>& pg, int h, float (&x)[8], f32x4_t (&o)[HD / 16]) {
+  bf16x8_t pf[NP];
+  f16x8 ph;
+  if constexpr (HALF) {
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x[2 * i], x[2 * i + 1]}, f16x2));
+    ph = __builtin_bit_cast(f16x8, w);
+  } else {
+    split8<NP>(x, pf);
+  }
 #pragma unroll
   for (int j = 0; j < HD / 32; ++j) {  // a pair of dimensions
-    uint32_t x[8];                     // of eight tokens
+    uint32_t v[8];                     // of eight tokens
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const float s = scale_of(pg.s[2 * h + (k >> 2)], k & 3);
       const uint32_t w = HD == 128 ? pg.v[2 * h + (k >> 2)][k & 3] : pg.v[h][k >> 1];
-      const int byte = HD == 128 ? j : 2 * (k & 1) + j;
-      x[k] = byte == 0 ? code_pair<0>(w, s) : byte == 1 ? code_pair<1>(w, s) : byte == 2 ? code_pair<2>(w, s) : code_pair<3>(w, s);
+      v[k] = value_pair<HALF>(w, scale_of(pg.s[2 * h + (k >> 2)], k & 3), HD == 128 ? j : 2 * (k & 1) + j);
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {  // its two dimensions: the low or high halves of neighbouring tokens' pairs
       u32x4 w;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], i ? 0x07060302u : 0x05040100u);
+      for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_perm(v[2 * e + 1], v[2 * e], i ? 0x07060302u : 0x05040100u);
+      if constexpr (HALF) {
+        o[2 * j + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, w), ph, o[2 * j + i], 0, 0, 0);
+      } else {
 #pragma unroll
-      for (int n = 0; n < NP; ++n) o[2 * j + i] = mfma16x16x32(__builtin_bit_cast(bf16x8_t, w), pf[n], o[2 * j + i]);
+        for (int n = 0; n < NP; ++n) o[2 * j + i] = mfma16x16x32(__builtin_bit_cast(bf16x8_t, w), pf[n], o[2 * j + i]);
+      }
     }
   }
 }
 
-// Whether any value block of the page may hold NaN: a scale byte of 192 or more (2^65), which is 255 or next to never met.
-__device__ __forceinline__ bool may_be_nan(const u32x4& s) {
+// Whether fp16 holds every value of these blocks exactly: scale bytes 104 .. 135 (2^-23 .. 2^8).  A byte that carries into
+// the next is out of range itself.
+__device__ __forceinline__ bool fits_half(const u32x4& s) {
   uint32_t t = 0;
 #pragma unroll
-  for (int u = 0; u < 4; ++u) t |= s[u] & (s[u] << 1);
-  return t & 0x80808080u;
+  for (int u = 0; u < 4; ++u) t |= (s[u] + 0x18181818u) ^ 0x80808080u;
+  return !(t & 0xe0e0e0e0u);
 }
 
-// Such a page: the scales of NaN blocks become 2^-127, which the zero probability of a key out of sight clears (as NaN it
+// A page with NaN blocks: their scales become 2^-127, which the zero probability of a key out of sight clears (as NaN it
 // would not), and the lane's outputs turn NaN if its column sees the token.  A lane's outputs all lie in one block of 32
 // dimensions.
 template <int HD>
@@ -404,14 +434,15 @@ __device__ __forceinline__ void nan_values(PageV<HD>& pg, const char* block, int
 // S^T = K Q^T, an online softmax in the log2 domain and O^T += V^T P^T with MFMA, straight from registers: no
 // value of the cache is used by more than one wave, so nothing passes through LDS but the waves' results.  The next
 // page's K is loaded when the scores are formed, its V when the outputs are.
-//   P is an operand in bf16: two pieces of it (16 bits), so that the output's own rounding is the only one that
-// counts; three for fp32.
+//   P is an operand rounded to fp16 (2^-12 of it; to 2^-25 below 2^-14), V exact in it: less than the output's own
+// rounding to bf16, where P in bf16 would add as much again.  Pages with values that fp16 does not hold, and fp32, take
+// bf16: P in two pieces, or three.
 //   The running maximum moves only when a score passes it by more than 2^8: probabilities up to 256 lose nothing in
 // fp32 or bf16, the outputs need rescaling a few times per item instead of every page, and no page waits for a maximum
 // over lanes.
 template <int HD, bool F32, int NW>
 __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendArgs a, Cut sh) {
-  constexpr int NT = HD / 16, OLD = HD + 4, NP = F32 ? 3 : 2;
+  constexpr int NT = HD / 16, OLD = HD + 4;
   __shared__ __attribute__((aligned(16))) float so[NW][16 * OLD];
   __shared__ float sm[NW][16], sl[NW][16];
   const KvqBatch& bt = a.batch;
@@ -454,67 +485,75 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendAr
       return base + static_cast<size_t>(lost_next ? 0 : id) * n_kv * bytes;
     };
     Query<HD, F32 ? 3 : 1> qf;
-    PageK<HD> pk;
-    PageV<HD> pv;
-    const char* at = block_of(0);
-    lost = lost_next;
-    pk.load(at);
     qf.load(a.q, sq.r0 + row, head);
-    pv.load(at);
-    for (int i = 0; i < nw; ++i) {
-      const int tok0 = (p0 + wave + NW * i) * kKvqPage;
-      f32x4_t s[4];
+    int i = 0;
+    // The wave's pages from i on.  HALF: V and P in fp16, up to the first page that does not fit; else in bf16.
+    auto walk = [&](auto half_tag) {
+      constexpr bool HALF = half_tag.value;
+      PageK<HD> pk;
+      PageV<HD> pv;
+      const char* at = block_of(i);
+      lost = lost_next;
+      pk.load(at);
+      pv.load(at);
+      for (; i < nw; ++i) {
+        const int tok0 = (p0 + wave + NW * i) * kKvqPage;
+        f32x4_t s[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) s[u] = qf.scores(pk, u);
-      const char* next = block_of(i + 1);
-      pk.load(next);
-      if (lost || tok0 + kKvqPage > open) {
+        for (int u = 0; u < 4; ++u) s[u] = qf.scores(pk, u);
+        const char* next = block_of(i + 1);
+        pk.load(next);
+        if (tok0 + kKvqPage > tl.end) {  // what lies behind the last key may be anything
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int n = min(max(tl.end - (tok0 + 16 * u + 4 * g), 0), 4);
+            const uint32_t keep = static_cast<uint32_t>((1ull << (8 * n)) - 1);
+            pv.s[u] = (pv.s[u] & keep) | (0x7f7f7f7fu & ~keep);
+          }
+        }
+        if (HALF && !__all(fits_half(pv.s))) return;
+        if (lost || tok0 + kKvqPage > open) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float v = lost ? __builtin_nanf("") : s[u][e];
+              s[u][e] = tok0 + 16 * u + 4 * g + e > lim ? -INFINITY : v;
+            }
+        }
+        float top = -INFINITY;
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float v = lost ? __builtin_nanf("") : s[u][e];
-            s[u][e] = tok0 + 16 * u + 4 * g + e > lim ? -INFINITY : v;
-          }
-      }
-      float top = -INFINITY;
+          for (int e = 0; e < 4; ++e) top = fmaxf(top, s[u][e]);
+        top *= scale_log2;
+        if (__any(top > m_run + 8.f)) {
+          top = fmaxf(top, __shfl_xor(top, 16, 64));
+          top = fmaxf(top, __shfl_xor(top, 32, 64));
+          const float m_new = top > m_run + 8.f ? top : m_run;
+          const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+          l_run *= alpha;
+          m_run = m_new;
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) top = fmaxf(top, s[u][e]);
-      top *= scale_log2;
-      if (__any(top > m_run + 8.f)) {
-        top = fmaxf(top, __shfl_xor(top, 16, 64));
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float m_new = top > m_run + 8.f ? top : m_run;
-        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
-        l_run *= alpha;
-        m_run = m_new;
-#pragma unroll
-        for (int t = 0; t < NT; ++t) o[t] *= alpha;
-      }
-      const float shift = m_run == -INFINITY ? 0.f : m_run;
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s[u][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e], scale_log2, -shift));
-          l_run += s[u][e];  // of this lane's tokens; the lanes of a column add up at the end
+          for (int t = 0; t < NT; ++t) o[t] *= alpha;
         }
-      if (__any(may_be_nan(pv.s))) nan_values<HD>(pv, at, tok0, lim, o);
+        const float shift = m_run == -INFINITY ? 0.f : m_run;
+        float x[2][8];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float x[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = s[2 * h + (k >> 2)][k & 3];
-        bf16x8_t pf[NP];
-        split8<NP>(x, pf);
-        half_values<HD, NP>(pv, h, pf, o);
+        for (int k = 0; k < 16; ++k) {
+          x[k >> 3][k & 7] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k >> 2][k & 3], scale_log2, -shift));
+          l_run += x[k >> 3][k & 7];  // of this lane's tokens; the lanes of a column add up at the end
+        }
+        if (!HALF && !__all(fits_half(pv.s))) nan_values<HD>(pv, at, tok0, lim, o);
+        half_values<HD, HALF, F32 ? 3 : 2>(pv, 0, x[0], o);
+        half_values<HD, HALF, F32 ? 3 : 2>(pv, 1, x[1], o);
+        at = next;
+        lost = lost_next;
+        pv.load(at);
       }
-      at = next;
-      lost = lost_next;
-      pv.load(at);
-    }
+    };
+    if constexpr (!F32) walk(std::true_type{});
+    if (F32 || i < nw) walk(std::false_type{});
     l_run += __shfl_xor(l_run, 16, 64);
     l_run += __shfl_xor(l_run, 32, 64);
   }

@@ -9,6 +9,7 @@
 //   s is the least power of two with amax <= 7 s: up to 7 s the code 6 is at most s off, which is also the half
 //   step of the codes below it, so a larger scale would lose more in the small elements than it gains in the largest.
 //   2^-125 <= s <= 2^125 keeps every value a normal bf16 number (or zero); amax above 7 * 2^125 saturates at 6 * 2^125.
+//   A block of zeros has s = 1.
 //   A block that holds an infinity or a NaN gets b = 255 and reads as NaN.
 //   A code is the nearest one, ties to the one with the even mantissa (v_cvt_scalef32_pk_fp4_f32's rounding).
 //
@@ -60,6 +61,7 @@ RP_HD int kvq_v_scale(int t, int i, int hd) {
 // The scale byte of a block whose largest magnitude has these fp32 bits (sign clear).
 RP_HD uint32_t kvq_scale_byte(uint32_t amax_bits) {
   if (amax_bits >= 0x7f800000u) return 255;
+  if (amax_bits == 0) return 127;
   // amax = m 2^e, 1 <= m < 2: the scale's exponent is e - 2 for m <= 1.75 and e - 1 above; the carry tells them apart
   const int b = static_cast<int>((amax_bits + 0x1fffffu) >> 23) - 2;
   return static_cast<uint32_t>(b < 2 ? 2 : b > 252 ? 252 : b);

@@ -58,7 +58,7 @@ static void scales() {
     std::memcpy(&a, &bits, 4);
     check(a);
   }
-  assert(kvq_scale_byte(0) == 2 && kvq_scale_byte(0x7f800000u) == 255 && kvq_scale_byte(0x7fc00000u) == 255);
+  assert(kvq_scale_byte(0) == 127 && kvq_scale_byte(1) == 2 && kvq_scale_byte(0x7f800000u) == 255 && kvq_scale_byte(0x7fc00000u) == 255);
 }
 
 // Device values out of bounds are not followed; tiles fit the bound that the launch and the workspace are made for, and

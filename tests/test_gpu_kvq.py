@@ -8,7 +8,9 @@ Attention's bar comes from its roundings.  With u = 2^-24 and ctx keys, hd dimen
            exponential 2^-21.  A probability is then off by the factor 1 + e_p, e_p = (hd + 6) u T + 2^-21,
            T the largest sum |q||k| scale; numerator and denominator both have it.
   sums     over keys, ctx additions and their products in fp32: (ctx + 64) u, twice.
-  P        in pieces of bf16: two hold 16 bits, 2^-16 (bf16), three 24, 2^-24 (fp32).
+  P        bf16 queries: rounded to fp16, 2^-11 of it, and where fp16 is subnormal 2^-25 for every key, the
+           probabilities being at least 1 in sum (of pages with values beyond fp16: two pieces of bf16,
+           2^-16).  fp32: three pieces of bf16, 2^-24.
   output   half a step: 2^-8 of the value in bf16, 2^-24 in fp32.
 All but the last are relative to sum p|v|.
 """
@@ -26,14 +28,15 @@ if not torch.cuda.is_available():
 
 DEV = torch.device("cuda:0")
 TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
-P_BITS = {"f32": 2.0 ** -24, "bf16": 2.0 ** -16}
+P_BITS = {"f32": 2.0 ** -24, "bf16": 2.0 ** -11}
 
 
-def _bound(ref, mag, top, ctx, hd, dtype):
+def _bound(ref, mag, top, ctx, hd, dtype, vmax=0.0):
     u = 2.0 ** -24
     e_p = (hd + 6) * u * top[..., None] + 2.0 ** -21
     out = 2.0 ** -8 if dtype == "bf16" else u
-    return out * np.abs(ref) * (1 + 2.0 ** -7) + mag * (2 * e_p + 2 * (ctx + 64) * u + P_BITS[dtype]) * 1.01 + 1e-37
+    return out * np.abs(ref) * (1 + 2.0 ** -7) + mag * (2 * e_p + 2 * (ctx + 64) * u + P_BITS[dtype]) * 1.01 \
+        + (ctx * vmax * 2.0 ** -25 if dtype == "bf16" else 0.0) + 1e-37
 
 
 def _f64(t):
@@ -93,7 +96,7 @@ class Setup:
             if n and (seqs is None or b in seqs):
                 pos = np.arange(c - n, c)
                 ref, mag, top = okvq.attend(q[at:at + n], *held[b], pos, self.hd ** -0.5)
-                err, bar = np.abs(out[at:at + n] - ref), _bound(ref, mag, top, c, self.hd, self.dtype)
+                err, bar = np.abs(out[at:at + n] - ref), _bound(ref, mag, top, c, self.hd, self.dtype, np.nanmax(np.abs(held[b][1]), initial=0))
                 assert (err <= bar).all(), (b, c, n, float((err / bar).max()), np.argwhere(~(err <= bar))[:4].tolist())
                 worst = max(worst, float((err / bar).max()))
             at += n
@@ -317,7 +320,7 @@ def test_nan_and_infinities_reach_only_rows_that_see_them(hd, rows):
             want[pos >= 1195, :3, hd - 32:] = True
         got = out[at:at + n]
         assert np.array_equal(np.isnan(got), want), b
-        bar = _bound(ref, mag, top, c, hd, "bf16")
+        bar = _bound(ref, mag, top, c, hd, "bf16", np.abs(clean[b][1]).max())
         assert (np.abs(got - ref)[~want] <= bar[~want]).all(), b
         at += n
     q = s.q.clone()
@@ -335,6 +338,20 @@ def test_large_scores_do_not_overflow():
         out = _f64(s.cache.attend(s.batch(), s.q))
         assert np.isfinite(out).all()
         s.q *= 0  # every key alike: the mean of the values
+        s.check(s.cache.attend(s.batch(), s.q))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_values_beyond_half_precision(hd):
+    """Value blocks that fp16 does not hold, tiny and huge, among ordinary ones; keys likewise."""
+    for dtype in ("bf16", "f32"):
+        s = Setup(7, 1, hd, [700, 130, 64, 200], rows=[1, 130, 3, 1], dtype=dtype, seed=21)
+        s.v[5::64] *= 2.0 ** 20
+        s.v[9::32, :, :32] *= 2.0 ** -40
+        s.v[700:830] *= 2.0 ** -30
+        s.v[830:894] *= 2.0 ** 90
+        s.k[3::16] *= 2.0 ** -20
+        s.fill()
         s.check(s.cache.attend(s.batch(), s.q))
 
 
