@@ -226,13 +226,6 @@ __global__ __launch_bounds__(256) void k_kvq_read(KvqCache c, KvqBatch bt, KvqTe
   store8<BF16>(v, p.row, p.kh, p.d, vf);
 }
 
-// How a launch cuts its tiles.
-struct Cut {
-  int find;   // tiles are found by their sequences' rows (0: tile b is sequence b's only one)
-  int items;  // of a tile at most
-  int least;  // pages of an item, unless it is its tile's only one
-};
-
 // ---- which tile a block has ------------------------------------------------------------
 
 // Sums over the wave's lanes up to each lane, in six additions across lanes.
@@ -246,21 +239,21 @@ __device__ __forceinline__ int wave_scan(int x) {
   return x;
 }
 
-// Tile `index` of the batch: its sequence (-1 past the last) and which of the sequence's.  Each wave finds it for itself;
+// Tile `index` of the cut: its sequence (-1 past the last) and which of the sequence's.  Each wave finds it for itself;
 // lane l counts the sequences l per .. (l + 1) per - 1.
-__device__ __forceinline__ int find_tile(const KvqBatch& bt, int group, int index, int& tile) {
+__device__ __forceinline__ int find_tile(const KvqBatch& bt, int group, const KvqCut& cut, int index, int& tile) {
   const int lane = threadIdx.x & 63;
   const int per = (bt.n_seqs + 63) >> 6, b0 = lane * per, b1 = min(b0 + per, bt.n_seqs);
   int mine = 0;
 #pragma unroll 4
-  for (int b = b0; b < b1; ++b) mine += kvq_tiles(kvq_rows(bt, b), group);
+  for (int b = b0; b < b1; ++b) mine += kvq_tiles(kvq_rows(bt, b), group, cut);
   const int scan = wave_scan(mine);
   const uint64_t past = __ballot(scan > index);
   if (!past) return -1;
   const int w = __ffsll(static_cast<unsigned long long>(past)) - 1;
   tile = index - __builtin_amdgcn_readlane(scan - mine, w);
   for (int b = w * per;; ++b) {  // within that lane's sequences
-    const int t = kvq_tiles(kvq_rows(bt, b), group);
+    const int t = kvq_tiles(kvq_rows(bt, b), group, cut);
     if (tile < t) return b;
     tile -= t;
   }
@@ -441,7 +434,7 @@ __device__ __forceinline__ void nan_values(PageV<HD>& pg, const char* block, int
 // fp32 or bf16, the outputs need rescaling a few times per item instead of every page, and no page waits for a maximum
 // over lanes.
 template <int HD, bool F32, int NW>
-__global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendArgs a, Cut sh) {
+__global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendArgs a, KvqCut cut) {
   constexpr int NT = HD / 16, OLD = HD + 4;
   __shared__ __attribute__((aligned(16))) float so[NW][16 * OLD];
   __shared__ float sm[NW][16], sl[NW][16];
@@ -451,12 +444,12 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendAr
   const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
   const int kh = blockIdx.y, split = blockIdx.z;
   int tile = 0;
-  const int b = sh.find ? find_tile(bt, G, blockIdx.x, tile) : static_cast<int>(blockIdx.x);
+  const int b = cut.find ? find_tile(bt, G, cut, blockIdx.x, tile) : static_cast<int>(blockIdx.x);
   if (b < 0) return;
   const KvqSeq sq = kvq_seq(bt, b);
-  const KvqTile tl = kvq_tile(sq, G, tile);
-  const int j0 = tile * kKvqCols, n_cols = tl.cols, first = tl.first;
-  const int pages = kvq_pages(tl.end), items = kvq_items(pages, sh.items, sh.least);
+  const KvqTile tl = kvq_tile(sq, G, tile, cut.cols);
+  const int j0 = tile * 16, n_cols = tl.cols, first = tl.first;
+  const int pages = kvq_pages(tl.end), items = kvq_items(pages, cut.items, cut.least);
   if (n_cols <= 0 || split >= items) return;
   const int per_item = kvq_item_pages(pages, items), p0 = split * per_item;
   const int np = max(0, min(per_item, pages - p0));
@@ -513,6 +506,7 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendAr
         }
         if (HALF && !__all(fits_half(pv.s))) return;
         if (lost || tok0 + kKvqPage > open) {
+          asm volatile("");  // a branch: as selects it would cost every page
 #pragma unroll
           for (int u = 0; u < 4; ++u)
 #pragma unroll
@@ -577,7 +571,7 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendAr
             f32x4_t{o[i][e], o[i + 1][e], o[i + 2][e], o[i + 3][e]} * fac;
   }
   __syncthreads();
-  const int64_t part = (static_cast<int64_t>(blockIdx.x) * sh.items + split) * n_kv + kh;
+  const int64_t part = (static_cast<int64_t>(blockIdx.x) * cut.items + split) * n_kv + kh;
   for (int q = tid; q < n_cols * (HD / 8); q += 64 * NW) {
     const int col = q / (HD / 8), d = q % (HD / 8) * 8;
     float m4 = sm[0][col], den = 0.f, x[8];
@@ -611,35 +605,393 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendAr
   }
 }
 
+// ---- attention of many rows -------------------------------------------------------------
+//
+// A block of NW waves owns 32 NW columns of a sequence and KV head, 32 a wave, and walks the pages that they see.  A page
+// is unpacked once per block, every thread a share of it, into LDS, from where the waves' 32x32x16 MFMAs take it: a wave
+// alone would spend more instructions on unpacking a page than on its softmax.  Two stages of LDS: page p + 1 is unpacked
+// from registers while the block's other waves compute page p, and page p + 2 is on its way to the registers.
+//   S^T = K Q^T in two tiles of 32 tokens: lane 32h + c gets tokens 8i + 4h + 0..3 of each, for column c, which in pairs
+// of i are the operand P^T of a 16-token step of O^T += V^T P^T; V's rows keep the cache's order of tokens, so that
+// nothing moves between lanes.  V's row c + 16 i of tile t is dimension hd/16 c + 2 t + i: the two that one byte holds.
+//   Bound by MFMA and the exponentials, which take about as long; two blocks share a CU, so that one's products run beside
+// the other's softmax.
+
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+
+// One thread's share of a page between its load and LDS (256 threads have a page): 32 codes of K at hd 128, 16 at 64,
+// and of V two dimension pairs (one) of eight tokens.
+template <int HD>
+struct PageShare {
+  static constexpr int KW = HD / 32, VB = HD / 64;  // words of K; bytes of V per token
+  uint32_t k[KW], v[8], ks, vs[2];
+  uint32_t all;  // four value scales of the page, a lane's share of all of them
+  bool lost;
+};
+
+template <int HD>
+__device__ __forceinline__ void share_load(PageShare<HD>& s, const char* block, int th) {
+  {
+    const int u = th >> 6, g = (th >> 4) & 3, c = th & 15;
+    const char* p = block + kvq_k_code(16 * u + c, g * (HD / 4), HD);
+    if constexpr (HD == 128) {
+      const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s.k[i] = w[i];
+    } else {
+      const uint2 w = *reinterpret_cast<const uint2*>(p);
+      s.k[0] = w.x;
+      s.k[1] = w.y;
+    }
+    s.ks = static_cast<unsigned char>(block[kvq_k_scale(16 * u + c, g * (HD / 4) / kKvqBlock, HD)]);
+  }
+  {
+    const int half = th >> 7, u = (th >> 5) & 3, h = (th >> 4) & 1, c = th & 15;
+    (void)half;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {  // token groups h and h + 2 of the tile
+      const char* p = block + kvq_v_code(16 * u + 4 * (h + 2 * e), c * (HD / 16), HD);
+      if constexpr (HD == 128) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s.v[4 * e + i] = w[i];
+      } else {
+        const uint2 w = *reinterpret_cast<const uint2*>(p);
+        s.v[2 * e] = w.x;
+        s.v[2 * e + 1] = w.y;
+      }
+      s.vs[e] = *reinterpret_cast<const uint32_t*>(block + kvq_v_scale(16 * u + 4 * (h + 2 * e), c * (HD / 16) / kKvqBlock, HD));
+    }
+  }
+  s.all = *(reinterpret_cast<const uint32_t*>(block + 66 * HD) + (threadIdx.x & (HD / 2 - 1)));
+}
+
+// Scale bytes of tokens t .. t + 3, those from `end` on as 1: what lies behind the last key may be anything.
+__device__ __forceinline__ uint32_t scales_below(uint32_t s, int t, int end) {
+  const uint32_t keep = static_cast<uint32_t>((1ull << (8 * min(max(end - t, 0), 4))) - 1);
+  return (s & keep) | (0x7f7f7f7fu & ~keep);
+}
+// NaN scales as 2^-127, which a zero probability clears.
+__device__ __forceinline__ uint32_t without_nan(uint32_t s) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (((s >> (8 * r)) & 255u) == 255u) s &= ~(255u << (8 * r));
+  return s;
+}
+
+template <int HD, bool HALF>
+__device__ __forceinline__ void share_values(const PageShare<HD>& s, const uint32_t (&vs)[2], int th, u32x4* lv) {
+  const int half = th >> 7, u = (th >> 5) & 3, h = (th >> 4) & 1, c = th & 15;
+#pragma unroll
+  for (int b = 0; b < HD / 64; ++b) {
+    const int t = HD == 128 ? 2 * half + b : half;  // the tile of dimensions, and the byte of a token's that holds its two
+    uint32_t x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float sc = scale_of(vs[k >> 2], k & 3);
+      if constexpr (HD == 128) {
+        const uint32_t w = half ? s.v[k] >> 16 : s.v[k];
+        x[k] = value_pair<HALF>(w, sc, b);
+      } else {
+        const uint32_t w = half ? s.v[k >> 1] >> 8 : s.v[k >> 1];
+        x[k] = value_pair<HALF>(w, sc, 2 * (k & 1));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      u32x4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], i ? 0x07060302u : 0x05040100u);
+      lv[(t * 4 + u) * 64 + h * 32 + i * 16 + c] = w;
+    }
+  }
+}
+
+// The share into LDS; half: V in fp16.
+template <int HD>
+__device__ __forceinline__ void share_store(const PageShare<HD>& s, int th, int tok0, int end, bool half, u32x4* lk, u32x4* lv) {
+  {
+    const int u = th >> 6, g = (th >> 4) & 3, c = th & 15, t = 16 * u + c;
+    const float sc = scale_of(s.ks, 0);
+#pragma unroll
+    for (int v = 0; v < HD / 32; ++v) {
+      const int d8 = g * (HD / 32) + v;  // eight dimensions
+      const uint32_t w = s.k[v];
+      lk[((t >> 5) * (HD / 16) + (d8 >> 1)) * 64 + (d8 & 1) * 32 + (t & 31)] =
+          u32x4{code_pair<0>(w, sc), code_pair<1>(w, sc), code_pair<2>(w, sc), code_pair<3>(w, sc)};
+    }
+  }
+  const int u = (th >> 5) & 3, h = (th >> 4) & 1, t = tok0 + 16 * u + 4 * h;
+  uint32_t vs[2] = {s.vs[0], s.vs[1]};
+  if (tok0 + kKvqPage > end) {
+    vs[0] = scales_below(vs[0], t, end);
+    vs[1] = scales_below(vs[1], t + 8, end);
+  }
+  if (half) {
+    share_values<HD, true>(s, vs, th, lv);
+  } else {
+    vs[0] = without_nan(vs[0]);
+    vs[1] = without_nan(vs[1]);
+    share_values<HD, false>(s, vs, th, lv);
+  }
+}
+
+// O^T += V^T P^T for a page: x are the lane's 32 probabilities, NP pieces of them in bf16 or one in fp16.
+template <int HD, bool HALF>
+__device__ __forceinline__ void page_values(const u32x4* lv, float (&x)[32], f32x16 (&o)[HD / 32]) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    float y[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) y[k] = x[8 * u + k];
+    f16x8 ph;
+    bf16x8_t pf[2];
+    if constexpr (HALF) {
+      u32x4 w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{y[2 * i], y[2 * i + 1]}, f16x2));
+      ph = __builtin_bit_cast(f16x8, w);
+    } else {
+      split8<2>(y, pf);
+    }
+#pragma unroll
+    for (int t = 0; t < HD / 32; ++t) {
+      const u32x4 v = lv[(t * 4 + u) * 64 + lane];
+      if constexpr (HALF) {
+        o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, v), ph, o[t], 0, 0, 0);
+      } else {
+        o[t] = mfma32x32x16(__builtin_bit_cast(bf16x8_t, v), pf[0], o[t]);
+        o[t] = mfma32x32x16(__builtin_bit_cast(bf16x8_t, v), pf[1], o[t]);
+      }
+    }
+  }
+}
+
+template <int HD, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void k_kvq_prompt(KvqAttendArgs a, KvqCut cut) {
+  constexpr int KS = HD / 16, NT = HD / 32, STAGE = 2 * 8 * HD;  // STAGE: 16-byte pieces of a page, K and V
+  static_assert(NW == 4, "256 threads share a page");
+  __shared__ __attribute__((aligned(16))) u32x4 lds[2][STAGE];
+  const KvqBatch& bt = a.batch;
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, c = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
+  const int kh = blockIdx.y, split = blockIdx.z;
+  int tile = 0;
+  const int b = find_tile(bt, G, cut, blockIdx.x, tile);
+  if (b < 0) return;
+  const KvqSeq sq = kvq_seq(bt, b);
+  tile = kvq_tiles(sq, G, cut) - 1 - tile;  // the last ones see most keys: they start first
+  const KvqTile tl = kvq_tile(sq, G, tile, cut.cols);
+  const int j0 = tile * cut.cols, first = tl.first;
+  const int pages = kvq_pages(tl.end), items = kvq_items(pages, cut.items, cut.least);
+  if (split >= items) return;
+  const int per_item = kvq_item_pages(pages, items), p0 = split * per_item;
+  const int np = max(0, min(per_item, pages - p0));
+
+  // The column, its query, and the last key that it sees; columns past the tile's last repeat that.
+  const int col = wave * 32 + c, cc = min(col, tl.cols - 1);
+  const int row = (j0 + cc) / G, head = kh * G + (j0 + cc) - row * G;
+  const int lim = sq.ok ? first + row : -1;
+  const int w0 = min(wave * 32, tl.cols - 1), w1 = min(wave * 32 + 31, tl.cols - 1);
+  const int open = first + (j0 + w0) / G + 1;                                       // keys that every column of the wave sees
+  const int wave_end = wave * 32 < tl.cols && sq.ok ? first + (j0 + w1) / G + 1 : 0;  // that some column of it does
+  const float scale_log2 = a.scale * kLog2e;
+  bf16x8_t qf[KS];
+  {
+    const bf16_t* q = static_cast<const bf16_t*>(a.q.p) + (sq.r0 + row) * a.q.row_stride + head * a.q.head_stride + 8 * h;
+    if (a.q.vec) {
+#pragma unroll
+      for (int j = 0; j < KS; ++j) qf[j] = load_bf16x8(q + 16 * j);
+    } else {
+#pragma unroll
+      for (int j = 0; j < KS; ++j) {
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          w[i] = static_cast<uint32_t>(q[16 * j + 2 * i]) | static_cast<uint32_t>(q[16 * j + 2 * i + 1]) << 16;
+        qf[j] = __builtin_bit_cast(bf16x8_t, w);
+      }
+    }
+  }
+  f32x16 o[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+
+  if (np > 0) {
+    const int32_t* pt = table_of(bt, b) + p0;
+    const size_t bytes = kvq_block_bytes(HD);
+    const char* base = a.cache.blocks + kh * bytes;
+    auto block_of = [&](int id, bool& lost) {  // page 0 stands in for an id outside the cache
+      lost = !kvq_page_ok(a.cache, id);
+      return base + static_cast<size_t>(lost ? 0 : id) * n_kv * bytes;
+    };
+    auto id_of = [&](int p) { return __builtin_amdgcn_readfirstlane(pt[min(p, np - 1)]); };
+    // Whether page p0 + p, whose share is s, has values that fp16 holds: the same in every wave.
+    auto fits = [&](const PageShare<HD>& s, int p) {
+      const int i = lane & (HD / 2 - 1), t = 16 * (i & 3) + 4 * ((i >> 2) & 3), tok0 = (p0 + p) * kKvqPage;
+      const uint32_t w = tok0 + kKvqPage > tl.end ? scales_below(s.all, tok0 + t, tl.end) : s.all;
+      return static_cast<bool>(__all((((w + 0x18181818u) ^ 0x80808080u) & 0xe0e0e0e0u) == 0));
+    };
+    PageShare<HD> share;
+    int id = id_of(1);
+    share_load<HD>(share, block_of(id_of(0), share.lost), tid);
+    bool half = fits(share, 0), lost = share.lost;
+    share_store<HD>(share, tid, p0 * kKvqPage, tl.end, half, lds[0], lds[0] + 8 * HD);
+    share_load<HD>(share, block_of(id, share.lost), tid);
+    id = id_of(2);
+    int p = 0;
+    // Pages from p on.  HALF: V and P in fp16, up to the first page that does not fit; else in bf16.
+    auto walk = [&](auto half_tag) {
+      constexpr bool HALF = half_tag.value;
+      for (; p < np && (!HALF || half); ++p) {
+        __syncthreads();  // page p is in its stage, and nobody reads the other one
+        const u32x4* lk = lds[p & 1];
+        const u32x4* lv = lk + 8 * HD;
+        const bool lost_now = lost;
+        if (p + 1 < np) {
+          half = HALF && fits(share, p + 1);
+          lost = share.lost;
+          share_store<HD>(share, tid, (p0 + p + 1) * kKvqPage, tl.end, half, lds[(p + 1) & 1], lds[(p + 1) & 1] + 8 * HD);
+          share_load<HD>(share, block_of(id, share.lost), tid);
+          id = id_of(p + 3);
+        }
+        const int tok0 = (p0 + p) * kKvqPage;
+        if (tok0 >= wave_end) continue;
+        f32x16 s[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[t][r] = 0.f;
+#pragma unroll
+        for (int j = 0; j < KS; ++j)
+#pragma unroll
+          for (int t = 0; t < 2; ++t) s[t] = mfma32x32x16(__builtin_bit_cast(bf16x8_t, lk[(t * KS + j) * 64 + lane]), qf[j], s[t]);
+        if (lost_now || tok0 + kKvqPage > open) {
+          asm volatile("");  // a branch: as selects it would cost every page
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const float v = lost_now ? __builtin_nanf("") : s[t][r];
+              s[t][r] = tok0 + 32 * t + 8 * (r >> 2) + 4 * h + (r & 3) > lim ? -INFINITY : v;
+            }
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
+        top *= scale_log2;
+        if (__any(top > m_run + 8.f)) {
+          top = fmaxf(top, __shfl_xor(top, 32, 64));
+          const float m_new = top > m_run + 8.f ? top : m_run;
+          const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+          l_run *= alpha;
+          m_run = m_new;
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[t][r] *= alpha;
+        }
+        const float shift = m_run == -INFINITY ? 0.f : m_run;
+        float x[32];
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+          x[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k >> 4][k & 15], scale_log2, -shift));
+          l_run += x[k];  // of this lane's tokens; the column's other lane adds its own at the end
+        }
+        if (!HALF) {  // NaN value blocks: the outputs that lie in one turn NaN if the column sees the token
+          bool ig;
+          const char* block = block_of(__builtin_amdgcn_readfirstlane(pt[p]), ig);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {  // rows 8 i + .. of each 16 are dimensions of this block
+            bool bad = false;
+            for (int t = 0; t < kKvqPage; ++t)
+              bad |= tok0 + t <= lim && static_cast<unsigned char>(block[kvq_v_scale(t, HD == 128 ? h + 2 * i : i, HD)]) == 255;
+            if (bad) {
+#pragma unroll
+              for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                  if (((r >> 2) & 1) == i) o[t][r] += __builtin_nanf("");
+            }
+          }
+        }
+        page_values<HD, HALF>(lv, x, o);
+      }
+    };
+    walk(std::true_type{});
+    if (p < np) walk(std::false_type{});
+    l_run += __shfl_xor(l_run, 32, 64);
+  }
+
+  if (col >= tl.cols) return;
+  // The lane's rows 8 i + 4 h + e of each tile: dimensions hd/16 c' + 2 t + (row >= 16), c' = row mod 16.
+  const float inv = !sq.ok ? __builtin_nanf("") : lim < 0 ? 0.f : 1.f / l_run;
+  const int64_t part = (static_cast<int64_t>(blockIdx.x) * cut.items + split) * n_kv + kh;
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+#pragma unroll
+    for (int e = 0; e < 4; e += 8 / (HD / 16)) {  // eight dimensions: of one c' at hd 128, of two at 64
+      const int cp = 8 * q + 4 * h + e;
+      float x[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int t = HD == 128 ? k >> 1 : (k >> 1) & 1, i = k & 1, ee = HD == 128 ? e : e + (k >> 2);
+        x[k] = o[t][8 * i + 4 * q + ee];
+      }
+      if (items == 1) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] *= inv;
+        store8<true>(a.out, sq.r0 + row, head, cp * (HD / 16), x);
+      } else {
+        float* po = a.part_o + (part * cut.cols + col) * HD + cp * (HD / 16);
+        *reinterpret_cast<f32x4_t*>(po) = f32x4_t{x[0], x[1], x[2], x[3]};
+        *reinterpret_cast<f32x4_t*>(po + 4) = f32x4_t{x[4], x[5], x[6], x[7]};
+      }
+    }
+  if (items > 1 && h == 0) {
+    float* ml = a.part_ml + part * 2 * cut.cols + col;
+    ml[0] = m_run;
+    ml[cut.cols] = l_run;
+  }
+}
+
 // Joins the items of a tile: one block per (tile, KV head, column).  Four dimensions to a thread, the items dealt out to
 // groups of threads whose loads are all in flight at once.
 template <int HD, bool F32>
-__global__ __launch_bounds__(256) void k_kvq_join(KvqAttendArgs a, Cut sh) {
+__global__ __launch_bounds__(256) void k_kvq_join(KvqAttendArgs a, KvqCut cut) {
   constexpr int LPC = HD / 4, NG = 256 / LPC, PER = kKvqTileItems / NG;
   __shared__ float sw[kKvqTileItems];
   __shared__ __attribute__((aligned(16))) f32x4_t sx[NG][LPC];
   const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
   const int kh = blockIdx.y, col = blockIdx.z;
   int tile = 0;
-  const int b = sh.find ? find_tile(a.batch, G, blockIdx.x, tile) : static_cast<int>(blockIdx.x);
+  const int b = cut.find ? find_tile(a.batch, G, cut, blockIdx.x, tile) : static_cast<int>(blockIdx.x);
   if (b < 0) return;
   const KvqSeq sq = kvq_seq(a.batch, b);
-  const KvqTile tl = kvq_tile(sq, G, tile);
-  const int n = kvq_items(kvq_pages(tl.end), sh.items, sh.least);
+  if (cut.cols > 16) tile = kvq_tiles(sq, G, cut) - 1 - tile;  // as k_kvq_prompt numbers them
+  const KvqTile tl = kvq_tile(sq, G, tile, cut.cols);
+  const int n = kvq_items(kvq_pages(tl.end), cut.items, cut.least);
   if (n == 1 || col >= tl.cols) return;  // one item has written the output itself
-  const int j0 = tile * kKvqCols;
-  const int64_t part = static_cast<int64_t>(blockIdx.x) * sh.items * n_kv + kh;  // of item 0; n_kv between items
+  const int j0 = tile * cut.cols;
+  const int64_t part = static_cast<int64_t>(blockIdx.x) * cut.items * n_kv + kh;  // of item 0; n_kv between items
   const int grp = threadIdx.x / LPC, d = threadIdx.x % LPC * 4;
-  const float* po = a.part_o + (part * 16 + col) * HD + d;
-  const int64_t step = static_cast<int64_t>(n_kv) * 16 * HD;
+  const float* po = a.part_o + (part * cut.cols + col) * HD + d;
+  const int64_t step = static_cast<int64_t>(n_kv) * cut.cols * HD;
   f32x4_t x[PER];
 #pragma unroll
   for (int k = 0; k < PER; ++k) x[k] = *reinterpret_cast<const f32x4_t*>(po + min(grp + NG * k, n - 1) * step);
   float den = 0.f;
   if (threadIdx.x < 64) {
     const int lane = threadIdx.x;
-    const float* ml = a.part_ml + (part + static_cast<int64_t>(min(lane, n - 1)) * n_kv) * 32 + col;
-    const float m = lane < n ? ml[0] : -INFINITY, l = lane < n ? ml[16] : 0.f;
+    const float* ml = a.part_ml + (part + static_cast<int64_t>(min(lane, n - 1)) * n_kv) * 2 * cut.cols + col;
+    const float m = lane < n ? ml[0] : -INFINITY, l = lane < n ? ml[cut.cols] : 0.f;
     const float mx = wave_max(m);
     const float w = m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - mx);
     sw[lane] = w;
@@ -668,42 +1020,73 @@ __global__ __launch_bounds__(256) void k_kvq_join(KvqAttendArgs a, Cut sh) {
   }
 }
 
-// What a launch of attention does, from the bounds of the call alone.
+// What a call of attention launches, from its bounds alone.
 struct AttendPlan {
-  Cut cut;
-  int waves;      // of a block
-  int64_t tiles;  // at most
+  KvqCut walk, prompt;              // k_kvq_attend's tiles and k_kvq_prompt's
+  int64_t walk_tiles = 0, prompt_tiles = 0;  // at most; 0: not launched
+  int waves = 4;                    // of a k_kvq_attend block
 };
 
-AttendPlan attend_plan(const KvqCache& c, const KvqBatch& b, int n_q) {
+constexpr int kPromptWaves = 4;
+
+AttendPlan attend_plan(const KvqCache& c, const KvqBatch& b, int n_q, bool bf16) {
   const int G = n_q / c.n_kv;
-  AttendPlan p;
-  p.tiles = kvq_tile_bound(b, G);
-  const int64_t blocks = std::max<int64_t>(1, p.tiles * c.n_kv);
+  const int64_t most = static_cast<int64_t>(kvq_max_rows(b)) * G;  // columns of a sequence
   const int pages = std::max(1, kvq_pages(b.max_context));
-  p.cut = Cut{!kvq_one_tile(b, G), 1, 4};
-  if (blocks < 256) p.cut.items = static_cast<int>(std::min<int64_t>(kvq_items(pages, kKvqTileItems, p.cut.least), (384 + blocks - 1) / blocks));
-  if (pages <= 16) p.cut.items = 1;
-  const int64_t all = blocks * p.cut.items;
-  const int per = kvq_item_pages(pages, p.cut.items);
+  AttendPlan p;
+  if (bf16 && most > 64) {
+    p.prompt.cols = 32 * kPromptWaves;
+    p.prompt.find = 1;
+    p.prompt.least = 8;
+    if (static_cast<int64_t>(b.n_seqs) * kvq_max_rows(b) > b.n_rows) p.prompt.above = p.walk.upto = 64;  // else all have as many rows
+    p.prompt_tiles = kvq_tile_bound(b, G, p.prompt);
+    const int64_t blocks = std::max<int64_t>(1, p.prompt_tiles * c.n_kv);
+    if (blocks < 512) p.prompt.items = static_cast<int>(std::min<int64_t>(kvq_items(pages, kKvqTileItems, p.prompt.least), (512 + blocks - 1) / blocks));
+  }
+  if (p.prompt_tiles && !p.prompt.above) return p;
+  p.walk.find = std::min<int64_t>(most, p.walk.upto) > p.walk.cols || p.prompt_tiles;
+  p.walk_tiles = kvq_tile_bound(b, G, p.walk);
+  const int64_t blocks = std::max<int64_t>(1, p.walk_tiles * c.n_kv);
+  p.walk.least = 4;
+  if (blocks < 256 && pages > 16) p.walk.items = static_cast<int>(std::min<int64_t>(kvq_items(pages, kKvqTileItems, p.walk.least), (384 + blocks - 1) / blocks));
+  const int64_t all = blocks * p.walk.items;
+  const int per = kvq_item_pages(pages, p.walk.items);
   p.waves = all >= 2048 && per <= 4 ? 1 : all <= 384 && per > 16 ? 8 : 4;
   return p;
 }
 
+size_t part_floats(const KvqCut& cut, int64_t tiles, int n_kv, int hd) {  // of the partial outputs; the maxima and sums are 2 / hd of them
+  return cut.items > 1 ? static_cast<size_t>(tiles) * cut.items * n_kv * cut.cols * hd : 0;
+}
+
 template <int HD, bool F32>
-hipError_t attend_launch(const KvqAttendArgs& a, const AttendPlan& p, hipStream_t s) {
+hipError_t attend_launch(KvqAttendArgs a, const AttendPlan& p, float* ws, hipStream_t s) {
   const int n_kv = a.cache.n_kv;
-  const dim3 grid(static_cast<uint32_t>(p.tiles), n_kv, p.cut.items);
-  switch (p.waves) {
-    case 1: launch_kernel((k_kvq_attend<HD, F32, 1>), grid, dim3(64), 0, s, a, p.cut); break;
-    case 2: launch_kernel((k_kvq_attend<HD, F32, 2>), grid, dim3(128), 0, s, a, p.cut); break;
-    case 4: launch_kernel((k_kvq_attend<HD, F32, 4>), grid, dim3(256), 0, s, a, p.cut); break;
-    case 8: launch_kernel((k_kvq_attend<HD, F32, 8>), grid, dim3(512), 0, s, a, p.cut); break;
-    default: return hipErrorInvalidValue;
+  auto join = [&](const KvqCut& cut, int64_t tiles) {
+    const int64_t most = std::min<int64_t>(cut.upto, static_cast<int64_t>(kvq_max_rows(a.batch)) * (a.n_q / n_kv));
+    launch_kernel((k_kvq_join<HD, F32>), dim3(static_cast<uint32_t>(tiles), n_kv, static_cast<uint32_t>(std::min<int64_t>(cut.cols, most))), dim3(256), 0, s, a, cut);
+  };
+  if (p.prompt_tiles) {
+    const size_t n = part_floats(p.prompt, p.prompt_tiles, n_kv, HD);
+    a.part_o = ws;
+    a.part_ml = n ? ws + n : nullptr;
+    ws = n ? ws + n + n / HD * 2 : ws;
+    if constexpr (!F32)
+      launch_kernel((k_kvq_prompt<HD, kPromptWaves>), dim3(static_cast<uint32_t>(p.prompt_tiles), n_kv, p.prompt.items), dim3(64 * kPromptWaves), 0, s, a, p.prompt);
+    if (n) join(p.prompt, p.prompt_tiles);
   }
-  if (p.cut.items > 1) {
-    const int cols = static_cast<int>(std::min<int64_t>(kKvqCols, static_cast<int64_t>(kvq_max_rows(a.batch)) * (a.n_q / n_kv)));
-    launch_kernel((k_kvq_join<HD, F32>), dim3(static_cast<uint32_t>(p.tiles), n_kv, cols), dim3(256), 0, s, a, p.cut);
+  if (p.walk_tiles) {
+    const size_t n = part_floats(p.walk, p.walk_tiles, n_kv, HD);
+    a.part_o = ws;
+    a.part_ml = n ? ws + n : nullptr;
+    const dim3 grid(static_cast<uint32_t>(p.walk_tiles), n_kv, p.walk.items);
+    switch (p.waves) {
+      case 1: launch_kernel((k_kvq_attend<HD, F32, 1>), grid, dim3(64), 0, s, a, p.walk); break;
+      case 4: launch_kernel((k_kvq_attend<HD, F32, 4>), grid, dim3(256), 0, s, a, p.walk); break;
+      case 8: launch_kernel((k_kvq_attend<HD, F32, 8>), grid, dim3(512), 0, s, a, p.walk); break;
+      default: return hipErrorInvalidValue;
+    }
+    if (n) join(p.walk, p.walk_tiles);
   }
   return hipGetLastError();
 }
@@ -716,9 +1099,21 @@ dim3 row_grid(const KvqCache& c, int n_rows) {
 }  // namespace
 
 size_t kvq_attend_bytes(const KvqCache& c, const KvqBatch& b, int n_q) {
-  const AttendPlan p = attend_plan(c, b, n_q);
-  if (p.cut.items == 1) return 0;
-  return static_cast<size_t>(p.tiles) * p.cut.items * c.n_kv * kKvqCols * (c.hd + 2) * 4;
+  size_t most = 0;  // whatever the type
+  for (const bool bf16 : {true, false}) {
+    const AttendPlan p = attend_plan(c, b, n_q, bf16);
+    const size_t n = part_floats(p.walk, p.walk_tiles, c.n_kv, c.hd) + part_floats(p.prompt, p.prompt_tiles, c.n_kv, c.hd);
+    most = std::max(most, (n + n / c.hd * 2) * 4);
+  }
+  return most;
+}
+
+bool kvq_attend_fits(const KvqCache& c, const KvqBatch& b, int n_q) {
+  for (const bool bf16 : {true, false}) {
+    const AttendPlan p = attend_plan(c, b, n_q, bf16);
+    if (p.walk_tiles >= (1 << 22) || p.prompt_tiles >= (1 << 22)) return false;  // blocks of up to 512 threads, 2^32 in a dimension
+  }
+  return true;
 }
 
 hipError_t launch_kvq_append(const KvqCache& c, const KvqBatch& b, const KvqTensor& k, const KvqTensor& v, hipStream_t s) {
@@ -739,12 +1134,11 @@ hipError_t launch_kvq_read(const KvqCache& c, const KvqBatch& b, const KvqTensor
   return hipGetLastError();
 }
 
-hipError_t launch_kvq_attend(KvqAttendArgs a, void* ws, hipStream_t s) {
-  const AttendPlan p = attend_plan(a.cache, a.batch, a.n_q);
-  a.part_o = static_cast<float*>(ws);
-  a.part_ml = a.part_o ? a.part_o + p.tiles * p.cut.items * a.cache.n_kv * kKvqCols * a.cache.hd : nullptr;
-  if (a.q.bf16) return a.cache.hd == 128 ? attend_launch<128, false>(a, p, s) : attend_launch<64, false>(a, p, s);
-  return a.cache.hd == 128 ? attend_launch<128, true>(a, p, s) : attend_launch<64, true>(a, p, s);
+hipError_t launch_kvq_attend(const KvqAttendArgs& a, void* ws, hipStream_t s) {
+  const AttendPlan p = attend_plan(a.cache, a.batch, a.n_q, a.q.bf16);
+  float* w = static_cast<float*>(ws);
+  if (a.q.bf16) return a.cache.hd == 128 ? attend_launch<128, false>(a, p, w, s) : attend_launch<64, false>(a, p, w, s);
+  return a.cache.hd == 128 ? attend_launch<128, true>(a, p, w, s) : attend_launch<64, true>(a, p, w, s);
 }
 
 }  // namespace rollpack

@@ -126,12 +126,11 @@ RP_HD KvqSeq kvq_seq(const KvqBatch& bt, int b) {
 
 // ---- how attention is cut --------------------------------------------------------------
 //
-// Work is counted in tiles: 16 columns of a sequence and KV head, a column being one query head of one row (the G
-// heads of a row side by side).  A tile's pages are cut into items, which blocks take; more than one item leaves partial
+// Work is counted in tiles: consecutive columns of a sequence and KV head, a column being one query head of one row (the
+// G heads of a row side by side).  A tile's pages are cut into items, which blocks take; more than one item leaves partial
 // outputs, which a second kernel joins.  Contexts are in device memory: the host bounds the items of a tile from the
 // call's bounds, and a block counts its tile's from the context it finds, so that a captured graph follows them.
 
-constexpr int kKvqCols = 16;
 constexpr int kKvqTileItems = 64;  // items of one tile at most: the join holds one per lane
 
 // Pages of `keys` keys; the items of a tile of so many pages, at most `most` of them and none below `least` pages unless
@@ -143,16 +142,28 @@ RP_HD int kvq_items(int pages, int most, int least) {
 }
 RP_HD int kvq_item_pages(int pages, int items) { return items == 1 ? pages : (pages + items - 1) / items; }
 
-RP_HD int kvq_tiles(const KvqSeq& s, int group) { return (s.n * group + kKvqCols - 1) / kKvqCols; }
+// How a launch cuts a batch: tiles of `cols` columns of the sequences with more than `above` and up to `upto` columns.
+struct KvqCut {
+  int cols = 16;
+  int find = 0;   // tiles are found by their sequences' rows (0: tile b is sequence b's only one)
+  int above = 0, upto = 0x7fffffff;
+  int items = 1;  // of a tile at most
+  int least = 1;  // pages of an item, unless it is its tile's only one
+};
+
+RP_HD int kvq_tiles(const KvqSeq& s, int group, const KvqCut& cut) {
+  const int n = s.n * group;
+  return n > cut.above && n <= cut.upto ? (n + cut.cols - 1) / cut.cols : 0;
+}
 
 // A tile of a sequence: its columns, the position of the sequence's first row, and the keys that some column sees.
 struct KvqTile {
   int cols, first, end;
 };
-RP_HD KvqTile kvq_tile(const KvqSeq& s, int group, int tile) {
+RP_HD KvqTile kvq_tile(const KvqSeq& s, int group, int tile, int cols) {
   KvqTile t;
-  const int j0 = tile * kKvqCols, left = s.n * group - j0;
-  t.cols = left < kKvqCols ? left : kKvqCols;
+  const int j0 = tile * cols, left = s.n * group - j0;
+  t.cols = left < cols ? left : cols;
   t.first = s.ctx - s.n;
   const int end = t.first + (j0 + t.cols - 1) / group + 1;
   t.end = s.ok && end > 0 ? end : 0;
@@ -165,27 +176,29 @@ struct KvqAttendArgs {
   KvqTensor q, out;
   int n_q = 0;
   float scale = 1.f;
-  // workspace: per item and KV head [16, hd] partial outputs, [2, 16] maxima and sums
+  // workspace: per item and KV head [cols, hd] partial outputs, [2, cols] maxima and sums
   float* part_o = nullptr;
   float* part_ml = nullptr;
 };
 
-// Tiles that a batch has at most (of one KV head).  Up to 16 columns a sequence: one each.
-inline bool kvq_one_tile(const KvqBatch& b, int group) { return static_cast<int64_t>(kvq_max_rows(b)) * group <= kKvqCols; }
-inline int64_t kvq_tile_bound(const KvqBatch& b, int group) {
-  if (kvq_one_tile(b, group)) return b.n_seqs;
-  const int64_t per_seq = (static_cast<int64_t>(kvq_max_rows(b)) * group + kKvqCols - 1) / kKvqCols;
-  const int64_t by_rows = static_cast<int64_t>(b.n_rows) * group / kKvqCols + b.n_seqs, by_seqs = per_seq * b.n_seqs;
+// Tiles of a cut that a batch has at most (of one KV head).
+inline int64_t kvq_tile_bound(const KvqBatch& b, int group, const KvqCut& cut) {
+  if (!cut.find) return b.n_seqs;
+  const int64_t most = static_cast<int64_t>(kvq_max_rows(b)) * group;
+  const int64_t per_seq = ((most < cut.upto ? most : cut.upto) + cut.cols - 1) / cut.cols;
+  const int64_t by_rows = static_cast<int64_t>(b.n_rows) * group / cut.cols + b.n_seqs, by_seqs = per_seq * b.n_seqs;
   return by_rows < by_seqs ? by_rows : by_seqs;
 }
 // Bytes of the workspace of launch_kvq_attend.
 size_t kvq_attend_bytes(const KvqCache& c, const KvqBatch& b, int n_q);
+// Whether its launches are within a grid's limits.
+bool kvq_attend_fits(const KvqCache& c, const KvqBatch& b, int n_q);
 
 #ifdef __HIPCC__
 hipError_t launch_kvq_append(const KvqCache& c, const KvqBatch& b, const KvqTensor& k, const KvqTensor& v, hipStream_t s);
 hipError_t launch_kvq_read(const KvqCache& c, const KvqBatch& b, const KvqTensor& k, const KvqTensor& v, hipStream_t s);
-// a.part_o and a.part_ml are set from `ws`, of kvq_attend_bytes bytes.
-hipError_t launch_kvq_attend(KvqAttendArgs a, void* ws, hipStream_t s);
+// ws: of kvq_attend_bytes bytes.
+hipError_t launch_kvq_attend(const KvqAttendArgs& a, void* ws, hipStream_t s);
 #endif
 
 }  // namespace rollpack

@@ -202,7 +202,7 @@ size_t kvq_attend_size(const rollpack::KvqCache& c, const rollpack::KvqBatch& b,
   kvq_require(n_q >= 1 && n_q <= 65536 && n_q % c.n_kv == 0, "n_q_heads must be a multiple of n_kv_heads");
   const int64_t group = n_q / c.n_kv;
   kvq_require(static_cast<int64_t>(b.row_off ? b.max_rows : 1) * group < (int64_t{1} << 30) &&
-                  rollpack::kvq_tile_bound(b, static_cast<int>(group)) < (int64_t{1} << 22),
+                  rollpack::kvq_attend_fits(c, b, n_q),
               "too many rows and heads for one call");
   return rollpack::kvq_attend_bytes(c, b, n_q);
 }

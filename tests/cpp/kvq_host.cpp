@@ -92,28 +92,39 @@ static void batches() {
     b.context = ctx.data();
     bool ascending = true;
     for (int i = 0; i < n; ++i) ascending = ascending && off[i] >= 0 && off[i + 1] >= off[i] && off[i + 1] <= b.n_rows;
-    int64_t tiles = 0;
-    const int most = pick(1, kKvqTileItems), least = pick(1, 20);
+    const int most = pick(1, kKvqTileItems), least = pick(1, 20), above = pick(0, 100);
+    KvqCut small, large;  // the classes that two launches share
+    small.find = large.find = 1;
+    large.cols = 128;
+    small.upto = large.above = above;
+    int64_t tiles[2] = {0, 0};
     for (int i = 0; i < n; ++i) {
       const KvqSeq s = kvq_seq(b, i);
       assert(s.r0 >= 0 && s.n >= 0 && s.r0 + s.n <= b.n_rows);
       assert(s.n <= kvq_max_rows(b) && (!s.ok || (s.ctx >= 0 && s.ctx <= b.max_context)));
-      const int nt = kvq_tiles(s, group);
-      assert(!kvq_one_tile(b, group) || nt <= 1);
-      for (int t = 0; t < nt; ++t) {
-        const KvqTile tl = kvq_tile(s, group, t);
-        assert(tl.cols >= 1 && tl.cols <= kKvqCols && t * kKvqCols + tl.cols <= s.n * group);
-        assert(tl.end >= 0 && tl.end <= b.max_context && (s.ok || tl.end == 0) && (!s.ok || tl.end <= s.ctx));
-        if (t + 1 == nt && s.ok) assert(tl.end == s.ctx);
-        const int pages = kvq_pages(tl.end), items = kvq_items(pages, most, least), per = kvq_item_pages(pages, items);
-        assert(items >= 1 && items <= most && (items == 1 || pages > least));
-        int sum = 0;
-        for (int k = 0; k < items; ++k) sum += std::max(0, std::min(per, pages - k * per));
-        assert(sum == pages);
+      assert(!(kvq_tiles(s, group, small) && kvq_tiles(s, group, large)) &&
+             (kvq_tiles(s, group, small) || kvq_tiles(s, group, large)) == (s.n > 0));
+      for (int k = 0; k < 2; ++k) {
+        const KvqCut& cut = k ? large : small;
+        const int nt = kvq_tiles(s, group, cut);
+        int covered = 0;
+        for (int t = 0; t < nt; ++t) {
+          const KvqTile tl = kvq_tile(s, group, t, cut.cols);
+          assert(tl.cols >= 1 && tl.cols <= cut.cols && t * cut.cols == covered);
+          covered += tl.cols;
+          assert(tl.end >= 0 && tl.end <= b.max_context && (s.ok || tl.end == 0) && (!s.ok || tl.end <= s.ctx));
+          if (t + 1 == nt && s.ok) assert(tl.end == s.ctx);
+          const int pages = kvq_pages(tl.end), items = kvq_items(pages, most, least), per = kvq_item_pages(pages, items);
+          assert(items >= 1 && items <= most && (items == 1 || pages > least));
+          int sum = 0;
+          for (int j = 0; j < items; ++j) sum += std::max(0, std::min(per, pages - j * per));
+          assert(sum == pages);
+        }
+        assert(nt == 0 || covered == s.n * group);
+        tiles[k] += nt;
       }
-      tiles += nt;
     }
-    if (ascending || !b.row_off) assert(tiles <= kvq_tile_bound(b, group));
+    if (ascending || !b.row_off) assert(tiles[0] <= kvq_tile_bound(b, group, small) && tiles[1] <= kvq_tile_bound(b, group, large));
   }
 }
 
