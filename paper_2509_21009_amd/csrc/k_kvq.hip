@@ -343,6 +343,61 @@ struct Query {
   }
 };
 
+// One page of an online softmax in the log2 domain, for a lane's N scores of one column.
+//   The reference m moves only when probabilities pass 2^8 (or there is none yet): up to that they lose nothing in fp32,
+// bf16 or fp16, the outputs need rescaling a few times per item instead of every page, and a page's own maximum is not
+// formed at all: its sum tells.  l is the lane's part of the sum; the lanes of a column add theirs at the end.
+struct Softmax {
+  float m = -INFINITY, l = 0.f;
+};
+
+// x: the scores, and then the probabilities; w: these as pairs of fp16 (HALF), whose own sum l takes.  rescale(alpha) scales
+// the outputs; ACROSS are the lanes (besides the first, as xor masks) that share the column.
+template <bool HALF, int N, typename Rescale, typename... Across>
+__device__ __forceinline__ void softmax_page(Softmax& st, float (&x)[N], uint32_t (&w)[N / 2], float scale_log2, Rescale rescale, Across... across) {
+  float s[N], sum;
+#pragma unroll
+  for (int k = 0; k < N; ++k) s[k] = x[k];
+  auto move = [&] {
+    float top = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < N; ++k) top = fmaxf(top, s[k]);
+    ((top = fmaxf(top, __shfl_xor(top, across, 64))), ...);
+    const float m_new = fmaxf(st.m, top * scale_log2);
+    const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m - m_new);
+    st.m = m_new;
+    st.l *= alpha;
+    rescale(alpha);
+  };
+  auto form = [&] {
+    const float shift = st.m == -INFINITY ? 0.f : st.m;
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k], scale_log2, -shift));
+    if constexpr (HALF) {
+      float part[2] = {0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < N / 2; ++k) {
+        const f16x2 p = __builtin_convertvector(f32x2{x[2 * k], x[2 * k + 1]}, f16x2);
+        w[k] = __builtin_bit_cast(uint32_t, p);
+        part[k & 1] = __builtin_amdgcn_fdot2(p, f16x2{1, 1}, part[k & 1], false);
+      }
+      sum = part[0] + part[1];
+    } else {
+      float part[2] = {0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < N; ++k) part[k & 1] += x[k];
+      sum = part[0] + part[1];
+    }
+  };
+  if (__any(st.m == -INFINITY)) move();
+  form();
+  if (__any(sum > 256.f)) {
+    move();
+    form();
+  }
+  st.l += sum;
+}
+
 // The two values of byte `i` of a word of codes, packed as the type's operand.
 template <bool HALF>
 __device__ __forceinline__ uint32_t value_pair(uint32_t w, float s, int i) {
@@ -356,19 +411,19 @@ __device__ __forceinline__ uint32_t value_pair(uint32_t w, float s, int i) {
   }
 }
 
-// O^T += V^T P^T over tokens 32h .. 32h + 31 of the page: accumulator i's rows are dimensions hd/16 c + i.  x: the
-// lane's eight probabilities.  HALF: V and P in fp16, P rounded to it; else V in bf16 and P as NP pieces of it.
+// O^T += V^T P^T over tokens 32h .. 32h + 31 of the page: accumulator i's rows are dimensions hd/16 c + i.  The lane's
+// probabilities are x + 8 h, or as fp16 w + 4 h (HALF: V and P in fp16; else V in bf16 and P as NP pieces of it).
 template <int HD, bool HALF, int NP>
-__device__ __forceinline__ void half_values(const PageV<HD>& pg, int h, float (&x)[8], f32x4_t (&o)[HD / 16]) {
+__device__ __forceinline__ void half_values(const PageV<HD>& pg, int h, const float (&x)[16], const uint32_t (&w16)[8], f32x4_t (&o)[HD / 16]) {
   bf16x8_t pf[NP];
   f16x8 ph;
   if constexpr (HALF) {
-    u32x4 w;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x[2 * i], x[2 * i + 1]}, f16x2));
-    ph = __builtin_bit_cast(f16x8, w);
+    ph = __builtin_bit_cast(f16x8, u32x4{w16[4 * h], w16[4 * h + 1], w16[4 * h + 2], w16[4 * h + 3]});
   } else {
-    split8<NP>(x, pf);
+    float y[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) y[k] = x[8 * h + k];
+    split8<NP>(y, pf);
   }
 #pragma unroll
   for (int j = 0; j < HD / 32; ++j) {  // a pair of dimensions
@@ -430,9 +485,6 @@ __device__ __forceinline__ void nan_values(PageV<HD>& pg, const char* block, int
 //   P is an operand rounded to fp16 (2^-12 of it; to 2^-25 below 2^-14), V exact in it: less than the output's own
 // rounding to bf16, where P in bf16 would add as much again.  Pages with values that fp16 does not hold, and fp32, take
 // bf16: P in two pieces, or three.
-//   The running maximum moves only when a score passes it by more than 2^8: probabilities up to 256 lose nothing in
-// fp32 or bf16, the outputs need rescaling a few times per item instead of every page, and no page waits for a maximum
-// over lanes.
 template <int HD, bool F32, int NW>
 __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendArgs a, KvqCut cut) {
   constexpr int NT = HD / 16, OLD = HD + 4;
@@ -464,7 +516,7 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendAr
   f32x4_t o[NT];
 #pragma unroll
   for (int i = 0; i < NT; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  float m_run = -INFINITY, l_run = 0.f;
+  Softmax st;
   if (nw > 0) {
     const int32_t* pt = table_of(bt, b) + p0;
     const int ptv = lane < np ? pt[lane] : 0;  // lane i has page i of the item, the first 64
@@ -515,32 +567,17 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendAr
               s[u][e] = tok0 + 16 * u + 4 * g + e > lim ? -INFINITY : v;
             }
         }
-        float top = -INFINITY;
+        float x[16];
+        uint32_t w[8];
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) top = fmaxf(top, s[u][e]);
-        top *= scale_log2;
-        if (__any(top > m_run + 8.f)) {
-          top = fmaxf(top, __shfl_xor(top, 16, 64));
-          top = fmaxf(top, __shfl_xor(top, 32, 64));
-          const float m_new = top > m_run + 8.f ? top : m_run;
-          const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
-          l_run *= alpha;
-          m_run = m_new;
+        for (int k = 0; k < 16; ++k) x[k] = s[k >> 2][k & 3];
+        softmax_page<HALF>(st, x, w, scale_log2, [&](float alpha) {
 #pragma unroll
           for (int t = 0; t < NT; ++t) o[t] *= alpha;
-        }
-        const float shift = m_run == -INFINITY ? 0.f : m_run;
-        float x[2][8];
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          x[k >> 3][k & 7] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k >> 2][k & 3], scale_log2, -shift));
-          l_run += x[k >> 3][k & 7];  // of this lane's tokens; the lanes of a column add up at the end
-        }
+        }, 16, 32);
         if (!HALF && !__all(fits_half(pv.s))) nan_values<HD>(pv, at, tok0, lim, o);
-        half_values<HD, HALF, F32 ? 3 : 2>(pv, 0, x[0], o);
-        half_values<HD, HALF, F32 ? 3 : 2>(pv, 1, x[1], o);
+        half_values<HD, HALF, F32 ? 3 : 2>(pv, 0, x, w, o);
+        half_values<HD, HALF, F32 ? 3 : 2>(pv, 1, x, w, o);
         at = next;
         lost = lost_next;
         pv.load(at);
@@ -548,20 +585,20 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendAr
     };
     if constexpr (!F32) walk(std::true_type{});
     if (F32 || i < nw) walk(std::false_type{});
-    l_run += __shfl_xor(l_run, 16, 64);
-    l_run += __shfl_xor(l_run, 32, 64);
+    st.l += __shfl_xor(st.l, 16, 64);
+    st.l += __shfl_xor(st.l, 32, 64);
   }
 
   // Combine the waves: one without a page has m = -inf, l = 0, o = 0.
   if (g == 0) {
-    sm[wave][c] = m_run;
-    sl[wave][c] = l_run;
+    sm[wave][c] = st.m;
+    sl[wave][c] = st.l;
   }
   __syncthreads();
   float mx = sm[0][c];
 #pragma unroll
   for (int w = 1; w < NW; ++w) mx = fmaxf(mx, sm[w][c]);
-  const float fac = m_run == -INFINITY ? (l_run == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m_run - mx);
+  const float fac = st.m == -INFINITY ? (st.l == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(st.m - mx);
   if (c < n_cols) {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -619,8 +656,8 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendAr
 
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
 
-// One thread's share of a page between its load and LDS (256 threads have a page): 32 codes of K at hd 128, 16 at 64,
-// and of V two dimension pairs (one) of eight tokens.
+// One thread's share of a page between its load and LDS.  256 threads unpack K, 32 codes each at hd 128 (16 at 64), and 256
+// V, two dimension pairs (one) of eight tokens: the same ones in a block of four waves, waves 0-3 and 4-7 in one of eight.
 template <int HD>
 struct PageShare {
   static constexpr int KW = HD / 32, VB = HD / 64;  // words of K; bytes of V per token
@@ -630,8 +667,8 @@ struct PageShare {
 };
 
 template <int HD>
-__device__ __forceinline__ void share_load(PageShare<HD>& s, const char* block, int th) {
-  {
+__device__ __forceinline__ void share_load(PageShare<HD>& s, const char* block, int th, bool has_k, bool has_v) {
+  if (has_k) {
     const int u = th >> 6, g = (th >> 4) & 3, c = th & 15;
     const char* p = block + kvq_k_code(16 * u + c, g * (HD / 4), HD);
     if constexpr (HD == 128) {
@@ -645,9 +682,8 @@ __device__ __forceinline__ void share_load(PageShare<HD>& s, const char* block, 
     }
     s.ks = static_cast<unsigned char>(block[kvq_k_scale(16 * u + c, g * (HD / 4) / kKvqBlock, HD)]);
   }
-  {
-    const int half = th >> 7, u = (th >> 5) & 3, h = (th >> 4) & 1, c = th & 15;
-    (void)half;
+  if (has_v) {
+    const int u = (th >> 5) & 3, h = (th >> 4) & 1, c = th & 15;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {  // token groups h and h + 2 of the tile
       const char* p = block + kvq_v_code(16 * u + 4 * (h + 2 * e), c * (HD / 16), HD);
@@ -709,8 +745,9 @@ __device__ __forceinline__ void share_values(const PageShare<HD>& s, const uint3
 
 // The share into LDS; half: V in fp16.
 template <int HD>
-__device__ __forceinline__ void share_store(const PageShare<HD>& s, int th, int tok0, int end, bool half, u32x4* lk, u32x4* lv) {
-  {
+__device__ __forceinline__ void share_store(const PageShare<HD>& s, int th, bool has_k, bool has_v, int tok0, int end, bool half, u32x4* lk,
+                                            u32x4* lv) {
+  if (has_k) {
     const int u = th >> 6, g = (th >> 4) & 3, c = th & 15, t = 16 * u + c;
     const float sc = scale_of(s.ks, 0);
 #pragma unroll
@@ -721,6 +758,7 @@ __device__ __forceinline__ void share_store(const PageShare<HD>& s, int th, int 
           u32x4{code_pair<0>(w, sc), code_pair<1>(w, sc), code_pair<2>(w, sc), code_pair<3>(w, sc)};
     }
   }
+  if (!has_v) return;
   const int u = (th >> 5) & 3, h = (th >> 4) & 1, t = tok0 + 16 * u + 4 * h;
   uint32_t vs[2] = {s.vs[0], s.vs[1]};
   if (tok0 + kKvqPage > end) {
@@ -736,23 +774,20 @@ __device__ __forceinline__ void share_store(const PageShare<HD>& s, int th, int 
   }
 }
 
-// O^T += V^T P^T for a page: x are the lane's 32 probabilities, NP pieces of them in bf16 or one in fp16.
+// O^T += V^T P^T for a page: the lane's 32 probabilities x in two pieces of bf16, or w in fp16.
 template <int HD, bool HALF>
-__device__ __forceinline__ void page_values(const u32x4* lv, float (&x)[32], f32x16 (&o)[HD / 32]) {
+__device__ __forceinline__ void page_values(const u32x4* lv, const float (&x)[32], const uint32_t (&w16)[16], f32x16 (&o)[HD / 32]) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
-    float y[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) y[k] = x[8 * u + k];
     f16x8 ph;
     bf16x8_t pf[2];
     if constexpr (HALF) {
-      u32x4 w;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{y[2 * i], y[2 * i + 1]}, f16x2));
-      ph = __builtin_bit_cast(f16x8, w);
+      ph = __builtin_bit_cast(f16x8, u32x4{w16[4 * u], w16[4 * u + 1], w16[4 * u + 2], w16[4 * u + 3]});
     } else {
+      float y[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] = x[8 * u + k];
       split8<2>(y, pf);
     }
 #pragma unroll
@@ -771,7 +806,7 @@ __device__ __forceinline__ void page_values(const u32x4* lv, float (&x)[32], f32
 template <int HD, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void k_kvq_prompt(KvqAttendArgs a, KvqCut cut) {
   constexpr int KS = HD / 16, NT = HD / 32, STAGE = 2 * 8 * HD;  // STAGE: 16-byte pieces of a page, K and V
-  static_assert(NW == 4, "256 threads share a page");
+  static_assert(NW == 4 || NW == 8, "256 threads unpack K, 256 V");
   __shared__ __attribute__((aligned(16))) u32x4 lds[2][STAGE];
   const KvqBatch& bt = a.batch;
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, c = lane & 31;
@@ -820,7 +855,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_kvq_prompt(KvqAttendArgs a, KvqC
   for (int t = 0; t < NT; ++t)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;
+  Softmax st;
 
   if (np > 0) {
     const int32_t* pt = table_of(bt, b) + p0;
@@ -838,11 +873,13 @@ __global__ __launch_bounds__(64 * NW, 2) void k_kvq_prompt(KvqAttendArgs a, KvqC
       return static_cast<bool>(__all((((w + 0x18181818u) ^ 0x80808080u) & 0xe0e0e0e0u) == 0));
     };
     PageShare<HD> share;
+    const int th = tid & 255;
+    const bool has_k = NW == 4 || wave < 4, has_v = NW == 4 || wave >= 4;
     int id = id_of(1);
-    share_load<HD>(share, block_of(id_of(0), share.lost), tid);
+    share_load<HD>(share, block_of(id_of(0), share.lost), th, has_k, has_v);
     bool half = fits(share, 0), lost = share.lost;
-    share_store<HD>(share, tid, p0 * kKvqPage, tl.end, half, lds[0], lds[0] + 8 * HD);
-    share_load<HD>(share, block_of(id, share.lost), tid);
+    share_store<HD>(share, th, has_k, has_v, p0 * kKvqPage, tl.end, half, lds[0], lds[0] + 8 * HD);
+    share_load<HD>(share, block_of(id, share.lost), th, has_k, has_v);
     id = id_of(2);
     int p = 0;
     // Pages from p on.  HALF: V and P in fp16, up to the first page that does not fit; else in bf16.
@@ -856,8 +893,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_kvq_prompt(KvqAttendArgs a, KvqC
         if (p + 1 < np) {
           half = HALF && fits(share, p + 1);
           lost = share.lost;
-          share_store<HD>(share, tid, (p0 + p + 1) * kKvqPage, tl.end, half, lds[(p + 1) & 1], lds[(p + 1) & 1] + 8 * HD);
-          share_load<HD>(share, block_of(id, share.lost), tid);
+          share_store<HD>(share, th, has_k, has_v, (p0 + p + 1) * kKvqPage, tl.end, half, lds[(p + 1) & 1], lds[(p + 1) & 1] + 8 * HD);
+          share_load<HD>(share, block_of(id, share.lost), th, has_k, has_v);
           id = id_of(p + 3);
         }
         const int tok0 = (p0 + p) * kKvqPage;
@@ -881,30 +918,16 @@ __global__ __launch_bounds__(64 * NW, 2) void k_kvq_prompt(KvqAttendArgs a, KvqC
               s[t][r] = tok0 + 32 * t + 8 * (r >> 2) + 4 * h + (r & 3) > lim ? -INFINITY : v;
             }
         }
-        float top = -INFINITY;
+        float x[32];
+        uint32_t w[16];
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
-        top *= scale_log2;
-        if (__any(top > m_run + 8.f)) {
-          top = fmaxf(top, __shfl_xor(top, 32, 64));
-          const float m_new = top > m_run + 8.f ? top : m_run;
-          const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
-          l_run *= alpha;
-          m_run = m_new;
+        for (int k = 0; k < 32; ++k) x[k] = s[k >> 4][k & 15];
+        softmax_page<HALF>(st, x, w, scale_log2, [&](float alpha) {
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int r = 0; r < 16; ++r) o[t][r] *= alpha;
-        }
-        const float shift = m_run == -INFINITY ? 0.f : m_run;
-        float x[32];
-#pragma unroll
-        for (int k = 0; k < 32; ++k) {
-          x[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k >> 4][k & 15], scale_log2, -shift));
-          l_run += x[k];  // of this lane's tokens; the column's other lane adds its own at the end
-        }
+        }, 32);
         if (!HALF) {  // NaN value blocks: the outputs that lie in one turn NaN if the column sees the token
           bool ig;
           const char* block = block_of(__builtin_amdgcn_readfirstlane(pt[p]), ig);
@@ -922,17 +945,17 @@ __global__ __launch_bounds__(64 * NW, 2) void k_kvq_prompt(KvqAttendArgs a, KvqC
             }
           }
         }
-        page_values<HD, HALF>(lv, x, o);
+        page_values<HD, HALF>(lv, x, w, o);
       }
     };
     walk(std::true_type{});
     if (p < np) walk(std::false_type{});
-    l_run += __shfl_xor(l_run, 32, 64);
+    st.l += __shfl_xor(st.l, 32, 64);
   }
 
   if (col >= tl.cols) return;
   // The lane's rows 8 i + 4 h + e of each tile: dimensions hd/16 c' + 2 t + (row >= 16), c' = row mod 16.
-  const float inv = !sq.ok ? __builtin_nanf("") : lim < 0 ? 0.f : 1.f / l_run;
+  const float inv = !sq.ok ? __builtin_nanf("") : lim < 0 ? 0.f : 1.f / st.l;
   const int64_t part = (static_cast<int64_t>(blockIdx.x) * cut.items + split) * n_kv + kh;
 #pragma unroll
   for (int q = 0; q < 2; ++q)
@@ -957,8 +980,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_kvq_prompt(KvqAttendArgs a, KvqC
     }
   if (items > 1 && h == 0) {
     float* ml = a.part_ml + part * 2 * cut.cols + col;
-    ml[0] = m_run;
-    ml[cut.cols] = l_run;
+    ml[0] = st.m;
+    ml[cut.cols] = st.l;
   }
 }
 
@@ -1024,10 +1047,8 @@ __global__ __launch_bounds__(256) void k_kvq_join(KvqAttendArgs a, KvqCut cut) {
 struct AttendPlan {
   KvqCut walk, prompt;              // k_kvq_attend's tiles and k_kvq_prompt's
   int64_t walk_tiles = 0, prompt_tiles = 0;  // at most; 0: not launched
-  int waves = 4;                    // of a k_kvq_attend block
+  int waves = 4, prompt_waves = 4;  // of a block
 };
-
-constexpr int kPromptWaves = 4;
 
 AttendPlan attend_plan(const KvqCache& c, const KvqBatch& b, int n_q, bool bf16) {
   const int G = n_q / c.n_kv;
@@ -1035,7 +1056,8 @@ AttendPlan attend_plan(const KvqCache& c, const KvqBatch& b, int n_q, bool bf16)
   const int pages = std::max(1, kvq_pages(b.max_context));
   AttendPlan p;
   if (bf16 && most > 64) {
-    p.prompt.cols = 32 * kPromptWaves;
+    p.prompt_waves = 4;
+    p.prompt.cols = 32 * p.prompt_waves;
     p.prompt.find = 1;
     p.prompt.least = 8;
     if (static_cast<int64_t>(b.n_seqs) * kvq_max_rows(b) > b.n_rows) p.prompt.above = p.walk.upto = 64;  // else all have as many rows
@@ -1071,8 +1093,11 @@ hipError_t attend_launch(KvqAttendArgs a, const AttendPlan& p, float* ws, hipStr
     a.part_o = ws;
     a.part_ml = n ? ws + n : nullptr;
     ws = n ? ws + n + n / HD * 2 : ws;
-    if constexpr (!F32)
-      launch_kernel((k_kvq_prompt<HD, kPromptWaves>), dim3(static_cast<uint32_t>(p.prompt_tiles), n_kv, p.prompt.items), dim3(64 * kPromptWaves), 0, s, a, p.prompt);
+    if constexpr (!F32) {
+      const dim3 grid(static_cast<uint32_t>(p.prompt_tiles), n_kv, p.prompt.items);
+      if (p.prompt_waves == 4) launch_kernel((k_kvq_prompt<HD, 4>), grid, dim3(256), 0, s, a, p.prompt);
+      else launch_kernel((k_kvq_prompt<HD, 8>), grid, dim3(512), 0, s, a, p.prompt);
+    }
     if (n) join(p.prompt, p.prompt_tiles);
   }
   if (p.walk_tiles) {
