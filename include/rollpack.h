@@ -50,8 +50,10 @@ typedef enum rp_status {
 
 typedef enum rp_dtype {
   RP_DTYPE_F32 = 0,   /* weights, GEMM inputs and KV in fp32 */
-  RP_DTYPE_BF16 = 1   /* weights, GEMM inputs and KV in bf16; fp32 accumulation,
+  RP_DTYPE_BF16 = 1,  /* weights, GEMM inputs and KV in bf16; fp32 accumulation,
                          residual stream, norms, softmax and logits */
+  RP_DTYPE_BF16_KV4 = 2 /* as RP_DTYPE_BF16 with the KV cache in 4.25 bits per element
+                         (rp_kvq_cache's format): 3.76 times the context in the same pool */
 } rp_dtype;
 
 /* Qwen2.5 decoder shape (the paper's models, section 6).  q/k/v carry a
@@ -240,6 +242,14 @@ rp_status rp_get_tokens(rp_engine* eng, int64_t seq_id, int32_t* out, int32_t ca
  * ratios; fp32, from the logits the step computed. */
 rp_status rp_get_logprobs(rp_engine* eng, int64_t seq_id, float* out, int32_t cap,
                           int32_t* len_out);
+
+/* K and V that the cache of a live sequence holds in one layer, for its
+ * positions first .. first + n - 1 (which its prompt and the tokens fed so far cover): after
+ * RoPE, with the bias, as attention reads them.  RP_DTYPE_BF16_KV4 engines only
+ * (RP_ERR_BAD_STATE otherwise).  The KV footprint of a request (section 4.4) is what a migration
+ * moves or, as in section 5, recomputes.
+ *   k_out, v_out   DEVICE [n, n_kv_heads, head_dim] bf16, ready in stream order */
+rp_status rp_read_kv(rp_engine* eng, int64_t seq_id, int32_t layer, int32_t first, int32_t n, void* k_out, void* v_out);
 
 /* End-of-sequence token (-1, the default: none); response lengths are what
  * the model decides, long-tailed (section 2.2).  A sequence that samples it
@@ -459,8 +469,9 @@ typedef enum rp_kernel_class {
   RP_K_EMBED_NORM = 0,   /* embedding gather + first RMSNorm */
   RP_K_ADD_NORM = 1,     /* residual add of split-K partials + RMSNorm */
   RP_K_GEMM_QKV = 2,
-  RP_K_ROPE_APPEND = 3,  /* q/k/v bias + RoPE + paged KV append (not in bf16 decode steps) */
-  RP_K_ATTN = 4,         /* prefill or decode attention; in bf16 decode steps with the work of RP_K_ROPE_APPEND */
+  RP_K_ROPE_APPEND = 3,  /* q/k/v bias + RoPE + paged KV append (not in decode steps of RP_DTYPE_BF16) */
+  RP_K_ATTN = 4,         /* prefill or decode attention; in decode steps of RP_DTYPE_BF16 with the work of RP_K_ROPE_APPEND,
+                            under RP_DTYPE_BF16_KV4 with that of RP_K_ATTN_MERGE */
   RP_K_ATTN_MERGE = 5,   /* decode split merge, in steps where some row has more than one split */
   RP_K_GEMM_O = 6,
   RP_K_GEMM_GATE_UP = 7, /* with the SiLU * up epilogue */

@@ -8,6 +8,8 @@ from __future__ import annotations
 
 import numpy as np
 
+from oracle import model as om
+
 BLOCK = 32
 GRID = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
 
@@ -66,3 +68,22 @@ def _weigh(p, v, see):
     if np.isfinite(v).all():
         return p @ v
     return np.stack([p[i, see[i]] @ v[see[i]] for i in range(len(p))])
+
+
+def forward_over_cache(w, shape, tokens, cache):
+    """The model's forward over a whole sequence whose attention reads cache[layer] = (K, V) [n, n_kv, hd] (what a
+    4-bit cache holds) in the place of its own.  Returns the logits [n, V] and its own (K, V) of every layer."""
+    tokens = np.asarray(tokens)
+    n = len(tokens)
+    pos = np.arange(n)
+    cos, sin = om.rope_cos_sin(pos, shape.head_dim, shape.theta)
+    x = w["embed"][tokens].astype(np.float64)
+    mine = []
+    for layer, (ck, cv) in zip(w["layers"], cache):
+        h = om.rmsnorm(x, layer["attn_norm"], shape.eps)
+        q, k, v = om._qkv(layer, h, shape)
+        q, k = om.apply_rope(q, cos, sin), om.apply_rope(k, cos, sin)
+        mine.append((k, v))
+        x = x + om.attention(q, ck, cv, pos, pos).reshape(n, -1) @ layer["wo"].T
+        x = x + om._mlp(layer, x, shape)
+    return om.lm_head(w, x, shape), mine

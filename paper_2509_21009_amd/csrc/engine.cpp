@@ -31,6 +31,8 @@ void hip_check(hipError_t e, const char* what) {
 }
 #define HIP_TRY(expr) hip_check((expr), #expr)
 
+bool is_bf16(const rp_model_config& c) { return c.dtype == RP_DTYPE_BF16 || c.dtype == RP_DTYPE_BF16_KV4; }
+
 size_t align256(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }
 
 }  // namespace
@@ -42,9 +44,10 @@ void validate_config(const rp_model_config& c) {
     bad("model config: sizes must be positive");
   if (c.n_q_heads % c.n_kv_heads != 0) bad("model config: n_q_heads must be a multiple of n_kv_heads");
   if (c.head_dim != 64 && c.head_dim != 128) bad("model config: head_dim must be 64 or 128");
-  if (c.dtype != RP_DTYPE_F32 && c.dtype != RP_DTYPE_BF16) bad("model config: unknown dtype");
+  if (c.dtype != RP_DTYPE_F32 && !is_bf16(c)) bad("model config: unknown dtype");
   if (!(c.rms_eps > 0.f) || !(c.rope_theta > 1.f)) bad("model config: rms_eps > 0 and rope_theta > 1 required");
-  if (c.dtype == RP_DTYPE_BF16) {
+  if (c.dtype == RP_DTYPE_BF16_KV4 && c.n_kv_heads > 1024) bad("4-bit cache: at most 1024 KV heads");
+  if (is_bf16(c)) {
     const int nqkv = (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim;
     if (c.n_q_heads / c.n_kv_heads > 16) bad("bf16 path: at most 16 query heads per KV head");
     if (c.hidden % 128 || c.intermediate % 128 || (c.n_q_heads * c.head_dim) % 128 || nqkv % 128 ||
@@ -63,21 +66,25 @@ void validate_limits(const rp_engine_limits& l) {
 }
 
 size_t packed_weights_bytes(const rp_model_config& c) {
-  if (c.dtype != RP_DTYPE_BF16) return 0;
+  if (!is_bf16(c)) return 0;
   const size_t H = c.hidden, I = c.intermediate, hd = c.head_dim, nq = c.n_q_heads, nkv = c.n_kv_heads;
   const size_t layer = align256(nq * hd * H * 2) + 2 * align256(nkv * hd * H * 2) + align256(H * nq * hd * 2) +
                        2 * align256(I * H * 2) + align256(H * I * 2);
   return layer * c.n_layers + align256(static_cast<size_t>(c.vocab) * H * 2);
 }
 
+size_t kv_token_bytes(const rp_model_config& c) {
+  if (c.dtype == RP_DTYPE_BF16_KV4) return c.n_kv_heads * kvq_block_bytes(c.head_dim) / kKvqPage;
+  return static_cast<size_t>(2) * c.n_kv_heads * c.head_dim * (is_bf16(c) ? 2 : 4);
+}
+
 size_t kv_pool_bytes(const rp_model_config& c, int64_t pages) {
-  const size_t esz = c.dtype == RP_DTYPE_BF16 ? 2 : 4;
-  return align256(static_cast<size_t>(pages) * c.n_layers * 2 * c.n_kv_heads * kPageTokens * c.head_dim * esz);
+  return align256(static_cast<size_t>(pages) * c.n_layers * kPageTokens * kv_token_bytes(c));
 }
 
 ScratchPlan plan_scratch(const rp_model_config& c, const rp_engine_limits& l) {
   ScratchPlan p{};
-  const size_t esz = c.dtype == RP_DTYPE_BF16 ? 2 : 4;
+  const size_t esz = is_bf16(c) ? 2 : 4;
   const size_t H = c.hidden, I = c.intermediate, V = c.vocab, hd = c.head_dim;
   const size_t nq = c.n_q_heads, nkv = c.n_kv_heads;
   const size_t nqkv = (nq + 2 * nkv) * hd;
@@ -102,6 +109,13 @@ ScratchPlan plan_scratch(const rp_model_config& c, const rp_engine_limits& l) {
   p.logits = take(S * V * 4);
   p.att_o = take(static_cast<size_t>(p.split_cap) * nkv * 16 * hd * 4);
   p.att_ml = take(static_cast<size_t>(p.split_cap) * nkv * 32 * 4);
+  if (c.dtype == RP_DTYPE_BF16_KV4) {
+    KvqCache kc;
+    kc.n_kv = c.n_kv_heads;
+    kc.hd = c.head_dim;
+    p.kvq_bytes = kvq_attend_bytes_most(kc, c.n_q_heads, l.max_seqs, l.max_prefill_tokens, l.max_context);
+    p.kvq = take(p.kvq_bytes);
+  }
   p.rope_cos = take(static_cast<size_t>(l.max_context) * (hd / 2) * 4);
   p.rope_sin = take(static_cast<size_t>(l.max_context) * (hd / 2) * 4);
   p.page_table = take(S * p.max_pages * 4);
@@ -128,7 +142,8 @@ Engine::Engine(const rp_model_config& cfg, const rp_weights& w, const rp_engine_
   no_alloc_ = no_alloc;
   validate_config(cfg);
   validate_limits(lim);
-  bf16_ = cfg.dtype == RP_DTYPE_BF16;
+  bf16_ = is_bf16(cfg);
+  kv4_ = cfg.dtype == RP_DTYPE_BF16_KV4;
   esz_ = bf16_ ? 2 : 4;
   nqkv_ = (cfg.n_q_heads + 2 * cfg.n_kv_heads) * cfg.head_dim;
   plan_ = plan_scratch(cfg, lim);
@@ -150,7 +165,7 @@ Engine::Engine(const rp_model_config& cfg, const rp_weights& w, const rp_engine_
   if (cfg.tied_embeddings) w_.lm_head = w.embed;
   kv_ = static_cast<char*>(kv_ws);
   scratch_ = static_cast<char*>(scratch_ws);
-  layer_kv_bytes_ = static_cast<size_t>(lim.kv_pages) * cfg.n_kv_heads * kPageTokens * cfg.head_dim * esz_;
+  layer_kv_bytes_ = static_cast<size_t>(lim.kv_pages) * kPageTokens * kv_token_bytes(cfg) / (kv4_ ? 1 : 2);
 
   slots_.resize(lim.max_seqs);
   for (int32_t s = lim.max_seqs - 1; s >= 0; --s) free_slots_.push_back(s);
@@ -496,6 +511,15 @@ void Engine::prof_harvest() {
   prof_pending_.clear();
 }
 
+KvqCache Engine::kvq_cache(int layer) const {
+  KvqCache c;
+  c.blocks = kv_ + static_cast<size_t>(layer) * layer_kv_bytes_;
+  c.n_pages = static_cast<int>(lim_.kv_pages);
+  c.n_kv = cfg_.n_kv_heads;
+  c.hd = cfg_.head_dim;
+  return c;
+}
+
 void Engine::forward(int M, bool pre, int n_seq, int total_items, int total_splits, int tps) {
   const int H = cfg_.hidden, I = cfg_.intermediate, V = cfg_.vocab, hd = cfg_.head_dim;
   const int nq = cfg_.n_q_heads, nkv = cfg_.n_kv_heads;
@@ -528,7 +552,8 @@ void Engine::forward(int M, bool pre, int n_seq, int total_items, int total_spli
   const int s_qkv = splits_for(nqkv_, H);
   const int s_o = splits_for(H, nq * hd);
   const int s_d = splits_for(H, I);
-  const double kv_tok_bytes = 2.0 * nkv * hd * e;  // one layer's K and V of one token
+  const double kv_tok_bytes = static_cast<double>(kv_token_bytes(cfg_));  // one layer's K and V of one token
+  const bool rotates = bf16_ && !kv4_;  // decode attention takes the queries and the newest K/V from the projection itself
   double attn_bytes, attn_flops;
   if (pre) {
     attn_bytes = Md * kv_tok_bytes + 2.0 * Md * nq * hd * e;
@@ -536,7 +561,7 @@ void Engine::forward(int M, bool pre, int n_seq, int total_items, int total_spli
   } else {
     // K/V of every attended token (the newest one's written instead of read), and the queries: the bf16 kernel forms
     // them, and the newest K/V, from the projection's partials
-    attn_bytes = sum_ctx_ * kv_tok_bytes + (bf16_ ? Md * (nqkv_ * 4.0 + nq * hd * e) : 2.0 * Md * nq * hd * e);
+    attn_bytes = sum_ctx_ * kv_tok_bytes + (rotates ? Md * (nqkv_ * 4.0 + nq * hd * e) : 2.0 * Md * nq * hd * e);
     attn_flops = 4.0 * nq * hd * sum_ctx_;
   }
   for (int l = 0; l < cfg_.n_layers; ++l) {
@@ -555,7 +580,10 @@ void Engine::forward(int M, bool pre, int n_seq, int total_items, int total_spli
 
     RopeArgs ra{part, s_qkv, M, L.bq, L.bk, L.bv, nq, nkv, hd, m_pos_, m_slot_, pt, plan_.max_pages,
                 sp<float>(plan_.rope_cos), sp<float>(plan_.rope_sin), q, kpool, vpool};
-    if (pre || !bf16_)  // the bf16 decode attention rotates and appends by itself
+    if (kv4_)
+      launch_timed(RP_K_ROPE_APPEND, Md * (nqkv_ * 4.0 + nq * hd * e + kv_tok_bytes), 0,
+                   [&] { return launch_kvq_rope_append(kvq_cache(l), ra, s); });
+    else if (pre || !rotates)
       launch_timed(RP_K_ROPE_APPEND, Md * nqkv_ * (4.0 + e), 0, [&] { return launch_rope_append(bf16_, ra, s); });
 
     AttnArgs aa{};
@@ -563,7 +591,26 @@ void Engine::forward(int M, bool pre, int n_seq, int total_items, int total_spli
     aa.n_q = nq; aa.n_kv = nkv; aa.hd = hd; aa.scale = 1.0f / std::sqrt(static_cast<float>(hd));
     aa.n_rows = M; aa.tok_slot = m_slot_; aa.tok_pos = m_pos_;
     aa.out = attn;
-    if (pre) {
+    if (kv4_) {
+      KvqAttendArgs ka;
+      ka.cache = kvq_cache(l);
+      ka.batch.n_seqs = pre ? n_seq : M;
+      ka.batch.n_rows = M;
+      ka.batch.max_rows = max_piece_;
+      ka.batch.max_context = max_ctx_;
+      ka.batch.row_off = pre ? m_item_off_ : nullptr;
+      ka.batch.context = m_gen_pos_;  // the position after a row's (a piece's last) token: its context
+      ka.batch.page_table = pt;
+      ka.batch.table_stride = plan_.max_pages;
+      ka.batch.table_row = pre ? m_seq_slot_ : m_slot_;
+      ka.q = KvqTensor{q, static_cast<int64_t>(nq) * hd, hd, 1, 1};
+      ka.out = KvqTensor{attn, static_cast<int64_t>(nq) * hd, hd, 1, 1};
+      ka.n_q = nq;
+      ka.scale = aa.scale;
+      if (l == 0 && kvq_attend_bytes(ka.cache, ka.batch, nq) > plan_.kvq_bytes)
+        throw RpError(RP_ERR_CAPACITY, "4-bit cache: attention's workspace is too small");
+      launch_timed(RP_K_ATTN, attn_bytes, attn_flops, [&] { return launch_kvq_attend(ka, scratch_ + plan_.kvq, s); });
+    } else if (pre) {
       aa.n_seq = n_seq; aa.seq_slot = m_seq_slot_; aa.seq_row0 = m_seq_row0_; aa.seq_pos0 = m_seq_pos0_;
       aa.seq_ntok = m_seq_ntok_; aa.item_off = m_item_off_; aa.total_items = total_items;
       launch_timed(RP_K_ATTN, attn_bytes, attn_flops, [&] { return launch_attn_prefill(bf16_, aa, s); });
@@ -654,6 +701,7 @@ void Engine::run_prefill_chunk(const std::vector<PrefillPiece>& pcs, float* logi
   const int tpi = attn_prefill_tokens_per_item(bf16_, cfg_.n_q_heads / cfg_.n_kv_heads);
   int row = 0, items = 0;
   sum_ctx_sq_ = 0;
+  max_ctx_ = max_piece_ = 0;
   for (int j = 0; j < n; ++j) {
     const PrefillPiece& pc = pcs[j];
     for (int t = 0; t < pc.ntok; ++t) {
@@ -667,8 +715,10 @@ void Engine::run_prefill_chunk(const std::vector<PrefillPiece>& pcs, float* logi
     seq_ntok[j] = pc.ntok;
     // attended keys summed over the piece's queries, x2 (the causal-attention flop count)
     sum_ctx_sq_ += 2.0 * pc.ntok * pc.pos0 + static_cast<double>(pc.ntok) * (pc.ntok + 1);
-    item_off[j] = items;
+    item_off[j] = kv4_ ? row : items;  // the 4-bit cache's attention finds its items by the rows' offsets
     items += (pc.ntok + tpi - 1) / tpi;
+    max_ctx_ = std::max(max_ctx_, pc.pos0 + pc.ntok);
+    max_piece_ = std::max(max_piece_, pc.ntok);
     last_row[j] = row + pc.ntok - 1;
     // A piece that does not end its sequence samples into the same history
     // entry the final piece overwrites later.
@@ -676,7 +726,7 @@ void Engine::run_prefill_chunk(const std::vector<PrefillPiece>& pcs, float* logi
     gen_hist[j] = pc.hist0;
     row += pc.ntok;
   }
-  item_off[n] = items;
+  item_off[n] = kv4_ ? row : items;
   upload_meta(m, ints);
   const int32_t* d = d_meta_;
   m_in_tok_ = d; m_slot_ = d + T; m_pos_ = d + 2 * T;
@@ -825,16 +875,20 @@ int32_t Engine::decode_step(const int32_t* forced, float* logits_out, int64_t* r
   ctx_h.resize(B);
   int64_t total_pages = 0, max_pages = 0;  // of cached keys, which exclude the step's own token
   sum_ctx_ = 0;
+  max_ctx_ = 0;
+  max_piece_ = 1;
   for (int i = 0; i < B; ++i) {
     const Seq& q = slots_[rows[i]];
     ctx_h[i] = q.prompt_len + q.n_gen;
+    max_ctx_ = std::max(max_ctx_, ctx_h[i]);
     const int64_t p = PagePool::pages_for(ctx_h[i] - 1, kPageTokens);
     total_pages += p;
     max_pages = std::max(max_pages, p);
     sum_ctx_ += ctx_h[i];
   }
   int tps = 0, total_splits = 0;
-  if (bf16_) {
+  const bool items = bf16_ && !kv4_;  // the bf16 cache's attention items are planned here
+  if (items) {
     tps = decode_pages_per_item(cfg_.n_kv_heads, cfg_.head_dim, total_pages, max_pages, B) * kPageTokens;
     max_row_splits_ = 0;
     for (int i = 0; i < B; ++i) {
@@ -863,9 +917,9 @@ int32_t Engine::decode_step(const int32_t* forced, float* logits_out, int64_t* r
     gen_pos[i] = pos[i] + 1;
     gen_hist[i] = q.n_gen;
     split_off[i] = sx;
-    if (bf16_) sx += (pos[i] + tps - 1) / tps;
+    if (items) sx += (pos[i] + tps - 1) / tps;
   }
-  if (bf16_) {
+  if (items) {
     // One descriptor per item, the longest first (by pages, counted per length), so that the last
     // blocks to start are the short ones.  When every block has a place at once but some CUs get two (the
     // first 256 blocks go to one CU each), the second ones are folded back: the longest items alone,
@@ -921,6 +975,39 @@ int32_t Engine::decode_step(const int32_t* forced, float* logits_out, int64_t* r
     if (q.n_gen >= q.max_new) q.finished = true;
   }
   return B;
+}
+
+void Engine::read_kv(int64_t id, int32_t layer, int32_t first, int32_t n, void* k_out, void* v_out) {
+  if (!kv4_) throw RpError(RP_ERR_BAD_STATE, "read_kv: the engine's cache is not in 4 bits");
+  if (layer < 0 || layer >= cfg_.n_layers || first < 0 || n < 0) throw RpError(RP_ERR_INVALID_ARG, "read_kv: layer or range out of bounds");
+  const auto it = id2slot_.find(id);
+  if (it == id2slot_.end()) throw RpError(RP_ERR_UNKNOWN_ID, "read_kv: sequence " + std::to_string(id) + " is not live");
+  const Seq& q = slots_[it->second];
+  const int64_t held = static_cast<int64_t>(q.prompt_len) + q.n_gen - 1;  // the newest token has not been fed yet
+  if (static_cast<int64_t>(first) + n > held) throw RpError(RP_ERR_INVALID_ARG, "read_kv: the cache holds " + std::to_string(held) + " positions");
+  if (n == 0) return;
+  const uintptr_t a = reinterpret_cast<uintptr_t>(k_out), b = reinterpret_cast<uintptr_t>(v_out);
+  if (!k_out || !v_out || k_out == v_out || (a | b) & 1) throw RpError(RP_ERR_INVALID_ARG, "read_kv: bad output");
+  int32_t* m = stage_meta(4);
+  m[0] = 0;
+  m[1] = n;
+  m[2] = first + n;
+  m[3] = it->second;
+  upload_meta(m, 4);
+  KvqBatch bt;
+  bt.n_seqs = 1;
+  bt.n_rows = bt.max_rows = n;
+  bt.max_context = first + n;
+  bt.row_off = d_meta_;
+  bt.context = d_meta_ + 2;
+  bt.page_table = sp<int32_t>(plan_.page_table);
+  bt.table_stride = plan_.max_pages;
+  bt.table_row = d_meta_ + 3;
+  KvqTensor k{k_out, static_cast<int64_t>(cfg_.n_kv_heads) * cfg_.head_dim, cfg_.head_dim, 1, 0}, v = k;
+  v.p = v_out;
+  k.vec = kvq_vec(k);
+  v.vec = kvq_vec(v);
+  HIP_TRY(launch_kvq_read(kvq_cache(layer), bt, k, v, stream_));
 }
 
 void Engine::set_packed_weights(void* ws, size_t bytes) {

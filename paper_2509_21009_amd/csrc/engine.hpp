@@ -13,6 +13,7 @@
 
 #include "../../include/rollpack.h"
 #include "kernels.hpp"
+#include "kvq.hpp"
 #include "kv_pool.hpp"
 
 namespace rollpack {
@@ -24,11 +25,12 @@ struct RpError : std::runtime_error {
 
 // Byte offsets of every buffer carved from the caller's scratch workspace.
 struct ScratchPlan {
-  size_t x, h, part, q, attn, act, hsel, logits, att_o, att_ml, rope_cos, rope_sin, page_table,
+  size_t x, h, part, q, attn, act, hsel, logits, att_o, att_ml, kvq, rope_cos, rope_sin, page_table,
       tokens_cur, hist, logp, resp, resp_logp, slot_seed, slot_id, slot_temp, meta, cand_val, cand_idx, cand_m,
       cand_s;
   size_t total;
   size_t part_elems;
+  size_t kvq_bytes;    // of the 4-bit cache's attention
   int32_t split_cap;   // decode attention work-item capacity (splits)
   int32_t max_pages;   // page-table row width
   int32_t meta_ints;
@@ -39,6 +41,7 @@ ScratchPlan plan_scratch(const rp_model_config& c, const rp_engine_limits& l);
 // the LM head), each tensor 256-byte aligned; 0 for the fp32 model.
 size_t packed_weights_bytes(const rp_model_config& c);
 size_t kv_pool_bytes(const rp_model_config& c, int64_t pages);
+size_t kv_token_bytes(const rp_model_config& c);  // one layer's K and V of one token
 void validate_config(const rp_model_config& c);
 void validate_limits(const rp_engine_limits& l);
 
@@ -129,6 +132,7 @@ class Engine {
   void abort(int32_t n, const int64_t* ids);
   int32_t get_tokens(int64_t id, int32_t* out, int32_t cap);
   int32_t get_logprobs(int64_t id, float* out, int32_t cap);
+  void read_kv(int64_t id, int32_t layer, int32_t first, int32_t n, void* k_out, void* v_out);
   void set_eos(int32_t token);
   int32_t rollout(int32_t n, const int64_t* ids, const int32_t* toks, const int64_t* offs,
                   const int32_t* max_new, uint64_t seed, float temp, const int32_t* round_ids,
@@ -223,12 +227,14 @@ class Engine {
   const void* packed_lm_ = nullptr;
   hipStream_t stream_;
   bool bf16_;
+  bool kv4_;  // bf16_ with the KV cache in 4 bits: each layer's pool is then a KvqCache
   size_t esz_;
   int nqkv_;
   ScratchPlan plan_;
   char* kv_;
   char* scratch_;
-  size_t layer_kv_bytes_;  // bytes of one layer's K (or V) pool
+  size_t layer_kv_bytes_;  // bytes of one layer's K (or V) pool; of both under kv4_
+  KvqCache kvq_cache(int layer) const;
   PagePool pool_;
   std::vector<Seq> slots_;
   std::vector<int32_t> free_slots_;
@@ -289,6 +295,7 @@ class Engine {
   std::vector<int32_t> ctx_scratch_;  // decode_step: per-row context lengths
   std::vector<int32_t> item_at_;      // decode_step: attention item counts by length
   int max_row_splits_ = 0;            // decode_step: most attention splits of any row
+  int max_ctx_ = 0, max_piece_ = 0;   // of the current forward: longest context, most rows of a sequence
   std::vector<hipEvent_t> events_;
 
   // per-kernel-class profiling (rp_profile_*)

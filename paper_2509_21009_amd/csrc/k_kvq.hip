@@ -226,6 +226,86 @@ __global__ __launch_bounds__(256) void k_kvq_read(KvqCache c, KvqBatch bt, KvqTe
   store8<BF16>(v, p.row, p.kh, p.d, vf);
 }
 
+// The engine's append.  A thread has eight rotated pairs of a query or key head (dimensions d .. d + 7 and d + hd/2 ..)
+// or eight dimensions of a value head of one row; the four threads of a scale block are neighbours.  The S partials are all
+// loaded before the first is added.  Keys and values are quantised from fp32: one rounding.
+template <int HD, int S>
+__global__ __launch_bounds__(256) void k_kvq_rope_append(KvqCache c, RopeArgs a) {
+  constexpr int HALF = HD / 2, PER = HALF / 8, VPER = HD / 8;
+  const int nq_el = a.n_q * HD, nk_el = a.n_kv * HD, nqkv = nq_el + 2 * nk_el;
+  const int units = (a.n_q + a.n_kv) * PER + a.n_kv * VPER;  // of a row, a multiple of four
+  const int64_t idx = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  const int i = static_cast<int>(idx / units), u = static_cast<int>(idx - static_cast<int64_t>(i) * units);
+  if (i >= a.M) return;
+  const bool value = u >= (a.n_q + a.n_kv) * PER;
+  const int uv = u - (a.n_q + a.n_kv) * PER;
+  const int head = value ? uv / VPER : u / PER, d = value ? uv % VPER * 8 : u % PER * 8;
+  const int n1 = value ? nq_el + nk_el + head * HD + d : head * HD + d;
+  const size_t plane = static_cast<size_t>(a.M) * nqkv;
+  const float* p = a.part + static_cast<size_t>(i) * nqkv + n1;
+  const int second = value ? 0 : HALF;
+  f32x4_t w[S][4];
+#pragma unroll
+  for (int s = 0; s < S; ++s)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[s][k] = *reinterpret_cast<const f32x4_t*>(p + s * plane + (k >= 2 ? second : 0) + 4 * (k & 1));
+  const int pos = a.pos[i], slot = a.slot[i];
+  const bool isq = !value && head < a.n_q;
+  const bf16_t* bias = value ? static_cast<const bf16_t*>(a.bv) + head * HD + d
+                       : isq ? static_cast<const bf16_t*>(a.bq) + n1
+                             : static_cast<const bf16_t*>(a.bk) + n1 - nq_el;
+  const u32x4 b1 = *reinterpret_cast<const u32x4*>(bias), b2 = *reinterpret_cast<const u32x4*>(bias + second);
+  const float* cs = a.rope_cos + static_cast<size_t>(pos) * HALF + (value ? 0 : d);
+  const float* sn = a.rope_sin + static_cast<size_t>(pos) * HALF + (value ? 0 : d);
+  float x[8], y[8];
+#pragma unroll
+  for (int s = 1; s < S; ++s)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[0][k] += w[s][k];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    x[e] = w[0][e >> 2][e & 3] + __uint_as_float(e & 1 ? b1[e >> 1] & 0xffff0000u : b1[e >> 1] << 16);
+    y[e] = w[0][2 + (e >> 2)][e & 3] + __uint_as_float(e & 1 ? b2[e >> 1] & 0xffff0000u : b2[e >> 1] << 16);
+  }
+  if (!value) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float r1 = x[e] * cs[e] - y[e] * sn[e], r2 = y[e] * cs[e] + x[e] * sn[e];
+      x[e] = r1;
+      y[e] = r2;
+    }
+    if (isq) {
+      const KvqTensor q{a.q_out, nq_el, HD, 1, 1};
+      store8<true>(q, i, head, d, x);
+      store8<true>(q, i, head, d + HALF, y);
+      return;
+    }
+  }
+  const int kh = value ? head : head - a.n_q, t = pos % kKvqPage;
+  const int page = a.page_table[static_cast<size_t>(slot) * a.pt_stride + pos / kKvqPage];
+  char* block = c.blocks + (static_cast<size_t>(page) * c.n_kv + kh) * kvq_block_bytes(HD);
+  uint32_t byte;
+  const uint32_t c1 = quantise8(x, byte);
+  if (value) {
+    if constexpr (HD == 128) {
+      *reinterpret_cast<uint32_t*>(block + kvq_v_code(t, d, HD)) = c1;
+    } else {
+      *reinterpret_cast<uint16_t*>(block + kvq_v_code(t, d, HD)) = static_cast<uint16_t>(c1);
+      *reinterpret_cast<uint16_t*>(block + kvq_v_code(t, d + 4, HD)) = static_cast<uint16_t>(c1 >> 16);
+    }
+    if (d % kKvqBlock == 0) block[kvq_v_scale(t, d / kKvqBlock, HD)] = static_cast<char>(byte);
+  } else {
+    uint32_t byte2;
+    const uint32_t c2 = quantise8(y, byte2);
+    *reinterpret_cast<uint32_t*>(block + kvq_k_code(t, d, HD)) = c1;
+    *reinterpret_cast<uint32_t*>(block + kvq_k_code(t, d + HALF, HD)) = c2;
+    if (d % kKvqBlock == 0) {
+      block[kvq_k_scale(t, d / kKvqBlock, HD)] = static_cast<char>(byte);
+      block[kvq_k_scale(t, (d + HALF) / kKvqBlock, HD)] = static_cast<char>(byte2);
+    }
+  }
+}
+
 // ---- which tile a block has ------------------------------------------------------------
 
 // Sums over the wave's lanes up to each lane, in six additions across lanes.
@@ -1133,12 +1213,44 @@ size_t kvq_attend_bytes(const KvqCache& c, const KvqBatch& b, int n_q) {
   return most;
 }
 
+size_t kvq_attend_bytes_most(const KvqCache& c, int n_q, int64_t max_seqs, int64_t max_rows, int max_context) {
+  // attend_plan splits to fewer than 384 + 256 items of 16 columns, or 512 + 512 of 128 (256), for all heads together, and
+  // none below 4 (8) pages; a call with both kinds has both
+  const int64_t pages = kvq_pages(max_context), G = n_q / c.n_kv;
+  auto most = [&](int64_t cols, int64_t target, int64_t under, int64_t least, int64_t tiles) {
+    const int64_t per_tile = std::min<int64_t>(kKvqTileItems, (pages + least - 1) / least);
+    const int64_t items = std::min((std::min(tiles, (under - 1) / c.n_kv + 1)) * c.n_kv * per_tile, target + under);
+    return per_tile > 1 ? static_cast<size_t>(items) * cols * (c.hd + 2) * 4 : size_t{0};
+  };
+  const int64_t rows = std::max(max_rows, max_seqs);
+  return most(16, 384, 256, 4, rows * G / 16 + max_seqs) + std::max(most(128, 512, 512, 8, rows * G / 128 + max_seqs), most(256, 512, 512, 8, rows * G / 256 + max_seqs));
+}
+
 bool kvq_attend_fits(const KvqCache& c, const KvqBatch& b, int n_q) {
   for (const bool bf16 : {true, false}) {
     const AttendPlan p = attend_plan(c, b, n_q, bf16);
     if (p.walk_tiles >= (1 << 22) || p.prompt_tiles >= (1 << 22)) return false;  // blocks of up to 512 threads, 2^32 in a dimension
   }
   return true;
+}
+
+template <int HD>
+static hipError_t rope_append_hd(const KvqCache& c, const RopeArgs& a, hipStream_t s) {
+  const int64_t units = static_cast<int64_t>(a.n_q + a.n_kv) * (HD / 16) + static_cast<int64_t>(a.n_kv) * (HD / 8);
+  const dim3 grid(static_cast<uint32_t>((a.M * units + 255) / 256));
+  switch (a.splits) {
+#define RP_ROPE(S) case S: launch_kernel((k_kvq_rope_append<HD, S>), grid, dim3(256), 0, s, c, a); break;
+    RP_ROPE(1) RP_ROPE(2) RP_ROPE(3) RP_ROPE(4) RP_ROPE(5) RP_ROPE(6) RP_ROPE(7) RP_ROPE(8)
+    RP_ROPE(9) RP_ROPE(10) RP_ROPE(11) RP_ROPE(12) RP_ROPE(13) RP_ROPE(14) RP_ROPE(15) RP_ROPE(16)
+#undef RP_ROPE
+    default: return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_kvq_rope_append(const KvqCache& c, const RopeArgs& a, hipStream_t s) {
+  if (a.M <= 0) return hipSuccess;
+  return c.hd == 128 ? rope_append_hd<128>(c, a, s) : rope_append_hd<64>(c, a, s);
 }
 
 hipError_t launch_kvq_append(const KvqCache& c, const KvqBatch& b, const KvqTensor& k, const KvqTensor& v, hipStream_t s) {

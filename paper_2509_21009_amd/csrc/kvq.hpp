@@ -191,11 +191,17 @@ inline int64_t kvq_tile_bound(const KvqBatch& b, int group, const KvqCut& cut) {
 }
 // Bytes of the workspace of launch_kvq_attend.
 size_t kvq_attend_bytes(const KvqCache& c, const KvqBatch& b, int n_q);
+// The most that any batch of up to these sequences, rows and contexts asks for.
+size_t kvq_attend_bytes_most(const KvqCache& c, int n_q, int64_t max_seqs, int64_t max_rows, int max_context);
 // Whether its launches are within a grid's limits.
 bool kvq_attend_fits(const KvqCache& c, const KvqBatch& b, int n_q);
 
 #ifdef __HIPCC__
 hipError_t launch_kvq_append(const KvqCache& c, const KvqBatch& b, const KvqTensor& k, const KvqTensor& v, hipStream_t s);
+struct RopeArgs;
+// The engine's append: bias and RoPE on the q/k/v projection's partials, the queries out in bf16, K and V of token i
+// into position a.pos[i] of page-table row a.slot[i].
+hipError_t launch_kvq_rope_append(const KvqCache& c, const RopeArgs& a, hipStream_t s);
 hipError_t launch_kvq_read(const KvqCache& c, const KvqBatch& b, const KvqTensor& k, const KvqTensor& v, hipStream_t s);
 // ws: of kvq_attend_bytes bytes.
 hipError_t launch_kvq_attend(const KvqAttendArgs& a, void* ws, hipStream_t s);

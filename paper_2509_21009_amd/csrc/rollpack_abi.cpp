@@ -215,8 +215,7 @@ rp_status rp_kv_bytes_per_token(const rp_model_config* cfg, size_t* bytes) {
   return guarded([&] {
     if (!cfg || !bytes) throw rollpack::RpError(RP_ERR_INVALID_ARG, "null argument");
     rollpack::validate_config(*cfg);
-    const size_t esz = cfg->dtype == RP_DTYPE_BF16 ? 2 : 4;
-    *bytes = static_cast<size_t>(cfg->n_layers) * 2 * cfg->n_kv_heads * cfg->head_dim * esz;
+    *bytes = cfg->n_layers * rollpack::kv_token_bytes(*cfg);
   });
 }
 
@@ -397,6 +396,10 @@ rp_status rp_get_logprobs(rp_engine* eng, int64_t seq_id, float* out, int32_t ca
     const int32_t k = e->get_logprobs(seq_id, out, cap);
     if (len_out) *len_out = k;
   });
+}
+
+rp_status rp_read_kv(rp_engine* eng, int64_t seq_id, int32_t layer, int32_t first, int32_t n, void* k_out, void* v_out) {
+  return engine_call(eng, [&](rollpack::Engine* e) { e->read_kv(seq_id, layer, first, n, k_out, v_out); });
 }
 
 rp_status rp_set_eos(rp_engine* eng, int32_t eos_token) {

@@ -15,7 +15,7 @@ import numpy as np
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "librollpack.so")
 
-RP_DTYPE_F32, RP_DTYPE_BF16 = 0, 1
+RP_DTYPE_F32, RP_DTYPE_BF16, RP_DTYPE_BF16_KV4 = 0, 1, 2
 STATUS = {0: "RP_OK", 1: "RP_ERR_INVALID_ARG", 2: "RP_ERR_OUT_OF_PAGES", 3: "RP_ERR_DUPLICATE_ID",
           4: "RP_ERR_UNKNOWN_ID", 5: "RP_ERR_BAD_STATE", 6: "RP_ERR_HIP", 7: "RP_ERR_CAPACITY"}
 
@@ -130,6 +130,7 @@ SIGNATURES = {
     "rp_abort": (ctypes.c_int, [_P, ctypes.c_int32, _I64P]),
     "rp_get_tokens": (ctypes.c_int, [_P, ctypes.c_int64, _I32P, ctypes.c_int32, _I32P]),
     "rp_get_logprobs": (ctypes.c_int, [_P, ctypes.c_int64, _F32P, ctypes.c_int32, _I32P]),
+    "rp_read_kv": (ctypes.c_int, [_P, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _P, _P]),
     "rp_set_eos": (ctypes.c_int, [_P, ctypes.c_int32]),
     "rp_rollout_generate": (ctypes.c_int, [_P, ctypes.c_int32, _I64P, _I32P, _I64P, _I32P, ctypes.c_uint64,
                                            ctypes.c_float, _I32P, _I32P, _F32P, _I32P, ctypes.POINTER(RpRoundStats),
@@ -365,6 +366,10 @@ def rp_get_logprobs(eng: int, seq_id: int, cap: int) -> np.ndarray:
     return out[:min(n.value, cap)]
 
 
+def rp_read_kv(eng: int, seq_id: int, layer: int, first: int, n: int, k_ptr: int, v_ptr: int) -> None:
+    _check(load_library().rp_read_kv(eng, seq_id, layer, first, n, k_ptr, v_ptr))
+
+
 def rp_set_eos(eng: int, eos_token: int) -> None:
     _check(load_library().rp_set_eos(eng, eos_token))
 
@@ -526,11 +531,13 @@ def rp_last_error() -> str:
 
 # ---- convenience owner of the device buffers ----------------------------------------
 
-def model_config(shape) -> RpModelConfig:
-    """RpModelConfig from any object with the Qwen2.5 shape attributes."""
+def model_config(shape, kv4: bool = False) -> RpModelConfig:
+    """RpModelConfig from any object with the Qwen2.5 shape attributes; kv4: the KV cache of a bf16 model in 4 bits."""
+    if kv4 and shape.dtype != "bf16":
+        raise ValueError("the 4-bit cache belongs to bf16 models")
     return RpModelConfig(shape.layers, shape.hidden, shape.n_q, shape.n_kv, shape.head_dim, shape.inter,
                          shape.vocab, shape.eps, shape.theta, 1 if shape.tied else 0,
-                         RP_DTYPE_BF16 if shape.dtype == "bf16" else RP_DTYPE_F32)
+                         RP_DTYPE_BF16_KV4 if kv4 else RP_DTYPE_BF16 if shape.dtype == "bf16" else RP_DTYPE_F32)
 
 
 class Engine:
@@ -541,14 +548,15 @@ class Engine:
     contiguous device tensors of the model dtype.  The dict is kept alive.
     pack_weights: for a bf16 model, also allocate the packed copy of the
     weights that the decode GEMMs stream (rp_engine_set_packed_weights).
+    kv4: for a bf16 model, keep the KV cache in 4 bits (RP_DTYPE_BF16_KV4).
     """
 
     def __init__(self, shape, weights: dict, max_seqs: int, max_prefill_tokens: int, max_context: int,
-                 kv_pages: int, stream=None, pack_weights: bool = True):
+                 kv_pages: int, stream=None, pack_weights: bool = True, kv4: bool = False):
         import torch
         self.torch = torch
         self.shape = shape
-        self.cfg = model_config(shape)
+        self.cfg = model_config(shape, kv4)
         self.limits = RpEngineLimits(max_seqs, max_prefill_tokens, max_context, 64, kv_pages)
         kv_bytes, sc_bytes = rp_workspace_size(self.cfg, self.limits)
         dev = weights["embed"].device
@@ -606,6 +614,13 @@ class Engine:
 
     def get_logprobs(self, seq_id: int, cap: int):
         return rp_get_logprobs(self.handle, seq_id, cap)
+
+    def read_kv(self, seq_id: int, layer: int, first: int, n: int):
+        """(K, V) [n, n_kv, head_dim] bf16 that a 4-bit cache holds of a live sequence's positions."""
+        torch = self.torch
+        k, v = (torch.empty((n, self.shape.n_kv, self.shape.head_dim), dtype=torch.bfloat16, device=self.kv.device) for _ in range(2))
+        rp_read_kv(self.handle, seq_id, layer, first, n, k.data_ptr(), v.data_ptr())
+        return k, v
 
     def set_eos(self, eos_token: int):
         rp_set_eos(self.handle, eos_token)
@@ -772,10 +787,10 @@ def weights_struct(shape, weights: dict):
 
 def generate(shape, weights: dict, seq_ids, prompt_tokens, prompt_offsets, max_new_tokens, seed: int,
              temperature: float, *, limits: RpEngineLimits, schedule_mode: int = SCHEDULE_NONE, round_ids=None,
-             tail: Optional[RpTailParams] = None, stream=None):
+             tail: Optional[RpTailParams] = None, stream=None, kv4: bool = False):
     """rp_generate with workspaces allocated here from torch (freed when the call returns)."""
     import torch
-    cfg = model_config(shape)
+    cfg = model_config(shape, kv4)
     kv_bytes, sc_bytes = rp_workspace_size(cfg, limits)
     dev = weights["embed"].device
     kv = torch.empty(kv_bytes, dtype=torch.uint8, device=dev)

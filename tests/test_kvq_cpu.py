@@ -147,3 +147,26 @@ def test_oracle_quantiser():
     assert np.isnan(okvq.held(np.r_[np.inf, np.zeros(31), np.ones(32)])[:32]).all()
     ties = np.r_[[0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0], np.zeros(24)]
     assert okvq.held(ties)[:8].tolist() == [0.0, 1.0, 1.0, 2.0, 2.0, 4.0, 4.0, 6.0]
+
+
+def test_engine_sizes_with_the_cache_in_four_bits(lib):
+    """A token takes 17/64 of its bf16 bytes, the pool with it; packed weights stay; fp32 models are refused."""
+    import dataclasses
+    from workloads import SHAPES
+    s = SHAPES["qwen2.5-7b"]
+    cfg, bf16 = rp.model_config(s, kv4=True), rp.model_config(s)
+    assert rp.rp_kv_bytes_per_token(cfg) == 57344 * 17 // 64
+    lim = rp.RpEngineLimits(64, 4096, 17408, 64, 1000)
+    assert rp.rp_workspace_size(cfg, lim)[0] == 1000 * 64 * 57344 * 17 // 64
+    assert rp.rp_packed_weights_bytes(cfg) == rp.rp_packed_weights_bytes(bf16) > 0
+    with pytest.raises(ValueError):
+        rp.model_config(SHAPES["tiny"], kv4=True)
+    bad = rp.model_config(dataclasses.replace(s, n_q=20, n_kv=1), kv4=True)
+    with pytest.raises(rp.RollpackError):
+        rp.rp_workspace_size(bad, lim)
+    cfg.dtype = 3
+    with pytest.raises(rp.RollpackError):
+        rp.rp_workspace_size(cfg, lim)
+    with pytest.raises(rp.RollpackError) as e:
+        rp.rp_read_kv(None, 1, 0, 0, 1, PTR, 2 * PTR)
+    assert e.value.status == 1
