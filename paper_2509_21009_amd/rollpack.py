@@ -681,6 +681,8 @@ class KvqCache:
             raise ValueError("the 4-bit cache lives in GPU memory")
         self.struct = RpKvqCache(self.blocks.data_ptr(), n_pages, n_kv_heads, head_dim)
         self._types = {torch.float32: RP_DTYPE_F32, torch.bfloat16: RP_DTYPE_BF16}
+        # the handle alone: a torch.cuda.Stream object would cost each call 1.7 us
+        self._raw_stream = torch._C._cuda_getCurrentRawStream
 
     def batch(self, contexts, page_table, row_offsets=None, n_rows: Optional[int] = None,
               max_rows: Optional[int] = None, max_context: Optional[int] = None) -> KvqBatch:
@@ -714,22 +716,21 @@ class KvqCache:
         return KvqBatch(b, (contexts, page_table, row_offsets))
 
     def _tensor(self, t, rows: int, heads: int) -> RpKvqTensor:
-        if t.device != self.device or tuple(t.shape) != (rows, heads, self.head_dim):
-            raise ValueError(f"expected [{rows}, {heads}, {self.head_dim}] on {self.device}, got {tuple(t.shape)} on {t.device}")
         dt = self._types.get(t.dtype)
-        if dt is None or (t.stride(2) != 1 and t.numel() > 0):
-            raise ValueError("tensors are float32 or bfloat16 with contiguous head dimensions")
-        return RpKvqTensor(t.data_ptr(), t.stride(0), t.stride(1), dt)
+        strides = t.stride()
+        if t.device != self.device or t.shape != (rows, heads, self.head_dim) or dt is None or (strides[2] != 1 and t.numel() > 0):
+            raise ValueError(f"expected float32 or bfloat16 [{rows}, {heads}, {self.head_dim}] with contiguous head dimensions on "
+                             f"{self.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        return RpKvqTensor(t.data_ptr(), strides[0], strides[1], dt)
 
     def _call(self, fn, *args):
         """fn(cache, *args, stream) with the cache's device current."""
         cuda = self.torch.cuda
-        stream = cuda.current_stream(self.device).cuda_stream
         if cuda.current_device() == self.device.index:
-            fn(self.struct, *args, stream)
+            fn(self.struct, *args, self._raw_stream(self.device.index))
         else:
             with cuda.device(self.device):
-                fn(self.struct, *args, stream)
+                fn(self.struct, *args, self._raw_stream(self.device.index))
 
     def append(self, batch: KvqBatch, k, v) -> None:
         """Quantise k and v [n_rows, n_kv_heads, head_dim] into the cache at the rows' positions."""
@@ -740,9 +741,8 @@ class KvqCache:
         """(k, v) that the cache holds of the batch's rows, in dtype (bfloat16) or into the tensors `out`."""
         torch, n = self.torch, batch.struct.n_rows
         if out is None:
-            dims = (n, self.n_kv_heads, self.head_dim)
-            dtype = torch.bfloat16 if dtype is None else dtype
-            out = (torch.empty(dims, dtype=dtype, device=self.device), torch.empty(dims, dtype=dtype, device=self.device))
+            out = torch.empty((2, n, self.n_kv_heads, self.head_dim), dtype=torch.bfloat16 if dtype is None else dtype,
+                              device=self.device).unbind()
         k, v = out
         self._call(rp_kvq_read, batch.struct, self._tensor(k, n, self.n_kv_heads), self._tensor(v, n, self.n_kv_heads))
         return k, v
@@ -759,7 +759,7 @@ class KvqCache:
             raise ValueError("q is [n_rows, n_q_heads, head_dim]")
         heads = q.shape[1]
         if out is None:
-            out = torch.empty(tuple(q.shape), dtype=q.dtype, device=self.device)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         if workspace is None:
             workspace = self.attend_workspace(batch, heads)
         elif workspace.device != self.device or not workspace.is_contiguous():
