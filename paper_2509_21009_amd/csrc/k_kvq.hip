@@ -889,6 +889,19 @@ __device__ __forceinline__ void share_store(const PageShare<HD>& s, int th, bool
   }
 }
 
+// Orders the N products before it, each of one 16-byte LDS read: six reads ahead of the first, then one to each.
+template <int N>
+__device__ __forceinline__ void reads_ahead() {
+  constexpr int A = N < 6 ? N : 6;
+  __builtin_amdgcn_sched_group_barrier(0x100, A, 0);  // LDS reads
+#pragma unroll
+  for (int i = 0; i < N - A; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // MFMA
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, A, 0);
+}
+
 // O^T += V^T P^T for a page: the lane's 32 probabilities x in two pieces of bf16, or w in fp16.
 template <int HD, bool HALF>
 __device__ __forceinline__ void page_values(const u32x4* lv, const float (&x)[32], const uint32_t (&w16)[16], f32x16 (&o)[HD / 32]) {
@@ -916,6 +929,7 @@ __device__ __forceinline__ void page_values(const u32x4* lv, const float (&x)[32
       }
     }
   }
+  if constexpr (HALF) reads_ahead<HD / 8>();
 }
 
 template <int HD, int NW>
@@ -1023,6 +1037,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_kvq_prompt(KvqAttendArgs a, KvqC
         for (int j = 0; j < KS; ++j)
 #pragma unroll
           for (int t = 0; t < 2; ++t) s[t] = mfma32x32x16(__builtin_bit_cast(bf16x8_t, lk[(t * KS + j) * 64 + lane]), qf[j], s[t]);
+        reads_ahead<2 * KS>();
         if (lost_now || tok0 + kKvqPage > open) {
           asm volatile("");  // a branch: as selects it would cost every page
 #pragma unroll
@@ -1113,7 +1128,6 @@ __global__ __launch_bounds__(256) void k_kvq_join(KvqAttendArgs a, KvqCut cut) {
   const int b = cut.find ? find_tile(a.batch, G, cut, blockIdx.x, tile) : static_cast<int>(blockIdx.x);
   if (b < 0) return;
   const KvqSeq sq = kvq_seq(a.batch, b);
-  if (cut.cols > 16) tile = kvq_tiles(sq, G, cut) - 1 - tile;  // as k_kvq_prompt numbers them
   const KvqTile tl = kvq_tile(sq, G, tile, cut.cols);
   const int n = kvq_items(kvq_pages(tl.end), cut.items, cut.least);
   if (n == 1 || col >= tl.cols) return;  // one item has written the output itself
@@ -1158,37 +1172,120 @@ __global__ __launch_bounds__(256) void k_kvq_join(KvqAttendArgs a, KvqCut cut) {
   }
 }
 
-// What a call of attention launches, from its bounds alone.
+// The same for k_kvq_prompt's tiles, which have many columns and few items: HD / 4 lanes to a column.
+template <int HD>
+__global__ __launch_bounds__(256) void k_kvq_join_prompt(KvqAttendArgs a, KvqCut cut) {
+  constexpr int LPC = HD / 4, PER = kKvqTileItems / LPC;
+  const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
+  const int kh = blockIdx.y, d4 = threadIdx.x % LPC, col = blockIdx.z * (256 / LPC) + threadIdx.x / LPC;
+  int tile = 0;
+  const int b = find_tile(a.batch, G, cut, blockIdx.x, tile);
+  if (b < 0) return;
+  const KvqSeq sq = kvq_seq(a.batch, b);
+  tile = kvq_tiles(sq, G, cut) - 1 - tile;  // as k_kvq_prompt numbers them
+  const KvqTile tl = kvq_tile(sq, G, tile, cut.cols);
+  const int n = kvq_items(kvq_pages(tl.end), cut.items, cut.least);
+  if (n == 1 || col >= tl.cols) return;  // one item has written the output itself
+  const int64_t part = static_cast<int64_t>(blockIdx.x) * cut.items * n_kv + kh;  // of item 0; n_kv between items
+  const float* ml = a.part_ml + part * 2 * cut.cols + col;
+  float m[PER], l[PER], mx = -INFINITY, den = 0.f;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {  // items d4, d4 + LPC, ...
+    const int i = d4 + LPC * k;
+    const float* p = ml + static_cast<int64_t>(min(i, n - 1)) * n_kv * 2 * cut.cols;
+    m[k] = i < n ? p[0] : -INFINITY;
+    l[k] = i < n ? p[cut.cols] : 0.f;
+    mx = fmaxf(mx, m[k]);
+  }
+#pragma unroll
+  for (int x = 1; x < LPC; x *= 2) mx = fmaxf(mx, __shfl_xor(mx, x, 64));
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    m[k] = m[k] == -INFINITY ? (l[k] == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m[k] - mx);
+    den += m[k] * l[k];
+  }
+#pragma unroll
+  for (int x = 1; x < LPC; x *= 2) den += __shfl_xor(den, x, 64);
+  const float* po = a.part_o + (part * cut.cols + col) * HD + 4 * d4;
+  const int64_t step = static_cast<int64_t>(n_kv) * cut.cols * HD;
+  f32x4_t sum{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < PER; ++k)
+    for (int i0 = LPC * k; i0 < min(n, LPC * (k + 1)); i0 += 4) {
+      f32x4_t x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const f32x4_t*>(po + min(i0 + i, n - 1) * step);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float w = __shfl(m[k], (i0 + i) % LPC, LPC);
+        if (i0 + i < n) sum += x[i] * w;
+      }
+    }
+  const int row = (tile * cut.cols + col) / G, head = kh * G + tile * cut.cols + col - row * G;
+  const float inv = tl.first + row < 0 ? 0.f : 1.f / den;
+  float out[8];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    out[e] = sum[e] * inv;
+    out[4 + e] = __shfl_xor(out[e], 1, 64);
+  }
+  if (!(d4 & 1)) store8<true>(a.out, sq.r0 + row, head, 4 * d4, out);
+}
+
+// What a call of attention launches, from its bounds alone.  Times in microseconds, bf16; 7 query heads to each of 4
+// KV heads of 128 dims where nothing else is said ("2 x 64" names KV heads and dims).
 struct AttendPlan {
   KvqCut walk, prompt;              // k_kvq_attend's tiles and k_kvq_prompt's
   int64_t walk_tiles = 0, prompt_tiles = 0;  // at most; 0: not launched
   int waves = 4, prompt_waves = 4;  // of a block
 };
 
+// Whether k_kvq_prompt takes the sequences of more than 64 columns.  It shares a page's unpacking among 128 columns, but
+// its blocks take their pages in turn and a page costs one ~2.2 us: it wants enough tiles to fill the card, or so much
+// work that it can be split over the keys.  k_kvq_prompt | k_kvq_attend:
+//   by tiles: 32 prompts of 128 tokens 28 | 39, 8 of 512 44 | 60, one of 2,048 63 | 75; one of 1,024 34 | 31, of 512 20 | 15,
+//     of 397 17 | 11; 2 x 64, 8 of 512 20 | 30, 32 last rows 64 of 1,000 keys 32 | 27
+//   by work: the last 512 rows of 14,000 keys 140 | 183, 128 of 14,000 55 | 69, 64 of 14,000 41 | 40, 128 of 3,000 29 | 29,
+//     256 of 2,000 30 | 20; 2 x 64, 512 of 14,000 55 | 73, one prompt of 2,048 35 | 27
+bool prompt_pays(const KvqCache& c, int64_t tiles, int pages) {  // of 16 columns, over all KV heads
+  return tiles >= 2048 || tiles * pages * c.hd >= int64_t{1} << 22;
+}
+
 AttendPlan attend_plan(const KvqCache& c, const KvqBatch& b, int n_q, bool bf16) {
   const int G = n_q / c.n_kv;
   const int64_t most = static_cast<int64_t>(kvq_max_rows(b)) * G;  // columns of a sequence
   const int pages = std::max(1, kvq_pages(b.max_context));
   AttendPlan p;
-  if (bf16 && most > 64) {
-    p.prompt_waves = 4;
-    p.prompt.cols = 32 * p.prompt_waves;
+  p.walk.find = most > p.walk.cols;
+  if (bf16 && most > 64 && prompt_pays(c, kvq_tile_bound(b, G, p.walk) * c.n_kv, pages)) {
     p.prompt.find = 1;
     p.prompt.least = 8;
     if (static_cast<int64_t>(b.n_seqs) * kvq_max_rows(b) > b.n_rows) p.prompt.above = p.walk.upto = 64;  // else all have as many rows
+    // Eight waves, 256 columns, halve the unpacking: 1,423 | 1,532 with four for one prompt of 14,500 tokens, 184 | 195 of
+    // 4,096, 404 | 446 for the last 2,048 rows of 14,000 keys; with fewer pages the start of a block counts: 69 | 63 for
+    // 2,048 tokens, 139 | 127 for 20 prompts of 128 to 1,024.  At 64 dims a page is half the work: 198 | 185 for 8,192.
+    p.prompt.cols = 256;
     p.prompt_tiles = kvq_tile_bound(b, G, p.prompt);
+    p.prompt_waves = c.hd == 128 && pages >= 64 && p.prompt_tiles * c.n_kv >= 192 ? 8 : 4;
+    p.prompt.cols = 32 * p.prompt_waves;
+    p.prompt_tiles = kvq_tile_bound(b, G, p.prompt);
+    // Up to 512 blocks, which the card holds at once: one more is another turn, and a split one writes 512 bytes of
+    // partial output per column.  One item | two: 452 blocks, 2,048 tokens, 63 | 88; 112, the last 512 rows of 14,000
+    // keys, 359 | 194, four 140, five 171.
     const int64_t blocks = std::max<int64_t>(1, p.prompt_tiles * c.n_kv);
-    if (blocks < 512) p.prompt.items = static_cast<int>(std::min<int64_t>(kvq_items(pages, kKvqTileItems, p.prompt.least), (512 + blocks - 1) / blocks));
+    if (p.prompt_waves == 4 && blocks <= 256) p.prompt.items = static_cast<int>(std::min<int64_t>(kvq_items(pages, kKvqTileItems, p.prompt.least), 512 / blocks));
   }
   if (p.prompt_tiles && !p.prompt.above) return p;
-  p.walk.find = std::min<int64_t>(most, p.walk.upto) > p.walk.cols || p.prompt_tiles;
   p.walk_tiles = kvq_tile_bound(b, G, p.walk);
   const int64_t blocks = std::max<int64_t>(1, p.walk_tiles * c.n_kv);
   p.walk.least = 4;
   if (blocks < 256 && pages > 16) p.walk.items = static_cast<int>(std::min<int64_t>(kvq_items(pages, kKvqTileItems, p.walk.least), (384 + blocks - 1) / blocks));
   const int64_t all = blocks * p.walk.items;
   const int per = kvq_item_pages(pages, p.walk.items);
-  p.waves = all >= 2048 && per <= 4 ? 1 : all <= 384 && per > 16 ? 8 : 4;
+  // One wave where the blocks are 512 to each page, which nothing has to join: 8 prompts of 128 tokens 13.8 | 21.8 with
+  // four; 64 decoded tokens of 600 to 4,500 keys (256 blocks) 83 | 28.  Eight for few blocks and many pages: the latter
+  // 23.4 | 28.0; 330 of 130 to 1,300 48 | 38.
+  p.waves = all >= 512 * per ? 1 : all <= 384 && per > 16 ? 8 : 4;
   return p;
 }
 
@@ -1199,10 +1296,6 @@ size_t part_floats(const KvqCut& cut, int64_t tiles, int n_kv, int hd) {  // of 
 template <int HD, bool F32>
 hipError_t attend_launch(KvqAttendArgs a, const AttendPlan& p, float* ws, hipStream_t s) {
   const int n_kv = a.cache.n_kv;
-  auto join = [&](const KvqCut& cut, int64_t tiles) {
-    const int64_t most = std::min<int64_t>(cut.upto, static_cast<int64_t>(kvq_max_rows(a.batch)) * (a.n_q / n_kv));
-    launch_kernel((k_kvq_join<HD, F32>), dim3(static_cast<uint32_t>(tiles), n_kv, static_cast<uint32_t>(std::min<int64_t>(cut.cols, most))), dim3(256), 0, s, a, cut);
-  };
   if (p.prompt_tiles) {
     const size_t n = part_floats(p.prompt, p.prompt_tiles, n_kv, HD);
     a.part_o = ws;
@@ -1211,9 +1304,11 @@ hipError_t attend_launch(KvqAttendArgs a, const AttendPlan& p, float* ws, hipStr
     if constexpr (!F32) {
       const dim3 grid(static_cast<uint32_t>(p.prompt_tiles), n_kv, p.prompt.items);
       if (p.prompt_waves == 4) launch_kernel((k_kvq_prompt<HD, 4>), grid, dim3(256), 0, s, a, p.prompt);
-      else launch_kernel((k_kvq_prompt<HD, 8>), grid, dim3(512), 0, s, a, p.prompt);
+      else if constexpr (HD == 128) launch_kernel((k_kvq_prompt<HD, 8>), grid, dim3(512), 0, s, a, p.prompt);
+      else return hipErrorInvalidValue;
+      constexpr int kCols = 1024 / HD;  // of a block of k_kvq_join_prompt
+      if (n) launch_kernel((k_kvq_join_prompt<HD>), dim3(grid.x, n_kv, p.prompt.cols / kCols), dim3(256), 0, s, a, p.prompt);
     }
-    if (n) join(p.prompt, p.prompt_tiles);
   }
   if (p.walk_tiles) {
     const size_t n = part_floats(p.walk, p.walk_tiles, n_kv, HD);
@@ -1226,7 +1321,8 @@ hipError_t attend_launch(KvqAttendArgs a, const AttendPlan& p, float* ws, hipStr
       case 8: launch_kernel((k_kvq_attend<HD, F32, 8>), grid, dim3(512), 0, s, a, p.walk); break;
       default: return hipErrorInvalidValue;
     }
-    if (n) join(p.walk, p.walk_tiles);
+    const int64_t most = std::min<int64_t>(p.walk.upto, static_cast<int64_t>(kvq_max_rows(a.batch)) * (a.n_q / n_kv));
+    if (n) launch_kernel((k_kvq_join<HD, F32>), dim3(grid.x, n_kv, static_cast<uint32_t>(std::min<int64_t>(p.walk.cols, most))), dim3(256), 0, s, a, p.walk);
   }
   return hipGetLastError();
 }
@@ -1257,16 +1353,15 @@ size_t kvq_attend_bytes(const KvqCache& c, const KvqBatch& b, int n_q) {
 }
 
 size_t kvq_attend_bytes_most(const KvqCache& c, int n_q, int64_t max_seqs, int64_t max_rows, int max_context) {
-  // attend_plan splits to fewer than 384 + 256 items of 16 columns, or 512 + 512 of 128 (256), for all heads together, and
-  // none below 4 (8) pages; a call with both kinds has both
-  const int64_t pages = kvq_pages(max_context), G = n_q / c.n_kv;
-  auto most = [&](int64_t cols, int64_t target, int64_t under, int64_t least, int64_t tiles) {
-    const int64_t per_tile = std::min<int64_t>(kKvqTileItems, (pages + least - 1) / least);
-    const int64_t items = std::min((std::min(tiles, (under - 1) / c.n_kv + 1)) * c.n_kv * per_tile, target + under);
+  // attend_plan splits fewer than 256 blocks of 16 columns to fewer than 384 + 256 items of at least 4 pages, and up to 256
+  // of 128 to at most 512 of 8; a call with both kinds has both
+  const int64_t pages = kvq_pages(max_context), G = n_q / c.n_kv, rows = std::max(max_rows, max_seqs);
+  auto most = [&](int64_t cols, int64_t blocks, int64_t most_items, int64_t least) {
+    const int64_t per_tile = std::min<int64_t>(kKvqTileItems, (pages + least - 1) / least), tiles = rows * G / cols + max_seqs;
+    const int64_t items = std::min(std::min(tiles * c.n_kv, blocks) * per_tile, most_items);
     return per_tile > 1 ? static_cast<size_t>(items) * cols * (c.hd + 2) * 4 : size_t{0};
   };
-  const int64_t rows = std::max(max_rows, max_seqs);
-  return most(16, 384, 256, 4, rows * G / 16 + max_seqs) + std::max(most(128, 512, 512, 8, rows * G / 128 + max_seqs), most(256, 512, 512, 8, rows * G / 256 + max_seqs));
+  return most(16, 255, 384 + 255, 4) + most(128, 256, 512, 8);
 }
 
 bool kvq_attend_fits(const KvqCache& c, const KvqBatch& b, int n_q) {

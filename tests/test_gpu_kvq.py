@@ -47,10 +47,18 @@ def _ints(a):
     return torch.tensor(a, dtype=torch.int32, device=DEV)
 
 
-class Setup:
-    """Sequences with random K and V in a cache whose pages are shuffled; numpy copies of what it holds."""
+def _room(kind, n_q, hd):
+    """Bounds of a call (rows, context) under which sequences of many rows go to each form of the kernel for them,
+    however few rows they have: many tiles; fewer of more pages, split over the keys; blocks of eight waves."""
+    return {"": None, "tiles": (-(-2048 * 16 // n_q), 0), "split": (-(-512 * 16 // n_q), 64 * 8192 // hd),
+            "eight": (-(-49152 // n_q), 4096)}[kind]
 
-    def __init__(self, n_q, n_kv, hd, ctx, rows=None, dtype="bf16", seed=0, spare=2, gain=1.0):
+
+class Setup:
+    """Sequences with random K and V in a cache whose pages are shuffled; numpy copies of what it holds.
+    room: rows and context of the calls' bounds, if more than the sequences'; the rows behind the last one are NaN."""
+
+    def __init__(self, n_q, n_kv, hd, ctx, rows=None, dtype="bf16", seed=0, spare=2, gain=1.0, room=None):
         self.n_q, self.n_kv, self.hd, self.ctx = n_q, n_kv, hd, list(ctx)
         self.rows = [1] * len(ctx) if rows is None else list(rows)
         self.dtype, self.dt = dtype, TYPES[dtype]
@@ -58,7 +66,8 @@ class Setup:
         need = [-(-c // 64) for c in ctx]
         self.cache = rp().KvqCache(sum(need) + spare, n_kv, hd, device=DEV)
         perm = rng.permutation(sum(need) + spare).astype(np.int32)
-        self.table = np.full((len(ctx), max(need + [1])), -1, np.int32)
+        self.room = room = room and (max(room[0], sum(self.rows)), room[1])
+        self.table = np.full((len(ctx), max(need + [1, room[1] // 64 if room else 0])), -1, np.int32)
         at = 0
         for b, n in enumerate(need):
             self.table[b, :n] = perm[at:at + n]
@@ -68,9 +77,14 @@ class Setup:
         chan = np.where(rng.random((n_kv, hd)) < 0.05, 6.0, 1.0) * gain
         self.k = torch.from_numpy((rng.standard_normal((tot, n_kv, hd)) * chan).astype(np.float32)).to(DEV).to(self.dt)
         self.v = torch.from_numpy(rng.standard_normal((tot, n_kv, hd)).astype(np.float32)).to(DEV).to(self.dt)
-        self.q = torch.from_numpy(rng.standard_normal((max(sum(self.rows), 0), n_q, hd)).astype(np.float32)).to(DEV).to(self.dt)
+        q = rng.standard_normal((sum(self.rows), n_q, hd)).astype(np.float32)
+        if room:
+            q = np.concatenate([q, np.full((room[0] - len(q), n_q, hd), np.nan, np.float32)])
+        self.q = torch.from_numpy(q).to(DEV).to(self.dt)
 
     def batch(self, rows=None, ctx=None, **kw):
+        if rows is None and self.room:
+            kw = {**dict(n_rows=self.room[0], max_rows=self.room[0]), **kw}
         rows = self.rows if rows is None else rows
         ctx = self.ctx if ctx is None else ctx
         off = _ints(np.concatenate([[0], np.cumsum(rows)]))
@@ -230,6 +244,41 @@ def test_attend_several_rows(n_q, n_kv, hd, dtype):
     s.check(s.cache.attend(s.batch(), s.q))
 
 
+@pytest.mark.parametrize("n_q,n_kv,hd,kind", [
+    (28, 4, 128, "tiles"), (28, 4, 128, "split"), (28, 4, 128, "eight"), (14, 2, 64, "tiles"), (14, 2, 64, "split"),
+    (40, 2, 128, "split"), (40, 2, 128, "eight"), (3, 3, 64, "tiles"), (3, 1, 128, "eight"), (6, 1, 64, "split"),
+])
+def test_attend_prompts_and_long_pieces(n_q, n_kv, hd, kind):
+    """Sequences below, at and above 64 columns, tiles of 128 and 256 columns that end anywhere, contexts of several
+    items, and rows behind the last sequence, which stay as they were."""
+    group = n_q // n_kv
+    edge = [max(1, c // group) for c in (63, 64, 65, 127, 128, 129, 255, 256, 257)]
+    rows = [1, 2] + edge + [e + 1 for e in edge] + [100, 1, 30, 0, 17]
+    ctx = [1, 9] + edge + [e + 64 for e in edge] + [700, 1100, 1200, 50, 513]
+    s = Setup(n_q, n_kv, hd, ctx, rows, seed=n_q + 2, room=_room(kind, n_q, hd)).fill()
+    out = torch.full_like(s.q, 5.0)
+    s.cache.attend(s.batch(), s.q, out=out)
+    s.check(out)
+    assert (out[sum(rows):] == 5).all()
+
+
+@pytest.mark.parametrize("n_q,n_kv,hd,kind", [(28, 4, 128, "tiles"), (28, 4, 128, "eight"), (28, 4, 128, "split"), (14, 2, 64, "split")])
+def test_attend_one_sequence_of_many_rows(n_q, n_kv, hd, kind):
+    """All sequences have as many rows as the bound: nothing is left for the other kernel."""
+    n, c = _room(kind, n_q, hd)
+    n = min(n, 300)
+    s = Setup(n_q, n_kv, hd, [900], [n], seed=31)
+    wide = torch.full((1, max(15, -(-c // 64))), -1, dtype=torch.int32, device=DEV)
+    wide[:, :15] = s.dev_table
+    s.fill()
+    rows = _room(kind, n_q, hd)[0]
+    q = torch.zeros((rows, n_q, hd), dtype=s.dt, device=DEV)
+    q[:n] = s.q
+    b = s.cache.batch(_ints([900]), wide, row_offsets=_ints([0, n]), n_rows=rows, max_rows=rows)
+    out = s.cache.attend(b, q)
+    s.check(out)
+
+
 @pytest.mark.parametrize("dtype,ctx,rows", [
     ("bf16", [5000], [1]),                              # one row, split over the GPU and joined
     ("f32", [4100], [2]),
@@ -293,13 +342,16 @@ def test_what_lies_behind_the_context_does_not_matter(n_q, n_kv, hd):
     assert torch.equal(s.cache.blocks, before)
 
 
-@pytest.mark.parametrize("hd", [64, 128])
-@pytest.mark.parametrize("rows", [[1, 1, 1], [90, 130, 20]])
-def test_nan_and_infinities_reach_only_rows_that_see_them(hd, rows):
+@pytest.mark.parametrize("hd,rows,kind", [
+    (64, [1, 1, 1], ""), (128, [1, 1, 1], ""), (64, [90, 130, 20], ""), (128, [90, 130, 20], ""),
+    (64, [90, 130, 30], "tiles"), (128, [90, 130, 30], "tiles"), (64, [90, 130, 30], "split"), (128, [90, 130, 30], "split"),
+    (128, [90, 130, 30], "eight"),
+])
+def test_nan_and_infinities_reach_only_rows_that_see_them(hd, rows, kind):
     """A NaN key makes its readers' rows NaN, a NaN value block its 32 dimensions of them; earlier rows are untouched."""
     n_q, n_kv = 6, 2
     ctx = [100, 130, 1200]
-    s = Setup(n_q, n_kv, hd, ctx, rows, seed=8)
+    s = Setup(n_q, n_kv, hd, ctx, rows, seed=8, room=_room(kind, n_q, hd))
     s.k[40, 0, 5] = float("nan")       # sequence 0, position 40, head 0
     s.v[100 + 60, 1, 40] = float("inf")  # sequence 1, position 60, head 1, dimensions 32..63
     s.v[230 + 1195, 0, hd - 1] = float("nan")
@@ -330,22 +382,23 @@ def test_nan_and_infinities_reach_only_rows_that_see_them(hd, rows):
     assert torch.isnan(out[0, 1:3]).all() and (rows[0] == 1 or not torch.isnan(out[0, 3:]).any())
 
 
-def test_large_scores_do_not_overflow():
+@pytest.mark.parametrize("kind", ["", "tiles", "split", "eight"])
+def test_large_scores_do_not_overflow(kind):
     """Scores in the thousands, and equal ones: the running maximum keeps every exponent in range."""
     for dtype in ("bf16", "f32"):
-        s = Setup(7, 1, 128, [700, 65, 1], rows=[3, 65, 1], dtype=dtype, seed=10, gain=30.0).fill()
+        s = Setup(7, 1, 128, [700, 65, 1], rows=[30 if kind else 3, 65, 1], dtype=dtype, seed=10, gain=30.0, room=_room(kind, 7, 128)).fill()
         s.q *= 20
-        out = _f64(s.cache.attend(s.batch(), s.q))
+        out = _f64(s.cache.attend(s.batch(), s.q))[:sum(s.rows)]
         assert np.isfinite(out).all()
         s.q *= 0  # every key alike: the mean of the values
         s.check(s.cache.attend(s.batch(), s.q))
 
 
-@pytest.mark.parametrize("hd", [64, 128])
-def test_values_beyond_half_precision(hd):
+@pytest.mark.parametrize("hd,kind", [(64, ""), (128, ""), (64, "tiles"), (128, "tiles"), (64, "split"), (128, "split"), (128, "eight")])
+def test_values_beyond_half_precision(hd, kind):
     """Value blocks that fp16 does not hold, tiny and huge, among ordinary ones; keys likewise."""
     for dtype in ("bf16", "f32"):
-        s = Setup(7, 1, hd, [700, 130, 64, 200], rows=[1, 130, 3, 1], dtype=dtype, seed=21)
+        s = Setup(7, 1, hd, [700, 130, 64, 200], rows=[12 if kind else 1, 130, 3, 1], dtype=dtype, seed=21, room=_room(kind, 7, hd))
         s.v[5::64] *= 2.0 ** 20
         s.v[9::32, :, :32] *= 2.0 ** -40
         s.v[700:830] *= 2.0 ** -30
@@ -388,6 +441,73 @@ def test_device_values_out_of_bounds_are_not_followed():
     s.cache.attend(wild, q)
     s.cache.read(wild)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("kind", ["tiles", "split", "eight"])
+def test_bad_pages_and_contexts_of_prompts(kind):
+    """As above where sequences have many rows: a bad page's readers are NaN, bad contexts' rows too, the rest right."""
+    ctx, rows = [600, 300, 300, 128, 70], [100, 80, 60, 128, 1]
+    s = Setup(28, 4, 128, ctx, rows, seed=32, room=_room(kind, 28, 128)).fill()
+    t = s.dev_table.clone()
+    t[0, 8] = s.cache.n_pages  # of tokens 512 to 575
+    t[3, 1] = -1
+    b = s.cache.batch(_ints([600, 2 ** 31 - 1, -5, 128, 70]), t, row_offsets=_ints(np.concatenate([[0], np.cumsum(rows)])),
+                      n_rows=s.room[0], max_rows=s.room[0])
+    out = torch.full_like(s.q, 5.0)
+    s.cache.attend(b, s.q, out=out)
+    nan = torch.isnan(out).flatten(1)
+    want = np.zeros(s.room[0], bool)
+    want[12:100] = True          # positions 512 on
+    want[100:240] = True
+    want[240 + 64:368] = True
+    assert np.array_equal(nan.all(1).cpu().numpy(), want) and np.array_equal(nan.any(1).cpu().numpy(), want)
+    assert (out[369:] == 5).all()
+    good = s.cache.attend(s.batch(), s.q)
+    keep = torch.from_numpy(~want[:369]).to(DEV)
+    assert torch.equal(out[:369][keep], good[:369][keep])
+    # too many rows for the bound
+    out = torch.full_like(s.q, 5.0)
+    s.cache.attend(s.batch(max_rows=90), s.q, out=out)
+    assert torch.isnan(out[:90]).all() and (out[90:100] == 5).all() and torch.isnan(out[240:330]).all() and (out[330:368] == 5).all()
+    assert torch.equal(out[100:240], s.cache.attend(s.batch(max_rows=90), s.q)[100:240]) and torch.isfinite(out[100:240]).all()
+    # offsets that descend or run away stay inside the tensors
+    s.cache.attend(s.cache.batch(_ints(ctx), s.dev_table, row_offsets=_ints([0, 2 ** 31 - 1, -5, 300, 90, 400]),
+                                 n_rows=s.room[0], max_rows=s.room[0]), s.q)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("kind", ["tiles", "split", "eight"])
+def test_prompts_captured_and_replayed(kind):
+    """One graph for steps whose rows and contexts change on the device, sequences moving between the two kernels."""
+    s = Setup(28, 4, 128, [700, 900, 64, 513], [100, 1, 64, 9], seed=33, room=_room(kind, 28, 128)).fill()
+    n = s.room[0]
+    ctx, off = _ints(s.ctx), _ints([0, 0, 0, 0, 0])
+    q = torch.zeros((n, 28, 128), dtype=s.dt, device=DEV)
+    b = s.cache.batch(ctx, s.dev_table, row_offsets=off, n_rows=n, max_rows=n)
+    ws = s.cache.attend_workspace(b, 28)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        s.cache.attend(b, q, workspace=ws)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    out = torch.zeros_like(q)
+    with torch.cuda.graph(graph):
+        s.cache.attend(b, q, out=out, workspace=ws)
+    held = s.held()
+    for i, (c, rows) in enumerate([([700, 900, 64, 513], [100, 1, 64, 9]), ([700, 900, 64, 513], [0, 90, 1, 100]),
+                                   ([1, 899, 0, 200], [1, 10, 0, 200])]):
+        ctx.copy_(_ints(c))
+        off.copy_(_ints(np.concatenate([[0], np.cumsum(rows)])))
+        q.copy_(torch.randn(q.shape, device=DEV, generator=torch.Generator(DEV).manual_seed(i)))
+        ws.fill_(float("nan")) if ws.is_floating_point() else ws.fill_(255)
+        out.fill_(5)
+        graph.replay()
+        torch.cuda.synchronize()
+        now = Setup(28, 4, 128, c, rows, seed=0)
+        now.check(out, q=q, held=[(k[:x], v[:x]) for (k, v), x in zip(held, c)])
+        assert (out[sum(rows):] == 5).all()
+        assert torch.equal(out, s.cache.attend(b, q, out=torch.full_like(q, 5.0)))
 
 
 def test_shared_pages_and_strided_tables():
