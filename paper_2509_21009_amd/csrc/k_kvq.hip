@@ -354,21 +354,36 @@ __device__ __forceinline__ int wave_scan(int x) {
   return x;
 }
 
-// Tile `index` of the cut: its sequence (-1 past the last) and which of the sequence's.  Each wave finds it for itself;
-// lane l counts the sequences l per .. (l + 1) per - 1.
-__device__ __forceinline__ int find_tile(const KvqBatch& bt, int group, const KvqCut& cut, int index, int& tile) {
+// Tile `index` of the cut: its sequence (-1 past the last) and which of the sequence's.  Each wave finds it for itself.
+// Up to 64 sequences: a lane has one, context and all, so that nothing is read twice.  More: lane l counts the sequences
+// l per .. (l + 1) per - 1 (no further than 2^24, should offsets that do not ascend say more).
+__device__ __forceinline__ int find_tile(const KvqBatch& bt, int group, const KvqCut& cut, int index, int& tile, KvqSeq& sq) {
   const int lane = threadIdx.x & 63;
+  if (bt.n_seqs <= 64) {
+    const KvqSeq s = kvq_seq(bt, min(lane, bt.n_seqs - 1));
+    const int mine = lane < bt.n_seqs ? min(kvq_tiles(s, group, cut), 1 << 24) : 0, scan = wave_scan(mine);
+    const uint64_t past = __ballot(scan > index);
+    if (!past) return -1;
+    const int w = __ffsll(static_cast<unsigned long long>(past)) - 1;
+    tile = index - __builtin_amdgcn_readlane(scan - mine, w);
+    sq.r0 = __builtin_amdgcn_readlane(s.r0, w);
+    sq.n = __builtin_amdgcn_readlane(s.n, w);
+    sq.ctx = __builtin_amdgcn_readlane(s.ctx, w);
+    sq.ok = __builtin_amdgcn_readlane(s.ok, w);
+    return w;
+  }
   const int per = (bt.n_seqs + 63) >> 6, b0 = lane * per, b1 = min(b0 + per, bt.n_seqs);
   int mine = 0;
 #pragma unroll 4
-  for (int b = b0; b < b1; ++b) mine += kvq_tiles(kvq_rows(bt, b), group, cut);
+  for (int b = b0; b < b1; ++b) mine = min(mine + min(kvq_tiles(kvq_rows(bt, b), group, cut), 1 << 24), 1 << 24);
   const int scan = wave_scan(mine);
   const uint64_t past = __ballot(scan > index);
   if (!past) return -1;
   const int w = __ffsll(static_cast<unsigned long long>(past)) - 1;
   tile = index - __builtin_amdgcn_readlane(scan - mine, w);
   for (int b = w * per;; ++b) {  // within that lane's sequences
-    const int t = kvq_tiles(kvq_rows(bt, b), group, cut);
+    sq = kvq_seq(bt, b);
+    const int t = kvq_tiles(sq, group, cut);
     if (tile < t) return b;
     tile -= t;
   }
@@ -611,9 +626,11 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendAr
   const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
   const int kh = blockIdx.y, split = blockIdx.z;
   int tile = 0;
-  const int b = cut.find ? find_tile(bt, G, cut, blockIdx.x, tile) : static_cast<int>(blockIdx.x);
+  KvqSeq sq;
+  int b = blockIdx.x;
+  if (cut.find) b = find_tile(bt, G, cut, blockIdx.x, tile, sq);
+  else sq = kvq_seq(bt, b);
   if (b < 0) return;
-  const KvqSeq sq = kvq_seq(bt, b);
   const KvqTile tl = kvq_tile(sq, G, tile, cut.cols);
   const int j0 = tile * 16, n_cols = tl.cols, first = tl.first;
   const int pages = kvq_pages(tl.end), items = kvq_items(pages, cut.items, cut.least);
@@ -943,9 +960,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_kvq_prompt(KvqAttendArgs a, KvqC
   const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
   const int kh = blockIdx.y, split = blockIdx.z;
   int tile = 0;
-  const int b = find_tile(bt, G, cut, blockIdx.x, tile);
+  KvqSeq sq;
+  const int b = find_tile(bt, G, cut, blockIdx.x, tile, sq);
   if (b < 0) return;
-  const KvqSeq sq = kvq_seq(bt, b);
   tile = kvq_tiles(sq, G, cut) - 1 - tile;  // the last ones see most keys: they start first
   const KvqTile tl = kvq_tile(sq, G, tile, cut.cols);
   const int j0 = tile * cut.cols, first = tl.first;
@@ -1125,9 +1142,11 @@ __global__ __launch_bounds__(256) void k_kvq_join(KvqAttendArgs a, KvqCut cut) {
   const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
   const int kh = blockIdx.y, col = blockIdx.z;
   int tile = 0;
-  const int b = cut.find ? find_tile(a.batch, G, cut, blockIdx.x, tile) : static_cast<int>(blockIdx.x);
+  KvqSeq sq;
+  int b = blockIdx.x;
+  if (cut.find) b = find_tile(a.batch, G, cut, blockIdx.x, tile, sq);
+  else sq = kvq_seq(a.batch, b);
   if (b < 0) return;
-  const KvqSeq sq = kvq_seq(a.batch, b);
   const KvqTile tl = kvq_tile(sq, G, tile, cut.cols);
   const int n = kvq_items(kvq_pages(tl.end), cut.items, cut.least);
   if (n == 1 || col >= tl.cols) return;  // one item has written the output itself
@@ -1179,9 +1198,9 @@ __global__ __launch_bounds__(256) void k_kvq_join_prompt(KvqAttendArgs a, KvqCut
   const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
   const int kh = blockIdx.y, d4 = threadIdx.x % LPC, col = blockIdx.z * (256 / LPC) + threadIdx.x / LPC;
   int tile = 0;
-  const int b = find_tile(a.batch, G, cut, blockIdx.x, tile);
+  KvqSeq sq;
+  const int b = find_tile(a.batch, G, cut, blockIdx.x, tile, sq);
   if (b < 0) return;
-  const KvqSeq sq = kvq_seq(a.batch, b);
   tile = kvq_tiles(sq, G, cut) - 1 - tile;  // as k_kvq_prompt numbers them
   const KvqTile tl = kvq_tile(sq, G, tile, cut.cols);
   const int n = kvq_items(kvq_pages(tl.end), cut.items, cut.least);

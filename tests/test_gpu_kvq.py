@@ -125,6 +125,9 @@ class Setup:
     (3, 64, "bf16", [5, 200, 1], [5, 3, 1]),
     (1, 128, "f32", [70, 64, 3, 129] * 20, [9, 64, 1, 2] * 20),     # 80 sequences: offsets past one wave's 64
     (5, 64, "bf16", [3] * 131, [1] * 131),
+    (2, 64, "bf16", [3, 1, 0, 70, 2, 0, 0] * 40, [2, 1, 0, 70, 2, 0, 0] * 40),
+    (2, 128, "f32", [2] * 65, [2] * 65),
+    (2, 64, "f32", [1, 2] * 64 + [9], [1, 2] * 64 + [0]),
 ])
 def test_append_then_read_holds_the_oracles_values(n_kv, hd, dtype, ctx, rows):
     s = Setup(n_kv, n_kv, hd, ctx, rows, dtype, seed=len(ctx)).fill()
@@ -508,6 +511,21 @@ def test_prompts_captured_and_replayed(kind):
         now.check(out, q=q, held=[(k[:x], v[:x]) for (k, v), x in zip(held, c)])
         assert (out[sum(rows):] == 5).all()
         assert torch.equal(out, s.cache.attend(b, q, out=torch.full_like(q, 5.0)))
+
+
+def test_offsets_that_claim_far_more_rows_than_there_are():
+    """Every second sequence claims all rows: 2^31 tiles between them, of which as many are taken as fit the bound."""
+    n_rows, n_seqs = 1 << 15, 1 << 15
+    cache = rp().KvqCache(2, 1, 64, device=DEV)
+    off = torch.zeros(n_seqs + 1, dtype=torch.int32, device=DEV)
+    off[1::2] = n_rows
+    b = cache.batch(torch.ones(n_seqs, dtype=torch.int32, device=DEV), torch.zeros((n_seqs, 1), dtype=torch.int32, device=DEV),
+                    row_offsets=off, n_rows=n_rows, max_rows=n_rows)
+    q = torch.zeros((n_rows, 64, 64), dtype=torch.bfloat16, device=DEV)
+    out = cache.attend(b, q)
+    k, v = cache.read(b)
+    torch.cuda.synchronize()
+    assert out.shape == q.shape and k.shape == (n_rows, 1, 64)
 
 
 def test_shared_pages_and_strided_tables():
