@@ -389,6 +389,37 @@ __device__ __forceinline__ int find_tile(const KvqBatch& bt, int group, const Kv
   }
 }
 
+// The same for k_kvq_prompt, whose blocks take long: tiles of more pages come first, so that the last ones to start are
+// short (20 prompts of 128 to 1,024 tokens, one after the other 126 us, so 112).  Up to 64 sequences over all of them, a lane
+// each: the pages of tile `index` are the most of which so many tiles have more, found by halves.  More sequences come in
+// their order, each with its last tile first.
+__device__ __forceinline__ int find_longest(const KvqBatch& bt, int group, const KvqCut& cut, int index, int& tile, KvqSeq& sq) {
+  if (bt.n_seqs == 1 || bt.n_seqs > 64) {
+    const int b = find_tile(bt, group, cut, index, tile, sq);
+    tile = kvq_tiles(sq, group, cut) - 1 - tile;
+    return b;
+  }
+  const int lane = threadIdx.x & 63;
+  const KvqSeq s = kvq_seq(bt, min(lane, bt.n_seqs - 1));
+  const int tiles = lane < bt.n_seqs ? min(kvq_tiles(s, group, cut), 1 << 24) : 0;
+  auto above = [&](int pages) { return kvq_tiles_above(s, group, cut.cols, tiles, pages); };  // of the lane's, with more pages
+  auto total = [&](int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); };
+  if (index >= total(tiles)) return -1;
+  int lo = -1, hi = kvq_pages(bt.max_context);  // more than `index` tiles have more pages than lo, no more than that than hi
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (total(above(mid)) > index) lo = mid; else hi = mid;
+  }
+  const int more = above(hi), mine = above(hi - 1) - more, scan = wave_scan(mine), left = index - total(more);
+  const int w = __ffsll(static_cast<unsigned long long>(__ballot(scan > left))) - 1;
+  tile = __builtin_amdgcn_readlane(tiles - 1 - more - (left - scan + mine), w);
+  sq.r0 = __builtin_amdgcn_readlane(s.r0, w);
+  sq.n = __builtin_amdgcn_readlane(s.n, w);
+  sq.ctx = __builtin_amdgcn_readlane(s.ctx, w);
+  sq.ok = __builtin_amdgcn_readlane(s.ok, w);
+  return w;
+}
+
 // ---- attention, 16 columns a block ------------------------------------------------------
 
 // Two fp32 to packed bf16, round to nearest even.
@@ -958,12 +989,11 @@ __global__ __launch_bounds__(64 * NW, 2) void k_kvq_prompt(KvqAttendArgs a, KvqC
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, c = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
-  const int kh = blockIdx.y, split = blockIdx.z;
+  const int index = blockIdx.x / n_kv, kh = blockIdx.x - index * n_kv, split = blockIdx.z;
   int tile = 0;
   KvqSeq sq;
-  const int b = find_tile(bt, G, cut, blockIdx.x, tile, sq);
+  const int b = find_longest(bt, G, cut, index, tile, sq);
   if (b < 0) return;
-  tile = kvq_tiles(sq, G, cut) - 1 - tile;  // the last ones see most keys: they start first
   const KvqTile tl = kvq_tile(sq, G, tile, cut.cols);
   const int j0 = tile * cut.cols, first = tl.first;
   const int pages = kvq_pages(tl.end), items = kvq_items(pages, cut.items, cut.least);
@@ -1103,7 +1133,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_kvq_prompt(KvqAttendArgs a, KvqC
   if (col >= tl.cols) return;
   // The lane's rows 8 i + 4 h + e of each tile: dimensions hd/16 c' + 2 t + (row >= 16), c' = row mod 16.
   const float inv = !sq.ok ? __builtin_nanf("") : lim < 0 ? 0.f : 1.f / st.l;
-  const int64_t part = (static_cast<int64_t>(blockIdx.x) * cut.items + split) * n_kv + kh;
+  const int64_t part = (static_cast<int64_t>(index) * cut.items + split) * n_kv + kh;
 #pragma unroll
   for (int q = 0; q < 2; ++q)
 #pragma unroll
@@ -1199,9 +1229,8 @@ __global__ __launch_bounds__(256) void k_kvq_join_prompt(KvqAttendArgs a, KvqCut
   const int kh = blockIdx.y, d4 = threadIdx.x % LPC, col = blockIdx.z * (256 / LPC) + threadIdx.x / LPC;
   int tile = 0;
   KvqSeq sq;
-  const int b = find_tile(a.batch, G, cut, blockIdx.x, tile, sq);
+  const int b = find_longest(a.batch, G, cut, blockIdx.x, tile, sq);
   if (b < 0) return;
-  tile = kvq_tiles(sq, G, cut) - 1 - tile;  // as k_kvq_prompt numbers them
   const KvqTile tl = kvq_tile(sq, G, tile, cut.cols);
   const int n = kvq_items(kvq_pages(tl.end), cut.items, cut.least);
   if (n == 1 || col >= tl.cols) return;  // one item has written the output itself
@@ -1321,12 +1350,12 @@ hipError_t attend_launch(KvqAttendArgs a, const AttendPlan& p, float* ws, hipStr
     a.part_ml = n ? ws + n : nullptr;
     ws = n ? ws + n + n / HD * 2 : ws;
     if constexpr (!F32) {
-      const dim3 grid(static_cast<uint32_t>(p.prompt_tiles), n_kv, p.prompt.items);
+      const dim3 grid(static_cast<uint32_t>(p.prompt_tiles * n_kv), 1, p.prompt.items);
       if (p.prompt_waves == 4) launch_kernel((k_kvq_prompt<HD, 4>), grid, dim3(256), 0, s, a, p.prompt);
       else if constexpr (HD == 128) launch_kernel((k_kvq_prompt<HD, 8>), grid, dim3(512), 0, s, a, p.prompt);
       else return hipErrorInvalidValue;
       constexpr int kCols = 1024 / HD;  // of a block of k_kvq_join_prompt
-      if (n) launch_kernel((k_kvq_join_prompt<HD>), dim3(grid.x, n_kv, p.prompt.cols / kCols), dim3(256), 0, s, a, p.prompt);
+      if (n) launch_kernel((k_kvq_join_prompt<HD>), dim3(static_cast<uint32_t>(p.prompt_tiles), n_kv, p.prompt.cols / kCols), dim3(256), 0, s, a, p.prompt);
     }
   }
   if (p.walk_tiles) {
@@ -1386,7 +1415,7 @@ size_t kvq_attend_bytes_most(const KvqCache& c, int n_q, int64_t max_seqs, int64
 bool kvq_attend_fits(const KvqCache& c, const KvqBatch& b, int n_q) {
   for (const bool bf16 : {true, false}) {
     const AttendPlan p = attend_plan(c, b, n_q, bf16);
-    if (p.walk_tiles >= (1 << 22) || p.prompt_tiles >= (1 << 22)) return false;  // blocks of up to 512 threads, 2^32 in a dimension
+    if (p.walk_tiles >= (1 << 22) || p.prompt_tiles * c.n_kv >= (1 << 22)) return false;  // blocks of up to 512 threads, 2^32 in a dimension
   }
   return true;
 }

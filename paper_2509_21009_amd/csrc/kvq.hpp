@@ -170,6 +170,18 @@ RP_HD KvqTile kvq_tile(const KvqSeq& s, int group, int tile, int cols) {
   return t;
 }
 
+// Of a sequence's `tiles` tiles of `cols` columns, a power of two, those that see more than `pages` pages: the last ones,
+// since the keys that tile i sees, first + ((i + 1) cols - 1) / group + 1 (or all, the last), grow with i.
+RP_HD int kvq_tiles_above(const KvqSeq& s, int group, int cols, int tiles, int pages) {
+  if (pages < 0 || tiles == 0) return tiles;
+  const int64_t keys = int64_t{kKvqPage} * pages;
+  if (!s.ok || s.ctx <= keys) return 0;
+  const int64_t rows = keys - (s.ctx - s.n);
+  if (rows <= 0) return tiles;
+  const int64_t i = (rows * group) >> __builtin_ctz(static_cast<unsigned>(cols));
+  return i < tiles - 1 ? static_cast<int>(tiles - i) : 1;
+}
+
 struct KvqAttendArgs {
   KvqCache cache;
   KvqBatch batch;

@@ -121,6 +121,12 @@ static void batches() {
           assert(sum == pages);
         }
         assert(nt == 0 || covered == s.n * group);
+        for (int p = -1; p <= kvq_pages(b.max_context); p += 1 + (round % 4 ? 0 : p / 8)) {
+          int more = 0;
+          for (int t = 0; t < nt; ++t) more += kvq_pages(kvq_tile(s, group, t, cut.cols).end) > p;
+          assert(kvq_tiles_above(s, group, cut.cols, nt, p) == more);
+        }
+        assert(kvq_tiles_above(s, group, cut.cols, nt, kvq_pages(b.max_context)) == 0);
         tiles[k] += nt;
       }
     }
