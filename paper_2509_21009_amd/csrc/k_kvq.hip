@@ -389,12 +389,12 @@ __device__ __forceinline__ int find_tile(const KvqBatch& bt, int group, const Kv
   }
 }
 
-// The same for k_kvq_prompt, whose blocks take long: tiles of more pages come first, so that the last ones to start are
-// short (20 prompts of 128 to 1,024 tokens, one after the other 126 us, so 112).  Up to 64 sequences over all of them, a lane
-// each: the pages of tile `index` are the most of which so many tiles have more, found by halves.  More sequences come in
-// their order, each with its last tile first.
+// The same with each sequence's last tile first, which sees most keys.  cut.longest, up to 64 sequences: over all of them,
+// a lane each, tiles of more pages first; the pages of tile `index` are the most of which so many tiles have more, found by
+// halves.  The last blocks to start are then short ones, and neighbours have the KV heads of a tile.  20 prompts of 128 to
+// 1,024 tokens 126 us sequence by sequence, 112 so; 32 sequences' last 20 rows of 1,000 keys 37 | 29 (k_kvq_attend).
 __device__ __forceinline__ int find_longest(const KvqBatch& bt, int group, const KvqCut& cut, int index, int& tile, KvqSeq& sq) {
-  if (bt.n_seqs == 1 || bt.n_seqs > 64) {
+  if (!cut.longest || bt.n_seqs == 1 || bt.n_seqs > 64) {
     const int b = find_tile(bt, group, cut, index, tile, sq);
     tile = kvq_tiles(sq, group, cut) - 1 - tile;
     return b;
@@ -655,12 +655,16 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendAr
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
-  const int kh = blockIdx.y, split = blockIdx.z;
-  int tile = 0;
+  const int split = blockIdx.z;
+  int index = blockIdx.x, kh = blockIdx.y, tile = 0, b = index;
   KvqSeq sq;
-  int b = blockIdx.x;
-  if (cut.find) b = find_tile(bt, G, cut, blockIdx.x, tile, sq);
-  else sq = kvq_seq(bt, b);
+  if (cut.find) {
+    index = blockIdx.x / n_kv;
+    kh = blockIdx.x - index * n_kv;
+    b = find_longest(bt, G, cut, index, tile, sq);
+  } else {
+    sq = kvq_seq(bt, b);
+  }
   if (b < 0) return;
   const KvqTile tl = kvq_tile(sq, G, tile, cut.cols);
   const int j0 = tile * 16, n_cols = tl.cols, first = tl.first;
@@ -771,7 +775,7 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendAr
             f32x4_t{o[i][e], o[i + 1][e], o[i + 2][e], o[i + 3][e]} * fac;
   }
   __syncthreads();
-  const int64_t part = (static_cast<int64_t>(blockIdx.x) * cut.items + split) * n_kv + kh;
+  const int64_t part = (static_cast<int64_t>(index) * cut.items + split) * n_kv + kh;
   for (int q = tid; q < n_cols * (HD / 8); q += 64 * NW) {
     const int col = q / (HD / 8), d = q % (HD / 8) * 8;
     float m4 = sm[0][col], den = 0.f, x[8];
@@ -1174,7 +1178,7 @@ __global__ __launch_bounds__(256) void k_kvq_join(KvqAttendArgs a, KvqCut cut) {
   int tile = 0;
   KvqSeq sq;
   int b = blockIdx.x;
-  if (cut.find) b = find_tile(a.batch, G, cut, blockIdx.x, tile, sq);
+  if (cut.find) b = find_longest(a.batch, G, cut, blockIdx.x, tile, sq);
   else sq = kvq_seq(a.batch, b);
   if (b < 0) return;
   const KvqTile tl = kvq_tile(sq, G, tile, cut.cols);
@@ -1289,12 +1293,12 @@ struct AttendPlan {
 };
 
 // Whether k_kvq_prompt takes the sequences of more than 64 columns.  It shares a page's unpacking among 128 columns, but
-// its blocks take their pages in turn and a page costs one ~2.2 us: it wants enough tiles to fill the card, or so much
-// work that it can be split over the keys.  k_kvq_prompt | k_kvq_attend:
-//   by tiles: 32 prompts of 128 tokens 28 | 39, 8 of 512 44 | 60, one of 2,048 63 | 75; one of 1,024 34 | 31, of 512 20 | 15,
-//     of 397 17 | 11; 2 x 64, 8 of 512 20 | 30, 32 last rows 64 of 1,000 keys 32 | 27
-//   by work: the last 512 rows of 14,000 keys 140 | 183, 128 of 14,000 55 | 69, 64 of 14,000 41 | 40, 128 of 3,000 29 | 29,
-//     256 of 2,000 30 | 20; 2 x 64, 512 of 14,000 55 | 73, one prompt of 2,048 35 | 27
+// its blocks take their pages in turn and a page costs one ~1.1 us of a compute unit: it wants enough tiles to fill the card,
+// or so much work that it can be split over the keys.  k_kvq_prompt | k_kvq_attend:
+//   by tiles: 32 prompts of 128 tokens 27 | 39, 8 of 512 37 | 60, one of 2,048 60 | 73; one of 1,024 34 | 26, of 512 20 | 13,
+//     of 397 17 | 10; 2 x 64, 8 of 512 18 | 29, 32 times the last 64 rows of 1,000 keys 32 | 27
+//   by work: the last 512 rows of 14,000 keys 134 | 182, 128 of 14,000 52 | 66, 64 of 14,000 41 | 37, 128 of 3,000 29 | 27,
+//     256 of 2,000 30 | 19; 2 x 64, 512 of 14,000 53 | 72, one prompt of 2,048 35 | 23
 bool prompt_pays(const KvqCache& c, int64_t tiles, int pages) {  // of 16 columns, over all KV heads
   return tiles >= 2048 || tiles * pages * c.hd >= int64_t{1} << 22;
 }
@@ -1309,25 +1313,28 @@ AttendPlan attend_plan(const KvqCache& c, const KvqBatch& b, int n_q, bool bf16)
     p.prompt.find = 1;
     p.prompt.least = 8;
     if (static_cast<int64_t>(b.n_seqs) * kvq_max_rows(b) > b.n_rows) p.prompt.above = p.walk.upto = 64;  // else all have as many rows
-    // Eight waves, 256 columns, halve the unpacking: 1,423 | 1,532 with four for one prompt of 14,500 tokens, 184 | 195 of
-    // 4,096, 404 | 446 for the last 2,048 rows of 14,000 keys; with fewer pages the start of a block counts: 69 | 63 for
-    // 2,048 tokens, 139 | 127 for 20 prompts of 128 to 1,024.  At 64 dims a page is half the work: 198 | 185 for 8,192.
+    // Eight waves, 256 columns, halve the unpacking: 1,384 | 1,474 with four for one prompt of 14,500 tokens, 128 | 142 of
+    // 4,096, 403 | 424 for the last 2,048 rows of 14,000 keys; with fewer pages the start of a block counts: 68 | 60 for 2,048
+    // tokens, 122 | 112 for 20 prompts of 128 to 1,024.  At 64 dims a page is half the work: 198 | 185 for 8,192.
     p.prompt.cols = 256;
     p.prompt_tiles = kvq_tile_bound(b, G, p.prompt);
     p.prompt_waves = c.hd == 128 && pages >= 64 && p.prompt_tiles * c.n_kv >= 192 ? 8 : 4;
     p.prompt.cols = 32 * p.prompt_waves;
     p.prompt_tiles = kvq_tile_bound(b, G, p.prompt);
     // Up to 512 blocks, which the card holds at once: one more is another turn, and a split one writes 512 bytes of
-    // partial output per column.  One item | two: 452 blocks, 2,048 tokens, 63 | 88; 112, the last 512 rows of 14,000
-    // keys, 359 | 194, four 140, five 171.
+    // partial output per column.  One item | two: 452 blocks, 2,048 tokens, 61 | 70; 112, the last 512 rows of 14,000
+    // keys, 359 | 191, four 134, five 171.
     const int64_t blocks = std::max<int64_t>(1, p.prompt_tiles * c.n_kv);
     if (p.prompt_waves == 4 && blocks <= 256) p.prompt.items = static_cast<int>(std::min<int64_t>(kvq_items(pages, kKvqTileItems, p.prompt.least), 512 / blocks));
+    p.prompt.longest = blocks > 256 && p.prompt.items == 1;
   }
   if (p.prompt_tiles && !p.prompt.above) return p;
   p.walk_tiles = kvq_tile_bound(b, G, p.walk);
   const int64_t blocks = std::max<int64_t>(1, p.walk_tiles * c.n_kv);
   p.walk.least = 4;
   if (blocks < 256 && pages > 16) p.walk.items = static_cast<int>(std::min<int64_t>(kvq_items(pages, kKvqTileItems, p.walk.least), (384 + blocks - 1) / blocks));
+  // Fewer blocks start together; for a few split ones the search costs more than it gives: 8 x 16 rows of 2,000 keys 26 | 30.
+  p.walk.longest = p.walk.find && blocks > 256 && p.walk.items == 1;
   const int64_t all = blocks * p.walk.items;
   const int per = kvq_item_pages(pages, p.walk.items);
   // One wave where the blocks are 512 to each page, which nothing has to join: 8 prompts of 128 tokens 13.8 | 21.8 with
@@ -1362,7 +1369,7 @@ hipError_t attend_launch(KvqAttendArgs a, const AttendPlan& p, float* ws, hipStr
     const size_t n = part_floats(p.walk, p.walk_tiles, n_kv, HD);
     a.part_o = ws;
     a.part_ml = n ? ws + n : nullptr;
-    const dim3 grid(static_cast<uint32_t>(p.walk_tiles), n_kv, p.walk.items);
+    const dim3 grid(static_cast<uint32_t>(p.walk.find ? p.walk_tiles * n_kv : p.walk_tiles), p.walk.find ? 1 : n_kv, p.walk.items);
     switch (p.waves) {
       case 1: launch_kernel((k_kvq_attend<HD, F32, 1>), grid, dim3(64), 0, s, a, p.walk); break;
       case 4: launch_kernel((k_kvq_attend<HD, F32, 4>), grid, dim3(256), 0, s, a, p.walk); break;
@@ -1370,7 +1377,7 @@ hipError_t attend_launch(KvqAttendArgs a, const AttendPlan& p, float* ws, hipStr
       default: return hipErrorInvalidValue;
     }
     const int64_t most = std::min<int64_t>(p.walk.upto, static_cast<int64_t>(kvq_max_rows(a.batch)) * (a.n_q / n_kv));
-    if (n) launch_kernel((k_kvq_join<HD, F32>), dim3(grid.x, n_kv, static_cast<uint32_t>(std::min<int64_t>(p.walk.cols, most))), dim3(256), 0, s, a, p.walk);
+    if (n) launch_kernel((k_kvq_join<HD, F32>), dim3(static_cast<uint32_t>(p.walk_tiles), n_kv, static_cast<uint32_t>(std::min<int64_t>(p.walk.cols, most))), dim3(256), 0, s, a, p.walk);
   }
   return hipGetLastError();
 }
@@ -1415,7 +1422,7 @@ size_t kvq_attend_bytes_most(const KvqCache& c, int n_q, int64_t max_seqs, int64
 bool kvq_attend_fits(const KvqCache& c, const KvqBatch& b, int n_q) {
   for (const bool bf16 : {true, false}) {
     const AttendPlan p = attend_plan(c, b, n_q, bf16);
-    if (p.walk_tiles >= (1 << 22) || p.prompt_tiles * c.n_kv >= (1 << 22)) return false;  // blocks of up to 512 threads, 2^32 in a dimension
+    if (std::max(p.walk_tiles, p.prompt_tiles) * c.n_kv >= (1 << 22)) return false;  // blocks of up to 512 threads, 2^32 in a dimension
   }
   return true;
 }

@@ -146,6 +146,7 @@ RP_HD int kvq_item_pages(int pages, int items) { return items == 1 ? pages : (pa
 struct KvqCut {
   int cols = 16;
   int find = 0;   // tiles are found by their sequences' rows (0: tile b is sequence b's only one)
+  int longest = 0;  // with find: tiles of more pages come first
   int above = 0, upto = 0x7fffffff;
   int items = 1;  // of a tile at most
   int least = 1;  // pages of an item, unless it is its tile's only one
