@@ -1332,15 +1332,20 @@ AttendPlan attend_plan(const KvqCache& c, const KvqBatch& b, int n_q, bool bf16)
   p.walk_tiles = kvq_tile_bound(b, G, p.walk);
   const int64_t blocks = std::max<int64_t>(1, p.walk_tiles * c.n_kv);
   p.walk.least = 4;
-  if (blocks < 256 && pages > 16) p.walk.items = static_cast<int>(std::min<int64_t>(kvq_items(pages, kKvqTileItems, p.walk.least), (384 + blocks - 1) / blocks));
+  // Few blocks of more than 16 pages are split into as many as run at once: one of eight waves to a compute unit where that
+  // comes out nearly even, else three of four waves (two in fp32, whose waves have more registers).  7 query heads to each of 4 KV
+  // heads, items of eight waves | of four: 16 tokens of 2,000 to 14,000 keys (64 blocks) 23.5 (4) | 24.5 (12), with 6 of eight
+  // waves 31; 32 of 1,000 to 14,000 36 (2) | 35 (6); 48 of 1,000 to 9,000 (192 blocks) 38 (1) | 32 (4); 64 of 4,000 25 (1) | 31 (3).
+  const bool few = blocks <= 256, even = few && 256 / blocks * blocks >= 224;
+  if (few && pages > 16) p.walk.items = static_cast<int>(std::min<int64_t>(kvq_items(pages, kKvqTileItems, p.walk.least), (even ? 256 : bf16 ? 768 : 512) / blocks));
   // Fewer blocks start together; for a few split ones the search costs more than it gives: 8 x 16 rows of 2,000 keys 26 | 30.
   p.walk.longest = p.walk.find && blocks > 256 && p.walk.items == 1;
   const int64_t all = blocks * p.walk.items;
   const int per = kvq_item_pages(pages, p.walk.items);
   // One wave where the blocks are 512 to each page, which nothing has to join: 8 prompts of 128 tokens 13.8 | 21.8 with
-  // four; 64 decoded tokens of 600 to 4,500 keys (256 blocks) 83 | 28.  Eight for few blocks and many pages: the latter
-  // 23.4 | 28.0; 330 of 130 to 1,300 48 | 38.
-  p.waves = all >= 512 * per ? 1 : all <= 384 && per > 16 ? 8 : 4;
+  // four; 64 decoded tokens of 600 to 4,500 keys (256 blocks) 83 | 28.  Eight, where the split made room for them, for at least
+  // two pages each: the latter 23 | 28, one token of 12,000 keys (64 items of 3 pages) 10.3 | 9.8.
+  p.waves = all >= 512 * per ? 1 : even && per > 16 ? 8 : 4;
   return p;
 }
 
@@ -1408,15 +1413,15 @@ size_t kvq_attend_bytes(const KvqCache& c, const KvqBatch& b, int n_q) {
 }
 
 size_t kvq_attend_bytes_most(const KvqCache& c, int n_q, int64_t max_seqs, int64_t max_rows, int max_context) {
-  // attend_plan splits fewer than 256 blocks of 16 columns to fewer than 384 + 256 items of at least 4 pages, and up to 256
-  // of 128 to at most 512 of 8; a call with both kinds has both
+  // attend_plan splits up to 256 blocks of 16 columns to at most 768 items of at least 4 pages, and up to 256 of 128 to at
+  // most 512 of 8; a call with both kinds has both
   const int64_t pages = kvq_pages(max_context), G = n_q / c.n_kv, rows = std::max(max_rows, max_seqs);
   auto most = [&](int64_t cols, int64_t blocks, int64_t most_items, int64_t least) {
     const int64_t per_tile = std::min<int64_t>(kKvqTileItems, (pages + least - 1) / least), tiles = rows * G / cols + max_seqs;
     const int64_t items = std::min(std::min(tiles * c.n_kv, blocks) * per_tile, most_items);
     return per_tile > 1 ? static_cast<size_t>(items) * cols * (c.hd + 2) * 4 : size_t{0};
   };
-  return most(16, 255, 384 + 255, 4) + most(128, 256, 512, 8);
+  return most(16, 256, 768, 4) + most(128, 256, 512, 8);
 }
 
 bool kvq_attend_fits(const KvqCache& c, const KvqBatch& b, int n_q) {
