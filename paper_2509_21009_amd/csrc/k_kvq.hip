@@ -193,6 +193,9 @@ __device__ __forceinline__ uint32_t get_values(const unsigned char* block, int t
   }
 }
 
+// 11,511 tokens of the 7B layer (4 KV heads of 128) 10.8 us, 2.8 TB/s in and out: the launch and the lookups (three to ten reads
+// that wait for each other) are half of it; one token each of 64 sequences 4.1 us.  Values come with plain loads: rows that the projection has just written
+// are in the caches (past them: 21.7 | 21.0 us with the read-back for the former, 151 | 164 for 67,000 tokens of 8 heads).
 template <int HD, bool BF16, int U>
 __global__ __launch_bounds__(256) void k_kvq_append(KvqCache c, KvqBatch bt, KvqTensor k, KvqTensor v, int rows) {
   const int lane = threadIdx.x & 63, d = lane % (HD / 8) * 8;
@@ -229,7 +232,8 @@ __global__ __launch_bounds__(256) void k_kvq_append(KvqCache c, KvqBatch bt, Kvq
   }
 }
 
-// What it writes goes past the caches: 104k tokens of the 7B layer 93 us (4.5 TB/s) against 112 with plain stores.
+// HBM bounds it: 163,000 tokens of the 7B layer 73 us, 5.8 TB/s.  What it writes goes past the caches; with plain stores it
+// took 19 us more.
 template <int HD, bool BF16, int U>
 __global__ __launch_bounds__(256) void k_kvq_read(KvqCache c, KvqBatch bt, KvqTensor k, KvqTensor v, int rows) {
   const int lane = threadIdx.x & 63, d = lane % (HD / 8) * 8;
@@ -267,7 +271,8 @@ __global__ __launch_bounds__(256) void k_kvq_read(KvqCache c, KvqBatch bt, KvqTe
 }
 
 // The engine's append.  A thread has eight rotated pairs of a query or key head (dimensions d .. d + 7 and d + hd/2 ..)
-// or eight dimensions of a value head of one row; the four threads of a scale block are neighbours.  The S partials are all
+// or eight dimensions of a value head of one row; the four threads of a scale block are neighbours.  A decode step of 64 rows
+// (7B layer) takes it 4.1 us, of 330 6.2; 16,384 prompt tokens 71 us, 4.6 TB/s: HBM, the partials.  The S partials are all
 // loaded before the first is added.  Keys and values are quantised from fp32: one rounding.
 template <int HD, int S>
 __global__ __launch_bounds__(256) void k_kvq_rope_append(KvqCache c, RopeArgs a) {
@@ -646,6 +651,10 @@ __device__ __forceinline__ void nan_values(PageV<HD>& pg, const char* block, int
 //   P is an operand rounded to fp16 (2^-12 of it; to 2^-25 below 2^-14), V exact in it: less than the output's own
 // rounding to bf16, where P in bf16 would add as much again.  Pages with values that fp16 does not hold, and fp32, take
 // bf16: P in two pieces, or three.
+//   HBM bounds decoding of many keys: one token each of 64 sequences of 600 to 4,500 (7B layer, 163,000 keys) 23 us, 3.9 TB/s;
+// of 330 of 130 to 1,300 38 us, 4.6; of 96 of 32B's layer, 442,000 keys, 95 us, 5.1, what a copy reaches.  Below that it is
+// the way to the first page (context, table, page: reads that wait for each other), the launch and the join: 12,000 keys of one
+// sequence 6.6 us and 4.1 for the join.
 template <int HD, bool F32, int NW>
 __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendArgs a, KvqCut cut) {
   constexpr int NT = HD / 16, OLD = HD + 4;
@@ -818,8 +827,11 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendAr
 //   S^T = K Q^T in two tiles of 32 tokens: lane 32h + c gets tokens 8i + 4h + 0..3 of each, for column c, which in pairs
 // of i are the operand P^T of a 16-token step of O^T += V^T P^T; V's rows keep the cache's order of tokens, so that
 // nothing moves between lanes.  V's row c + 16 i of tile t is dimension hd/16 c + 2 t + i: the two that one byte holds.
-//   Bound by MFMA and the exponentials, which take about as long; two blocks share a CU, so that one's products run beside
-// the other's softmax.
+//   Bound by MFMA and the vector ALU together: of a long prompt's SIMD cycles the one takes about 40%, the other (unpacking,
+// softmax) 45 to 50, hardly at the same time though two blocks (waves of eight) share a compute unit; products and softmax of
+// neighbouring pages interleaved in one wave took more registers than that hid.  One prompt of 14,500 tokens (7B layer)
+// 1,400 us, 1,070 TFLOP/s, with blocks of eight waves; 20 of 128 to 1,024 tokens 110 us, 520, where the way to a block's
+// first page and the first unpacking, ~7 us, are as long as its five pages.
 
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
 
@@ -1167,7 +1179,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_kvq_prompt(KvqAttendArgs a, KvqC
 }
 
 // Joins the items of a tile: one block per (tile, KV head, column).  Four dimensions to a thread, the items dealt out to
-// groups of threads whose loads are all in flight at once.
+// groups of threads whose loads are all in flight at once: 4 us for 64 items of 7 columns and 4 KV heads, most of it the launch.
 template <int HD, bool F32>
 __global__ __launch_bounds__(256) void k_kvq_join(KvqAttendArgs a, KvqCut cut) {
   constexpr int LPC = HD / 4, NG = 256 / LPC, PER = kKvqTileItems / NG;
@@ -1225,7 +1237,8 @@ __global__ __launch_bounds__(256) void k_kvq_join(KvqAttendArgs a, KvqCut cut) {
   }
 }
 
-// The same for k_kvq_prompt's tiles, which have many columns and few items: HD / 4 lanes to a column.
+// The same for k_kvq_prompt's tiles, which have many columns and few items: HD / 4 lanes to a column.  (A block to a column, as
+// above, made 29,000 blocks for a prompt of 1,024 tokens, 50 us.)
 template <int HD>
 __global__ __launch_bounds__(256) void k_kvq_join_prompt(KvqAttendArgs a, KvqCut cut) {
   constexpr int LPC = HD / 4, PER = kKvqTileItems / LPC;
@@ -1295,10 +1308,10 @@ struct AttendPlan {
 // Whether k_kvq_prompt takes the sequences of more than 64 columns.  It shares a page's unpacking among 128 columns, but
 // its blocks take their pages in turn and a page costs one ~1.1 us of a compute unit: it wants enough tiles to fill the card,
 // or so much work that it can be split over the keys.  k_kvq_prompt | k_kvq_attend:
-//   by tiles: 32 prompts of 128 tokens 27 | 39, 8 of 512 37 | 60, one of 2,048 60 | 73; one of 1,024 34 | 26, of 512 20 | 13,
+//   by tiles: 32 prompts of 128 tokens 27 | 34, 8 of 512 38 | 48, one of 2,048 61 | 63; one of 1,024 34 | 26, of 512 20 | 13,
 //     of 397 17 | 10; 2 x 64, 8 of 512 18 | 29, 32 times the last 64 rows of 1,000 keys 32 | 27
-//   by work: the last 512 rows of 14,000 keys 134 | 182, 128 of 14,000 52 | 66, 64 of 14,000 41 | 37, 128 of 3,000 29 | 27,
-//     256 of 2,000 30 | 19; 2 x 64, 512 of 14,000 53 | 72, one prompt of 2,048 35 | 23
+//   by work: the last 512 rows of 14,000 keys 134 | 176, 128 of 14,000 52 | 54, 64 of 14,000 41 | 38, 128 of 3,000 29 | 16,
+//     256 of 2,000 30 | 19; 2 x 64, 512 of 14,000 53 | 68, one prompt of 2,048 35 | 23
 bool prompt_pays(const KvqCache& c, int64_t tiles, int pages) {  // of 16 columns, over all KV heads
   return tiles >= 2048 || tiles * pages * c.hd >= int64_t{1} << 22;
 }
@@ -1388,6 +1401,7 @@ hipError_t attend_launch(KvqAttendArgs a, const AttendPlan& p, float* ws, hipStr
 }
 
 // Rows of a wave of the row kernels: one step, or four to as many as a wave's lanes look up, while 2,048 waves are left.
+// Append and read-back of 11,511 tokens of the 7B layer: 21.0 us, with 1,024 waves 27.1, with 4,096 22.6.
 int rows_per_wave(const KvqCache& c, int n_rows) {
   const int step = 512 / c.hd;
   const int64_t want = static_cast<int64_t>(n_rows) * c.n_kv / 2048;

@@ -308,6 +308,37 @@ def test_attend_many_sequences():
     s.check(out, q=s.q[:1].expand(300, 14, 64))
 
 
+@pytest.mark.parametrize("kind", ["tiles", "eight"])
+def test_prompts_of_more_sequences_than_lanes(kind):
+    rng = np.random.default_rng(34)
+    ctx = rng.integers(1, 200, 150).tolist()
+    rows = [int(min(c, rng.integers(0, 25))) for c in ctx]
+    s = Setup(28, 4, 128, ctx, rows, seed=35, room=_room(kind, 28, 128)).fill()
+    out = torch.full_like(s.q, 5.0)
+    s.cache.attend(s.batch(), s.q, out=out)
+    s.check(out)
+    assert (out[sum(rows):] == 5).all()
+
+
+@pytest.mark.parametrize("kind", ["", "tiles", "split", "eight"])
+def test_more_rows_than_tokens(kind):
+    """Rows before a sequence's first token are zero, in the middle of a tile and a page too; the others are right."""
+    ctx, rows = [70, 1, 40, 300, 0], [100, 90, 40, 310, 20]
+    s = Setup(14, 2, 64, ctx, rows, seed=36, room=_room(kind if kind != "eight" else "", 14, 64)) if kind != "eight" else \
+        Setup(28, 4, 128, ctx, rows, seed=36, room=_room(kind, 28, 128))
+    s.fill()
+    out = _f64(s.cache.attend(s.batch(), s.q))
+    q, at = _f64(s.q), 0
+    for b, (c, n) in enumerate(zip(ctx, rows)):
+        assert (out[at:at + n - c] == 0).all()
+        if c:
+            k, v = s.held()[b]
+            ref, mag, top = okvq.attend(q[at + n - c:at + n], k, v, np.arange(c), s.hd ** -0.5)
+            bar = _bound(ref, mag, top, c, s.hd, "bf16", np.abs(v).max())
+            assert (np.abs(out[at + n - c:at + n] - ref) <= bar).all(), b
+        at += n
+
+
 def test_rows_without_keys_are_zero():
     """Empty contexts and rows before their sequence's first token."""
     s = Setup(14, 2, 64, [0, 3, 0, 70], rows=[2, 5, 1, 1], seed=6)
