@@ -739,12 +739,19 @@ class KvqCache:
 
     def read(self, batch: KvqBatch, dtype=None, out=None):
         """(k, v) that the cache holds of the batch's rows, in dtype (bfloat16) or into the tensors `out`."""
-        torch, n = self.torch, batch.struct.n_rows
+        n, heads, hd = batch.struct.n_rows, self.n_kv_heads, self.head_dim
         if out is None:
-            out = torch.empty((2, n, self.n_kv_heads, self.head_dim), dtype=torch.bfloat16 if dtype is None else dtype,
-                              device=self.device).unbind()
-        k, v = out
-        self._call(rp_kvq_read, batch.struct, self._tensor(k, n, self.n_kv_heads), self._tensor(v, n, self.n_kv_heads))
+            out = self.torch.empty((2, n, heads, hd), dtype=self.torch.bfloat16 if dtype is None else dtype, device=self.device)
+            dt, at = self._types.get(out.dtype), out.data_ptr()
+            if dt is None:
+                raise ValueError(f"the cache reads as float32 or bfloat16, not {out.dtype}")
+            k, v = out.unbind()
+            k_t = RpKvqTensor(at, heads * hd, hd, dt)  # our own tensors need no checks
+            v_t = RpKvqTensor(at + n * heads * hd * out.itemsize, heads * hd, hd, dt)
+        else:
+            k, v = out
+            k_t, v_t = self._tensor(k, n, heads), self._tensor(v, n, heads)
+        self._call(rp_kvq_read, batch.struct, k_t, v_t)
         return k, v
 
     def attend_workspace(self, batch: KvqBatch, n_q_heads: int):

@@ -700,5 +700,8 @@ def test_python_refusals():
         s.cache.attend(b, s.q, scale=0.0)
     with pytest.raises(R.RollpackError):
         s.cache.attend(b, s.q, out=s.q)
+    for dt in (torch.float16, torch.int32):
+        with pytest.raises(ValueError):
+            s.cache.read(b, dtype=dt)
     with pytest.raises(ValueError):
         R.KvqCache(4, 2, 64, device="cpu")
