@@ -1305,15 +1305,23 @@ struct AttendPlan {
   int waves = 4, prompt_waves = 4;  // of a block
 };
 
-// Whether k_kvq_prompt takes the sequences of more than 64 columns.  It shares a page's unpacking among 128 columns, but
-// its blocks take their pages in turn and a page costs one ~1.1 us of a compute unit: it wants enough tiles to fill the card,
-// or so much work that it can be split over the keys.  k_kvq_prompt | k_kvq_attend:
-//   by tiles: 32 prompts of 128 tokens 27 | 34, 8 of 512 38 | 48, one of 2,048 61 | 63; one of 1,024 34 | 26, of 512 20 | 13,
-//     of 397 17 | 10; 2 x 64, 8 of 512 18 | 29, 32 times the last 64 rows of 1,000 keys 32 | 27
-//   by work: the last 512 rows of 14,000 keys 134 | 176, 128 of 14,000 52 | 54, 64 of 14,000 41 | 38, 128 of 3,000 29 | 16,
-//     256 of 2,000 30 | 19; 2 x 64, 512 of 14,000 53 | 68, one prompt of 2,048 35 | 23
-bool prompt_pays(const KvqCache& c, int64_t tiles, int pages) {  // of 16 columns, over all KV heads
-  return tiles >= 2048 || tiles * pages * c.hd >= int64_t{1} << 22;
+// Whether k_kvq_prompt takes the sequences of more than 64 columns.  It shares a page's unpacking among 128 columns, but a
+// block of it takes its pages in turn, at ~1.9 us each beside another block (1.4 at 64 dims) after a start of 8: a batch that
+// does not fill the card several times takes as long as its longest tile.  k_kvq_attend splits a tile's pages among its waves and
+// takes about 7 ns + 0.66 ns (0.34) a page for each 16 columns on the whole card; prompts see half of their pages on average.
+// k_kvq_prompt | k_kvq_attend:
+//   32 prompts of 128 tokens 27 | 34, 8 of 512 38 | 48, 4 of 2,000 147 | 261, one of 8,192 483 | 703, of 3,000 89 | 115, of 2,048
+//     61 | 63, of 1,024 34 | 26, of 397 17 | 10; 2 x 64, 8 of 512 18 | 29, 2 of 2,500 59 | 63, one of 8,192 181 | 212, of 4,500 96 | 75,
+//     of 2,400 50 | 28
+//   32 times the last 64 rows of 1,000 keys 46 | 72, 8 times 512 of 6,000 349 | 518; 2 x 64, the latter 140 | 163
+// Fewer tiles than fill the card once are split over the keys of a long context:
+//   the last 512 rows of 14,000 keys 134 | 176, 128 of 14,000 52 | 54, 64 of 14,000 41 | 38, 128 of 3,000 29 | 16,
+//     256 of 2,000 30 | 19; 2 x 64, 512 of 14,000 53 | 68
+bool prompt_pays(const KvqCache& c, const KvqBatch& b, int64_t tiles, int64_t pages) {  // tiles of 16 columns, over all KV heads
+  const bool whole = 2 * static_cast<int64_t>(kvq_max_rows(b)) > b.max_context;
+  if (tiles < 2048) return !whole && tiles * pages * c.hd >= int64_t{1} << 22;
+  const int64_t seen = whole ? pages : 2 * pages;  // in halves
+  return c.hd == 128 ? tiles * (20 + seen) > 24000 + 5760 * pages : tiles * (42 + seen) > 47000 + 8100 * pages;
 }
 
 AttendPlan attend_plan(const KvqCache& c, const KvqBatch& b, int n_q, bool bf16) {
@@ -1322,7 +1330,7 @@ AttendPlan attend_plan(const KvqCache& c, const KvqBatch& b, int n_q, bool bf16)
   const int pages = std::max(1, kvq_pages(b.max_context));
   AttendPlan p;
   p.walk.find = most > p.walk.cols;
-  if (bf16 && most > 64 && prompt_pays(c, kvq_tile_bound(b, G, p.walk) * c.n_kv, pages)) {
+  if (bf16 && most > 64 && prompt_pays(c, b, kvq_tile_bound(b, G, p.walk) * c.n_kv, pages)) {
     p.prompt.find = 1;
     p.prompt.least = 8;
     if (static_cast<int64_t>(b.n_seqs) * kvq_max_rows(b) > b.n_rows) p.prompt.above = p.walk.upto = 64;  // else all have as many rows

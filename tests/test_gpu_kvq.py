@@ -50,8 +50,8 @@ def _ints(a):
 def _room(kind, n_q, hd):
     """Bounds of a call (rows, context) under which sequences of many rows go to each form of the kernel for them,
     however few rows they have: many tiles; fewer of more pages, split over the keys; blocks of eight waves."""
-    return {"": None, "tiles": (-(-2048 * 16 // n_q), 0), "split": (-(-512 * 16 // n_q), 64 * 8192 // hd),
-            "eight": (-(-49152 // n_q), 4096)}[kind]
+    return {"": None, "tiles": (-(-8192 * 16 // n_q), 0), "split": (-(-512 * 16 // n_q), 64 * 8192 // hd),
+            "eight": (-(-81920 // n_q), 4096)}[kind]
 
 
 class Setup:
@@ -293,6 +293,16 @@ def test_attend_long_contexts(dtype, ctx, rows):
     s = Setup(7, 1, 128, ctx, rows, dtype, seed=3).fill()
     s.check(s.cache.attend(s.batch(), s.q))
     s = Setup(6, 2, 64, ctx, rows, dtype, seed=4).fill()
+    s.check(s.cache.attend(s.batch(), s.q))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_attend_as_many_blocks_as_compute_units(hd, dtype):
+    """256 blocks with long contexts among them: blocks of eight waves."""
+    rng = np.random.default_rng(37)
+    ctx = [1300, 1100, 0] + rng.integers(1, 90, 61).tolist()
+    s = Setup(12, 4, hd, ctx, [1, 1, 0] + [1] * 61, dtype=dtype, seed=38).fill()
     s.check(s.cache.attend(s.batch(), s.q))
 
 
