@@ -194,8 +194,9 @@ __device__ __forceinline__ uint32_t get_values(const unsigned char* block, int t
 }
 
 // 11,511 tokens of the 7B layer (4 KV heads of 128) 10.8 us, 2.8 TB/s in and out: the launch and the lookups (three to ten reads
-// that wait for each other) are half of it; one token each of 64 sequences 4.1 us.  Values come with plain loads: rows that the projection has just written
-// are in the caches (past them: 21.7 | 21.0 us with the read-back for the former, 151 | 164 for 67,000 tokens of 8 heads).
+// that wait for each other) are half of it; one token each of 64 sequences 4.1 us.  Values come with plain loads: rows that the
+// projection has just written are in the caches (past them: 21.7 | 21.0 us with the read-back for the former, 151 | 164 for
+// 67,000 tokens of 8 heads).
 template <int HD, bool BF16, int U>
 __global__ __launch_bounds__(256) void k_kvq_append(KvqCache c, KvqBatch bt, KvqTensor k, KvqTensor v, int rows) {
   const int lane = threadIdx.x & 63, d = lane % (HD / 8) * 8;
@@ -232,8 +233,8 @@ __global__ __launch_bounds__(256) void k_kvq_append(KvqCache c, KvqBatch bt, Kvq
   }
 }
 
-// HBM bounds it: 163,000 tokens of the 7B layer 73 us, 5.8 TB/s.  What it writes goes past the caches; with plain stores it
-// took 19 us more.
+// HBM bounds it: 163,000 tokens of the 7B layer 73 us alone, 5.8 TB/s, 84 to 100 one after another.  What it writes goes past
+// the caches; with plain stores it took 19 us more.
 template <int HD, bool BF16, int U>
 __global__ __launch_bounds__(256) void k_kvq_read(KvqCache c, KvqBatch bt, KvqTensor k, KvqTensor v, int rows) {
   const int lane = threadIdx.x & 63, d = lane % (HD / 8) * 8;
