@@ -141,6 +141,9 @@ rollpack::KvqBatch kvq_batch(const rp_kvq_batch* b, bool need_memory) {
   return k;
 }
 
+// Whether some sequence may have a row: without one a launch has a grid of no blocks.
+bool kvq_any_row(const rollpack::KvqBatch& b) { return b.n_seqs > 0 && b.n_rows > 0 && rollpack::kvq_max_rows(b) > 0; }
+
 rollpack::KvqTensor kvq_tensor(const rp_kvq_tensor* t, int64_t rows, int64_t heads, int64_t hd, bool written) {
   kvq_require(t, "null tensor");
   kvq_require(t->data, "null tensor data");
@@ -187,7 +190,7 @@ rp_status kvq_rows_call(const rp_kvq_cache* cache, const rp_kvq_batch* batch, co
   return guarded([&] {
     const rollpack::KvqCache c = kvq_cache(cache, true);
     const rollpack::KvqBatch b = kvq_batch(batch, true);
-    if (b.n_seqs == 0 || b.n_rows == 0) return;
+    if (!kvq_any_row(b)) return;
     kvq_require(static_cast<int64_t>(b.n_rows) * c.n_kv <= (int64_t{1} << 26), "too many rows and heads for one call");
     const rollpack::KvqTensor kt = kvq_tensor(k, b.n_rows, c.n_kv, c.hd, written);
     const rollpack::KvqTensor vt = kvq_tensor(v, b.n_rows, c.n_kv, c.hd, written);
@@ -546,7 +549,7 @@ rp_status rp_kvq_attend(const rp_kvq_cache* cache, const rp_kvq_batch* batch, in
     a.batch = kvq_batch(batch, true);
     const size_t need = kvq_attend_size(a.cache, a.batch, n_q_heads);
     kvq_require(scale > 0.f && std::isfinite(scale), "scale must be positive and finite");
-    if (a.batch.n_seqs == 0 || a.batch.n_rows == 0) return;
+    if (!kvq_any_row(a.batch)) return;
     a.q = kvq_tensor(q, a.batch.n_rows, n_q_heads, a.cache.hd, false);
     a.out = kvq_tensor(out, a.batch.n_rows, n_q_heads, a.cache.hd, true);
     kvq_require(a.q.bf16 == a.out.bf16, "q and out must have one dtype");

@@ -124,6 +124,16 @@ def test_empty_batches_do_nothing(lib):
         rp.rp_kvq_attend(_cache(), _batch(**kw), 6, 0.1, _tensor(6), _tensor(6), 4 * PTR, 1 << 40, 0)
 
 
+def test_batches_whose_sequences_have_no_row_do_nothing(lib):
+    """max_rows = 0: the tensors' rows are all behind the last sequence, however many there are; also where a long context
+    splits attention into items and a second kernel joins them (its grid has as many blocks as a tile has columns)."""
+    for kw in (dict(max_rows=0), dict(max_rows=0, n_seqs=1, max_context=8192, table_stride=128)):
+        b = _batch(**kw)
+        rp.rp_kvq_append(_cache(), b, _tensor(), _tensor(data=2 * PTR), 0)
+        rp.rp_kvq_read(_cache(), b, _tensor(), _tensor(data=2 * PTR), 0)
+        rp.rp_kvq_attend(_cache(), b, 6, 0.1, _tensor(6), _tensor(6, data=2 * PTR), 4 * PTR, 1 << 40, 0)
+
+
 def test_workspace_is_bounded(lib):
     """Long contexts do not grow it without end, and a context of a page needs none."""
     c = _cache(n_kv_heads=4)
