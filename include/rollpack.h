@@ -651,7 +651,11 @@ rp_status rp_kvq_attend_workspace(const rp_kvq_cache* cache, const rp_kvq_batch*
  * (section 2.1): for row r of a sequence, at position p, and query head h
  *   out[r, h] = sum_t softmax_t(scale q[r, h] . k[t, h / G]) v[t, h / G],  t = 0 .. p,
  * G = n_q_heads / n_kv_heads.  The rows' own keys must be in the cache (rp_kvq_append
- * before this call on the same stream).  Scores, softmax and sums are fp32.
+ * before this call on the same stream).  Scores, exponentials and sums are fp32.  A weight is
+ * rounded once for its product with v: to 24 bits in fp32 calls, to 11 in bf16 ones, where weights below
+ * 2^-21 of a row's largest may be off by 2^-11 of what the 32 keys around them weigh together.
+ * The division by the sum comes last: the sums are finite while the largest |v| times the context
+ * is below 2^119.
  *   n_q_heads  a multiple of n_kv_heads
  *   scale      positive and finite (1 / sqrt(head_dim))
  *   q, out     [n_rows, n_q_heads, head_dim] of one dtype; out may not overlap q

@@ -511,17 +511,59 @@ struct Query {
 };
 
 // One page of an online softmax in the log2 domain, for a lane's N scores of one column.
-//   The reference m moves only when probabilities pass 2^8 (or there is none yet): up to that they lose nothing in fp32,
-// bf16 or fp16, the outputs need rescaling a few times per item instead of every page, and a page's own maximum is not
+//   The reference m moves only when the sum of a page's probabilities passes kSumMost (or there is none yet): up to that they
+// lose nothing, the outputs need rescaling a few times per item instead of every page, and a page's own maximum is not
 // formed at all: its sum tells.  l is the lane's part of the sum; the lanes of a column add theirs at the end.
+//   In fp16 (HALF) the largest probability of a page that moves m is 2^7, and none passes 2^15: from 2^-14 on, 2^-21 of that
+// largest one, each is rounded once, to 2^-11 of itself.  Smaller ones fp16 would hold with fewer bits or not at all, to 2^-25,
+// and a row whose largest weights meet values of zero is made of them.  So where that could count, small_page takes them as a
+// second operand, 2^29 times as large and normal down to 2^-43: in pages of which a lane's sum is below 2^-9, as 2^-25 for
+// each of its N keys is less than 2^-11 of more, and in pages that move m, whose sum may be one key's.  With every page looked at
+// a prompt of 14,500 tokens took 2,130 us (1,405 so, 1,393 with none): among the columns of a wave one has a weight below
+// 2^-21 in up to half of the pages.
 struct Softmax {
   float m = -INFINITY, l = 0.f;
 };
+constexpr float kLift = 7.f;
+constexpr float kSmallBelow = 0x1p-14f;
+constexpr float kSumLeast = 0x1p-9f;
+template <bool HALF> constexpr float kSumMost = HALF ? 0x1p15f : 0x1p8f;
+
+// Two probabilities as fp16, rounded to nearest; sum: theirs as rounded, added to it.
+__device__ __forceinline__ uint32_t half_pair(float a, float b, float& sum) {
+  const f16x2 p = __builtin_convertvector(f32x2{a, b}, f16x2);
+  sum = __builtin_amdgcn_fdot2(p, f16x2{1, 1}, sum, false);
+  return __builtin_bit_cast(uint32_t, p);
+}
+
+// The small probabilities of a page of fp16 ones x, w: products(small) of the operand that holds them, between scalings of the
+// outputs by 2^29 and back, which are exact.  w is left without them.  Returns the sum of all, as rounded.
+template <int N, typename Rescale, typename Products>
+__device__ __forceinline__ float small_page(const float (&x)[N], uint32_t (&w)[N / 2], float sum, Rescale rescale, Products products) {
+  uint32_t least = ~0u;  // by their bits less one: zeros, of keys out of sight, come last
+#pragma unroll
+  for (int k = 0; k < N; ++k) least = min(least, __float_as_uint(x[k]) - 1);
+  if (__builtin_expect(!__any(least < __builtin_bit_cast(uint32_t, kSmallBelow) - 1), 1)) return sum;
+  uint32_t small[N / 2];
+  float large_sum = 0.f, small_sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < N / 2; ++k) {
+    const bool a = x[2 * k] < kSmallBelow, b = x[2 * k + 1] < kSmallBelow;
+    w[k] = half_pair(a ? 0.f : x[2 * k], b ? 0.f : x[2 * k + 1], large_sum);
+    small[k] = half_pair(a ? x[2 * k] * 0x1p29f : 0.f, b ? x[2 * k + 1] * 0x1p29f : 0.f, small_sum);
+  }
+  rescale(0x1p29f);
+  products(small);
+  rescale(0x1p-29f);
+  return __builtin_fmaf(small_sum, 0x1p-29f, large_sum);
+}
 
 // x: the scores, and then the probabilities; w: these as pairs of fp16 (HALF), whose own sum l takes.  rescale(alpha) scales
-// the outputs; ACROSS are the lanes (besides the first, as xor masks) that share the column.
-template <bool HALF, int N, typename Rescale, typename... Across>
-__device__ __forceinline__ void softmax_page(Softmax& st, float (&x)[N], uint32_t (&w)[N / 2], float scale_log2, Rescale rescale, Across... across) {
+// the outputs, products(w) adds the page's products of such pairs to them (HALF: of small probabilities; those of w are the
+// caller's); ACROSS are the lanes (besides the first, as xor masks) that share the column.
+template <bool HALF, int N, typename Rescale, typename Products, typename... Across>
+__device__ __forceinline__ void softmax_page(Softmax& st, float (&x)[N], uint32_t (&w)[N / 2], float scale_log2, Rescale rescale,
+                                             Products products, Across... across) {
   float s[N], sum;
 #pragma unroll
   for (int k = 0; k < N; ++k) s[k] = x[k];
@@ -530,7 +572,7 @@ __device__ __forceinline__ void softmax_page(Softmax& st, float (&x)[N], uint32_
 #pragma unroll
     for (int k = 0; k < N; ++k) top = fmaxf(top, s[k]);
     ((top = fmaxf(top, __shfl_xor(top, across, 64))), ...);
-    const float m_new = fmaxf(st.m, top * scale_log2);
+    const float m_new = fmaxf(st.m, HALF ? __builtin_fmaf(top, scale_log2, -kLift) : top * scale_log2);
     const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m - m_new);
     st.m = m_new;
     st.l *= alpha;
@@ -540,29 +582,40 @@ __device__ __forceinline__ void softmax_page(Softmax& st, float (&x)[N], uint32_
     const float shift = st.m == -INFINITY ? 0.f : st.m;
 #pragma unroll
     for (int k = 0; k < N; ++k) x[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k], scale_log2, -shift));
+    float part[2] = {0.f, 0.f};
     if constexpr (HALF) {
-      float part[2] = {0.f, 0.f};
 #pragma unroll
-      for (int k = 0; k < N / 2; ++k) {
-        const f16x2 p = __builtin_convertvector(f32x2{x[2 * k], x[2 * k + 1]}, f16x2);
-        w[k] = __builtin_bit_cast(uint32_t, p);
-        part[k & 1] = __builtin_amdgcn_fdot2(p, f16x2{1, 1}, part[k & 1], false);
-      }
-      sum = part[0] + part[1];
+      for (int k = 0; k < N / 2; ++k) w[k] = half_pair(x[2 * k], x[2 * k + 1], part[k & 1]);
     } else {
-      float part[2] = {0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < N; ++k) part[k & 1] += x[k];
-      sum = part[0] + part[1];
     }
+    sum = part[0] + part[1];
   };
-  if (__any(st.m == -INFINITY)) move();
+  const bool none = __any(st.m == -INFINITY);
+  if (none) move();
   form();
-  if (__any(sum > 256.f)) {
+  if constexpr (HALF) {
+    if (none || __any(sum < kSumLeast || sum > kSumMost<HALF>)) {
+      if (__any(sum > kSumMost<HALF>)) {
+        move();
+        form();
+      }
+      sum = small_page(x, w, sum, rescale, products);
+    }
+  } else if (__any(sum > kSumMost<HALF>)) {
     move();
     form();
   }
   st.l += sum;
+}
+
+// From probabilities in fp16 to those in bf16, whose reference is a page's largest.
+template <typename Rescale>
+__device__ __forceinline__ void leave_half(Softmax& st, Rescale rescale) {
+  st.m += kLift;
+  st.l *= 0x1p-7f;
+  rescale(0x1p-7f);
 }
 
 // The two values of byte `i` of a word of codes, packed as the type's operand.
@@ -649,8 +702,8 @@ __device__ __forceinline__ void nan_values(PageV<HD>& pg, const char* block, int
 // S^T = K Q^T, an online softmax in the log2 domain and O^T += V^T P^T with MFMA, straight from registers: no
 // value of the cache is used by more than one wave, so nothing passes through LDS but the waves' results.  The next
 // page's K is loaded when the scores are formed, its V when the outputs are.
-//   P is an operand rounded to fp16 (2^-12 of it; to 2^-25 below 2^-14), V exact in it: less than the output's own
-// rounding to bf16, where P in bf16 would add as much again.  Pages with values that fp16 does not hold, and fp32, take
+//   P is an operand rounded to fp16 (2^-11 of it at most, and see Softmax), V exact in it: less than the output's own
+// rounding to bf16, 2^-8, where P in bf16 would add as much again.  Pages with values that fp16 does not hold, and fp32, take
 // bf16: P in two pieces, or three.
 //   HBM bounds decoding of many keys: one token each of 64 sequences of 600 to 4,500 (7B layer, 163,000 keys) 23 us, 3.9 TB/s;
 // of 330 of 130 to 1,300 38 us, 4.6; of 96 of 32B's layer, 442,000 keys, 95 us, 5.1, what a copy reaches.  Below that it is
@@ -708,6 +761,10 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendAr
     };
     Query<HD, F32 ? 3 : 1> qf;
     qf.load(a.q, sq.r0 + row, head);
+    auto rescale = [&](float alpha) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) o[t] *= alpha;
+    };
     int i = 0;
     // The wave's pages from i on.  HALF: V and P in fp16, up to the first page that does not fit; else in bf16.
     auto walk = [&](auto half_tag) {
@@ -748,9 +805,11 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendAr
         uint32_t w[8];
 #pragma unroll
         for (int k = 0; k < 16; ++k) x[k] = s[k >> 2][k & 3];
-        softmax_page<HALF>(st, x, w, scale_log2, [&](float alpha) {
-#pragma unroll
-          for (int t = 0; t < NT; ++t) o[t] *= alpha;
+        softmax_page<HALF>(st, x, w, scale_log2, rescale, [&](const uint32_t (&small)[8]) {
+          if constexpr (HALF) {
+            half_values<HD, true, 1>(pv, 0, x, small, o);
+            half_values<HD, true, 1>(pv, 1, x, small, o);
+          }
         }, 16, 32);
         if (!HALF && !__all(fits_half(pv.s))) nan_values<HD>(pv, at, tok0, lim, o);
         half_values<HD, HALF, F32 ? 3 : 2>(pv, 0, x, w, o);
@@ -760,7 +819,10 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendAr
         pv.load(at);
       }
     };
-    if constexpr (!F32) walk(std::true_type{});
+    if constexpr (!F32) {
+      walk(std::true_type{});
+      if (i < nw) leave_half(st, rescale);
+    }
     if (F32 || i < nw) walk(std::false_type{});
     st.l += __shfl_xor(st.l, 16, 64);
     st.l += __shfl_xor(st.l, 32, 64);
@@ -1074,6 +1136,12 @@ __global__ __launch_bounds__(64 * NW, 2) void k_kvq_prompt(KvqAttendArgs a, KvqC
     share_store<HD>(share, th, has_k, has_v, p0 * kKvqPage, tl.end, half, lds[0], lds[0] + 8 * HD);
     share_load<HD>(share, block_of(id, share.lost), th, has_k, has_v);
     id = id_of(2);
+    auto rescale = [&](float alpha) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[t][r] *= alpha;
+    };
     int p = 0;
     // Pages from p on.  HALF: V and P in fp16, up to the first page that does not fit; else in bf16.
     auto walk = [&](auto half_tag) {
@@ -1116,11 +1184,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_kvq_prompt(KvqAttendArgs a, KvqC
         uint32_t w[16];
 #pragma unroll
         for (int k = 0; k < 32; ++k) x[k] = s[k >> 4][k & 15];
-        softmax_page<HALF>(st, x, w, scale_log2, [&](float alpha) {
-#pragma unroll
-          for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[t][r] *= alpha;
+        softmax_page<HALF>(st, x, w, scale_log2, rescale, [&](const uint32_t (&small)[16]) {
+          if constexpr (HALF) page_values<HD, true>(lv, x, small, o);
         }, 32);
         if (!HALF) {  // NaN value blocks: the outputs that lie in one turn NaN if the column sees the token
           bool ig;
@@ -1143,7 +1208,10 @@ __global__ __launch_bounds__(64 * NW, 2) void k_kvq_prompt(KvqAttendArgs a, KvqC
       }
     };
     walk(std::true_type{});
-    if (p < np) walk(std::false_type{});
+    if (p < np) {
+      leave_half(st, rescale);
+      walk(std::false_type{});
+    }
     st.l += __shfl_xor(st.l, 32, 64);
   }
 

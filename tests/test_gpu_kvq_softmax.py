@@ -1,4 +1,4 @@
-"""Attention over the 4-bit cache where the softmax is hard: maxima that move.
+"""Attention over the 4-bit cache where the softmax is hard: weights far below a row's largest, and maxima that move.
 
 Every key has its first block of 32 dimensions aimed at the queries' first block, so that a count 0 .. 32 sets its score;
 the other dimensions are random.  The bar is test_gpu_kvq's, from the roundings: scores and sums in fp32, a weight
@@ -68,6 +68,30 @@ def _types(form):
     return ("bf16",) if form.startswith("prompt") else ("bf16", "f32")
 
 
+@pytest.mark.parametrize("form", FORMS)
+def test_weights_far_below_the_largest(form):
+    """One key carries the weight and its value is zero: the output is made of weights of any size."""
+    for dtype in _types(form):
+        for nats in (10.0, 13.0, 16.0, 27.0):
+            s = _setup(form, dtype, 41)
+            off, counts = np.concatenate([[0], np.cumsum(s.ctx)]), []
+            for b, c in enumerate(s.ctx):
+                at = 0 if b % 2 == 0 else c // 2  # the first key, or one with smaller ones before it
+                counts.append(np.where(np.arange(c) == at, 32, 0))
+                s.v[off[b] + at] = 0
+            _aim(s, counts, nats).fill()
+            _check(s, s.cache.attend(s.batch(), s.q))
+
+
+def test_many_keys_beside_a_dominant_one():
+    """A tenth of a percent of the weight in 40,000 keys of a wave, each about 2^-25 of the first, whose value is zero."""
+    s = Setup(2, 1, 64, [40000] + [1] * 257, seed=42)
+    s.v[:, 0] = 1.0 + s.v[:, 0].abs()
+    s.v[0] = 0
+    _aim(s, [np.where(np.arange(40000) == 0, 32, 0)] + [np.zeros(1)] * 257, 18.0).fill()
+    _check(s, s.cache.attend(s.batch(), s.q))
+
+
 STEPS = {
     "steep": lambda page: np.minimum(32, 5 * page),   # ~14 bits a page
     "slow": lambda page: np.minimum(32, page),        # ~3
@@ -98,4 +122,13 @@ def test_values_beyond_half_precision_after_a_move(form):
             s.v[off[b] + c // 2:off[b + 1]:7] *= 2.0 ** 30
             s.v[off[b] + c // 2 + 3:off[b + 1]:11] *= 2.0 ** -40
         s.fill()
+        _check(s, s.cache.attend(s.batch(), s.q))
+
+
+@pytest.mark.parametrize("kind", ["", "tiles", "split", "eight"])
+def test_large_scores_have_the_right_values(kind):
+    """Scores in the thousands: one key takes nearly all of the weight, and which one changes all the time."""
+    for dtype in ("bf16", "f32"):
+        s = Setup(7, 1, 128, [700, 65, 1], rows=[30 if kind else 3, 65, 1], dtype=dtype, seed=45, gain=6.0, room=_room(kind, 7, 128)).fill()
+        s.q *= 4
         _check(s, s.cache.attend(s.batch(), s.q))
