@@ -677,6 +677,12 @@ __device__ __forceinline__ bool fits_half(const u32x4& s) {
   return !(t & 0xe0e0e0e0u);
 }
 
+// Scale bytes of tokens t .. t + 3, those from `end` on as 1: what lies behind the last key may be anything.
+__device__ __forceinline__ uint32_t scales_below(uint32_t s, int t, int end) {
+  const uint32_t keep = static_cast<uint32_t>((1ull << (8 * min(max(end - t, 0), 4))) - 1);
+  return (s & keep) | (0x7f7f7f7fu & ~keep);
+}
+
 // A page with NaN blocks: their scales become 2^-127, which the zero probability of a key out of sight clears (as NaN it
 // would not), and the lane's outputs turn NaN if its column sees the token.  A lane's outputs all lie in one block of 32
 // dimensions.
@@ -782,13 +788,10 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendAr
         for (int u = 0; u < 4; ++u) s[u] = qf.scores(pk, u);
         const char* next = block_of(i + 1);
         pk.load(next);
-        if (tok0 + kKvqPage > tl.end) {  // what lies behind the last key may be anything
+        const int held = lost ? tok0 : tl.end;  // what lies behind the last key, or in a page that stands in, may be anything
+        if (tok0 + kKvqPage > held) {
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int n = min(max(tl.end - (tok0 + 16 * u + 4 * g), 0), 4);
-            const uint32_t keep = static_cast<uint32_t>((1ull << (8 * n)) - 1);
-            pv.s[u] = (pv.s[u] & keep) | (0x7f7f7f7fu & ~keep);
-          }
+          for (int u = 0; u < 4; ++u) pv.s[u] = scales_below(pv.s[u], tok0 + 16 * u + 4 * g, held);
         }
         if (HALF && !__all(fits_half(pv.s))) return;
         if (lost || tok0 + kKvqPage > open) {
@@ -944,11 +947,6 @@ __device__ __forceinline__ void share_load(PageShare<HD>& s, const char* block, 
   s.all = *(reinterpret_cast<const uint32_t*>(block + 66 * HD) + (threadIdx.x & (HD / 2 - 1)));
 }
 
-// Scale bytes of tokens t .. t + 3, those from `end` on as 1: what lies behind the last key may be anything.
-__device__ __forceinline__ uint32_t scales_below(uint32_t s, int t, int end) {
-  const uint32_t keep = static_cast<uint32_t>((1ull << (8 * min(max(end - t, 0), 4))) - 1);
-  return (s & keep) | (0x7f7f7f7fu & ~keep);
-}
 // NaN scales as 2^-127, which a zero probability clears.
 __device__ __forceinline__ uint32_t without_nan(uint32_t s) {
 #pragma unroll
@@ -1121,10 +1119,12 @@ __global__ __launch_bounds__(64 * NW, 2) void k_kvq_prompt(KvqAttendArgs a, KvqC
       return base + static_cast<size_t>(lost ? 0 : id) * n_kv * bytes;
     };
     auto id_of = [&](int p) { return __builtin_amdgcn_readfirstlane(pt[min(p, np - 1)]); };
+    // The end of the keys of page p0 + p, whose share is s: none where another page stands in.
+    auto held = [&](const PageShare<HD>& s, int p) { return s.lost ? (p0 + p) * kKvqPage : tl.end; };
     // Whether page p0 + p, whose share is s, has values that fp16 holds: the same in every wave.
     auto fits = [&](const PageShare<HD>& s, int p) {
-      const int i = lane & (HD / 2 - 1), t = 16 * (i & 3) + 4 * ((i >> 2) & 3), tok0 = (p0 + p) * kKvqPage;
-      const uint32_t w = tok0 + kKvqPage > tl.end ? scales_below(s.all, tok0 + t, tl.end) : s.all;
+      const int i = lane & (HD / 2 - 1), t = 16 * (i & 3) + 4 * ((i >> 2) & 3), tok0 = (p0 + p) * kKvqPage, end = held(s, p);
+      const uint32_t w = tok0 + kKvqPage > end ? scales_below(s.all, tok0 + t, end) : s.all;
       return static_cast<bool>(__all((((w + 0x18181818u) ^ 0x80808080u) & 0xe0e0e0e0u) == 0));
     };
     PageShare<HD> share;
@@ -1133,7 +1133,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_kvq_prompt(KvqAttendArgs a, KvqC
     int id = id_of(1);
     share_load<HD>(share, block_of(id_of(0), share.lost), th, has_k, has_v);
     bool half = fits(share, 0), lost = share.lost;
-    share_store<HD>(share, th, has_k, has_v, p0 * kKvqPage, tl.end, half, lds[0], lds[0] + 8 * HD);
+    share_store<HD>(share, th, has_k, has_v, p0 * kKvqPage, held(share, 0), half, lds[0], lds[0] + 8 * HD);
     share_load<HD>(share, block_of(id, share.lost), th, has_k, has_v);
     id = id_of(2);
     auto rescale = [&](float alpha) {
@@ -1154,7 +1154,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_kvq_prompt(KvqAttendArgs a, KvqC
         if (p + 1 < np) {
           half = HALF && fits(share, p + 1);
           lost = share.lost;
-          share_store<HD>(share, th, has_k, has_v, (p0 + p + 1) * kKvqPage, tl.end, half, lds[(p + 1) & 1], lds[(p + 1) & 1] + 8 * HD);
+          share_store<HD>(share, th, has_k, has_v, (p0 + p + 1) * kKvqPage, held(share, p + 1), half, lds[(p + 1) & 1], lds[(p + 1) & 1] + 8 * HD);
           share_load<HD>(share, block_of(id, share.lost), th, has_k, has_v);
           id = id_of(p + 3);
         }
