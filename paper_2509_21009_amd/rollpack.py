@@ -668,7 +668,7 @@ class KvqCache:
 
     Calls run on torch's current stream of the cache's device, with every tensor on that device.
     They allocate their results (unless `out` is given) and can be captured into a graph; the
-    batch's arrays are then read at each replay.
+    batch's arrays are then read at each replay.  They have no backward.
     """
 
     def __init__(self, n_pages: int, n_kv_heads: int, head_dim: int, device="cuda"):
@@ -721,6 +721,8 @@ class KvqCache:
         if t.device != self.device or t.shape != (rows, heads, self.head_dim) or dt is None or (strides[2] != 1 and t.numel() > 0):
             raise ValueError(f"expected float32 or bfloat16 [{rows}, {heads}, {self.head_dim}] with contiguous head dimensions on "
                              f"{self.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        if t.requires_grad and self.torch.is_grad_enabled():
+            raise ValueError("the 4-bit cache passes no gradient back: detach its tensors, or call it under torch.no_grad()")
         return RpKvqTensor(t.data_ptr(), strides[0], strides[1], dt)
 
     def _call(self, fn, *args):

@@ -180,3 +180,31 @@ def test_engine_sizes_with_the_cache_in_four_bits(lib):
     with pytest.raises(rp.RollpackError) as e:
         rp.rp_read_kv(None, 1, 0, 0, 1, PTR, 2 * PTR)
     assert e.value.status == 1
+
+
+def _host_cache(torch):
+    """A KvqCache over host memory, for calls that are refused before the library is called."""
+    c = object.__new__(rp.KvqCache)
+    c.torch, c.n_pages, c.n_kv_heads, c.head_dim = torch, 4, 2, 64
+    c.blocks = torch.zeros(rp.rp_kvq_cache_bytes(4, 2, 64), dtype=torch.uint8)
+    c.device, c.struct = c.blocks.device, rp.RpKvqCache(c.blocks.data_ptr(), 4, 2, 64)
+    c._types = {torch.float32: rp.RP_DTYPE_F32, torch.bfloat16: rp.RP_DTYPE_BF16}
+    c._call = lambda *a: pytest.fail("called")
+    return c
+
+
+def test_tensors_that_need_gradients_are_refused(lib):
+    """The calls have no backward: a gradient would end at them without a word."""
+    torch = pytest.importorskip("torch")
+    c = _host_cache(torch)
+    b = c.batch(torch.ones(3, dtype=torch.int32), torch.zeros((3, 1), dtype=torch.int32))
+    q, k = torch.zeros(3, 4, 64), torch.zeros(3, 2, 64)
+    grad = lambda t: t.clone().requires_grad_()
+    for call in (lambda: c.attend(b, grad(q)), lambda: c.attend(b, q, out=grad(q)), lambda: c.append(b, grad(k), k),
+                 lambda: c.append(b, k, grad(k)), lambda: c.read(b, out=(k, grad(k)))):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+    c._call = lambda *a: None
+    with torch.no_grad():
+        c.attend(b, grad(q))
+        c.append(b, grad(k), k)
