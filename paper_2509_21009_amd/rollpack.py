@@ -661,6 +661,7 @@ class KvqBatch:
 
     def __init__(self, struct: RpKvqBatch, tensors):
         self.struct, self.tensors = struct, tensors
+        self.device = tensors[0].device
 
 
 class KvqCache:
@@ -725,19 +726,21 @@ class KvqCache:
             raise ValueError("the 4-bit cache passes no gradient back: detach its tensors, or call it under torch.no_grad()")
         return RpKvqTensor(t.data_ptr(), strides[0], strides[1], dt)
 
-    def _call(self, fn, *args):
-        """fn(cache, *args, stream) with the cache's device current."""
+    def _call(self, fn, batch: KvqBatch, *args):
+        """fn(cache, batch, *args, stream) with the cache's device current."""
+        if batch.device != self.device:
+            raise ValueError(f"the batch's arrays are on {batch.device}, the cache on {self.device}")
         cuda = self.torch.cuda
         if cuda.current_device() == self.device.index:
-            fn(self.struct, *args, self._raw_stream(self.device.index))
+            fn(self.struct, batch.struct, *args, self._raw_stream(self.device.index))
         else:
             with cuda.device(self.device):
-                fn(self.struct, *args, self._raw_stream(self.device.index))
+                fn(self.struct, batch.struct, *args, self._raw_stream(self.device.index))
 
     def append(self, batch: KvqBatch, k, v) -> None:
         """Quantise k and v [n_rows, n_kv_heads, head_dim] into the cache at the rows' positions."""
         n = batch.struct.n_rows
-        self._call(rp_kvq_append, batch.struct, self._tensor(k, n, self.n_kv_heads), self._tensor(v, n, self.n_kv_heads))
+        self._call(rp_kvq_append, batch, self._tensor(k, n, self.n_kv_heads), self._tensor(v, n, self.n_kv_heads))
 
     def read(self, batch: KvqBatch, dtype=None, out=None):
         """(k, v) that the cache holds of the batch's rows, in dtype (bfloat16) or into the tensors `out`."""
@@ -753,7 +756,7 @@ class KvqCache:
         else:
             k, v = out
             k_t, v_t = self._tensor(k, n, heads), self._tensor(v, n, heads)
-        self._call(rp_kvq_read, batch.struct, k_t, v_t)
+        self._call(rp_kvq_read, batch, k_t, v_t)
         return k, v
 
     def attend_workspace(self, batch: KvqBatch, n_q_heads: int):
@@ -773,7 +776,7 @@ class KvqCache:
             workspace = self.attend_workspace(batch, heads)
         elif workspace.device != self.device or not workspace.is_contiguous():
             raise ValueError("the workspace is a contiguous tensor on the cache's device")
-        self._call(rp_kvq_attend, batch.struct, heads, self.head_dim ** -0.5 if scale is None else scale,
+        self._call(rp_kvq_attend, batch, heads, self.head_dim ** -0.5 if scale is None else scale,
                    self._tensor(q, n, heads), self._tensor(out, n, heads), workspace.data_ptr(),
                    workspace.numel() * workspace.element_size())
         return out

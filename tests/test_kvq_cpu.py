@@ -208,3 +208,17 @@ def test_tensors_that_need_gradients_are_refused(lib):
     with torch.no_grad():
         c.attend(b, grad(q))
         c.append(b, grad(k), k)
+
+
+def test_a_batch_on_another_device_is_refused(lib):
+    """A batch's arrays are read by kernels on the cache's device."""
+    torch = pytest.importorskip("torch")
+    c = _host_cache(torch)
+    far = _host_cache(torch)
+    far.device = torch.device("meta")
+    b = far.batch(torch.ones(3, dtype=torch.int32, device="meta"), torch.zeros((3, 1), dtype=torch.int32, device="meta"))
+    q, k = torch.zeros(3, 4, 64), torch.zeros(3, 2, 64)
+    c._call = lambda *a: rp.KvqCache._call(c, *a)
+    for call in (lambda: c.attend(b, q), lambda: c.append(b, k, k), lambda: c.read(b), lambda: c.read(b, out=(k, k.clone()))):
+        with pytest.raises(ValueError, match="batch"):
+            call()
