@@ -500,6 +500,8 @@ def rp_stream_read_gbs(buf, reps: int = 5) -> float:
 
 
 def rp_kvq_cache_bytes(n_pages: int, n_kv_heads: int, head_dim: int) -> int:
+    if n_pages >> 63 not in (0, -1) or n_kv_heads >> 31 not in (0, -1) or head_dim >> 31 not in (0, -1):
+        raise ValueError("n_pages must fit 64 bits, n_kv_heads and head_dim 32")  # ctypes would pass their lower halves
     b = ctypes.c_size_t()
     _check(load_library().rp_kvq_cache_bytes(n_pages, n_kv_heads, head_dim, ctypes.byref(b)))
     return b.value
@@ -710,8 +712,12 @@ class KvqCache:
             max_context = min(held, 1 << 30)
         if max_context > held:
             raise ValueError("max_context is past the page table's rows")
+        max_rows = n_rows if max_rows is None else max_rows
+        for name, x in (("n_rows", n_rows), ("max_rows", max_rows), ("max_context", max_context)):
+            if not 0 <= x < 1 << 31:  # ctypes would pass its lower half
+                raise ValueError(f"{name} must be between 0 and 2^31 - 1, got {x}")
         stride = page_table.stride(0) if n > 1 else page_table.shape[1]
-        b = RpKvqBatch(n, n_rows, n_rows if max_rows is None else max_rows, max_context,
+        b = RpKvqBatch(n, n_rows, max_rows, max_context,
                        None if row_offsets is None else row_offsets.data_ptr(), contexts.data_ptr(),
                        page_table.data_ptr(), stride)
         return KvqBatch(b, (contexts, page_table, row_offsets))

@@ -222,3 +222,21 @@ def test_a_batch_on_another_device_is_refused(lib):
     for call in (lambda: c.attend(b, q), lambda: c.append(b, k, k), lambda: c.read(b), lambda: c.read(b, out=(k, k.clone()))):
         with pytest.raises(ValueError, match="batch"):
             call()
+
+
+def test_bounds_that_do_not_fit_an_int_are_refused(lib):
+    """The C structure has 32-bit fields, which would hold a larger number's lower half."""
+    torch = pytest.importorskip("torch")
+    c = _host_cache(torch)
+    ctx, table, off = torch.ones(3, dtype=torch.int32), torch.zeros((3, 1), dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
+    for kw in (dict(n_rows=2 ** 32 + 6), dict(max_rows=2 ** 32 + 1), dict(max_rows=2 ** 31), dict(max_context=-2 ** 32 + 5), dict(n_rows=-1),
+               dict(max_rows=-1)):
+        with pytest.raises(ValueError, match="between"):
+            c.batch(ctx, table, row_offsets=off, **{**dict(n_rows=6), **kw})
+    b = c.batch(ctx, table, row_offsets=off, n_rows=6, max_rows=4, max_context=64)
+    assert (b.struct.n_rows, b.struct.max_rows, b.struct.max_context) == (6, 4, 64)
+    for args in ((4, 2 ** 32 + 2, 64), (4, 2, 2 ** 32 + 64), (2 ** 64 + 4, 2, 64)):
+        with pytest.raises((ValueError, rp.RollpackError)):
+            rp.KvqCache(*args, device="cpu")
+        with pytest.raises((ValueError, rp.RollpackError)):
+            rp.rp_kvq_cache_bytes(*args)
