@@ -542,6 +542,18 @@ def model_config(shape, kv4: bool = False) -> RpModelConfig:
                          RP_DTYPE_BF16_KV4 if kv4 else RP_DTYPE_BF16 if shape.dtype == "bf16" else RP_DTYPE_F32)
 
 
+def _engine_stream(dev, stream):
+    """The engine's stream: torch's current one, or `stream`, behind what is queued on the current one (the weights'
+    last writes)."""
+    import torch
+    cur = torch.cuda.current_stream(dev)
+    if stream is None:
+        return cur
+    if stream != cur:
+        stream.wait_stream(cur)
+    return stream
+
+
 class Engine:
     """An engine over torch-allocated workspaces on the current CUDA (HIP) device.
 
@@ -551,6 +563,8 @@ class Engine:
     pack_weights: for a bf16 model, also allocate the packed copy of the
     weights that the decode GEMMs stream (rp_engine_set_packed_weights).
     kv4: for a bf16 model, keep the KV cache in 4 bits (RP_DTYPE_BF16_KV4).
+    stream: the engine's (torch's current one by default).  Device outputs are ready on the stream that is
+    current when they are returned.
     """
 
     def __init__(self, shape, weights: dict, max_seqs: int, max_prefill_tokens: int, max_context: int,
@@ -562,18 +576,20 @@ class Engine:
         self.limits = RpEngineLimits(max_seqs, max_prefill_tokens, max_context, 64, kv_pages)
         kv_bytes, sc_bytes = rp_workspace_size(self.cfg, self.limits)
         dev = weights["embed"].device
-        self.kv = torch.empty(kv_bytes, dtype=torch.uint8, device=dev)
-        self.scratch = torch.empty(sc_bytes, dtype=torch.uint8, device=dev)
+        self.stream = _engine_stream(dev, stream)
+        with torch.cuda.stream(self.stream):
+            self.kv = torch.empty(kv_bytes, dtype=torch.uint8, device=dev)
+            self.scratch = torch.empty(sc_bytes, dtype=torch.uint8, device=dev)
         self.weights = weights
         self._w, self._layers = weights_struct(shape, weights)
-        self.stream = stream if stream is not None else torch.cuda.current_stream(dev)
         self.handle = rp_engine_create(self.cfg, self._w, self.limits, self.kv.data_ptr(), kv_bytes,
                                        self.scratch.data_ptr(), sc_bytes, self.stream.cuda_stream)
         self.max_seqs = max_seqs
         self.packed = None
         if pack_weights and shape.dtype == "bf16":
             nbytes = rp_packed_weights_bytes(self.cfg)
-            self.packed = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+            with torch.cuda.stream(self.stream):
+                self.packed = torch.empty(nbytes, dtype=torch.uint8, device=dev)
             rp_engine_set_packed_weights(self.handle, self.packed.data_ptr(), nbytes)
 
     def close(self):
@@ -587,22 +603,37 @@ class Engine:
         except Exception:
             pass
 
+    def _empty(self, shape, dtype):
+        """A device output, in memory of the engine's stream, which writes it."""
+        with self.torch.cuda.stream(self.stream):
+            return self.torch.empty(shape, dtype=dtype, device=self.kv.device)
+
+    def _hand_over(self, *outs):
+        """Outputs that the engine's stream has been given to write, to the caller's stream."""
+        cur = self.torch.cuda.current_stream(self.kv.device)
+        if cur != self.stream:
+            cur.wait_stream(self.stream)
+            for t in outs:
+                t.record_stream(cur)
+
     def prefill(self, seq_ids, prompt_tokens, prompt_offsets, max_new_tokens, seed=0, temperature=0.0,
                 logits: bool = False, first_tokens: bool = False):
-        torch = self.torch
         out = None
         if logits:
-            out = torch.empty((len(seq_ids), self.shape.vocab), dtype=torch.float32, device=self.kv.device)
+            out = self._empty((len(seq_ids), self.shape.vocab), self.torch.float32)
         first = rp_prefill(self.handle, seq_ids, prompt_tokens, prompt_offsets, max_new_tokens, seed, temperature,
                            None if out is None else out.data_ptr(), first_tokens)
+        if out is not None:
+            self._hand_over(out)
         return out, first
 
     def decode_step(self, forced_tokens=None, logits: bool = False):
-        torch = self.torch
         out = None
         if logits:
-            out = torch.empty((self.max_seqs, self.shape.vocab), dtype=torch.float32, device=self.kv.device)
+            out = self._empty((self.max_seqs, self.shape.vocab), self.torch.float32)
         n, rows = rp_decode_step(self.handle, forced_tokens, None if out is None else out.data_ptr(), self.max_seqs)
+        if out is not None:
+            self._hand_over(out)
         return n, rows, (None if out is None else out[:n])
 
     def free_finished(self):
@@ -619,9 +650,9 @@ class Engine:
 
     def read_kv(self, seq_id: int, layer: int, first: int, n: int):
         """(K, V) [n, n_kv, head_dim] bf16 that a 4-bit cache holds of a live sequence's positions."""
-        torch = self.torch
-        k, v = (torch.empty((n, self.shape.n_kv, self.shape.head_dim), dtype=torch.bfloat16, device=self.kv.device) for _ in range(2))
+        k, v = (self._empty((n, self.shape.n_kv, self.shape.head_dim), self.torch.bfloat16) for _ in range(2))
         rp_read_kv(self.handle, seq_id, layer, first, n, k.data_ptr(), v.data_ptr())
+        self._hand_over(k, v)
         return k, v
 
     def set_eos(self, eos_token: int):
@@ -811,10 +842,11 @@ def generate(shape, weights: dict, seq_ids, prompt_tokens, prompt_offsets, max_n
     cfg = model_config(shape, kv4)
     kv_bytes, sc_bytes = rp_workspace_size(cfg, limits)
     dev = weights["embed"].device
-    kv = torch.empty(kv_bytes, dtype=torch.uint8, device=dev)
-    scratch = torch.empty(sc_bytes, dtype=torch.uint8, device=dev)
+    stream = _engine_stream(dev, stream)
+    with torch.cuda.stream(stream):
+        kv = torch.empty(kv_bytes, dtype=torch.uint8, device=dev)
+        scratch = torch.empty(sc_bytes, dtype=torch.uint8, device=dev)
     w, layers = weights_struct(shape, weights)
-    stream = stream if stream is not None else torch.cuda.current_stream(dev)
     return rp_generate(cfg, w, limits, kv.data_ptr(), kv_bytes, scratch.data_ptr(), sc_bytes, stream.cuda_stream,
                        seq_ids, prompt_tokens, prompt_offsets, max_new_tokens, seed, temperature, schedule_mode,
                        round_ids, tail)
