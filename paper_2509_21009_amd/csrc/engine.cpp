@@ -981,7 +981,10 @@ void Engine::read_kv(int64_t id, int32_t layer, int32_t first, int32_t n, void* 
   if (!kv4_) throw RpError(RP_ERR_BAD_STATE, "read_kv: the engine's cache is not in 4 bits");
   if (layer < 0 || layer >= cfg_.n_layers || first < 0 || n < 0) throw RpError(RP_ERR_INVALID_ARG, "read_kv: layer or range out of bounds");
   const auto it = id2slot_.find(id);
-  if (it == id2slot_.end()) throw RpError(RP_ERR_UNKNOWN_ID, "read_kv: sequence " + std::to_string(id) + " is not live");
+  if (it == id2slot_.end()) {
+    if (find_waiting(id)) throw RpError(RP_ERR_BAD_STATE, "read_kv: sequence " + std::to_string(id) + " was preempted and holds no pages");
+    throw RpError(RP_ERR_UNKNOWN_ID, "read_kv: sequence " + std::to_string(id) + " is not live");
+  }
   const Seq& q = slots_[it->second];
   const int64_t held = static_cast<int64_t>(q.prompt_len) + q.n_gen - 1;  // the newest token has not been fed yet
   if (static_cast<int64_t>(first) + n > held) throw RpError(RP_ERR_INVALID_ARG, "read_kv: the cache holds " + std::to_string(held) + " positions");
