@@ -248,7 +248,7 @@ rp_status rp_get_logprobs(rp_engine* eng, int64_t seq_id, float* out, int32_t ca
  * RoPE, with the bias, as attention reads them.  RP_DTYPE_BF16_KV4 engines only
  * (RP_ERR_BAD_STATE otherwise, and for a preempted sequence, which holds no pages).  The KV footprint of a request (section 4.4) is what a migration
  * moves or, as in section 5, recomputes.
- *   k_out, v_out   DEVICE [n, n_kv_heads, head_dim] bf16, ready in stream order */
+ *   k_out, v_out   DEVICE [n, n_kv_heads, head_dim] bf16 that do not overlap, ready in stream order */
 rp_status rp_read_kv(rp_engine* eng, int64_t seq_id, int32_t layer, int32_t first, int32_t n, void* k_out, void* v_out);
 
 /* End-of-sequence token (-1, the default: none); response lengths are what

@@ -990,7 +990,9 @@ void Engine::read_kv(int64_t id, int32_t layer, int32_t first, int32_t n, void* 
   if (static_cast<int64_t>(first) + n > held) throw RpError(RP_ERR_INVALID_ARG, "read_kv: the cache holds " + std::to_string(held) + " positions");
   if (n == 0) return;
   const uintptr_t a = reinterpret_cast<uintptr_t>(k_out), b = reinterpret_cast<uintptr_t>(v_out);
-  if (!k_out || !v_out || k_out == v_out || (a | b) & 1) throw RpError(RP_ERR_INVALID_ARG, "read_kv: bad output");
+  const uintptr_t bytes = static_cast<uintptr_t>(n) * cfg_.n_kv_heads * cfg_.head_dim * 2;
+  if (!k_out || !v_out || (a | b) & 1) throw RpError(RP_ERR_INVALID_ARG, "read_kv: null or misaligned output");
+  if (a < b + bytes && b < a + bytes) throw RpError(RP_ERR_INVALID_ARG, "read_kv: the outputs overlap");
   int32_t* m = stage_meta(4);
   m[0] = 0;
   m[1] = n;

@@ -41,3 +41,20 @@ def test_a_preempted_sequence_holds_no_cache():
         eng.read_kv(7, 0, 0, 1)
     assert e.value.status == 4
     eng.close()
+
+
+def test_overlapping_outputs_are_refused():
+    """Each element would hold either's value."""
+    R, eng = _engine([60], 4, 1)
+    row = 2 * 64 * 2  # bytes of a position
+    buf = torch.full((40 * row // 2,), 7.0, dtype=torch.bfloat16, device=DEV)
+    at = buf.data_ptr()
+    for k, v in ((at, at), (at, at + 19 * row), (at + 19 * row, at), (at, at + 2)):
+        with pytest.raises(R.RollpackError) as e:
+            R.rp_read_kv(eng.handle, 5, 0, 0, 20, k, v)
+        assert e.value.status == 1
+    assert (buf == 7).all()
+    R.rp_read_kv(eng.handle, 5, 0, 0, 20, at + 20 * row, at)  # side by side
+    k, v = eng.read_kv(5, 0, 0, 20)
+    assert torch.equal(buf.view(2, 20, 2, 64)[1], k) and torch.equal(buf.view(2, 20, 2, 64)[0], v)
+    eng.close()
