@@ -402,7 +402,7 @@ __device__ __forceinline__ int find_tile(const KvqBatch& bt, int group, const Kv
 __device__ __forceinline__ int find_longest(const KvqBatch& bt, int group, const KvqCut& cut, int index, int& tile, KvqSeq& sq) {
   if (!cut.longest || bt.n_seqs == 1 || bt.n_seqs > 64) {
     const int b = find_tile(bt, group, cut, index, tile, sq);
-    tile = kvq_tiles(sq, group, cut) - 1 - tile;
+    if (b >= 0) tile = kvq_tiles(sq, group, cut) - 1 - tile;
     return b;
   }
   const int lane = threadIdx.x & 63;
