@@ -171,3 +171,36 @@ def test_read_kv_refusals():
         R.rp_read_kv(eng.handle, 5, 0, 0, 1, k, v)
     assert e.value.status == 5
     eng.close()
+
+
+def test_every_layer_holds_its_own_keys_and_values():
+    """What each layer's cache holds is the oracle's own K and V of that layer, over the same held cache: within the quantiser's
+    step for a block whose largest element, and each element, may be off by the bf16 forward's error.  Another layer's is not."""
+    shape = ModelShape("three", 3, 384, 6, 2, 64, 640, 1152, False, "bf16")
+    wd = make_weights(shape, seed=4, device=DEV)
+    w64 = weights_to_numpy(wd)
+    plens, n_new = [70, 129, 5], 4
+    prompts, toks, offs, rng = _prompts(shape, plens, 9)
+    ids = np.arange(3, dtype=np.int64)
+    eng = _engine(shape, wd, plens, n_new, max_prefill=96)  # the second prompt in two pieces
+    forced = rng.integers(0, shape.vocab, size=(3, n_new)).astype(np.int32)
+    eng.prefill(ids, toks, offs, np.full(3, n_new, np.int32), 11, 1.0)
+    for j in range(n_new - 1):
+        eng.decode_step(forced_tokens=forced[:, j])
+
+    def within(own, held):
+        noise = 2e-2 * np.abs(own).max(axis=(1, 2), keepdims=True)
+        top = np.abs(own.reshape(*own.shape[:2], -1, 32)).max(-1) + noise
+        step = 2.0 ** np.ceil(np.log2(np.maximum(top / 7, 2.0 ** -125)))
+        return np.abs(own - held) <= np.repeat(step, 32, -1) + noise
+
+    for i in range(3):
+        seq = np.concatenate([prompts[i], forced[i, :n_new - 1]])
+        cache = [tuple(t.double().cpu().numpy() for t in eng.read_kv(i, li, 0, len(seq))) for li in range(3)]
+        _, mine = okvq.forward_over_cache(w64, shape, seq, cache)
+        for a in range(3):
+            for b in range(3):
+                for own, held in zip(mine[a], cache[b]):
+                    ok = within(own, held)
+                    assert ok.all() if a == b else ok.mean() < 0.9, (i, a, b, float(ok.mean()))
+    eng.close()
