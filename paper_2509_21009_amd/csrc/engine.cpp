@@ -7,7 +7,9 @@
 // All device work is enqueued on one stream; per-step metadata is O(rows)
 // integers copied from pinned staging buffers.
 #include "engine.hpp"
+
 #include "decode_plan.hpp"
+#include "kvq_plan.hpp"
 #include "tail_batch.hpp"
 
 #include <algorithm>

@@ -202,12 +202,6 @@ inline int64_t kvq_tile_bound(const KvqBatch& b, int group, const KvqCut& cut) {
   const int64_t by_rows = static_cast<int64_t>(b.n_rows) * group / cut.cols + b.n_seqs, by_seqs = per_seq * b.n_seqs;
   return by_rows < by_seqs ? by_rows : by_seqs;
 }
-// Bytes of the workspace of launch_kvq_attend.
-size_t kvq_attend_bytes(const KvqCache& c, const KvqBatch& b, int n_q);
-// The most that any batch of up to these sequences, rows and contexts asks for.
-size_t kvq_attend_bytes_most(const KvqCache& c, int n_q, int64_t max_seqs, int64_t max_rows, int max_context);
-// Whether its launches are within a grid's limits.
-bool kvq_attend_fits(const KvqCache& c, const KvqBatch& b, int n_q);
 
 #ifdef __HIPCC__
 hipError_t launch_kvq_append(const KvqCache& c, const KvqBatch& b, const KvqTensor& k, const KvqTensor& v, hipStream_t s);

@@ -9,6 +9,7 @@
 
 #include "engine.hpp"
 #include "kvq.hpp"
+#include "kvq_plan.hpp"
 #include "static_ws.hpp"
 #include "tail_batch.hpp"
 
