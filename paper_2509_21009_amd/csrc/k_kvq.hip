@@ -517,15 +517,20 @@ struct Query {
 // formed at all: its sum tells.  l is the lane's part of the sum; the lanes of a column add theirs at the end.
 //   In fp16 (HALF) the largest probability of a page that moves m is 2^7, and none passes 2^15: from 2^-14 on, 2^-21 of that
 // largest one, each is rounded once, to 2^-11 of itself.  Smaller ones fp16 would hold with fewer bits or not at all, to 2^-25,
-// and a row whose largest weights meet values of zero is made of them.  So where that could count, small_page takes them as a
-// second operand, 2^29 times as large and normal down to 2^-43: in pages of which a lane's sum is below 2^-9, as 2^-25 for
-// each of its N keys is less than 2^-11 of more, and in pages that move m, whose sum may be one key's.  With every page looked at
-// a prompt of 14,500 tokens took 2,130 us (1,405 so, 1,393 with none): among the columns of a wave one has a weight below
-// 2^-21 in up to half of the pages.
+// and a row whose largest weights meet values of zero is made of them.  So
+// - m also moves down, where a page's largest is below 2^-9 (2^kDrop below): the sums are in fp32 and hold 2^kDropMost more, and
+//   pages of small weights, as behind one strong key, come to lie like any other;
+// - in pages that have just moved m, or of which a lane's sum is below kSumLeast, small_page takes those below 2^-14 as a
+//   second operand, 2^29 times as large and normal down to 2^-43.  Elsewhere 2^-25 for each of the lane's N keys is
+//   less than 2^-11 of their sum.
+// Without all this | with it: a prompt of 14,500 tokens 1,400 | 1,421 us, 64 of 512 tokens with 64 dims 94 | 100 (every fifth page
+// is a first one, whose look for small ones takes most of that), decoding 23.3 | 23.6. Every key 15 nats below the first: 1,372 |
+// 1,395, with small_page in the place of moves down 2,550; with every page looked through for small ones 2,130 for any keys.
 struct Softmax {
   float m = -INFINITY, l = 0.f;
+  float high = -INFINITY;  // the highest m
 };
-constexpr float kLift = 7.f;
+constexpr float kLift = 7.f, kDrop = 16.f, kDropMost = 40.f;
 constexpr float kSmallBelow = 0x1p-14f;
 constexpr float kSumLeast = 0x1p-9f;
 template <bool HALF> constexpr float kSumMost = HALF ? 0x1p15f : 0x1p8f;
@@ -573,7 +578,12 @@ __device__ __forceinline__ void softmax_page(Softmax& st, float (&x)[N], uint32_
 #pragma unroll
     for (int k = 0; k < N; ++k) top = fmaxf(top, s[k]);
     ((top = fmaxf(top, __shfl_xor(top, across, 64))), ...);
-    const float m_new = fmaxf(st.m, HALF ? __builtin_fmaf(top, scale_log2, -kLift) : top * scale_log2);
+    float m_new = fmaxf(st.m, top * scale_log2);
+    if constexpr (HALF) {
+      m_new = __builtin_fmaf(top, scale_log2, -kLift);
+      if (!(m_new > st.m)) m_new = m_new < st.m - kDrop && top > -INFINITY ? fmaxf(m_new, st.high - kDropMost) : st.m;
+      st.high = fmaxf(st.high, m_new);
+    }
     const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m - m_new);
     st.m = m_new;
     st.l *= alpha;
@@ -597,12 +607,17 @@ __device__ __forceinline__ void softmax_page(Softmax& st, float (&x)[N], uint32_
   if (none) move();
   form();
   if constexpr (HALF) {
-    if (none || __any(sum < kSumLeast || sum > kSumMost<HALF>)) {
-      if (__any(sum > kSumMost<HALF>)) {
+    bool out = __any(sum < kSumLeast || sum > kSumMost<HALF>);
+    if (__builtin_expect(none || out, 0)) {  // out of line: a prompt of 8,192 tokens with 64 dims 197 | 189 us
+      float top = 0.f;
+#pragma unroll
+      for (int k = 0; k < N; ++k) top = fmaxf(top, x[k]);
+      out = __any((sum < kSumLeast && top > 0.f) || sum > kSumMost<HALF>);  // not for lanes whose keys are all out of sight
+      if (out) {
         move();
         form();
       }
-      sum = small_page(x, w, sum, rescale, products);
+      if (none || out) sum = small_page(x, w, sum, rescale, products);
     }
   } else if (__any(sum > kSumMost<HALF>)) {
     move();

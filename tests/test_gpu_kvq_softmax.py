@@ -96,6 +96,7 @@ STEPS = {
     "steep": lambda page: np.minimum(32, 5 * page),   # ~14 bits a page
     "slow": lambda page: np.minimum(32, page),        # ~3
     "down": lambda page: np.maximum(0, 32 - 5 * page),
+    "spikes": lambda page: np.where(page % 3 == 2, 32, 0),
     "mixed": lambda page: (page * 2654435761 >> 7) % 33,
 }
 
