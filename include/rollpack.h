@@ -246,8 +246,9 @@ rp_status rp_get_logprobs(rp_engine* eng, int64_t seq_id, float* out, int32_t ca
 /* K and V that the cache of a live sequence holds in one layer, for its
  * positions first .. first + n - 1 (which its prompt and the tokens fed so far cover): after
  * RoPE, with the bias, as attention reads them.  RP_DTYPE_BF16_KV4 engines only
- * (RP_ERR_BAD_STATE otherwise, and for a preempted sequence, which holds no pages).  The KV footprint of a request (section 4.4) is what a migration
- * moves or, as in section 5, recomputes.
+ * (RP_ERR_BAD_STATE otherwise, and for a preempted sequence, which holds no pages).  For
+ * looking at what the KV footprint of a request (section 4.4) holds: no call gives an engine a
+ * sequence's K and V, which it recomputes, as section 5's migration does.
  *   k_out, v_out   DEVICE [n, n_kv_heads, head_dim] bf16 that do not overlap, ready in stream order */
 rp_status rp_read_kv(rp_engine* eng, int64_t seq_id, int32_t layer, int32_t first, int32_t n, void* k_out, void* v_out);
 
@@ -634,9 +635,10 @@ rp_status rp_kvq_cache_bytes(int64_t n_pages, int32_t n_kv_heads, int32_t head_d
 rp_status rp_kvq_append(const rp_kvq_cache* cache, const rp_kvq_batch* batch, const rp_kvq_tensor* k,
                         const rp_kvq_tensor* v, void* hip_stream);
 
-/* The values that the cache holds of the batch's rows, into k and v (as
- * rp_kvq_append; fp32 and bf16 both hold every value exactly): what a request takes along
- * when it moves to another replica (the migration of section 5 recomputes it instead). */
+/* The values that the cache holds of the batch's rows, into k and v, which may not
+ * overlap (as rp_kvq_append; fp32 and bf16 both hold every value exactly, and appended they are
+ * held again): what a request takes along when it moves to another cache (the migration of
+ * section 5 recomputes it instead). */
 rp_status rp_kvq_read(const rp_kvq_cache* cache, const rp_kvq_batch* batch, const rp_kvq_tensor* k,
                       const rp_kvq_tensor* v, void* hip_stream);
 

@@ -728,9 +728,9 @@ __device__ __forceinline__ void nan_values(PageV<HD>& pg, const char* block, int
 // rounding to bf16, 2^-8, where P in bf16 would add as much again.  Pages with values that fp16 does not hold, and fp32, take
 // bf16: P in two pieces, or three.
 //   HBM bounds decoding of many keys: one token each of 64 sequences of 600 to 4,500 (7B layer, 163,000 keys) 23 us, 3.9 TB/s;
-// of 330 of 130 to 1,300 38 us, 4.6; of 96 of 32B's layer, 442,000 keys, 95 us, 5.1, what a copy reaches.  Below that it is
+// of 330 of 200 to 1,700 38.5 us, 4.6; of 96 of 32B's layer, 442,000 keys, 96 us, 5.1, what a copy reaches.  Below that it is
 // the way to the first page (context, table, page: reads that wait for each other), the launch and the join: 12,000 keys of one
-// sequence 6.6 us and 4.1 for the join.
+// sequence 6.6 us and 4.2 for the join.
 template <int HD, bool F32, int NW>
 __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendArgs a, KvqCut cut) {
   constexpr int NT = HD / 16, OLD = HD + 4;
@@ -910,10 +910,10 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend(KvqAttendAr
 // of i are the operand P^T of a 16-token step of O^T += V^T P^T; V's rows keep the cache's order of tokens, so that
 // nothing moves between lanes.  V's row c + 16 i of tile t is dimension hd/16 c + 2 t + i: the two that one byte holds.
 //   Bound by MFMA and the vector ALU together: of a long prompt's SIMD cycles the one takes about 40%, the other (unpacking,
-// softmax) 45 to 50, hardly at the same time though two blocks (waves of eight) share a compute unit; products and softmax of
-// neighbouring pages interleaved in one wave took more registers than that hid.  One prompt of 14,500 tokens (7B layer)
-// 1,400 us, 1,070 TFLOP/s, with blocks of eight waves; 20 of 128 to 1,024 tokens 110 us, 520, where the way to a block's
-// first page and the first unpacking, ~7 us, are as long as its five pages.
+// softmax) 45 to 50, hardly at the same time though a SIMD has two waves (of two blocks of four waves, or of one of eight: 240
+// registers); products and softmax of neighbouring pages interleaved in one wave took more registers than that hid.  One prompt
+// of 14,500 tokens (7B layer) 1,420 to 1,510 us from card to card, 1,000 to 1,060 TFLOP/s, with blocks of eight waves; 20 of 128 to
+// 1,024 tokens 114 us, 510, where the way to a block's first page and the first unpacking, ~7 us, are as long as its five pages.
 
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
 

@@ -64,8 +64,8 @@ inline AttendPlan attend_plan(const KvqCache& c, const KvqBatch& b, int n_q, boo
   const int64_t blocks = std::max<int64_t>(1, p.walk_tiles * c.n_kv);
   p.walk.least = 4;
   // Few blocks of more than 16 pages are split into as many as run at once: one of eight waves to a compute unit where that
-  // comes out nearly even, else three of four waves (two in fp32, whose waves have more registers).  7 query heads to each of 4 KV
-  // heads, items of eight waves | of four: 16 tokens of 2,000 to 14,000 keys (64 blocks) 23.5 (4) | 24.5 (12), with 6 of eight
+  // comes out nearly even, else three of four waves, two in fp32: what 128 dims' registers allow (154 and 188; at 64 dims, 111 and
+  // 124, four would fit).  7 query heads to each of 4 KV heads, items of eight waves | of four: 16 tokens of 2,000 to 14,000 keys (64 blocks) 23.5 (4) | 24.5 (12), with 6 of eight
   // waves 31; 32 of 1,000 to 14,000 36 (2) | 35 (6); 48 of 1,000 to 9,000 (192 blocks) 38 (1) | 32 (4); 64 of 4,000 25 (1) | 31 (3).
   const bool few = blocks <= 256, even = few && 256 / blocks * blocks >= 224;
   if (few && pages > 16) p.walk.items = static_cast<int>(std::min<int64_t>(kvq_items(pages, kKvqTileItems, p.walk.least), (even ? 256 : bf16 ? 768 : 512) / blocks));

@@ -133,3 +133,14 @@ def test_large_scores_have_the_right_values(kind):
         s = Setup(7, 1, 128, [700, 65, 1], rows=[30 if kind else 3, 65, 1], dtype=dtype, seed=45, gain=6.0, room=_room(kind, 7, 128)).fill()
         s.q *= 4
         _check(s, s.cache.attend(s.batch(), s.q))
+
+
+@pytest.mark.parametrize("form", ["four", "joined-64", "prompt-tiles", "prompt-eight"])
+def test_values_near_the_end_of_the_range(form):
+    """Sums stay finite while the largest value times the context is below 2^119 (include/rollpack.h)."""
+    for dtype in _types(form):
+        s = _setup(form, dtype, 46)
+        s.v *= 2.0 ** (118 - 13 - 3)  # contexts below 2^13, values below 2^3
+        s.q *= 0.25
+        s.fill()
+        _check(s, s.cache.attend(s.batch(), s.q))
