@@ -655,7 +655,8 @@ rp_status rp_kvq_attend_workspace(const rp_kvq_cache* cache, const rp_kvq_batch*
  * G = n_q_heads / n_kv_heads.  The rows' own keys must be in the cache (rp_kvq_append
  * before this call on the same stream).  Scores, exponentials and sums are fp32.  A weight is
  * rounded once for its product with v: to 24 bits in fp32 calls, to 11 in bf16 ones, where weights below
- * 2^-21 of a row's largest may be off by 2^-11 of what the 32 keys around them weigh together.
+ * 2^-21 of a row's largest may be off by 2^-11 of what the 32 keys around them weigh together, and those
+ * below 2^-50 of it may count nothing.
  * The division by the sum comes last: the sums are finite while the largest |v| times the context
  * is below 2^119.
  *   n_q_heads  a multiple of n_kv_heads

@@ -521,8 +521,8 @@ struct Query {
 // - m also moves down, where a page's largest is below 2^-9 (2^kDrop below): the sums are in fp32 and hold 2^kDropMost more, and
 //   pages of small weights, as behind one strong key, come to lie like any other;
 // - in pages that have just moved m, or of which a lane's sum is below kSumLeast, small_page takes those below 2^-14 as a
-//   second operand, 2^29 times as large and normal down to 2^-43.  Elsewhere 2^-25 for each of the lane's N keys is
-//   less than 2^-11 of their sum.
+//   second operand, 2^29 times as large and normal down to 2^-43, 2^-50 of the largest.  Elsewhere 2^-25 for each of the
+//   lane's N keys is less than 2^-11 of their sum.
 // Without all this | with it: a prompt of 14,500 tokens 1,400 | 1,421 us, 64 of 512 tokens with 64 dims 94 | 100 (every fifth page
 // is a first one, whose look for small ones takes most of that), decoding 23.3 | 23.6. Every key 15 nats below the first: 1,372 |
 // 1,395, with small_page in the place of moves down 2,550; with every page looked through for small ones 2,130 for any keys.
