@@ -83,6 +83,32 @@ def test_weights_far_below_the_largest(form):
             _check(s, s.cache.attend(s.batch(), s.q))
 
 
+@pytest.mark.parametrize("form", ["four", "four-64", "prompt-tiles", "prompt-split-64", "prompt-eight"])
+def test_strong_keys_everywhere(form):
+    """Strong keys with a value of zero in all pages: the weights beside them are off by 2^-11 of what the keys around them weigh
+    together at most (include/rollpack.h), times the largest of their values."""
+    for nats in (12.0, 18.0, 27.0):
+        s = _setup(form, "bf16", 47)
+        pos = np.concatenate([np.arange(c) for c in s.ctx])
+        s.v[torch.from_numpy(pos % 11 == 3).to(DEV)] = 0
+        _aim(s, [np.where(np.arange(c) % 11 == 3, 32, 0) for c in s.ctx], nats).fill()
+        out, q, at, g = _f64(s.cache.attend(s.batch(), s.q)), _f64(s.q), 0, s.n_q // s.n_kv
+        for b, (c, n) in enumerate(zip(s.ctx, s.rows)):
+            k, v = s.held()[b]
+            ref, mag, top = okvq.attend(q[at:at + n], k, v, np.arange(c - n, c), s.hd ** -0.5)
+            bar = _bar(ref, mag, top, c, s.hd, "bf16", np.abs(v).max())
+            for h in range(s.n_q):
+                z = np.where(np.arange(c)[None] <= np.arange(c - n, c)[:, None], q[at:at + n, h] @ k[:, h // g].T * s.hd ** -0.5, -np.inf)
+                p = np.exp(z - z.max(1, keepdims=True))
+                p /= p.sum(1, keepdims=True)
+                pad = -(-c // 64) * 64 - c
+                around = np.pad(p, ((0, 0), (0, pad))).reshape(n, -1, 64).sum(-1)                         # of a page
+                most = np.pad(np.abs(v[:, h // g]), ((0, pad), (0, 0))).reshape(-1, 64, s.hd).max(1)
+                bar[:, h] += 2.0 ** -11 * around @ most
+            assert (np.abs(out[at:at + n] - ref) <= bar).all(), (b, c, n, nats)
+            at += n
+
+
 def test_many_keys_beside_a_dominant_one():
     """A tenth of a percent of the weight in 40,000 keys of a wave, each about 2^-25 of the first, whose value is zero."""
     s = Setup(2, 1, 64, [40000] + [1] * 257, seed=42)
