@@ -668,6 +668,118 @@ rp_status rp_kvq_attend(const rp_kvq_cache* cache, const rp_kvq_batch* batch, in
                         const rp_kvq_tensor* q, const rp_kvq_tensor* out, void* workspace, size_t workspace_bytes,
                         void* hip_stream);
 
+/* ---- The 4-bit cache's pages: handed out, and picked for each query ----------------
+ *
+ * Long responses are few and read long contexts (section 2.2), of which a query needs
+ * few keys.  These calls let a step touch only the pages that it picks:
+ *   rp_kvq_fit_pages    pages and slots of the new tokens, from the lengths alone
+ *   rp_kvq_append       (above) K and V into them
+ *   rp_kvq_key_ranges   the ranges of the keys of the pages that they went to
+ *   rp_kvq_page_scores  a bound of every page's scores for each query
+ *   rp_kvq_pick_pages   the pages to attend to
+ *   rp_kvq_attend_picked  attention over them
+ * all on the GPU, with nothing for the host to wait for. */
+
+/* A pool of pages and what its sequences hold, in caller-owned device memory that the
+ * calls keep up to date; one call at a time.  Before the first call the caller writes
+ * free_pages (every page once, in any order: the last ones are taken first), zeros to
+ * contexts, and {n_pages, 0, 0, 0} to state.
+ *   page_table   [n_seqs] rows of table_stride entries, as an rp_kvq_batch has it; entries past a
+ *                sequence's pages are left as they are
+ *   contexts     [n_seqs] tokens of each sequence
+ *   free_pages   [n_pages] the free ones are the first state[0]
+ *   state        [4]: free pages; the last call's error (0, or below), its rows, and how many
+ *                pages it was short of
+ *   workspace    [n_seqs + 1], the calls' own
+ *   n_seqs       0 .. 2^20
+ *   n_pages      1 .. 2^24
+ *   max_context  most tokens of a sequence, 0 .. 2^30; at most 64 * table_stride */
+typedef struct rp_kvq_pool {
+  int32_t* page_table;
+  int64_t table_stride;
+  int32_t* contexts;
+  int32_t* free_pages;
+  int32_t* state;
+  int32_t* workspace;
+  int32_t n_seqs;
+  int32_t max_context;
+  int64_t n_pages;
+} rp_kvq_pool;
+
+/* Give each sequence the pages that its new length needs, and take back those that it
+ * does not (the KV pages of a rollout step: requests are admitted, grow, finish, are
+ * aborted or preempted, section 4.2 and section 5).  lengths [n_seqs] are the tokens
+ * that each sequence then has: more than its context (new tokens: rows of the batch that
+ * rp_kvq_append and the others take), fewer (0: it is gone), or as many.
+ *   Counted over the sequences in order, and the pages of each in order: of R pages given
+ * back the j-th (from 0) becomes entry n + R - 1 - j of free_pages, n being state[0], and the k-th needed
+ * page is entry n + R - 1 - k.  So a call and one that takes it back leave the pool as it was.
+ *   row_offsets  out [n_seqs + 1]: sequence b's new tokens are rows off[b] .. off[b + 1] - 1
+ *   positions    out [n_rows]: of each row, -1 behind the last
+ *   slots        out [n_rows]: 64 * page + position mod 64, -1 behind the last
+ *   n_rows       0 .. 2^24, the most new tokens of all sequences (a padded batch)
+ * An error that only the device can see goes to state[1]; the call then changes nothing else of
+ * the pool and has no rows: 1 too few free pages (state[3]: how many are missing), 2 a length
+ * outside 0 .. max_context, 3 more than n_rows new tokens, 4 a state that no calls have made.
+ * Returned errors: RP_ERR_INVALID_ARG, RP_ERR_HIP. */
+rp_status rp_kvq_fit_pages(const rp_kvq_pool* pool, const int32_t* lengths, int32_t n_rows, int32_t* row_offsets,
+                           int32_t* positions, int32_t* slots, void* hip_stream);
+
+/* The ranges of the pages that the batch's rows are in, after rp_kvq_append of these rows:
+ * for each KV head and dimension the smallest and the largest of the keys that the cache
+ * holds at positions below the sequence's context (what bounds the reads of section 2.2's memory-bound
+ * decode steps).  Exact.  A dimension with a NaN key has NaN for both.
+ *   ranges  device [n_pages, n_kv_heads, 2, head_dim] bf16, smallest first, 16-byte aligned;
+ *           other pages' are left as they are
+ * Where no key is appended (rp_kvq_batch) no range is written.  No two sequences may have the same
+ * page where rows are.  Errors: RP_ERR_INVALID_ARG, RP_ERR_HIP. */
+rp_status rp_kvq_key_ranges(const rp_kvq_cache* cache, const rp_kvq_batch* batch, void* ranges, void* hip_stream);
+
+/* For each row, KV head and page a score that no key of the page exceeds for any of the KV
+ * head's query heads (a decode step's cheap look at a long context, section 2.2):
+ *   score = max_h sum_d max(q[h, d], 0) largest[d] + min(q[h, d], 0) smallest[d],
+ * over the G = n_q_heads / n_kv_heads heads, in fp32, and minus infinity for pages past the one of
+ * the row's position.  A NaN among them makes it NaN, as does a page id outside the cache; all
+ * scores of a row are NaN where its sequence is out of the batch's bounds.
+ *   ranges     as rp_kvq_key_ranges has written them; the cache's blocks are not read
+ *   q          [n_rows, n_q_heads, head_dim]
+ *   scores     device [n_rows, n_kv_heads, n_columns] fp32; rows of no sequence are left as they are
+ *   n_columns  pages of max_context at least
+ * Errors: RP_ERR_INVALID_ARG, RP_ERR_HIP. */
+rp_status rp_kvq_page_scores(const rp_kvq_cache* cache, const rp_kvq_batch* batch, int32_t n_q_heads, const rp_kvq_tensor* q,
+                             const void* ranges, float* scores, int32_t n_columns, void* hip_stream);
+
+/* The pages that each row and KV head attends to in a decode step over a long context
+ * (section 2.2): all that the row sees if these are n_picks at most; else the first `first`, the
+ * last `last` (the one of the row's position among them), and of the others those of the highest scores, n_picks in
+ * all.  Equal scores: the lower page first (0 and -0 are equal); NaN is above every number.
+ *   scores  as rp_kvq_page_scores writes them, or any others
+ *   picks   device [n_rows, n_kv_heads, n_picks]: pages of the sequence (0: positions 0 .. 63),
+ *           ascending, then -1; rows of no sequence are left as they are, a row of a sequence out of
+ *           the batch's bounds and one before the first token has -1 alone
+ * 0 <= first, 0 <= last, first + last <= n_picks, 1 <= n_picks <= 2^24.  Of the batch the offsets, contexts and
+ * bounds are used.  Errors: RP_ERR_INVALID_ARG, RP_ERR_HIP. */
+rp_status rp_kvq_pick_pages(const rp_kvq_batch* batch, int32_t n_kv_heads, const float* scores, int32_t n_columns,
+                            int32_t first, int32_t last, int32_t n_picks, int32_t* picks, void* hip_stream);
+
+/* Bytes of the workspace of rp_kvq_attend_picked for this batch's n_rows and lists of n_picks pages (section
+ * 2.2: the lists of few rows are split over the whole GPU). */
+rp_status rp_kvq_attend_picked_workspace(const rp_kvq_cache* cache, const rp_kvq_batch* batch, int32_t n_q_heads,
+                                         int32_t n_picks, size_t* bytes);
+
+/* rp_kvq_attend over the tokens of picked pages alone (a decode step that reads n_picks pages of each
+ * long context, section 2.2): for row r at position p and query head h of KV head k
+ *   out[r, h] = sum_t softmax_t(scale q[r, h] . k[t]) v[t],  t <= p in the pages of picks[r, k].
+ * Entries that name no page that the row sees (-1, or past its position's) count nothing; a page that is
+ * listed twice counts twice; the order does not matter but for the rounding of sums.  A row whose list leaves no
+ * token gives zeros.  With all pages listed it is rp_kvq_attend's sum; precision, refusals, and what becomes of bad contexts and
+ * page ids are as there.
+ *   picks  device [n_rows, n_kv_heads, n_picks], n_picks 1 .. 2^24
+ * Errors: RP_ERR_INVALID_ARG, RP_ERR_HIP. */
+rp_status rp_kvq_attend_picked(const rp_kvq_cache* cache, const rp_kvq_batch* batch, int32_t n_q_heads, float scale,
+                               const rp_kvq_tensor* q, const int32_t* picks, int32_t n_picks, const rp_kvq_tensor* out,
+                               void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Message of the last failed call on this thread ("" if none). */
 const char* rp_last_error(void);
 

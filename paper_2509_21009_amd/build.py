@@ -27,8 +27,8 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
 DEVICE = [f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
           "-munsafe-fp-atomics"]
 
-SOURCES = ["k_gemm.hip", "k_attention.hip", "k_elementwise.hip", "k_kvq.hip", "static_ws.hip", "engine.cpp", "tail_batch.cpp",
-           "rollpack_abi.cpp"]
+SOURCES = ["k_gemm.hip", "k_attention.hip", "k_elementwise.hip", "k_kvq.hip", "k_kvq_pages.hip", "k_kvq_picked.hip",
+           "static_ws.hip", "engine.cpp", "tail_batch.cpp", "rollpack_abi.cpp"]
 
 
 def _compile(src: str) -> str:

@@ -1,0 +1,634 @@
+// Pages of the 4-bit KV cache (kvq_pages.hpp): handing them out, the ranges of their keys, their scores for a query, and the
+// pages that are picked by these.
+#include <algorithm>
+
+#include "kernels.hpp"
+#include "kvq_device.hpp"
+#include "kvq_pages.hpp"
+
+namespace rollpack {
+
+namespace {
+
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+
+// ---- pages handed out ------------------------------------------------------------------
+//
+// With have = ceil(context / 64) and want = ceil(length / 64) pages, a sequence gives back pages want .. have - 1 or needs pages
+// have .. want - 1.  Counted over the sequences in order and each one's pages in order, of R given back the j-th becomes
+// entry n_free + R - 1 - j of the list, and the k-th needed is entry n_free + R - 1 - k: a call and the one that takes it back are
+// each other's inverse, and what is given back is handed out again first.
+//   k_kvq_fit, one block: checks, sums over the sequences, offsets, contexts, pages given back.  Then the rows (in the
+// same launch where they are few): a row's page is new or in the table, and the first row of a new page enters it there.
+
+constexpr int kFitThreads = 1024;
+
+// Sums over the block's threads up to each thread (its own included), of three values; the totals in `total`.
+__device__ __forceinline__ void block_scan3(int (&x)[3], int (&total)[3], int (*lds)[3]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int kWaves = kFitThreads / 64;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    x[i] = wave_scan(x[i]);
+    if (lane == 63) lds[wave][i] = x[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const int s = wave_scan(lane < kWaves ? lds[lane][i] : 0);
+    total[i] = __builtin_amdgcn_readlane(s, 63);
+    const int before = __shfl(s, wave > 0 ? wave - 1 : 0, 64);
+    x[i] += wave > 0 ? before : 0;
+  }
+  __syncthreads();
+}
+
+// The last of 0 .. n - 1 whose start is not past j, of starts that do not descend.
+template <typename F>
+__device__ __forceinline__ int last_from(int lo, int n, int j, F start) {
+  int hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (start(mid) <= j) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+// Row r of a sequence: its position and slot, and the page's entry where it is the first of a new one.  top: entries of the
+// list with those given back, from whose end the needed pages are taken.
+__device__ __forceinline__ void fit_row(const KvqFitArgs& a, int r, int b, int off, int end, int first_need, int top) {
+  const int len = a.pool.context[b], first = len - (end - off), pos = first + (r - off);
+  const int page = pos / kKvqPage, have = kvq_pages(first);
+  int32_t* entry = a.pool.page_table + b * a.pool.table_stride + page;
+  int id;
+  if (page >= have) {
+    id = a.pool.free_pages[top - 1 - (first_need + page - have)];
+    if (pos % kKvqPage == 0) *entry = id;
+  } else {
+    id = *entry;
+  }
+  a.position[r] = pos;
+  a.slot[r] = id * kKvqPage + pos % kKvqPage;
+}
+
+__global__ __launch_bounds__(kFitThreads) void k_kvq_fit(KvqFitArgs a, int with_rows) {
+  __shared__ int scan[kFitThreads / 64][3];
+  __shared__ int64_t sums[kFitThreads / 64][3];
+  __shared__ int flags;
+  __shared__ int back_from[kFitThreads], want_of[kFitThreads];
+  const KvqPool& pool = a.pool;
+  const int tid = threadIdx.x, lane = tid & 63, n = pool.n_seqs;
+  const int n_free = pool.state[0];
+
+  // What all sequences need and give back, in 64 bits; anything out of bounds.
+  if (tid == 0) flags = 0;
+  __syncthreads();
+  int64_t all[3] = {0, 0, 0};  // needed, given back, rows
+  bool bad_len = false, bad_pool = n_free < 0 || n_free > pool.n_pages;
+  for (int b = tid; b < n; b += kFitThreads) {
+    const int old = pool.context[b], len = a.length[b];
+    const bool bl = len < 0 || len > pool.max_context, bp = old < 0 || old > pool.max_context;
+    bad_len |= bl;
+    bad_pool |= bp;
+    if (bl || bp) continue;
+    const int have = kvq_pages(old), want = kvq_pages(len);
+    all[0] += max(0, want - have);
+    all[1] += max(0, have - want);
+    all[2] += max(0, len - old);
+  }
+  if (bad_len) atomicOr(&flags, 1);
+  if (bad_pool) atomicOr(&flags, 2);
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) all[i] += __shfl_xor(static_cast<long long>(all[i]), m, 64);
+    if (lane == 0) sums[tid >> 6][i] = all[i];
+  }
+  __syncthreads();
+  int64_t need = 0, back = 0, rows = 0;
+  for (int w = 0; w < kFitThreads / 64; ++w) {
+    need += sums[w][0];
+    back += sums[w][1];
+    rows += sums[w][2];
+  }
+  const int64_t short_of = need - back - n_free;
+  const int error = (flags & 2) || n_free + back > pool.n_pages ? kFitPool : (flags & 1) ? kFitLength : short_of > 0 ? kFitPages
+                    : rows > a.n_rows ? kFitRows : kFitOk;
+  const bool failed = error != kFitOk;  // nothing changes: no rows
+  const int top = n_free + static_cast<int>(failed ? 0 : back);
+  int carry[3] = {0, 0, 0};
+  for (int b0 = 0; b0 < n; b0 += kFitThreads) {
+    const int b = b0 + tid, here = min(kFitThreads, n - b0);
+    int x[3] = {0, 0, 0}, total[3], len = 0, want = 0;
+    if (b < n && !failed) {
+      const int old = pool.context[b];
+      len = a.length[b];
+      const int have = kvq_pages(old);
+      want = kvq_pages(len);
+      x[0] = max(0, want - have);
+      x[1] = max(0, have - want);
+      x[2] = max(0, len - old);
+    }
+    const int mine[3] = {x[0], x[1], x[2]};
+    block_scan3(x, total, scan);
+    if (b < n) {
+      a.row_off[b] = carry[2] + x[2] - mine[2];
+      pool.first_need[b] = carry[0] + x[0] - mine[0];
+      if (!failed) pool.context[b] = len;
+    }
+    back_from[tid] = x[1] - mine[1];
+    want_of[tid] = want;
+    __syncthreads();
+    for (int j = tid; j < total[1]; j += kFitThreads) {
+      const int s = last_from(0, here, j, [&](int i) { return back_from[i]; });
+      pool.free_pages[top - 1 - (carry[1] + j)] = pool.page_table[(b0 + s) * pool.table_stride + want_of[s] + (j - back_from[s])];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 3; ++i) carry[i] += total[i];
+  }
+  if (tid == 0) {
+    a.row_off[n] = carry[2];
+    pool.first_need[n] = top;
+    pool.state[1] = error;
+    pool.state[2] = carry[2];
+    pool.state[3] = error == kFitPages ? static_cast<int>(min(short_of, int64_t{0x7fffffff})) : 0;
+    if (!failed) pool.state[0] = top - carry[0];
+  }
+  if (!with_rows) return;
+  __syncthreads();
+  for (int r = tid; r < a.n_rows; r += kFitThreads) {
+    if (r >= carry[2]) {
+      a.position[r] = a.slot[r] = -1;
+      continue;
+    }
+    const int b = last_from(0, n, r, [&](int i) { return a.row_off[i]; });
+    fit_row(a, r, b, a.row_off[b], a.row_off[b + 1], pool.first_need[b], top);
+  }
+}
+
+__global__ __launch_bounds__(256) void k_kvq_fit_rows(KvqFitArgs a) {
+  const int n = a.pool.n_seqs, r = blockIdx.x * 256 + threadIdx.x;
+  if (r >= a.n_rows) return;
+  if (r >= a.row_off[n]) {
+    a.position[r] = a.slot[r] = -1;
+    return;
+  }
+  const int b = last_from(0, n, r, [&](int i) { return a.row_off[i]; });
+  fit_row(a, r, b, a.row_off[b], a.row_off[b + 1], a.pool.first_need[b], a.pool.first_need[n]);
+}
+
+// ---- ranges ------------------------------------------------------------------------------
+
+// Order of bf16 bits as that of 16-bit integers, both halves; its own inverse.  -0 comes before 0.
+__device__ __forceinline__ s16x2 ordered(s16x2 x) { return x ^ ((x >> 15) & s16x2{0x7fff, 0x7fff}); }
+
+__device__ __forceinline__ s16x2 as_pair(uint32_t x) { return __builtin_bit_cast(s16x2, x); }
+
+template <int CTRL>
+__device__ __forceinline__ s16x2 from_lane(s16x2 x) {
+  return as_pair(static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true)));
+}
+
+// Half of the pairs of lo and hi go to the lane's partner (CTRL), half of its come back.
+template <int CTRL, int N>
+__device__ __forceinline__ void halve(s16x2 (&lo)[N], s16x2 (&hi)[N], bool upper) {
+#pragma unroll
+  for (int k = 0; k < N / 2; ++k) {
+    const s16x2 l = upper ? lo[k] : lo[k + N / 2], h = upper ? hi[k] : hi[k + N / 2];
+    lo[k] = __builtin_elementwise_min(upper ? lo[k + N / 2] : lo[k], from_lane<CTRL>(l));
+    hi[k] = __builtin_elementwise_max(upper ? hi[k + N / 2] : hi[k], from_lane<CTRL>(h));
+  }
+}
+template <int N>
+__device__ __forceinline__ void first_half(const s16x2 (&x)[N], s16x2 (&y)[N / 2]) {
+#pragma unroll
+  for (int k = 0; k < N / 2; ++k) y[k] = x[k];
+}
+
+__device__ __forceinline__ bool is_nan16(short x) { return (x & 0x7fff) > 0x7f80; }
+
+// A wave has `rows` consecutive rows of a KV head; for each page that one of them is the first of its sequence's rows in, it
+// reads the page's K whole: lane 16g + c has hd/4 dimensions of tokens c, 16 + c, 32 + c, 48 + c as packed bf16; lo and hi over
+// these, and then over the 16 lanes, which end with a pair of dimensions each.
+template <int HD>
+__global__ __launch_bounds__(256) void k_kvq_ranges(KvqCache c, KvqBatch bt, uint16_t* ranges, int rows) {
+  constexpr int NP = HD / 8;  // pairs of a lane
+  const int lane = threadIdx.x & 63, col = lane & 15;
+  const int wave = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = wave / c.n_kv, kh = wave - g * c.n_kv, base = g * rows;
+  if (base >= bt.n_rows) return;
+  const RowPlace place = lane < rows ? row_place(c, bt, base + lane) : RowPlace{};
+  uint64_t todo = __ballot(place.state == 1 && (place.t == 0 || place.i == 0));
+  while (todo) {
+    const int src = __ffsll(static_cast<unsigned long long>(todo)) - 1;
+    todo &= todo - 1;
+    const int page = __builtin_amdgcn_readlane(place.page, src);
+    const int held = __builtin_amdgcn_readlane(place.t + place.left, src);  // tokens of the page below the context, or more than 64
+    const size_t at = static_cast<size_t>(page) * c.n_kv + kh;
+    PageK<HD> pk;
+    pk.load(c.blocks + at * kvq_block_bytes(HD));
+    s16x2 lo[NP], hi[NP];
+#pragma unroll
+    for (int k = 0; k < NP; ++k) {
+      lo[k] = s16x2{0x7fff, 0x7fff};
+      hi[k] = s16x2{-0x8000, -0x8000};
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (16 * u + col < held) {
+        const float s = scale_of(pk.s, u);
+#pragma unroll
+        for (int j = 0; j < HD / 32; ++j) {
+          const uint32_t w = HD == 128 ? pk.k[u][j] : pk.k[u >> 1][2 * (u & 1) + j];
+          const uint32_t x[4] = {code_pair<0>(w, s), code_pair<1>(w, s), code_pair<2>(w, s), code_pair<3>(w, s)};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const s16x2 y = ordered(as_pair(x[i]));
+            lo[4 * j + i] = __builtin_elementwise_min(lo[4 * j + i], y);
+            hi[4 * j + i] = __builtin_elementwise_max(hi[4 * j + i], y);
+          }
+        }
+      }
+    }
+    halve<0x140>(lo, hi, col & 8);  // lane 15 - c of the 16
+    s16x2 l8[NP / 2], h8[NP / 2], l4[NP / 4], h4[NP / 4], l2[NP / 8], h2[NP / 8];
+    first_half(lo, l8);
+    first_half(hi, h8);
+    halve<0x141>(l8, h8, col & 4);  // 7 - c of eight
+    first_half(l8, l4);
+    first_half(h8, h4);
+    halve<0x4e>(l4, h4, col & 2);  // c ^ 2
+    first_half(l4, l2);
+    first_half(h4, h2);
+    if constexpr (HD == 128) {
+      halve<0xb1>(l2, h2, col & 1);  // c ^ 1
+    } else {
+      l2[0] = __builtin_elementwise_min(l2[0], from_lane<0xb1>(l2[0]));
+      h2[0] = __builtin_elementwise_max(h2[0], from_lane<0xb1>(h2[0]));
+    }
+    s16x2 l = ordered(l2[0]), h = ordered(h2[0]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (is_nan16(l[i]) || is_nan16(h[i])) l[i] = h[i] = 0x7fc0;
+    uint32_t* out = reinterpret_cast<uint32_t*>(ranges) + at * HD;
+    const int d2 = HD == 128 ? lane : (lane >> 4) * 8 + (col >> 1);
+    if (HD == 128 || !(col & 1)) {
+      out[d2] = __builtin_bit_cast(uint32_t, l);
+      out[HD / 2 + d2] = __builtin_bit_cast(uint32_t, h);
+    }
+  }
+}
+
+// ---- scores ------------------------------------------------------------------------------
+
+// The largest value orders last, and NaN, of either sign, after it.
+__device__ __forceinline__ int score_key(float x) {
+  const int b = x != x ? 0x7fc00000 : __float_as_int(x);
+  return b ^ ((b >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ float score_of(int key) { return __int_as_float(key ^ ((key >> 31) & 0x7fffffff)); }
+
+// Eight queries of a lane as operands: NQ pieces of bf16 each of max(q, 0) and of min(q, 0).
+template <int NQ>
+__device__ __forceinline__ void split_signs(float (&x)[8], bf16x8_t (&above)[NQ], bf16x8_t (&below)[NQ]) {
+  u32x4 neg;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    neg[i] = (__float_as_int(x[2 * i]) < 0 ? 0xffffu : 0u) | (__float_as_int(x[2 * i + 1]) < 0 ? 0xffff0000u : 0u);
+  bf16x8_t q[NQ];
+  split8<NQ>(x, q);
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    const u32x4 w = __builtin_bit_cast(u32x4, q[n]);
+    above[n] = __builtin_bit_cast(bf16x8_t, w & ~neg);
+    below[n] = __builtin_bit_cast(bf16x8_t, w & neg);
+  }
+}
+
+// A block's four waves have 16 PT pages each of one KV head, for up to `rows` consecutive rows: the ranges of 16 pages are
+// the 16-row operands of 16x16x32 products, 2 hd long, the queries (RT rows' G heads side by side) the 16 columns.  The
+// heads' maximum is taken across lanes.
+template <int HD, bool F32, int PT>
+__global__ __launch_bounds__(256) void k_kvq_scores(KvqScoreArgs a, int rows) {
+  constexpr int NJ = HD / 32, NQ = F32 ? 3 : 1;
+  const KvqBatch& bt = a.batch;
+  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n_kv = a.cache.n_kv, G = a.n_q / n_kv, seg = min(G, 16), rt = 16 / seg;
+  const int group = blockIdx.x / n_kv, kh = blockIdx.x - group * n_kv;
+  const int p0 = (blockIdx.y * 4 + wave) * 16 * PT;
+  if (p0 >= a.columns) return;
+  const int last_row = min((group + 1) * rows, bt.n_rows);
+  const int col_row = c / seg, col_head = c - col_row * seg;
+  for (int r = group * rows; r < last_row;) {
+    const int b = wave_find_seq(bt, r);
+    if (b < 0) return;
+    const KvqSeq sq = kvq_seq(bt, b);
+    const int i = r - sq.r0;
+    if (i < 0 || i >= sq.n) {  // past max_rows
+      r = max(r + 1, bt.row_off ? min(bt.row_off[b + 1], bt.n_rows) : 0);
+      continue;
+    }
+    const int n = min(last_row, sq.r0 + sq.n) - r, first = sq.ctx - sq.n + i;  // rows, the first one's position
+    const int seen = sq.ok ? (first + n - 1) >> 6 : -1;                           // the last page that some row sees
+    bf16x8_t hi[PT][NJ], lo[PT][NJ];
+    uint64_t lost[PT];
+    if (p0 <= seen) {
+      const int32_t* pt = table_of(bt, b);
+#pragma unroll
+      for (int t = 0; t < PT; ++t) {
+        const int p = p0 + 16 * t + c;
+        const int id = pt[min(p, seen)];
+        const bool ok = kvq_page_ok(a.cache, id);
+        lost[t] = __ballot(!ok);
+        const uint16_t* at = a.ranges + (static_cast<size_t>(ok ? id : 0) * n_kv + kh) * 2 * HD + 16 * g;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          lo[t][j] = load_bf16x8(at + 64 * (j >> 1) + 8 * (j & 1));
+          hi[t][j] = load_bf16x8(at + HD + 64 * (j >> 1) + 8 * (j & 1));
+        }
+      }
+    }
+    for (int q0 = 0; q0 < n; q0 += rt) {
+      const int mine = q0 + min(col_row, rt - 1), row = r + min(mine, n - 1);
+      const bool real = col_row < rt && mine < n;
+      int best[PT][4];
+#pragma unroll
+      for (int t = 0; t < PT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) best[t][e] = -0x7fffffff - 1;
+      if (p0 <= seen) {
+        for (int h0 = 0; h0 < G; h0 += 16) {
+          const bool some = col_head + h0 < G;
+          const int head = kh * G + min(h0 + col_head, G - 1);
+          f32x4_t acc[PT];
+#pragma unroll
+          for (int t = 0; t < PT; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+          float x[NJ][8];
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) load8<!F32>(a.q, row, head, 64 * (j >> 1) + 16 * g + 8 * (j & 1), x[j]);
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) {
+            bf16x8_t above[NQ], below[NQ];
+            split_signs<NQ>(x[j], above, below);
+#pragma unroll
+            for (int t = 0; t < PT; ++t)
+#pragma unroll
+              for (int m = 0; m < NQ; ++m) {
+                acc[t] = mfma16x16x32(hi[t][j], above[m], acc[t]);
+                acc[t] = mfma16x16x32(lo[t][j], below[m], acc[t]);
+              }
+          }
+#pragma unroll
+          for (int t = 0; t < PT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (some) best[t][e] = max(best[t][e], score_key(acc[t][e]));
+        }
+        // Over the row's lanes: the first one's maximum covers 1, 2, 4, 8 and 16 of them, no further than the row's.
+        auto over = [&](auto tag, int step) {
+          const bool in = col_head + step < seg;
+#pragma unroll
+          for (int t = 0; t < PT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int y = __builtin_amdgcn_update_dpp(0, best[t][e], decltype(tag)::value, 0xf, 0xf, true);
+              if (in) best[t][e] = max(best[t][e], y);
+            }
+        };
+        if (seg > 1) over(std::integral_constant<int, 0x101>{}, 1);
+        if (seg > 2) over(std::integral_constant<int, 0x102>{}, 2);
+        if (seg > 4) over(std::integral_constant<int, 0x104>{}, 4);
+        if (seg > 8) over(std::integral_constant<int, 0x108>{}, 8);
+      }
+      if (real && col_head == 0) {
+        const int pages = (first + mine) >> 6;  // the last one that the row sees
+        float* out = a.scores + (static_cast<size_t>(row) * n_kv + kh) * a.columns;
+#pragma unroll
+        for (int t = 0; t < PT; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int p = p0 + 16 * t + 4 * g + e;
+            float v = !sq.ok ? __builtin_nanf("") : -INFINITY;
+            if (sq.ok && p <= pages) v = (lost[t] >> (4 * g + e)) & 1 ? __builtin_nanf("") : score_of(best[t][e]);
+            if (p < a.columns) out[p] = v;
+          }
+      }
+    }
+    r += n;
+  }
+}
+
+// ---- picks -------------------------------------------------------------------------------
+
+// The order of scores as that of unsigned numbers above 0: -0 is 0, NaN comes last.
+__device__ __forceinline__ uint32_t pick_key(float x) {
+  if (x != x) return 0xffffffffu;
+  const uint32_t b = __float_as_uint(x + 0.f);
+  return b ^ (b >> 31 ? 0xffffffffu : 0x80000000u);
+}
+
+// Lanes of a ballot, as a signed number.
+__device__ __forceinline__ int lanes(uint64_t ballot) { return static_cast<int>(__popcll(ballot)); }
+
+// Pages of the row's list to choose from: `seen` pages, or -1 where the row is not the call's.
+__device__ __forceinline__ int row_pages(const KvqBatch& bt, int row) {
+  const int b = wave_find_seq(bt, row);
+  if (b < 0) return -1;
+  const KvqSeq s = kvq_seq(bt, b);
+  const int i = row - s.r0;
+  if (i < 0 || i >= s.n) return -1;
+  return s.ok ? max(0, s.ctx - s.n + i + kKvqPage) >> 6 : 0;  // none before the first token
+}
+
+// A wave has the list of a row and KV head, E of its up to 64 E pages in each lane.  The least key that is picked is found bit
+// by bit from the highest in which the keys differ: so many keys are at or above a value as a ballot has bits.
+template <int E>
+__global__ __launch_bounds__(256) void k_kvq_pick(KvqPickArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = static_cast<int>(unit / a.n_kv);
+  if (row >= a.batch.n_rows) return;
+  const int m = row_pages(a.batch, row);
+  if (m < 0) return;
+  int32_t* out = a.picks + unit * a.n;
+  if (m <= a.n) {
+    for (int i = lane; i < a.n; i += 64) out[i] = i < m ? i : -1;
+    return;
+  }
+  const float* scores = a.scores + unit * a.columns;
+  const int from = a.first, to = m - a.last, want = a.n - a.first - a.last;  // `want` of pages from .. to - 1
+  uint32_t key[E], top = 0, low = 0xffffffffu;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int p = 64 * e + lane;
+    const bool in = p >= from && p < to;
+    key[e] = in ? pick_key(scores[p]) : 0;
+    top = max(top, key[e]);
+    low = min(low, in ? key[e] : 0xffffffffu);
+  }
+#pragma unroll
+  for (int x = 32; x >= 1; x >>= 1) {
+    top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), x, 64)));
+    low = min(low, static_cast<uint32_t>(__shfl_xor(static_cast<int>(low), x, 64)));
+  }
+  auto count = [&](uint32_t t) {
+    int k = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) k += lanes(__ballot(key[e] >= t));
+    return k;
+  };
+  // The largest t with `want` keys at or above it; where the count meets `want` before, it is far enough.
+  uint32_t least = top;
+  if (top != low) {
+    int bit = 31 - __clz(top ^ low);
+    least = top & ~((2u << bit) - 1);
+    for (; bit >= 0; --bit) {
+      const int k = count(least | 1u << bit);
+      if (k >= want) least |= 1u << bit;
+      if (k == want) break;
+    }
+  }
+  int above = 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) above += lanes(__ballot(key[e] > least));
+  int ties = want - above, at = 0;  // of keys equal to `least`, the first so many
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int p = 64 * e + lane;
+    const uint64_t below = (uint64_t{1} << lane) - 1;
+    const bool in = p >= from && p < to, tie = in && key[e] == least;
+    const uint64_t tied = __ballot(tie);
+    const bool take = (p < m && !in) || (in && key[e] > least) || (tie && lanes(tied & below) < ties);
+    ties -= lanes(tied);
+    const uint64_t taken = __ballot(take);
+    if (take) out[at + lanes(taken & below)] = p;
+    at += lanes(taken);
+  }
+}
+
+// The same for longer lists, a block to each: a digit of eight bits at a time, its keys counted in LDS, the scores read anew for
+// each digit.
+constexpr int kPickThreads = 1024;
+__global__ __launch_bounds__(kPickThreads) void k_kvq_pick_long(KvqPickArgs a) {
+  __shared__ int counts[256];
+  __shared__ int found[2];  // the digit, and how many keys are above it
+  __shared__ int waves[2][kPickThreads / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t unit = blockIdx.x;
+  const int row = static_cast<int>(unit / a.n_kv);
+  const int m = row_pages(a.batch, row);
+  if (m < 0) return;
+  int32_t* out = a.picks + unit * a.n;
+  if (m <= a.n) {
+    for (int i = tid; i < a.n; i += kPickThreads) out[i] = i < m ? i : -1;
+    return;
+  }
+  const float* scores = a.scores + unit * a.columns;
+  const int from = a.first, to = m - a.last;
+  int want = a.n - a.first - a.last;
+  uint32_t least = 0;  // its digits so far; `want` counts what is still to come from keys that begin with them
+  for (int shift = 24; shift >= 0 && want > 0; shift -= 8) {
+    if (tid < 256) counts[tid] = 0;
+    __syncthreads();
+    for (int p = from + tid; p < to; p += kPickThreads) {
+      const uint32_t k = pick_key(scores[p]);
+      if (shift == 24 || (k >> (shift + 8)) == (least >> (shift + 8))) atomicAdd(&counts[(k >> shift) & 255], 1);
+    }
+    __syncthreads();
+    if (wave == 0) {  // lane l has digits 255 - 4l .. 252 - 4l
+      int x[4], sum = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum += x[i] = counts[255 - 4 * lane - i];
+      int above = wave_scan(sum) - sum;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (above < want && above + x[i] >= want) {
+          found[0] = 255 - 4 * lane - i;
+          found[1] = above;
+        }
+        above += x[i];
+      }
+    }
+    __syncthreads();
+    least |= static_cast<uint32_t>(found[0]) << shift;
+    want -= found[1];
+  }
+  if (a.n == a.first + a.last) least = 0xffffffffu;  // and want = 0 of them
+  int at = 0;
+  for (int p0 = 0; p0 < m; p0 += kPickThreads) {
+    const int p = p0 + tid;
+    const uint64_t below = (uint64_t{1} << lane) - 1;
+    const bool in = p >= from && p < to;
+    const uint32_t k = in ? pick_key(scores[p]) : 0;
+    const bool tie = in && k == least;
+    const uint64_t tied = __ballot(tie);
+    if (lane == 0) waves[0][wave] = lanes(tied);
+    __syncthreads();
+    int before = 0, ties = 0;
+    for (int w = 0; w < kPickThreads / 64; ++w) {
+      before += w < wave ? waves[0][w] : 0;
+      ties += waves[0][w];
+    }
+    const bool take = (p < m && !in) || (in && k > least) || (tie && before + lanes(tied & below) < want);
+    want -= ties;
+    const uint64_t taken = __ballot(take);
+    if (lane == 0) waves[1][wave] = lanes(taken);
+    __syncthreads();
+    int mine = at;
+    for (int w = 0; w < kPickThreads / 64; ++w) {
+      mine += w < wave ? waves[1][w] : 0;
+      at += waves[1][w];
+    }
+    if (take) out[mine + lanes(taken & below)] = p;
+    __syncthreads();
+  }
+}
+
+}  // namespace
+
+hipError_t launch_kvq_fit(const KvqFitArgs& a, hipStream_t s) {
+  const int with_rows = a.n_rows <= 4096;
+  launch_kernel(k_kvq_fit, dim3(1), dim3(kFitThreads), 0, s, a, with_rows);
+  if (!with_rows) launch_kernel(k_kvq_fit_rows, dim3(static_cast<uint32_t>((a.n_rows + 255) / 256)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_kvq_ranges(const KvqCache& c, const KvqBatch& b, uint16_t* ranges, hipStream_t s) {
+  // rows of a wave: 64 where that leaves 2,048 waves, as few as one where there are few rows
+  int rows = 64;
+  while (rows > 1 && static_cast<int64_t>(b.n_rows) * c.n_kv / rows < 2048) rows /= 2;
+  const int64_t waves = (static_cast<int64_t>(b.n_rows) + rows - 1) / rows * c.n_kv;
+  const dim3 grid(static_cast<uint32_t>((waves + 3) / 4));
+  if (c.hd == 128) launch_kernel((k_kvq_ranges<128>), grid, dim3(256), 0, s, c, b, ranges, rows);
+  else launch_kernel((k_kvq_ranges<64>), grid, dim3(256), 0, s, c, b, ranges, rows);
+  return hipGetLastError();
+}
+
+hipError_t launch_kvq_scores(const KvqScoreArgs& a, hipStream_t s) {
+  const int n_kv = a.cache.n_kv;
+  int rows = 1;
+  const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>((a.batch.n_rows + rows - 1) / rows) * n_kv), static_cast<uint32_t>((a.columns + 63) / 64));
+#define RP_SCORES(HD, BF16) \
+  if (a.cache.hd == HD && static_cast<bool>(a.q.bf16) == BF16) launch_kernel((k_kvq_scores<HD, !BF16, 1>), grid, dim3(256), 0, s, a, rows);
+  RP_SCORES(128, true) RP_SCORES(128, false) RP_SCORES(64, true) RP_SCORES(64, false)
+#undef RP_SCORES
+  return hipGetLastError();
+}
+
+hipError_t launch_kvq_pick(const KvqPickArgs& a, hipStream_t s) {
+  const int64_t units = static_cast<int64_t>(a.batch.n_rows) * a.n_kv;
+  const int pages = kvq_pages(a.batch.max_context);
+  const dim3 grid(static_cast<uint32_t>((units + 3) / 4)), block(256);
+  if (pages <= 64) launch_kernel((k_kvq_pick<1>), grid, block, 0, s, a);
+  else if (pages <= 128) launch_kernel((k_kvq_pick<2>), grid, block, 0, s, a);
+  else if (pages <= 256) launch_kernel((k_kvq_pick<4>), grid, block, 0, s, a);
+  else if (pages <= 512) launch_kernel((k_kvq_pick<8>), grid, block, 0, s, a);
+  else if (pages <= 1024) launch_kernel((k_kvq_pick<16>), grid, block, 0, s, a);
+  else if (pages <= 2048) launch_kernel((k_kvq_pick<32>), grid, block, 0, s, a);
+  else launch_kernel(k_kvq_pick_long, dim3(static_cast<uint32_t>(units)), dim3(kPickThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace rollpack

@@ -29,10 +29,11 @@ __device__ __forceinline__ const int32_t* table_of(const KvqBatch& bt, int b) {
 
 struct RowPlace {
   int state, t, page;  // state: 0 nothing to do, 1 a position of the cache, 2 before the sequence's first token, 3 bad
+  int i, left;         // which of its sequence's rows; with state 1, tokens from its own to the context's end
 };
 
 __device__ __forceinline__ RowPlace row_place(const KvqCache& c, const KvqBatch& bt, int row) {
-  RowPlace p{0, 0, 0};
+  RowPlace p{0, 0, 0, 0, 0};
   if (row >= bt.n_rows) return p;
   int b = row;
   if (bt.row_off) {  // the last sequence whose first row is not past it
@@ -47,6 +48,7 @@ __device__ __forceinline__ RowPlace row_place(const KvqCache& c, const KvqBatch&
   const KvqSeq s = kvq_seq(bt, b);
   const int i = row - s.r0, pos = s.ctx - s.n + i;
   if (i < 0 || i >= s.n) return p;  // past max_rows, or offsets that do not ascend
+  p.i = i;
   if (!s.ok) {
     p.state = 3;
   } else if (pos < 0) {
@@ -55,9 +57,26 @@ __device__ __forceinline__ RowPlace row_place(const KvqCache& c, const KvqBatch&
     const int id = table_of(bt, b)[pos / kKvqPage];
     p.state = kvq_page_ok(c, id) ? 1 : 3;
     p.t = pos % kKvqPage;
+    p.left = s.ctx - pos;
     p.page = p.state == 1 ? id : 0;
   }
   return p;
+}
+
+// The sequence of a row that the whole wave looks up: the first that ends past it, 64 ends at a time; -1 if none does.
+__device__ __forceinline__ int wave_find_seq(const KvqBatch& bt, int row) {
+  if (!bt.row_off) return row < bt.n_seqs ? row : -1;
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = bt.n_seqs;
+  for (;;) {
+    const int step = (n + 63) >> 6, i = min((lane + 1) * step, n) - 1;
+    const uint64_t past = __ballot(bt.row_off[lo + i + 1] > row);
+    if (!past) return -1;
+    const int w = __ffsll(static_cast<unsigned long long>(past)) - 1;
+    lo += w * step;
+    if (step == 1) return lo;
+    n = min(step, n - w * step);
+  }
 }
 
 // ---- tensors ---------------------------------------------------------------------------

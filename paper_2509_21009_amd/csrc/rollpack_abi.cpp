@@ -9,6 +9,7 @@
 
 #include "engine.hpp"
 #include "kvq.hpp"
+#include "kvq_pages.hpp"
 #include "kvq_plan.hpp"
 #include "static_ws.hpp"
 #include "tail_batch.hpp"
@@ -209,6 +210,28 @@ size_t kvq_attend_size(const rollpack::KvqCache& c, const rollpack::KvqBatch& b,
                   rollpack::kvq_attend_fits(c, b, n_q),
               "too many rows and heads for one call");
   return rollpack::kvq_attend_bytes(c, b, n_q);
+}
+
+void kvq_require_ints(const void* p, const char* what) { kvq_require(p && reinterpret_cast<uintptr_t>(p) % 4 == 0, what); }
+
+// Rows and heads of the page calls, which take a block, or a quarter of one, to each: 2^22 blocks of 1,024 threads are a grid.
+void kvq_require_lists(const rollpack::KvqBatch& b, int64_t n_kv) {
+  kvq_require(static_cast<int64_t>(b.n_rows) * n_kv < (int64_t{1} << 22), "too many rows and heads for one call");
+}
+
+void kvq_require_ranges(const void* p) { kvq_require(p && reinterpret_cast<uintptr_t>(p) % 16 == 0, "ranges must be 16-byte aligned device memory"); }
+
+void kvq_require_columns(const rollpack::KvqBatch& b, int32_t n) {
+  kvq_require(n >= rollpack::kvq_pages(b.max_context) && n >= 1 && n <= (1 << 21), "n_columns: the pages of max_context at least, 2^21 at most");
+}
+
+// The bytes of an attention call over lists of n pages.
+size_t kvq_picked_size(const rollpack::KvqCache& c, const rollpack::KvqBatch& b, int32_t n_q, int32_t n) {
+  kvq_require(n_q >= 1 && n_q <= 65536 && n_q % c.n_kv == 0, "n_q_heads must be a multiple of n_kv_heads");
+  kvq_require(n >= 1 && n <= (1 << 24), "1 <= n_picks <= 2^24");
+  const rollpack::PickedPlan p = rollpack::picked_plan(c, b.n_rows, n, n_q);
+  kvq_require(rollpack::picked_blocks(c, b.n_rows, p) < (int64_t{1} << 22), "too many rows and heads for one call");
+  return rollpack::kvq_picked_bytes(c, b.n_rows, n, n_q);
 }
 
 }  // namespace
@@ -560,6 +583,137 @@ rp_status rp_kvq_attend(const rp_kvq_cache* cache, const rp_kvq_batch* batch, in
     a.n_q = n_q_heads;
     a.scale = scale;
     kvq_launched(rollpack::launch_kvq_attend(a, workspace, kvq_stream(hip_stream)), "rp_kvq_attend");
+  });
+}
+
+rp_status rp_kvq_fit_pages(const rp_kvq_pool* pool, const int32_t* lengths, int32_t n_rows, int32_t* row_offsets,
+                           int32_t* positions, int32_t* slots, void* hip_stream) {
+  return guarded([&] {
+    kvq_require(pool, "null pool");
+    kvq_require(pool->n_seqs >= 0 && pool->n_seqs <= (1 << 20), "0 <= n_seqs <= 2^20");
+    kvq_require(pool->n_pages >= 1 && pool->n_pages <= (int64_t{1} << 24), "1 <= n_pages <= 2^24");
+    kvq_require(pool->max_context >= 0 && pool->max_context <= (1 << 30), "0 <= max_context <= 2^30");
+    kvq_require(pool->table_stride >= 1 && pool->table_stride <= (int64_t{1} << 32), "1 <= table_stride <= 2^32");
+    kvq_require(pool->max_context <= pool->table_stride * rollpack::kKvqPage, "max_context is past the page table's rows");
+    kvq_require(n_rows >= 0 && n_rows <= (1 << 24), "0 <= n_rows <= 2^24");
+    if (pool->n_seqs > 0) {
+      kvq_require_ints(pool->page_table, "page_table must be device memory of 32-bit numbers");
+      kvq_require_ints(pool->contexts, "contexts must be device memory of 32-bit numbers");
+      kvq_require_ints(lengths, "lengths must be device memory of 32-bit numbers");
+    }
+    kvq_require_ints(pool->free_pages, "free_pages must be device memory of 32-bit numbers");
+    kvq_require_ints(pool->state, "state must be device memory of 32-bit numbers");
+    kvq_require_ints(pool->workspace, "workspace must be device memory of 32-bit numbers");
+    kvq_require_ints(row_offsets, "row_offsets must be device memory of 32-bit numbers");
+    if (n_rows > 0) {
+      kvq_require_ints(positions, "positions must be device memory of 32-bit numbers");
+      kvq_require_ints(slots, "slots must be device memory of 32-bit numbers");
+    }
+    rollpack::KvqFitArgs a;
+    a.pool.page_table = pool->page_table;
+    a.pool.table_stride = pool->table_stride;
+    a.pool.context = pool->contexts;
+    a.pool.free_pages = pool->free_pages;
+    a.pool.state = pool->state;
+    a.pool.first_need = pool->workspace;
+    a.pool.n_seqs = pool->n_seqs;
+    a.pool.n_pages = static_cast<int>(pool->n_pages);
+    a.pool.max_context = pool->max_context;
+    a.length = lengths;
+    a.row_off = row_offsets;
+    a.position = positions;
+    a.slot = slots;
+    a.n_rows = n_rows;
+    kvq_launched(rollpack::launch_kvq_fit(a, kvq_stream(hip_stream)), "rp_kvq_fit_pages");
+  });
+}
+
+rp_status rp_kvq_key_ranges(const rp_kvq_cache* cache, const rp_kvq_batch* batch, void* ranges, void* hip_stream) {
+  return guarded([&] {
+    const rollpack::KvqCache c = kvq_cache(cache, true);
+    const rollpack::KvqBatch b = kvq_batch(batch, true);
+    if (!kvq_any_row(b)) return;
+    kvq_require(static_cast<int64_t>(b.n_rows) * c.n_kv <= (int64_t{1} << 26), "too many rows and heads for one call");
+    kvq_require_ranges(ranges);
+    kvq_launched(rollpack::launch_kvq_ranges(c, b, static_cast<uint16_t*>(ranges), kvq_stream(hip_stream)), "rp_kvq_key_ranges");
+  });
+}
+
+rp_status rp_kvq_page_scores(const rp_kvq_cache* cache, const rp_kvq_batch* batch, int32_t n_q_heads, const rp_kvq_tensor* q,
+                             const void* ranges, float* scores, int32_t n_columns, void* hip_stream) {
+  return guarded([&] {
+    rollpack::KvqScoreArgs a;
+    a.cache = kvq_cache(cache, false);
+    a.batch = kvq_batch(batch, true);
+    kvq_require(n_q_heads >= 1 && n_q_heads <= 65536 && n_q_heads % a.cache.n_kv == 0, "n_q_heads must be a multiple of n_kv_heads");
+    if (!kvq_any_row(a.batch)) return;
+    kvq_require_lists(a.batch, a.cache.n_kv);
+    kvq_require_columns(a.batch, n_columns);
+    a.q = kvq_tensor(q, a.batch.n_rows, n_q_heads, a.cache.hd, false);
+    kvq_require_ranges(ranges);
+    kvq_require_ints(scores, "scores must be device memory of 32-bit numbers");
+    a.ranges = static_cast<const uint16_t*>(ranges);
+    a.scores = scores;
+    a.n_q = n_q_heads;
+    a.columns = n_columns;
+    kvq_launched(rollpack::launch_kvq_scores(a, kvq_stream(hip_stream)), "rp_kvq_page_scores");
+  });
+}
+
+rp_status rp_kvq_pick_pages(const rp_kvq_batch* batch, int32_t n_kv_heads, const float* scores, int32_t n_columns,
+                            int32_t first, int32_t last, int32_t n_picks, int32_t* picks, void* hip_stream) {
+  return guarded([&] {
+    rollpack::KvqPickArgs a;
+    a.batch = kvq_batch(batch, true);
+    kvq_require(n_kv_heads >= 1 && n_kv_heads <= 1024, "1 <= n_kv_heads <= 1024");
+    kvq_require(n_picks >= 1 && n_picks <= (1 << 24), "1 <= n_picks <= 2^24");
+    kvq_require(first >= 0 && first <= n_picks && last >= 0 && last <= n_picks - first, "first + last is at most n_picks, neither below 0");
+    if (!kvq_any_row(a.batch)) return;
+    kvq_require_lists(a.batch, n_kv_heads);
+    kvq_require_columns(a.batch, n_columns);
+    kvq_require_ints(scores, "scores must be device memory of 32-bit numbers");
+    kvq_require_ints(picks, "picks must be device memory of 32-bit numbers");
+    a.scores = scores;
+    a.picks = picks;
+    a.n_kv = n_kv_heads;
+    a.columns = n_columns;
+    a.first = first;
+    a.last = last;
+    a.n = n_picks;
+    kvq_launched(rollpack::launch_kvq_pick(a, kvq_stream(hip_stream)), "rp_kvq_pick_pages");
+  });
+}
+
+rp_status rp_kvq_attend_picked_workspace(const rp_kvq_cache* cache, const rp_kvq_batch* batch, int32_t n_q_heads,
+                                         int32_t n_picks, size_t* bytes) {
+  return guarded([&] {
+    kvq_require(bytes, "null argument");
+    *bytes = kvq_picked_size(kvq_cache(cache, false), kvq_batch(batch, false), n_q_heads, n_picks);
+  });
+}
+
+rp_status rp_kvq_attend_picked(const rp_kvq_cache* cache, const rp_kvq_batch* batch, int32_t n_q_heads, float scale,
+                               const rp_kvq_tensor* q, const int32_t* picks, int32_t n_picks, const rp_kvq_tensor* out,
+                               void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return guarded([&] {
+    rollpack::KvqPickedArgs a;
+    a.cache = kvq_cache(cache, true);
+    a.batch = kvq_batch(batch, true);
+    const size_t need = kvq_picked_size(a.cache, a.batch, n_q_heads, n_picks);
+    kvq_require(scale > 0.f && std::isfinite(scale), "scale must be positive and finite");
+    if (!kvq_any_row(a.batch)) return;
+    a.q = kvq_tensor(q, a.batch.n_rows, n_q_heads, a.cache.hd, false);
+    a.out = kvq_tensor(out, a.batch.n_rows, n_q_heads, a.cache.hd, true);
+    kvq_require(a.q.bf16 == a.out.bf16, "q and out must have one dtype");
+    kvq_require(a.q.p != a.out.p, "out is q's memory");
+    kvq_require_ints(picks, "picks must be device memory of 32-bit numbers");
+    kvq_require(need == 0 || (workspace && reinterpret_cast<uintptr_t>(workspace) % 256 == 0), "workspace must be 256-byte aligned device memory");
+    kvq_require(workspace_bytes >= need, "workspace smaller than rp_kvq_attend_picked_workspace");
+    a.picks = picks;
+    a.n = n_picks;
+    a.n_q = n_q_heads;
+    a.scale = scale;
+    kvq_launched(rollpack::launch_kvq_attend_picked(a, workspace, kvq_stream(hip_stream)), "rp_kvq_attend_picked");
   });
 }
 

@@ -100,6 +100,16 @@ class RpKvqTensor(ctypes.Structure):
                 ("dtype", ctypes.c_int32)]
 
 
+class RpKvqPool(ctypes.Structure):
+    _fields_ = [("page_table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("contexts", ctypes.c_void_p),
+                ("free_pages", ctypes.c_void_p), ("state", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+                ("n_seqs", ctypes.c_int32), ("max_context", ctypes.c_int32), ("n_pages", ctypes.c_int64)]
+
+
+KVQ_FIT_ERRORS = ("none", "too few free pages", "a length outside 0 .. max_context", "more new tokens than n_rows",
+                  "a state that no calls have made")
+
+
 class RollpackError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"{STATUS.get(status, status)}: {msg}")
@@ -112,6 +122,7 @@ _I64P = ctypes.POINTER(ctypes.c_int64)
 _F32P = ctypes.POINTER(ctypes.c_float)
 _SZP = ctypes.POINTER(ctypes.c_size_t)
 _KC, _KB, _KT = ctypes.POINTER(RpKvqCache), ctypes.POINTER(RpKvqBatch), ctypes.POINTER(RpKvqTensor)
+_KP = ctypes.POINTER(RpKvqPool)
 
 # name -> (restype, argtypes), in the order of include/rollpack.h
 SIGNATURES = {
@@ -165,6 +176,14 @@ SIGNATURES = {
     "rp_kvq_read": (ctypes.c_int, [_KC, _KB, _KT, _KT, _P]),
     "rp_kvq_attend_workspace": (ctypes.c_int, [_KC, _KB, ctypes.c_int32, _SZP]),
     "rp_kvq_attend": (ctypes.c_int, [_KC, _KB, ctypes.c_int32, ctypes.c_float, _KT, _KT, _P, ctypes.c_size_t, _P]),
+    "rp_kvq_fit_pages": (ctypes.c_int, [_KP, _P, ctypes.c_int32, _P, _P, _P, _P]),
+    "rp_kvq_key_ranges": (ctypes.c_int, [_KC, _KB, _P, _P]),
+    "rp_kvq_page_scores": (ctypes.c_int, [_KC, _KB, ctypes.c_int32, _KT, _P, _P, ctypes.c_int32, _P]),
+    "rp_kvq_pick_pages": (ctypes.c_int, [_KB, ctypes.c_int32, _P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                         _P, _P]),
+    "rp_kvq_attend_picked_workspace": (ctypes.c_int, [_KC, _KB, ctypes.c_int32, ctypes.c_int32, _SZP]),
+    "rp_kvq_attend_picked": (ctypes.c_int, [_KC, _KB, ctypes.c_int32, ctypes.c_float, _KT, _P, ctypes.c_int32, _KT, _P,
+                                            ctypes.c_size_t, _P]),
     "rp_last_error": (ctypes.c_char_p, []),
 }
 
@@ -527,6 +546,38 @@ def rp_kvq_attend(cache: RpKvqCache, batch: RpKvqBatch, n_q_heads: int, scale: f
                                         stream_ptr))
 
 
+def rp_kvq_fit_pages(pool: RpKvqPool, lengths_ptr: int, n_rows: int, row_offsets_ptr: int, positions_ptr: int,
+                     slots_ptr: int, stream_ptr: int) -> None:
+    _check(load_library().rp_kvq_fit_pages(pool, lengths_ptr, n_rows, row_offsets_ptr, positions_ptr, slots_ptr, stream_ptr))
+
+
+def rp_kvq_key_ranges(cache: RpKvqCache, batch: RpKvqBatch, ranges_ptr: int, stream_ptr: int) -> None:
+    _check(load_library().rp_kvq_key_ranges(cache, batch, ranges_ptr, stream_ptr))
+
+
+def rp_kvq_page_scores(cache: RpKvqCache, batch: RpKvqBatch, n_q_heads: int, q: RpKvqTensor, ranges_ptr: int, scores_ptr: int,
+                       n_columns: int, stream_ptr: int) -> None:
+    _check(load_library().rp_kvq_page_scores(cache, batch, n_q_heads, q, ranges_ptr, scores_ptr, n_columns, stream_ptr))
+
+
+def rp_kvq_pick_pages(batch: RpKvqBatch, n_kv_heads: int, scores_ptr: int, n_columns: int, first: int, last: int, n_picks: int,
+                      picks_ptr: int, stream_ptr: int) -> None:
+    _check(load_library().rp_kvq_pick_pages(batch, n_kv_heads, scores_ptr, n_columns, first, last, n_picks, picks_ptr, stream_ptr))
+
+
+def rp_kvq_attend_picked_workspace(cache: RpKvqCache, batch: RpKvqBatch, n_q_heads: int, n_picks: int) -> int:
+    b = ctypes.c_size_t()
+    _check(load_library().rp_kvq_attend_picked_workspace(cache, batch, n_q_heads, n_picks, ctypes.byref(b)))
+    return b.value
+
+
+def rp_kvq_attend_picked(cache: RpKvqCache, batch: RpKvqBatch, n_q_heads: int, scale: float, q: RpKvqTensor, picks_ptr: int,
+                         n_picks: int, out: RpKvqTensor, workspace_ptr: Optional[int], workspace_bytes: int,
+                         stream_ptr: int) -> None:
+    _check(load_library().rp_kvq_attend_picked(cache, batch, n_q_heads, scale, q, picks_ptr, n_picks, out, workspace_ptr,
+                                               workspace_bytes, stream_ptr))
+
+
 def rp_last_error() -> str:
     return load_library().rp_last_error().decode()
 
@@ -694,6 +745,7 @@ class KvqBatch:
 
     def __init__(self, struct: RpKvqBatch, tensors):
         self.struct, self.tensors = struct, tensors
+        self.contexts, self.page_table, self.row_offsets = tensors
         self.device = tensors[0].device
 
 
@@ -817,6 +869,143 @@ class KvqCache:
                    self._tensor(q, n, heads), self._tensor(out, n, heads), workspace.data_ptr(),
                    workspace.numel() * workspace.element_size())
         return out
+
+    # ---- pages: ranges of their keys, scores, picks, attention over the picked ones
+
+    def new_ranges(self):
+        """Zeros [n_pages, n_kv_heads, 2, head_dim] bfloat16 for update_ranges."""
+        return self.torch.zeros((self.n_pages, self.n_kv_heads, 2, self.head_dim), dtype=self.torch.bfloat16, device=self.device)
+
+    def _ranges(self, ranges) -> int:
+        if ranges.dtype != self.torch.bfloat16 or ranges.device != self.device or not ranges.is_contiguous() or \
+                ranges.shape != (self.n_pages, self.n_kv_heads, 2, self.head_dim):
+            raise ValueError(f"ranges are a contiguous bfloat16 tensor [{self.n_pages}, {self.n_kv_heads}, 2, {self.head_dim}] on "
+                             f"{self.device}, got {ranges.dtype} {tuple(ranges.shape)} on {ranges.device}")
+        return ranges.data_ptr()
+
+    def _per_list(self, t, batch: KvqBatch, dtype, name: str) -> int:
+        """A contiguous tensor [n_rows, n_kv_heads, ..] of a batch; its last dimension."""
+        if t.dtype != dtype or t.device != self.device or t.dim() != 3 or not t.is_contiguous() or \
+                t.shape[:2] != (batch.struct.n_rows, self.n_kv_heads):
+            raise ValueError(f"{name} are a contiguous {dtype} tensor [{batch.struct.n_rows}, {self.n_kv_heads}, n] on {self.device}, "
+                             f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+        if t.shape[2] >= 1 << 31:
+            raise ValueError(f"{name} have too long a last dimension")
+        return t.shape[2]
+
+    def update_ranges(self, batch: KvqBatch, ranges):
+        """The smallest and largest key of each dimension, KV head and page, for the pages that the batch's rows are in,
+        after append: into `ranges` (new_ranges()), which is returned."""
+        self._call(rp_kvq_key_ranges, batch, self._ranges(ranges))
+        return ranges
+
+    def page_scores(self, batch: KvqBatch, q, ranges, out=None):
+        """[n_rows, n_kv_heads, pages] float32: for each page that a row sees, what no q . k with a key of it exceeds, for any
+        of the KV head's query heads; minus infinity past them.  pages: those of the batch's max_context, or of `out`."""
+        if q.dim() != 3:
+            raise ValueError("q is [n_rows, n_q_heads, head_dim]")
+        n, heads = batch.struct.n_rows, q.shape[1]
+        if out is None:
+            out = self.torch.empty((n, self.n_kv_heads, max(1, -(-batch.struct.max_context // 64))), dtype=self.torch.float32,
+                                   device=self.device)
+            columns = out.shape[2]
+        else:
+            columns = self._per_list(out, batch, self.torch.float32, "scores")
+        self._call(rp_kvq_page_scores, batch, heads, self._tensor(q, n, heads), self._ranges(ranges), out.data_ptr(), columns)
+        return out
+
+    def pick_pages(self, batch: KvqBatch, scores, n_picks: int, first: int = 1, last: int = 1, out=None):
+        """[n_rows, n_kv_heads, n_picks] int32: the pages to attend to, ascending, then -1.  All that the row sees, or its first
+        `first`, its last `last`, and of the others those of the highest scores (ties: the lower page)."""
+        for name, x in (("n_picks", n_picks), ("first", first), ("last", last)):
+            if not 0 <= x < 1 << 31:  # ctypes would pass its lower half
+                raise ValueError(f"{name} must be between 0 and 2^31 - 1, got {x}")
+        columns = self._per_list(scores, batch, self.torch.float32, "scores")
+        if out is None:
+            out = self.torch.empty((batch.struct.n_rows, self.n_kv_heads, n_picks), dtype=self.torch.int32, device=self.device)
+        elif self._per_list(out, batch, self.torch.int32, "picks") != n_picks:
+            raise ValueError(f"out has lists of {out.shape[2]} pages, not {n_picks}")
+        self._call(lambda cache, *args: rp_kvq_pick_pages(*args), batch, self.n_kv_heads, scores.data_ptr(), columns, first, last,
+                   n_picks, out.data_ptr())
+        return out
+
+    def attend_picked_workspace(self, batch: KvqBatch, n_q_heads: int, n_picks: int):
+        """A workspace for attend_picked with this batch's rows, for callers who keep one (one per call in flight)."""
+        n = rp_kvq_attend_picked_workspace(self.struct, batch.struct, n_q_heads, n_picks)
+        return self.torch.empty(n, dtype=self.torch.uint8, device=self.device)
+
+    def attend_picked(self, batch: KvqBatch, q, picks, scale: Optional[float] = None, out=None, workspace=None):
+        """attend over the tokens of the pages in picks [n_rows, n_kv_heads, n] (pick_pages) alone."""
+        torch, n = self.torch, batch.struct.n_rows
+        if q.dim() != 3:
+            raise ValueError("q is [n_rows, n_q_heads, head_dim]")
+        heads, n_picks = q.shape[1], self._per_list(picks, batch, torch.int32, "picks")
+        if out is None:
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        if workspace is None:
+            workspace = self.attend_picked_workspace(batch, heads, n_picks)
+        elif workspace.device != self.device or not workspace.is_contiguous():
+            raise ValueError("the workspace is a contiguous tensor on the cache's device")
+        self._call(rp_kvq_attend_picked, batch, heads, self.head_dim ** -0.5 if scale is None else scale, self._tensor(q, n, heads),
+                   picks.data_ptr(), n_picks, self._tensor(out, n, heads), workspace.data_ptr(),
+                   workspace.numel() * workspace.element_size())
+        return out
+
+
+class KvqPages:
+    """The pages of a 4-bit cache handed out on the GPU (rp_kvq_fit_pages): page_table [n_seqs, pages], contexts [n_seqs],
+    free_pages [n_pages] and state [4], int32 tensors that fit() keeps up to date on torch's current stream.
+
+    One pool serves the caches of all layers.  fit() can be captured into a graph; its replays read the lengths then there.
+    """
+
+    def __init__(self, n_pages: int, n_seqs: int, max_context: int, device="cuda"):
+        import torch
+        for name, x, most in (("n_pages", n_pages, 1 << 24), ("n_seqs", n_seqs, 1 << 20), ("max_context", max_context, 1 << 30)):
+            if not (n_pages >= 1 and 0 <= x <= most):
+                raise ValueError(f"{name} must be between {int(name == 'n_pages')} and {most}, got {x}")
+        self.torch, self.n_pages, self.n_seqs, self.max_context = torch, n_pages, n_seqs, max_context
+        ints = lambda *dims: torch.zeros(dims, dtype=torch.int32, device=device)  # noqa: E731
+        self.page_table = ints(n_seqs, max(1, -(-max_context // 64)))
+        self.contexts = ints(n_seqs)
+        self.free_pages = torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device)  # page 0 goes first
+        self.state, self._workspace = ints(4), ints(n_seqs + 1)
+        self.state[0] = n_pages
+        self.device = self.state.device
+        if self.device.type != "cuda":
+            raise ValueError("the pool lives in GPU memory")
+        self.struct = RpKvqPool(self.page_table.data_ptr(), self.page_table.shape[1], self.contexts.data_ptr(),
+                                self.free_pages.data_ptr(), self.state.data_ptr(), self._workspace.data_ptr(), n_seqs, max_context,
+                                n_pages)
+
+    def fit(self, lengths, n_rows: int, max_rows: Optional[int] = None, max_context: Optional[int] = None):
+        """Give each sequence the pages of its new length (int32 tensor [n_seqs]), take back those of what it no longer has.
+        Returns (batch, positions, slots) of the up to n_rows new tokens: the batch for a KvqCache's calls until the next fit,
+        each row's position, and 64 * page + position % 64, -1 in padded rows (int32 tensors).
+        n_rows bounds the new tokens of all sequences, max_rows those of one (n_rows), max_context the lengths (the pool's).
+        What does not fit shows in state[1] (status()): then nothing changed and there are no rows."""
+        torch = self.torch
+        if lengths.dtype != torch.int32 or lengths.device != self.device or lengths.shape != (self.n_seqs,) or not lengths.is_contiguous():
+            raise ValueError(f"lengths are a contiguous int32 tensor [{self.n_seqs}] on {self.device}, got {lengths.dtype} "
+                             f"{tuple(lengths.shape)} on {lengths.device}")
+        max_rows = n_rows if max_rows is None else max_rows
+        max_context = self.max_context if max_context is None else max_context
+        for name, x, most in (("n_rows", n_rows, 1 << 24), ("max_rows", max_rows, n_rows), ("max_context", max_context, self.max_context)):
+            if not 0 <= x <= most:
+                raise ValueError(f"{name} must be between 0 and {most}, got {x}")
+        ints = lambda n: torch.empty(n, dtype=torch.int32, device=self.device)  # noqa: E731
+        off, positions, slots = ints(self.n_seqs + 1), ints(n_rows), ints(n_rows)
+        with torch.cuda.device(self.device):
+            rp_kvq_fit_pages(self.struct, lengths.data_ptr(), n_rows, off.data_ptr(), positions.data_ptr(), slots.data_ptr(),
+                             torch._C._cuda_getCurrentRawStream(self.device.index))
+        b = RpKvqBatch(self.n_seqs, n_rows, max_rows, max_context, off.data_ptr(), self.contexts.data_ptr(),
+                       self.page_table.data_ptr(), self.page_table.shape[1])
+        return KvqBatch(b, (self.contexts, self.page_table, off)), positions, slots
+
+    def status(self) -> dict:
+        """What the last fit left, read from the GPU (which it waits for)."""
+        free, error, rows, missing = self.state.tolist()
+        return {"free_pages": free, "error": error, "message": KVQ_FIT_ERRORS[error], "rows": rows, "missing_pages": missing}
 
 
 def weights_struct(shape, weights: dict):
