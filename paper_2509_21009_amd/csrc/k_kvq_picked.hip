@@ -47,7 +47,7 @@ __device__ __forceinline__ PickedBlock picked_block(int index, int n_kv, int col
 // entries the waves take in turn, 64 looked up at a time (entry, then its page).  What a wave does with a page is
 // k_kvq_attend's: S^T = K Q^T, an online softmax in base 2 and O^T += V^T P^T from registers, P in fp16 while V's scales
 // allow it.
-template <int HD, bool F32, int NW>
+template <int HD, bool F32, int NW, bool KEEP>
 __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend_picked(KvqPickedArgs a, PickedPlan plan) {
   constexpr int NT = HD / 16, OLD = HD + 4;
   __shared__ __attribute__((aligned(16))) float so[NW][16 * OLD];
@@ -59,13 +59,15 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend_picked(KvqP
   const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
   const int index = blockIdx.x, split = blockIdx.y;
   const PickedBlock pb = picked_block(index, n_kv, plan.col_tiles);
-  const PickedRow pr = picked_row(bt, pb.row);
-  if (!pr.mine) return;
   const int per_item = (a.n + plan.items - 1) / plan.items, e0 = split * per_item;
   const int entries = max(0, min(per_item, a.n - e0));
   const int n_cols = min(16, G - 16 * pb.ct), head0 = pb.kh * G + 16 * pb.ct;
   const float scale_log2 = a.scale * kLog2e;
   const int32_t* list = a.picks + (static_cast<size_t>(pb.row) * n_kv + pb.kh) * a.n + e0;
+  auto entry_of = [&](int i) { return i < entries ? list[i] : -1; };
+  int entry = entry_of(wave + NW * lane);  // on its way while the row is looked up
+  const PickedRow pr = picked_row(bt, pb.row);
+  if (!pr.mine) return;
 
   f32x4_t o[NT];
 #pragma unroll
@@ -73,7 +75,7 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend_picked(KvqP
   Softmax st;
   // The wave's entries: `todo` has a bit for each of the 64 looked up that names a page the row sees.
   uint64_t todo = 0;
-  int looked = wave, entry = 0, id = 0;
+  int looked = wave, id = 0;
   const size_t bytes = kvq_block_bytes(HD);
   const char* base = a.cache.blocks + pb.kh * bytes;
   struct Page {
@@ -83,8 +85,7 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend_picked(KvqP
   };
   auto advance = [&]() {
     while (!todo && looked < entries) {
-      const int i = looked + NW * lane;
-      entry = i < entries ? list[i] : -1;
+      if (looked != wave) entry = entry_of(looked + NW * lane);
       const bool seen = entry >= 0 && entry <= (pr.pos >> 6);  // the position -1 sees none
       id = seen ? pr.table[entry] : 0;
       todo = __ballot(seen);
@@ -116,13 +117,13 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend_picked(KvqP
       constexpr bool HALF = half_tag.value;
       PageK<HD> pk;
       PageV<HD> pv;
-      pk.load(now.at);
-      pv.load(now.at);
+      pk.template load<!KEEP>(now.at);
+      pv.template load<!KEEP>(now.at);
       while (now.there) {
         f32x4_t s[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) s[u] = qf.scores(pk, u);
-        pk.load(next.at);
+        pk.template load<!KEEP>(next.at);
         const int held = now.lost ? now.tok0 : pr.pos + 1;  // what lies behind, or in a page that stands in, may be anything
         if (now.tok0 + kKvqPage > held) {
 #pragma unroll
@@ -153,7 +154,7 @@ __global__ __launch_bounds__(64 * NW, F32 ? 2 : 3) void k_kvq_attend_picked(KvqP
         half_values<HD, HALF, F32 ? 3 : 2>(pv, 0, x, w, o);
         half_values<HD, HALF, F32 ? 3 : 2>(pv, 1, x, w, o);
         now = next;
-        pv.load(now.at);
+        pv.template load<!KEEP>(now.at);
         if (now.there) next = advance();
       }
     };
@@ -278,12 +279,22 @@ __global__ __launch_bounds__(256) void k_kvq_join_picked(KvqPickedArgs a, Picked
 
 template <int HD, bool F32>
 hipError_t picked_launch(KvqPickedArgs a, float* ws, hipStream_t s) {
-  const PickedPlan p = picked_plan(a.cache, a.batch.n_rows, a.n, a.n_q);
-  const size_t n = picked_part_floats(a.cache, a.batch.n_rows, p);
+  const PickedPlan p = picked_plan(a.cache, a.batch, a.n, a.n_q);
+  const size_t n = picked_part_floats(a.cache, a.batch, p);
   a.part_o = ws;
   a.part_ml = n ? ws + n : nullptr;
-  const uint32_t blocks = static_cast<uint32_t>(picked_blocks(a.cache, a.batch.n_rows, p));
-  launch_kernel((k_kvq_attend_picked<HD, F32, 4>), dim3(blocks, p.items), dim3(256), 0, s, a, p);
+  const uint32_t blocks = static_cast<uint32_t>(picked_blocks(a.cache, a.batch, p));
+  const dim3 grid(blocks, p.items);
+#define RP_PICKED(W)                                                                                              \
+  case W:                                                                                                         \
+    if (p.shared) launch_kernel((k_kvq_attend_picked<HD, F32, W, true>), grid, dim3(64 * W), 0, s, a, p);         \
+    else launch_kernel((k_kvq_attend_picked<HD, F32, W, false>), grid, dim3(64 * W), 0, s, a, p);                 \
+    break;
+  switch (p.waves) {
+    RP_PICKED(4) RP_PICKED(8)
+    default: return hipErrorInvalidValue;
+  }
+#undef RP_PICKED
   if (n) launch_kernel((k_kvq_join_picked<HD, F32>), dim3(blocks, p.cols), dim3(256), 0, s, a, p);
   return hipGetLastError();
 }

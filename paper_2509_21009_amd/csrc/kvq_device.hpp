@@ -182,28 +182,35 @@ __device__ __forceinline__ void split8(float (&x)[8], bf16x8_t (&out)[N]) {
   }
 }
 
-// A page of one head as a lane holds it.
+// A page of one head as a lane holds it.  NT: not to be kept in the caches, what one wave alone reads.
+template <bool NT, typename T>
+__device__ __forceinline__ T load_page(const T* p) {
+  if constexpr (NT) return __builtin_nontemporal_load(p);
+  else return *p;
+}
 template <int HD>
 struct PageK {
   u32x4 k[HD / 32];
   uint32_t s;
+  template <bool NT = true>
   __device__ __forceinline__ void load(const char* block) {
     const int lane = threadIdx.x & 63;
     const u32x4* p = reinterpret_cast<const u32x4*>(block) + lane;
 #pragma unroll
-    for (int i = 0; i < HD / 32; ++i) k[i] = __builtin_nontemporal_load(p + 64 * i);
-    s = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(block + 64 * HD) + ((lane >> 4) * HD / 128) * 16 + (lane & 15));
+    for (int i = 0; i < HD / 32; ++i) k[i] = load_page<NT>(p + 64 * i);
+    s = load_page<NT>(reinterpret_cast<const uint32_t*>(block + 64 * HD) + ((lane >> 4) * HD / 128) * 16 + (lane & 15));
   }
 };
 template <int HD>
 struct PageV {
   u32x4 v[HD / 32], s;
+  template <bool NT = true>
   __device__ __forceinline__ void load(const char* block) {
     const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
     const u32x4* p = reinterpret_cast<const u32x4*>(block + 32 * HD) + lane;
 #pragma unroll
-    for (int i = 0; i < HD / 32; ++i) v[i] = __builtin_nontemporal_load(p + 64 * i);
-    s = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(block + 66 * HD) + (c * HD / 512) * 4 + g);
+    for (int i = 0; i < HD / 32; ++i) v[i] = load_page<NT>(p + 64 * i);
+    s = load_page<NT>(reinterpret_cast<const u32x4*>(block + 66 * HD) + (c * HD / 512) * 4 + g);
   }
 };
 

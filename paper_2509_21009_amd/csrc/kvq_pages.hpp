@@ -72,26 +72,36 @@ struct KvqPickedArgs {
 struct PickedPlan {
   int cols = 0, col_tiles = 0;  // columns of a block; blocks of a row and KV head, but for the items
   int items = 1, waves = 4;
+  int shared = 0;  // rows of a sequence may read the same pages, which the caches then keep
 };
 
-inline PickedPlan picked_plan(const KvqCache& c, int n_rows, int n, int n_q) {
+//   A wave takes 1 us a page, and the start and end of a block 6; a split's second launch and partial outputs take 4.5 and
+// more.  7 query heads to each of 4 KV heads of 128 dims, us, whole with four waves | with eight | split: lists of 64 pages of 1 row (4
+// blocks) 21.5 | 18.8 | 9.4, of 8 rows 28 | 22 | 12.3, of 16 rows 29 | 22 | 16.3; of 32 pages of 4 rows 13.4 | 12.0 | 9.8, of 16 rows 16.9 | 14.7 | 12.9,
+// of 32 rows 17.6 | 15.7 | 17.0; of 16 pages of 8 rows 10.6 | 10.4 | 10.3; of 96 of 32 rows 42.6 | 34.1 | 28.7, of 64 rows 50.7 | 43.9 | 47.7; of 32
+// of 96 rows (384 blocks) 25.0 | 31.8 | 33.
+//   Pages that one row alone reads go past the caches; of 512 rows of 14,000 keys with 32 pages each 61 us with plain loads, 70
+// so; of 64 rows of their own 43 so, 51 with plain loads (40/8 heads, 48 pages).
+inline PickedPlan picked_plan(const KvqCache& c, const KvqBatch& b, int n, int n_q) {
   const int G = n_q / c.n_kv;
   PickedPlan p;
   p.cols = G < 16 ? G : 16;
   p.col_tiles = (G + 15) / 16;
-  const int64_t blocks = std::max<int64_t>(1, static_cast<int64_t>(n_rows) * c.n_kv * p.col_tiles);
-  if (blocks < 512) p.items = static_cast<int>(std::min<int64_t>(kvq_items(n, kKvqTileItems, 8), std::max<int64_t>(1, 768 / blocks)));
+  const int64_t blocks = std::max<int64_t>(1, static_cast<int64_t>(b.n_rows) * c.n_kv * p.col_tiles);
+  p.shared = kvq_max_rows(b) > 1;
+  if (blocks <= 128 && n >= 32 && 2 * n >= blocks) p.items = static_cast<int>(std::min<int64_t>(kvq_items(n, kKvqTileItems, 4), 512 / blocks));
+  else if (blocks <= 256 && n > 16) p.waves = 8;
   return p;
 }
 
-inline int64_t picked_blocks(const KvqCache& c, int n_rows, const PickedPlan& p) { return static_cast<int64_t>(n_rows) * c.n_kv * p.col_tiles; }
+inline int64_t picked_blocks(const KvqCache& c, const KvqBatch& b, const PickedPlan& p) { return static_cast<int64_t>(b.n_rows) * c.n_kv * p.col_tiles; }
 
-inline size_t picked_part_floats(const KvqCache& c, int n_rows, const PickedPlan& p) {  // of the partial outputs
-  return p.items > 1 ? static_cast<size_t>(picked_blocks(c, n_rows, p)) * p.items * p.cols * c.hd : 0;
+inline size_t picked_part_floats(const KvqCache& c, const KvqBatch& b, const PickedPlan& p) {  // of the partial outputs
+  return p.items > 1 ? static_cast<size_t>(picked_blocks(c, b, p)) * p.items * p.cols * c.hd : 0;
 }
 // Bytes of the workspace of launch_kvq_attend_picked.
-inline size_t kvq_picked_bytes(const KvqCache& c, int n_rows, int n, int n_q) {
-  const size_t o = picked_part_floats(c, n_rows, picked_plan(c, n_rows, n, n_q));
+inline size_t kvq_picked_bytes(const KvqCache& c, const KvqBatch& b, int n, int n_q) {
+  const size_t o = picked_part_floats(c, b, picked_plan(c, b, n, n_q));
   return (o + o / c.hd * 2) * 4;
 }
 

@@ -229,9 +229,9 @@ void kvq_require_columns(const rollpack::KvqBatch& b, int32_t n) {
 size_t kvq_picked_size(const rollpack::KvqCache& c, const rollpack::KvqBatch& b, int32_t n_q, int32_t n) {
   kvq_require(n_q >= 1 && n_q <= 65536 && n_q % c.n_kv == 0, "n_q_heads must be a multiple of n_kv_heads");
   kvq_require(n >= 1 && n <= (1 << 24), "1 <= n_picks <= 2^24");
-  const rollpack::PickedPlan p = rollpack::picked_plan(c, b.n_rows, n, n_q);
-  kvq_require(rollpack::picked_blocks(c, b.n_rows, p) < (int64_t{1} << 22), "too many rows and heads for one call");
-  return rollpack::kvq_picked_bytes(c, b.n_rows, n, n_q);
+  const rollpack::PickedPlan p = rollpack::picked_plan(c, b, n, n_q);
+  kvq_require(rollpack::picked_blocks(c, b, p) < (int64_t{1} << 22), "too many rows and heads for one call");
+  return rollpack::kvq_picked_bytes(c, b, n, n_q);
 }
 
 }  // namespace
