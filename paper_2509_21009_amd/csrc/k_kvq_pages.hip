@@ -1,6 +1,7 @@
 // Pages of the 4-bit KV cache (kvq_pages.hpp): handing them out, the ranges of their keys, their scores for a query, and the
 // pages that are picked by these.
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.hpp"
 #include "kvq_device.hpp"
@@ -282,48 +283,96 @@ __global__ __launch_bounds__(256) void k_kvq_ranges(KvqCache c, KvqBatch bt, uin
 
 // ---- scores ------------------------------------------------------------------------------
 
-// The largest value orders last, and NaN, of either sign, after it.
-__device__ __forceinline__ int score_key(float x) {
-  const int b = x != x ? 0x7fc00000 : __float_as_int(x);
-  return b ^ ((b >> 31) & 0x7fffffff);
+// The larger of the two, NaN if one is.
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+// The same of a lane and the one of the next group of 16, of an even one, or of the one two groups on.
+__device__ __forceinline__ float larger_of_16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return larger(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
-__device__ __forceinline__ float score_of(int key) { return __int_as_float(key ^ ((key >> 31) & 0x7fffffff)); }
+__device__ __forceinline__ float larger_of_32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return larger(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
 
-// Eight queries of a lane as operands: NQ pieces of bf16 each of max(q, 0) and of min(q, 0).
-template <int NQ>
-__device__ __forceinline__ void split_signs(float (&x)[8], bf16x8_t (&above)[NQ], bf16x8_t (&below)[NQ]) {
+// Eight queries of a lane, as loaded.
+template <bool F32>
+struct Eight {
+  std::conditional_t<F32, float[8], u32x4> x;
+  __device__ __forceinline__ void load(const KvqTensor& t, int row, int head, int d) {
+    const int64_t at = row * t.row_stride + head * t.head_stride + d;
+    if constexpr (F32) {
+      load8<false>(t, row, head, d, x);
+    } else {
+      const bf16_t* p = static_cast<const bf16_t*>(t.p) + at;
+      if (t.vec) {
+        x = *reinterpret_cast<const u32x4*>(p);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = static_cast<uint32_t>(p[2 * i]) | static_cast<uint32_t>(p[2 * i + 1]) << 16;
+      }
+    }
+  }
+};
+
+// These as operands: pieces of bf16 (one, or three of fp32) of max(q, 0) and of min(q, 0).
+__device__ __forceinline__ void split_signs(const Eight<false>& q, bf16x8_t (&above)[1], bf16x8_t (&below)[1]) {
+  u32x4 up, down;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t neg = __builtin_bit_cast(uint32_t, as_pair(q.x[i]) >> 15);
+    up[i] = q.x[i] & ~neg;
+    down[i] = q.x[i] & neg;
+  }
+  above[0] = __builtin_bit_cast(bf16x8_t, up);
+  below[0] = __builtin_bit_cast(bf16x8_t, down);
+}
+__device__ __forceinline__ void split_signs(Eight<true>& q, bf16x8_t (&above)[3], bf16x8_t (&below)[3]) {
   u32x4 neg;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    neg[i] = (__float_as_int(x[2 * i]) < 0 ? 0xffffu : 0u) | (__float_as_int(x[2 * i + 1]) < 0 ? 0xffff0000u : 0u);
-  bf16x8_t q[NQ];
-  split8<NQ>(x, q);
+    neg[i] = (__float_as_int(q.x[2 * i]) < 0 ? 0xffffu : 0u) | (__float_as_int(q.x[2 * i + 1]) < 0 ? 0xffff0000u : 0u);
+  bf16x8_t p[3];
+  split8<3>(q.x, p);
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    const u32x4 w = __builtin_bit_cast(u32x4, q[n]);
+  for (int n = 0; n < 3; ++n) {
+    const u32x4 w = __builtin_bit_cast(u32x4, p[n]);
     above[n] = __builtin_bit_cast(bf16x8_t, w & ~neg);
     below[n] = __builtin_bit_cast(bf16x8_t, w & neg);
   }
 }
 
-// A block's four waves have 16 PT pages each of one KV head, for up to `rows` consecutive rows: the ranges of 16 pages are
-// the 16-row operands of 16x16x32 products, 2 hd long, the queries (RT rows' G heads side by side) the 16 columns.  The
-// heads' maximum is taken across lanes.
-template <int HD, bool F32, int PT>
-__global__ __launch_bounds__(256) void k_kvq_scores(KvqScoreArgs a, int rows) {
+// A block's four waves have 16 PT pages each of one KV head, for up to `rows` consecutive rows.  Queries are the 16 rows
+// of 16x16x32 products, 2 hd long, the ranges of 16 pages the 16 columns.  The G heads of a row take `seg` of the 16, a power of
+// two, the last head again in what is left of them, so that lane 16g + c gets four heads' scores of page c or whole rows':
+// their maximum is mostly the lane's own (with the heads in the columns, the maximum over lanes took 2,000 rows 51 us for 33).
+//   KEEP: rows of a sequence read the same ranges, a wave those of 32 or 64 pages for many rows.  Else they are read once, past
+// the caches, whole pages to an instruction, which LDS turns into operands: 64 rows of 6,000 to 33,000 keys (8 KV heads of 128)
+// 22 us, 3.7 TB/s, from HBM; read as operands, 64 bytes of a page to an instruction, 27.7 (24.5 with plain loads).  A wave's
+// way there is context and table, ranges, product: three reads that wait for each other; four heads of a page to a block took
+// 26 us, 32 pages to a wave 25.
+template <int HD, bool F32, int PT, bool KEEP>
+__global__ __launch_bounds__(256, KEEP || F32 ? 2 : 4) void k_kvq_scores(KvqScoreArgs a, int rows) {
   constexpr int NJ = HD / 32, NQ = F32 ? 3 : 1;
+  constexpr int NPC = HD / 4, NI = NPC / 4;  // 16-byte pieces of a page's ranges; loads of 16 pages
+  __shared__ u32x4 turn[KEEP ? 1 : 4][KEEP ? 1 : 16 * NPC];
   const KvqBatch& bt = a.batch;
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n_kv = a.cache.n_kv, G = a.n_q / n_kv, seg = min(G, 16), rt = 16 / seg;
+  const int n_kv = a.cache.n_kv, G = a.n_q / n_kv;
+  const int seg_log = G > 8 ? 4 : G > 4 ? 3 : G > 2 ? 2 : G > 1 ? 1 : 0, seg = 1 << seg_log, rt = 16 >> seg_log;
   const int group = blockIdx.x / n_kv, kh = blockIdx.x - group * n_kv;
   const int p0 = (blockIdx.y * 4 + wave) * 16 * PT;
   if (p0 >= a.columns) return;
-  const int last_row = min((group + 1) * rows, bt.n_rows);
-  const int col_row = c / seg, col_head = c - col_row * seg;
+  const int last_row = min((group + 1) * rows, bt.n_rows), most = kvq_pages(bt.max_context) - 1;
   for (int r = group * rows; r < last_row;) {
     const int b = wave_find_seq(bt, r);
     if (b < 0) return;
+    // entries of the table beside the context; those past it may be anything
+    int id[PT];
+    const int32_t* pt = table_of(bt, b);
+#pragma unroll
+    for (int t = 0; t < PT; ++t) id[t] = most >= 0 ? pt[min(p0 + 16 * t + c, most)] : -1;
     const KvqSeq sq = kvq_seq(bt, b);
     const int i = r - sq.r0;
     if (i < 0 || i >= sq.n) {  // past max_rows
@@ -333,87 +382,106 @@ __global__ __launch_bounds__(256) void k_kvq_scores(KvqScoreArgs a, int rows) {
     const int n = min(last_row, sq.r0 + sq.n) - r, first = sq.ctx - sq.n + i;  // rows, the first one's position
     const int seen = sq.ok ? (first + n - 1) >> 6 : -1;                           // the last page that some row sees
     bf16x8_t hi[PT][NJ], lo[PT][NJ];
-    uint64_t lost[PT];
-    if (p0 <= seen) {
-      const int32_t* pt = table_of(bt, b);
+    bool ok[PT];  // the lane's page is in the cache
 #pragma unroll
-      for (int t = 0; t < PT; ++t) {
-        const int p = p0 + 16 * t + c;
-        const int id = pt[min(p, seen)];
-        const bool ok = kvq_page_ok(a.cache, id);
-        lost[t] = __ballot(!ok);
-        const uint16_t* at = a.ranges + (static_cast<size_t>(ok ? id : 0) * n_kv + kh) * 2 * HD + 16 * g;
+    for (int t = 0; t < PT; ++t) {
+      ok[t] = kvq_page_ok(a.cache, id[t]);
+      if (p0 + 16 * t > seen) continue;
+      const int use = ok[t] && p0 + 16 * t + c <= seen ? id[t] : 0;  // others read what page 0 has
+      const u32x4* ranges = reinterpret_cast<const u32x4*>(a.ranges);
+      if constexpr (KEEP) {
+        const u32x4* at = ranges + (static_cast<size_t>(use) * n_kv + kh) * NPC + 2 * g;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {  // a line of 128 bytes is four lanes' two pieces
+          lo[t][j] = __builtin_bit_cast(bf16x8_t, at[8 * (j >> 1) + (j & 1)]);
+          hi[t][j] = __builtin_bit_cast(bf16x8_t, at[NPC / 2 + 8 * (j >> 1) + (j & 1)]);
+        }
+      } else {
+        u32x4 x[NI];
+#pragma unroll
+        for (int k = 0; k < NI; ++k) {
+          const size_t page = __shfl(use, k * (64 / NPC) + lane / NPC, 64);
+          x[k] = load_page<true>(ranges + (page * n_kv + kh) * NPC + lane % NPC);
+        }
+#pragma unroll
+        for (int k = 0; k < NI; ++k) {
+          const int page = k * (64 / NPC) + lane / NPC;
+          turn[wave][page * NPC + (lane % NPC ^ page)] = x[k];
+        }
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
-          lo[t][j] = load_bf16x8(at + 64 * (j >> 1) + 8 * (j & 1));
-          hi[t][j] = load_bf16x8(at + HD + 64 * (j >> 1) + 8 * (j & 1));
+          const int piece = 8 * (j >> 1) + 2 * g + (j & 1);
+          lo[t][j] = __builtin_bit_cast(bf16x8_t, turn[wave][c * NPC + (piece ^ c)]);
+          hi[t][j] = __builtin_bit_cast(bf16x8_t, turn[wave][c * NPC + ((piece + NPC / 2) ^ c)]);
         }
       }
     }
-    for (int q0 = 0; q0 < n; q0 += rt) {
-      const int mine = q0 + min(col_row, rt - 1), row = r + min(mine, n - 1);
-      const bool real = col_row < rt && mine < n;
-      int best[PT][4];
+    // The scores of the mine-th of these rows for the lane's pages: those that it does not see have minus infinity.
+    auto store = [&](int mine, int t, float x) {
+      const int p = p0 + 16 * t + c;
+      if (!ok[t] || !sq.ok) x = __builtin_nanf("");
+      if (sq.ok && p > (first + mine) >> 6) x = -INFINITY;
+      if (mine < n && p < a.columns) a.scores[(static_cast<size_t>(r + mine) * n_kv + kh) * a.columns + p] = x;
+    };
+    if (p0 > seen) {  // nothing to see for any row, or for none to know
+      for (int q0 = 0; q0 < n; q0 += 4)
 #pragma unroll
-      for (int t = 0; t < PT; ++t)
+        for (int t = 0; t < PT; ++t) store(q0 + g, t, 0.f);
+      r += n;
+      continue;
+    }
+    // Units of 16 query rows: `parts` of each rt rows; a unit's queries are loaded a unit ahead.
+    const int parts = (G + 15) >> 4, units = (n + rt - 1) / rt * parts;
+    Eight<F32> q[NJ];
+    auto load = [&](int u) {
+      const int tile = u / parts, h0 = 16 * (u - tile * parts);
+      const int row = r + min(tile * rt + (c >> seg_log), n - 1), head = kh * G + min(h0 + (c & (seg - 1)), G - 1);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) best[t][e] = -0x7fffffff - 1;
-      if (p0 <= seen) {
-        for (int h0 = 0; h0 < G; h0 += 16) {
-          const bool some = col_head + h0 < G;
-          const int head = kh * G + min(h0 + col_head, G - 1);
-          f32x4_t acc[PT];
+      for (int j = 0; j < NJ; ++j) q[j].load(a.q, row, head, 64 * (j >> 1) + 16 * g + 8 * (j & 1));
+    };
+    load(0);
+    f32x4_t best[PT];
+    for (int u = 0; u < units; ++u) {
+      const int tile = u / parts, part = u - tile * parts;
+      f32x4_t acc[PT];
 #pragma unroll
-          for (int t = 0; t < PT; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-          float x[NJ][8];
+      for (int t = 0; t < PT; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      bf16x8_t above[NJ][NQ], below[NJ][NQ];
 #pragma unroll
-          for (int j = 0; j < NJ; ++j) load8<!F32>(a.q, row, head, 64 * (j >> 1) + 16 * g + 8 * (j & 1), x[j]);
+      for (int j = 0; j < NJ; ++j) split_signs(q[j], above[j], below[j]);
+      if (u + 1 < units) load(u + 1);
 #pragma unroll
-          for (int j = 0; j < NJ; ++j) {
-            bf16x8_t above[NQ], below[NQ];
-            split_signs<NQ>(x[j], above, below);
+      for (int j = 0; j < NJ; ++j)
 #pragma unroll
-            for (int t = 0; t < PT; ++t)
+        for (int m = 0; m < NQ; ++m)
 #pragma unroll
-              for (int m = 0; m < NQ; ++m) {
-                acc[t] = mfma16x16x32(hi[t][j], above[m], acc[t]);
-                acc[t] = mfma16x16x32(lo[t][j], below[m], acc[t]);
-              }
+          for (int t = 0; t < PT; ++t) {
+            acc[t] = mfma16x16x32(above[j][m], hi[t][j], acc[t]);
+            acc[t] = mfma16x16x32(below[j][m], lo[t][j], acc[t]);
           }
-#pragma unroll
-          for (int t = 0; t < PT; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (some) best[t][e] = max(best[t][e], score_key(acc[t][e]));
-        }
-        // Over the row's lanes: the first one's maximum covers 1, 2, 4, 8 and 16 of them, no further than the row's.
-        auto over = [&](auto tag, int step) {
-          const bool in = col_head + step < seg;
-#pragma unroll
-          for (int t = 0; t < PT; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int y = __builtin_amdgcn_update_dpp(0, best[t][e], decltype(tag)::value, 0xf, 0xf, true);
-              if (in) best[t][e] = max(best[t][e], y);
-            }
-        };
-        if (seg > 1) over(std::integral_constant<int, 0x101>{}, 1);
-        if (seg > 2) over(std::integral_constant<int, 0x102>{}, 2);
-        if (seg > 4) over(std::integral_constant<int, 0x104>{}, 4);
-        if (seg > 8) over(std::integral_constant<int, 0x108>{}, 8);
-      }
-      if (real && col_head == 0) {
-        const int pages = (first + mine) >> 6;  // the last one that the row sees
-        float* out = a.scores + (static_cast<size_t>(row) * n_kv + kh) * a.columns;
+      if (parts > 1) {  // of one row
 #pragma unroll
         for (int t = 0; t < PT; ++t)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int p = p0 + 16 * t + 4 * g + e;
-            float v = !sq.ok ? __builtin_nanf("") : -INFINITY;
-            if (sq.ok && p <= pages) v = (lost[t] >> (4 * g + e)) & 1 ? __builtin_nanf("") : score_of(best[t][e]);
-            if (p < a.columns) out[p] = v;
-          }
+          for (int e = 0; e < 4; ++e) best[t][e] = acc[t][e] = part ? larger(best[t][e], acc[t][e]) : acc[t][e];
+        if (part + 1 < parts) continue;
+      }
+      const int row0 = tile * rt;
+#pragma unroll
+      for (int t = 0; t < PT; ++t) {
+        if (seg >= 4) {
+          float x = larger(larger(larger(acc[t][0], acc[t][1]), acc[t][2]), acc[t][3]);
+          if (seg >= 8) x = larger_of_16(x);
+          if (seg == 16) x = larger_of_32(x);
+          if ((4 * g & (seg - 1)) == 0) store(row0 + (4 * g >> seg_log), t, x);
+        } else if (seg == 2) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) store(row0 + 2 * g + e, t, larger(acc[t][2 * e], acc[t][2 * e + 1]));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) store(row0 + 4 * g + e, t, acc[t][e]);
+        }
       }
     }
     r += n;
@@ -607,12 +675,14 @@ hipError_t launch_kvq_ranges(const KvqCache& c, const KvqBatch& b, uint16_t* ran
 }
 
 hipError_t launch_kvq_scores(const KvqScoreArgs& a, hipStream_t s) {
-  const int n_kv = a.cache.n_kv;
-  int rows = 1;
-  const dim3 grid(static_cast<uint32_t>(static_cast<int64_t>((a.batch.n_rows + rows - 1) / rows) * n_kv), static_cast<uint32_t>((a.columns + 63) / 64));
-#define RP_SCORES(HD, BF16) \
-  if (a.cache.hd == HD && static_cast<bool>(a.q.bf16) == BF16) launch_kernel((k_kvq_scores<HD, !BF16, 1>), grid, dim3(256), 0, s, a, rows);
-  RP_SCORES(128, true) RP_SCORES(128, false) RP_SCORES(64, true) RP_SCORES(64, false)
+  const ScorePlan p = score_plan(a.cache, a.batch, a.columns, a.q.bf16);
+  const dim3 grid(static_cast<uint32_t>(p.groups * a.cache.n_kv), static_cast<uint32_t>((a.columns + 64 * p.tiles - 1) / (64 * p.tiles)));
+#define RP_SCORES(HD, BF16, PT, KEEP)                                                                                \
+  if (a.cache.hd == HD && static_cast<bool>(a.q.bf16) == BF16 && p.tiles == PT && static_cast<bool>(p.shared) == KEEP) \
+    launch_kernel((k_kvq_scores<HD, !BF16, PT, KEEP>), grid, dim3(256), 0, s, a, p.rows);
+#define RP_SCORES_HD(HD) RP_SCORES(HD, true, 1, false) RP_SCORES(HD, false, 1, false) RP_SCORES(HD, true, 2, true) RP_SCORES(HD, false, 2, true) RP_SCORES(HD, true, 4, true)
+  RP_SCORES_HD(128) RP_SCORES_HD(64)
+#undef RP_SCORES_HD
 #undef RP_SCORES
   return hipGetLastError();
 }

@@ -46,6 +46,26 @@ struct KvqScoreArgs {
   int n_q = 0, columns = 0;
 };
 
+// How a call of scores is cut: `rows` consecutive rows and 16 `tiles` pages to a wave, more rows the more waves there are.
+// 28/4 heads of 128, us, tiles/rows: 512 rows of 14,000 keys 1/1 42, 2/4 12.8, 2/8 10.0, 2/16 10.5, 4/16 14.2; 2,000 of 30,000
+// 2/8 58, 2/16 52, 4/8 52, 4/32 33, 4/64 42; 9 rows each of 64 sequences in fp32 2/1 23, 2/4 16.7, 2/16 20.5.
+struct ScorePlan {
+  int rows = 1, tiles = 1;
+  int64_t groups = 0;  // of rows
+  int shared = 0;      // rows of a sequence read the same ranges
+};
+inline ScorePlan score_plan(const KvqCache& c, const KvqBatch& b, int columns, bool bf16) {
+  ScorePlan p;
+  p.shared = kvq_max_rows(b) > 1;
+  auto waves = [&](int rows, int tiles) { return (static_cast<int64_t>(b.n_rows) + rows - 1) / rows * c.n_kv * ((columns + 16 * tiles - 1) / (16 * tiles)); };
+  if (p.shared) {
+    p.tiles = bf16 && waves(32, 4) >= 1600 ? 4 : 2;
+    while (p.rows < 32 && waves(2 * p.rows, p.tiles) >= 1600) p.rows *= 2;
+  }
+  p.groups = (static_cast<int64_t>(b.n_rows) + p.rows - 1) / p.rows;
+  return p;
+}
+
 struct KvqPickArgs {
   KvqBatch batch;
   const float* scores = nullptr;  // [n_rows][n_kv][columns]
