@@ -23,31 +23,11 @@ typedef short s16x2 __attribute__((ext_vector_type(2)));
 // same launch where they are few): a row's page is new or in the table, and the first row of a new page enters it there.
 
 constexpr int kFitThreads = 1024;
+constexpr int kFitRows1 = 8192;  // rows that the first launch takes, four to a thread at a time
 
-// Sums over the block's threads up to each thread (its own included), of three values; the totals in `total`.
-__device__ __forceinline__ void block_scan3(int (&x)[3], int (&total)[3], int (*lds)[3]) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  constexpr int kWaves = kFitThreads / 64;
-#pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    x[i] = wave_scan(x[i]);
-    if (lane == 63) lds[wave][i] = x[i];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    const int s = wave_scan(lane < kWaves ? lds[lane][i] : 0);
-    total[i] = __builtin_amdgcn_readlane(s, 63);
-    const int before = __shfl(s, wave > 0 ? wave - 1 : 0, 64);
-    x[i] += wave > 0 ? before : 0;
-  }
-  __syncthreads();
-}
-
-// The last of 0 .. n - 1 whose start is not past j, of starts that do not descend.
+// The last of lo .. hi whose start is not past j, of starts that do not descend.
 template <typename F>
-__device__ __forceinline__ int last_from(int lo, int n, int j, F start) {
-  int hi = n - 1;
+__device__ __forceinline__ int last_from(int lo, int hi, int j, F start) {
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (start(mid) <= j) lo = mid; else hi = mid - 1;
@@ -55,39 +35,41 @@ __device__ __forceinline__ int last_from(int lo, int n, int j, F start) {
   return lo;
 }
 
-// Row r of a sequence: its position and slot, and the page's entry where it is the first of a new one.  top: entries of the
-// list with those given back, from whose end the needed pages are taken.
-__device__ __forceinline__ void fit_row(const KvqFitArgs& a, int r, int b, int off, int end, int first_need, int top) {
-  const int len = a.pool.context[b], first = len - (end - off), pos = first + (r - off);
-  const int page = pos / kKvqPage, have = kvq_pages(first);
-  int32_t* entry = a.pool.page_table + b * a.pool.table_stride + page;
-  int id;
-  if (page >= have) {
-    id = a.pool.free_pages[top - 1 - (first_need + page - have)];
-    if (pos % kKvqPage == 0) *entry = id;
-  } else {
-    id = *entry;
-  }
-  a.position[r] = pos;
-  a.slot[r] = id * kKvqPage + pos % kKvqPage;
+// Row r, of a sequence whose rows are off .. end - 1 and that needs pages from the first_need-th on: its position and slot, and
+// the page's entry where it is the first of a new one.  top: entries of the list with those given back, from whose end pages are
+// taken.
+struct FitRow {
+  int pos, id;
+  bool enters;  // its page into the table
+};
+__device__ __forceinline__ FitRow fit_row(const KvqFitArgs& a, int r, int b, int len, int off, int end, int first_need, int top) {
+  const int first = len - (end - off), pos = first + (r - off), page = pos / kKvqPage, have = kvq_pages(first);
+  const bool fresh = page >= have;
+  const int32_t* from = fresh ? a.pool.free_pages + (top - 1 - (first_need + page - have)) : a.pool.page_table + b * a.pool.table_stride + page;
+  return {pos, *from, fresh && pos % kKvqPage == 0};
+}
+__device__ __forceinline__ void fit_store(const KvqFitArgs& a, int r, int b, const FitRow& f) {
+  if (f.enters) a.pool.page_table[b * a.pool.table_stride + f.pos / kKvqPage] = f.id;
+  a.position[r] = f.pos;
+  a.slot[r] = f.id * kKvqPage + f.pos % kKvqPage;
 }
 
 __global__ __launch_bounds__(kFitThreads) void k_kvq_fit(KvqFitArgs a, int with_rows) {
-  __shared__ int scan[kFitThreads / 64][3];
-  __shared__ int64_t sums[kFitThreads / 64][3];
-  __shared__ int flags;
-  __shared__ int back_from[kFitThreads], want_of[kFitThreads];
+  constexpr int kWaves = kFitThreads / 64;
+  __shared__ int64_t sums[kWaves][3];
+  __shared__ int scan[kWaves][3], flags[kWaves];
+  __shared__ int start[3][kFitThreads + 1], length_of[kFitThreads];  // of a tile's sequences: pages needed, given back, rows before
   const KvqPool& pool = a.pool;
-  const int tid = threadIdx.x, lane = tid & 63, n = pool.n_seqs;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = pool.n_seqs;
   const int n_free = pool.state[0];
 
-  // What all sequences need and give back, in 64 bits; anything out of bounds.
-  if (tid == 0) flags = 0;
-  __syncthreads();
-  int64_t all[3] = {0, 0, 0};  // needed, given back, rows
-  bool bad_len = false, bad_pool = n_free < 0 || n_free > pool.n_pages;
+  // What all sequences need, give back and add, in 64 bits; anything out of bounds.
+  int64_t all[3] = {0, 0, 0};
+  bool bad_len = false, bad_pool = false;
+  int old = 0, len = 0;  // the thread's last sequence, its only one where there are no more than threads
   for (int b = tid; b < n; b += kFitThreads) {
-    const int old = pool.context[b], len = a.length[b];
+    old = pool.context[b];
+    len = a.length[b];
     const bool bl = len < 0 || len > pool.max_context, bp = old < 0 || old > pool.max_context;
     bad_len |= bl;
     bad_pool |= bp;
@@ -97,56 +79,81 @@ __global__ __launch_bounds__(kFitThreads) void k_kvq_fit(KvqFitArgs a, int with_
     all[1] += max(0, have - want);
     all[2] += max(0, len - old);
   }
-  if (bad_len) atomicOr(&flags, 1);
-  if (bad_pool) atomicOr(&flags, 2);
+  const uint64_t any_len = __ballot(bad_len), any_pool = __ballot(bad_pool);
 #pragma unroll
-  for (int i = 0; i < 3; ++i) {
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) all[i] += __shfl_xor(static_cast<long long>(all[i]), m, 64);
-    if (lane == 0) sums[tid >> 6][i] = all[i];
+  for (int i = 0; i < 3; ++i) {  // at most 2^10 sequences of 2^30 to a thread: halves of 20 bits, whose sums fit
+    const int low = wave_scan(static_cast<int>(all[i] & 0xfffff)), high = wave_scan(static_cast<int>(all[i] >> 20));
+    if (lane == 63) sums[wave][i] = (static_cast<int64_t>(high) << 20) + low;
   }
+  if (lane == 0) flags[wave] = (any_len ? 1 : 0) | (any_pool ? 2 : 0);
   __syncthreads();
   int64_t need = 0, back = 0, rows = 0;
-  for (int w = 0; w < kFitThreads / 64; ++w) {
+  int flag = n_free < 0 || n_free > pool.n_pages ? 2 : 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
     need += sums[w][0];
     back += sums[w][1];
     rows += sums[w][2];
+    flag |= flags[w];
   }
   const int64_t short_of = need - back - n_free;
-  const int error = (flags & 2) || n_free + back > pool.n_pages ? kFitPool : (flags & 1) ? kFitLength : short_of > 0 ? kFitPages
+  const int error = (flag & 2) || n_free + back > pool.n_pages ? kFitPool : (flag & 1) ? kFitLength : short_of > 0 ? kFitPages
                     : rows > a.n_rows ? kFitRows : kFitOk;
   const bool failed = error != kFitOk;  // nothing changes: no rows
   const int top = n_free + static_cast<int>(failed ? 0 : back);
   int carry[3] = {0, 0, 0};
   for (int b0 = 0; b0 < n; b0 += kFitThreads) {
     const int b = b0 + tid, here = min(kFitThreads, n - b0);
-    int x[3] = {0, 0, 0}, total[3], len = 0, want = 0;
-    if (b < n && !failed) {
-      const int old = pool.context[b];
+    if (n > kFitThreads && b < n) {
+      old = pool.context[b];
       len = a.length[b];
-      const int have = kvq_pages(old);
-      want = kvq_pages(len);
+    }
+    int x[3] = {0, 0, 0}, mine[3], total[3];
+    if (b < n && !failed) {
+      const int have = kvq_pages(old), want = kvq_pages(len);
       x[0] = max(0, want - have);
       x[1] = max(0, have - want);
       x[2] = max(0, len - old);
     }
-    const int mine[3] = {x[0], x[1], x[2]};
-    block_scan3(x, total, scan);
-    if (b < n) {
-      a.row_off[b] = carry[2] + x[2] - mine[2];
-      pool.first_need[b] = carry[0] + x[0] - mine[0];
-      if (!failed) pool.context[b] = len;
-    }
-    back_from[tid] = x[1] - mine[1];
-    want_of[tid] = want;
-    __syncthreads();
-    for (int j = tid; j < total[1]; j += kFitThreads) {
-      const int s = last_from(0, here, j, [&](int i) { return back_from[i]; });
-      pool.free_pages[top - 1 - (carry[1] + j)] = pool.page_table[(b0 + s) * pool.table_stride + want_of[s] + (j - back_from[s])];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      mine[i] = wave_scan(x[i]);
+      if (lane == 63) scan[wave][i] = mine[i];
+      mine[i] -= x[i];
     }
     __syncthreads();
 #pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      const int before = wave_scan(lane < kWaves ? scan[lane][i] : 0);
+      total[i] = __builtin_amdgcn_readlane(before, 63);
+      mine[i] += wave > 0 ? __builtin_amdgcn_readlane(before, wave - 1) : 0;
+      start[i][tid] = mine[i];
+    }
+    length_of[tid] = len;
+    if (b < n) {
+      a.row_off[b] = carry[2] + mine[2];
+      pool.first_need[b] = carry[0] + mine[0];
+      if (!failed) pool.context[b] = len;
+    }
+    __syncthreads();
+    for (int j0 = tid; j0 < total[1]; j0 += 4 * kFitThreads) {  // pages given back, four at a time
+      int page[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int j = j0 + k * kFitThreads;
+        if (j >= total[1]) continue;
+        const int s = last_from(0, here - 1, j, [&](int i) { return start[1][i]; });
+        page[k] = pool.page_table[(b0 + s) * pool.table_stride + kvq_pages(length_of[s]) + (j - start[1][s])];
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int j = j0 + k * kFitThreads;
+        if (j < total[1]) pool.free_pages[top - 1 - (carry[1] + j)] = page[k];
+      }
+    }
+#pragma unroll
     for (int i = 0; i < 3; ++i) carry[i] += total[i];
+    __syncthreads();
   }
   if (tid == 0) {
     a.row_off[n] = carry[2];
@@ -157,26 +164,69 @@ __global__ __launch_bounds__(kFitThreads) void k_kvq_fit(KvqFitArgs a, int with_
     if (!failed) pool.state[0] = top - carry[0];
   }
   if (!with_rows) return;
+  // The rows, of sequences that are all in LDS.
+  if (tid == 0) start[2][n] = carry[2];
   __syncthreads();
-  for (int r = tid; r < a.n_rows; r += kFitThreads) {
-    if (r >= carry[2]) {
-      a.position[r] = a.slot[r] = -1;
-      continue;
+  for (int r0 = tid; r0 < a.n_rows; r0 += 4 * kFitThreads) {
+    FitRow f[4];
+    int b[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int r = r0 + k * kFitThreads;
+      if (r >= carry[2]) continue;
+      b[k] = last_from(0, n - 1, r, [&](int i) { return start[2][i]; });
+      f[k] = fit_row(a, r, b[k], length_of[b[k]], start[2][b[k]], start[2][b[k] + 1], start[0][b[k]], top);
     }
-    const int b = last_from(0, n, r, [&](int i) { return a.row_off[i]; });
-    fit_row(a, r, b, a.row_off[b], a.row_off[b + 1], pool.first_need[b], top);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int r = r0 + k * kFitThreads;
+      if (r < carry[2]) fit_store(a, r, b[k], f[k]);
+      else if (r < a.n_rows) a.position[r] = a.slot[r] = -1;
+    }
   }
 }
 
+// A block has 1,024 rows, a wave 256: its first and last row's sequences are found 64 at a time.  Up to 64 sequences from the one to
+// the other are a lane's each, where the rows look theirs up.
 __global__ __launch_bounds__(256) void k_kvq_fit_rows(KvqFitArgs a) {
-  const int n = a.pool.n_seqs, r = blockIdx.x * 256 + threadIdx.x;
-  if (r >= a.n_rows) return;
-  if (r >= a.row_off[n]) {
-    a.position[r] = a.slot[r] = -1;
-    return;
+  const int n = a.pool.n_seqs, lane = threadIdx.x & 63;
+  const int r0 = blockIdx.x * 1024 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 256;
+  if (r0 >= a.n_rows) return;
+  KvqBatch bt;
+  bt.n_seqs = n;
+  bt.row_off = a.row_off;
+  const int total = a.row_off[n], top = a.pool.first_need[n], last = min(r0 + 255, a.n_rows - 1);
+  const int lo = wave_find_seq(bt, r0);  // -1: all behind the last
+  int hi = wave_find_seq(bt, last);
+  FitRow f[4];
+  int b[4];
+  if (lo >= 0) {
+    if (hi < 0) hi = n - 1;
+    const int mine = min(lo + lane, n - 1);
+    const int off = a.row_off[mine], end = a.row_off[mine + 1], len = a.pool.context[mine], need = a.pool.first_need[mine];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int r = r0 + k * 64 + lane;
+      if (hi - lo < 64) {  // the same in every lane
+        int s = 0;
+#pragma unroll
+        for (int step = 32; step >= 1; step >>= 1)
+          if (__shfl(off, s + step, 64) <= r && lo + s + step <= hi) s += step;
+        b[k] = lo + s;
+        const int l = __shfl(len, s, 64), o = __shfl(off, s, 64), e = __shfl(end, s, 64), d = __shfl(need, s, 64);
+        if (r < total) f[k] = fit_row(a, r, b[k], l, o, e, d, top);
+      } else if (r < total) {
+        b[k] = last_from(lo, hi, r, [&](int i) { return a.row_off[i]; });
+        f[k] = fit_row(a, r, b[k], a.pool.context[b[k]], a.row_off[b[k]], a.row_off[b[k] + 1], a.pool.first_need[b[k]], top);
+      }
+    }
   }
-  const int b = last_from(0, n, r, [&](int i) { return a.row_off[i]; });
-  fit_row(a, r, b, a.row_off[b], a.row_off[b + 1], a.pool.first_need[b], a.pool.first_need[n]);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int r = r0 + k * 64 + lane;
+    if (r < total) fit_store(a, r, b[k], f[k]);
+    else if (r < a.n_rows) a.position[r] = a.slot[r] = -1;
+  }
 }
 
 // ---- ranges ------------------------------------------------------------------------------
@@ -657,9 +707,9 @@ __global__ __launch_bounds__(kPickThreads) void k_kvq_pick_long(KvqPickArgs a) {
 }  // namespace
 
 hipError_t launch_kvq_fit(const KvqFitArgs& a, hipStream_t s) {
-  const int with_rows = a.n_rows <= 4096;
+  const int with_rows = a.n_rows <= kFitRows1 && a.pool.n_seqs <= kFitThreads;
   launch_kernel(k_kvq_fit, dim3(1), dim3(kFitThreads), 0, s, a, with_rows);
-  if (!with_rows) launch_kernel(k_kvq_fit_rows, dim3(static_cast<uint32_t>((a.n_rows + 255) / 256)), dim3(256), 0, s, a);
+  if (!with_rows && a.n_rows > 0) launch_kernel(k_kvq_fit_rows, dim3(static_cast<uint32_t>((a.n_rows + 1023) / 1024)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -961,22 +961,24 @@ class KvqPages:
 
     def __init__(self, n_pages: int, n_seqs: int, max_context: int, device="cuda"):
         import torch
-        for name, x, most in (("n_pages", n_pages, 1 << 24), ("n_seqs", n_seqs, 1 << 20), ("max_context", max_context, 1 << 30)):
-            if not (n_pages >= 1 and 0 <= x <= most):
-                raise ValueError(f"{name} must be between {int(name == 'n_pages')} and {most}, got {x}")
+        for name, x, least, most in (("n_pages", n_pages, 1, 1 << 24), ("n_seqs", n_seqs, 0, 1 << 20),
+                                     ("max_context", max_context, 0, 1 << 30)):
+            if not least <= x <= most:
+                raise ValueError(f"{name} must be between {least} and {most}, got {x}")
         self.torch, self.n_pages, self.n_seqs, self.max_context = torch, n_pages, n_seqs, max_context
-        ints = lambda *dims: torch.zeros(dims, dtype=torch.int32, device=device)  # noqa: E731
-        self.page_table = ints(n_seqs, max(1, -(-max_context // 64)))
-        self.contexts = ints(n_seqs)
-        self.free_pages = torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device)  # page 0 goes first
-        self.state, self._workspace = ints(4), ints(n_seqs + 1)
+        self._ints = dict(dtype=torch.int32, device=device)
+        self.page_table = torch.zeros((n_seqs, max(1, -(-max_context // 64))), **self._ints)
+        self.contexts = torch.zeros(n_seqs, **self._ints)
+        self.free_pages = torch.arange(n_pages - 1, -1, -1, **self._ints)  # page 0 goes first
+        self.state, self._workspace = torch.zeros(4, **self._ints), torch.zeros(n_seqs + 1, **self._ints)
         self.state[0] = n_pages
-        self.device = self.state.device
+        self.device = self._ints["device"] = self.state.device
         if self.device.type != "cuda":
             raise ValueError("the pool lives in GPU memory")
-        self.struct = RpKvqPool(self.page_table.data_ptr(), self.page_table.shape[1], self.contexts.data_ptr(),
-                                self.free_pages.data_ptr(), self.state.data_ptr(), self._workspace.data_ptr(), n_seqs, max_context,
-                                n_pages)
+        self._contexts_at, self._table_at, self._table_stride = self.contexts.data_ptr(), self.page_table.data_ptr(), self.page_table.shape[1]
+        self.struct = RpKvqPool(self._table_at, self._table_stride, self._contexts_at, self.free_pages.data_ptr(), self.state.data_ptr(),
+                                self._workspace.data_ptr(), n_seqs, max_context, n_pages)
+        self._raw_stream = torch._C._cuda_getCurrentRawStream  # the handle alone, as KvqCache has it
 
     def fit(self, lengths, n_rows: int, max_rows: Optional[int] = None, max_context: Optional[int] = None):
         """Give each sequence the pages of its new length (int32 tensor [n_seqs]), take back those of what it no longer has.
@@ -984,22 +986,26 @@ class KvqPages:
         each row's position, and 64 * page + position % 64, -1 in padded rows (int32 tensors).
         n_rows bounds the new tokens of all sequences, max_rows those of one (n_rows), max_context the lengths (the pool's).
         What does not fit shows in state[1] (status()): then nothing changed and there are no rows."""
-        torch = self.torch
-        if lengths.dtype != torch.int32 or lengths.device != self.device or lengths.shape != (self.n_seqs,) or not lengths.is_contiguous():
-            raise ValueError(f"lengths are a contiguous int32 tensor [{self.n_seqs}] on {self.device}, got {lengths.dtype} "
+        torch, n_seqs = self.torch, self.n_seqs
+        if lengths.dtype != torch.int32 or lengths.device != self.device or lengths.shape != (n_seqs,) or not lengths.is_contiguous():
+            raise ValueError(f"lengths are a contiguous int32 tensor [{n_seqs}] on {self.device}, got {lengths.dtype} "
                              f"{tuple(lengths.shape)} on {lengths.device}")
         max_rows = n_rows if max_rows is None else max_rows
         max_context = self.max_context if max_context is None else max_context
-        for name, x, most in (("n_rows", n_rows, 1 << 24), ("max_rows", max_rows, n_rows), ("max_context", max_context, self.max_context)):
-            if not 0 <= x <= most:
-                raise ValueError(f"{name} must be between 0 and {most}, got {x}")
-        ints = lambda n: torch.empty(n, dtype=torch.int32, device=self.device)  # noqa: E731
-        off, positions, slots = ints(self.n_seqs + 1), ints(n_rows), ints(n_rows)
-        with torch.cuda.device(self.device):
-            rp_kvq_fit_pages(self.struct, lengths.data_ptr(), n_rows, off.data_ptr(), positions.data_ptr(), slots.data_ptr(),
-                             torch._C._cuda_getCurrentRawStream(self.device.index))
-        b = RpKvqBatch(self.n_seqs, n_rows, max_rows, max_context, off.data_ptr(), self.contexts.data_ptr(),
-                       self.page_table.data_ptr(), self.page_table.shape[1])
+        if not (0 <= n_rows <= 1 << 24 and 0 <= max_rows <= n_rows and 0 <= max_context <= self.max_context):
+            raise ValueError(f"n_rows must be between 0 and 2^24, max_rows between 0 and n_rows, max_context between 0 and "
+                             f"{self.max_context}, got {n_rows}, {max_rows}, {max_context}")
+        off = torch.empty(n_seqs + 1, **self._ints)
+        positions, slots = torch.empty(n_rows, **self._ints), torch.empty(n_rows, **self._ints)
+        at = off.data_ptr()
+        if torch.cuda.current_device() == self.device.index:
+            rp_kvq_fit_pages(self.struct, lengths.data_ptr(), n_rows, at, positions.data_ptr(), slots.data_ptr(),
+                             self._raw_stream(self.device.index))
+        else:
+            with torch.cuda.device(self.device):
+                rp_kvq_fit_pages(self.struct, lengths.data_ptr(), n_rows, at, positions.data_ptr(), slots.data_ptr(),
+                                 self._raw_stream(self.device.index))
+        b = RpKvqBatch(n_seqs, n_rows, max_rows, max_context, at, self._contexts_at, self._table_at, self._table_stride)
         return KvqBatch(b, (self.contexts, self.page_table, off)), positions, slots
 
     def status(self) -> dict:
