@@ -231,102 +231,137 @@ __global__ __launch_bounds__(256) void k_kvq_fit_rows(KvqFitArgs a) {
 
 // ---- ranges ------------------------------------------------------------------------------
 
+__device__ __forceinline__ s16x2 as_pair(uint32_t x) { return __builtin_bit_cast(s16x2, x); }
+__device__ __forceinline__ uint32_t as_word(s16x2 x) { return __builtin_bit_cast(uint32_t, x); }
+
+// Two values of packed keys, the smaller (larger) of each: of fp16, NaN if one is; of bf16 in the order of `ordered`.
+template <bool HALF>
+__device__ __forceinline__ uint32_t smaller2(uint32_t a, uint32_t b) {
+  if constexpr (HALF) return __builtin_bit_cast(uint32_t, __builtin_elementwise_minimum(__builtin_bit_cast(f16x2, a), __builtin_bit_cast(f16x2, b)));
+  else return as_word(__builtin_elementwise_min(as_pair(a), as_pair(b)));
+}
+template <bool HALF>
+__device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b) {
+  if constexpr (HALF) return __builtin_bit_cast(uint32_t, __builtin_elementwise_maximum(__builtin_bit_cast(f16x2, a), __builtin_bit_cast(f16x2, b)));
+  else return as_word(__builtin_elementwise_max(as_pair(a), as_pair(b)));
+}
+
 // Order of bf16 bits as that of 16-bit integers, both halves; its own inverse.  -0 comes before 0.
 __device__ __forceinline__ s16x2 ordered(s16x2 x) { return x ^ ((x >> 15) & s16x2{0x7fff, 0x7fff}); }
-
-__device__ __forceinline__ s16x2 as_pair(uint32_t x) { return __builtin_bit_cast(s16x2, x); }
-
-template <int CTRL>
-__device__ __forceinline__ s16x2 from_lane(s16x2 x) {
-  return as_pair(static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true)));
-}
-
-// Half of the pairs of lo and hi go to the lane's partner (CTRL), half of its come back.
-template <int CTRL, int N>
-__device__ __forceinline__ void halve(s16x2 (&lo)[N], s16x2 (&hi)[N], bool upper) {
-#pragma unroll
-  for (int k = 0; k < N / 2; ++k) {
-    const s16x2 l = upper ? lo[k] : lo[k + N / 2], h = upper ? hi[k] : hi[k + N / 2];
-    lo[k] = __builtin_elementwise_min(upper ? lo[k + N / 2] : lo[k], from_lane<CTRL>(l));
-    hi[k] = __builtin_elementwise_max(upper ? hi[k + N / 2] : hi[k], from_lane<CTRL>(h));
-  }
-}
-template <int N>
-__device__ __forceinline__ void first_half(const s16x2 (&x)[N], s16x2 (&y)[N / 2]) {
-#pragma unroll
-  for (int k = 0; k < N / 2; ++k) y[k] = x[k];
-}
-
 __device__ __forceinline__ bool is_nan16(short x) { return (x & 0x7fff) > 0x7f80; }
 
-// A wave has `rows` consecutive rows of a KV head; for each page that one of them is the first of its sequence's rows in, it
-// reads the page's K whole: lane 16g + c has hd/4 dimensions of tokens c, 16 + c, 32 + c, 48 + c as packed bf16; lo and hi over
-// these, and then over the 16 lanes, which end with a pair of dimensions each.
-template <int HD>
-__global__ __launch_bounds__(256) void k_kvq_ranges(KvqCache c, KvqBatch bt, uint16_t* ranges, int rows) {
-  constexpr int NP = HD / 8;  // pairs of a lane
-  const int lane = threadIdx.x & 63, col = lane & 15;
-  const int wave = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int g = wave / c.n_kv, kh = wave - g * c.n_kv, base = g * rows;
-  if (base >= bt.n_rows) return;
-  const RowPlace place = lane < rows ? row_place(c, bt, base + lane) : RowPlace{};
-  uint64_t todo = __ballot(place.state == 1 && (place.t == 0 || place.i == 0));
-  while (todo) {
-    const int src = __ffsll(static_cast<unsigned long long>(todo)) - 1;
-    todo &= todo - 1;
-    const int page = __builtin_amdgcn_readlane(place.page, src);
-    const int held = __builtin_amdgcn_readlane(place.t + place.left, src);  // tokens of the page below the context, or more than 64
-    const size_t at = static_cast<size_t>(page) * c.n_kv + kh;
-    PageK<HD> pk;
-    pk.load(c.blocks + at * kvq_block_bytes(HD));
-    s16x2 lo[NP], hi[NP];
+// Over the 16 lanes of a group, which have NP words each: lane c gets word c mod NP of all of them (of half of them and
+// its partner's half, where there are eight), through LDS of the wave's own.  A row of NP words to a lane, turned by quarters
+// so that neither writes nor reads meet in a bank.
+template <int NP>
+constexpr int kTurnGroup = 16 * NP + 16;
+template <int NP, typename F>
+__device__ __forceinline__ uint32_t across(const uint32_t (&x)[NP], uint32_t* lds, F op) {
+  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15, half = NP == 16 ? 0 : c >> 3, word = c & (NP - 1);
+  auto turn = [](int row) { return NP == 16 ? row >> 2 : 0; };
+  uint32_t* mine = lds + g * kTurnGroup<NP>;
+#pragma unroll
+  for (int k = 0; k < NP / 4; ++k)
+    *reinterpret_cast<u32x4*>(mine + c * NP + 4 * (k ^ turn(c))) = u32x4{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]};
+  __builtin_amdgcn_wave_barrier();
+  uint32_t y[NP];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int row = NP == 16 ? i : half * 8 + (i ^ half);
+    y[i] = mine[row * NP + 4 * ((word >> 2) ^ turn(row)) + (word & 3)];
+  }
+  __builtin_amdgcn_wave_barrier();
+  uint32_t r = y[0];
+#pragma unroll
+  for (int i = 1; i < NP; ++i) r = op(r, y[i]);
+  if constexpr (NP == 8) r = op(r, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(r), 0x128, 0xf, 0xf, false)));  // lane c ^ 8
+  return r;
+}
+
+// The page's smallest and largest pair of the lane's two dimensions, of tokens below `held`, as bf16.  HALF: all 64, whose
+// scales lie where fp16 holds every value: two conversions' instructions for each pair, a minimum and a maximum for each two.
+template <int HD, bool HALF>
+__device__ __forceinline__ void page_range(const PageK<HD>& pk, int held, uint32_t* lds, s16x2& lo, s16x2& hi) {
+  constexpr int NP = HD / 8;  // pairs of a lane and token
+  const int c = threadIdx.x & 15;
+  uint32_t low[NP], high[NP];
+#pragma unroll
+  for (int k = 0; k < NP; ++k) {
+    low[k] = 0x7fff7fffu;  // not HALF: past every value's order
+    high[k] = 0x80008000u;
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const float s = scale_of(pk.s, u);
+    if (!HALF && 16 * u + c >= held) continue;
 #pragma unroll
     for (int k = 0; k < NP; ++k) {
-      lo[k] = s16x2{0x7fff, 0x7fff};
-      hi[k] = s16x2{-0x8000, -0x8000};
+      const uint32_t w = HD == 128 ? pk.k[u][k >> 2] : pk.k[u >> 1][2 * (u & 1) + (k >> 2)];
+      uint32_t x = value_pair<HALF>(w, s, k & 3);
+      if constexpr (!HALF) x = as_word(ordered(as_pair(x)));
+      low[k] = HALF && u == 0 ? x : smaller2<HALF>(low[k], x);
+      high[k] = HALF && u == 0 ? x : larger2<HALF>(high[k], x);
     }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      if (16 * u + col < held) {
-        const float s = scale_of(pk.s, u);
-#pragma unroll
-        for (int j = 0; j < HD / 32; ++j) {
-          const uint32_t w = HD == 128 ? pk.k[u][j] : pk.k[u >> 1][2 * (u & 1) + j];
-          const uint32_t x[4] = {code_pair<0>(w, s), code_pair<1>(w, s), code_pair<2>(w, s), code_pair<3>(w, s)};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const s16x2 y = ordered(as_pair(x[i]));
-            lo[4 * j + i] = __builtin_elementwise_min(lo[4 * j + i], y);
-            hi[4 * j + i] = __builtin_elementwise_max(hi[4 * j + i], y);
-          }
-        }
-      }
-    }
-    halve<0x140>(lo, hi, col & 8);  // lane 15 - c of the 16
-    s16x2 l8[NP / 2], h8[NP / 2], l4[NP / 4], h4[NP / 4], l2[NP / 8], h2[NP / 8];
-    first_half(lo, l8);
-    first_half(hi, h8);
-    halve<0x141>(l8, h8, col & 4);  // 7 - c of eight
-    first_half(l8, l4);
-    first_half(h8, h4);
-    halve<0x4e>(l4, h4, col & 2);  // c ^ 2
-    first_half(l4, l2);
-    first_half(h4, h2);
-    if constexpr (HD == 128) {
-      halve<0xb1>(l2, h2, col & 1);  // c ^ 1
-    } else {
-      l2[0] = __builtin_elementwise_min(l2[0], from_lane<0xb1>(l2[0]));
-      h2[0] = __builtin_elementwise_max(h2[0], from_lane<0xb1>(h2[0]));
-    }
-    s16x2 l = ordered(l2[0]), h = ordered(h2[0]);
+  }
+  const uint32_t l = across(low, lds, smaller2<HALF>), h = across(high, lds, larger2<HALF>);
+  if constexpr (HALF) {
+    auto bf16 = [](uint32_t w) {  // two bits of mantissa: exact
+      const f16x2 v = __builtin_bit_cast(f16x2, w);
+      return as_pair(__builtin_amdgcn_perm(__float_as_uint(static_cast<float>(v[1])), __float_as_uint(static_cast<float>(v[0])), 0x07060302u));
+    };
+    lo = bf16(l);
+    hi = bf16(h);
+  } else {
+    lo = ordered(as_pair(l));
+    hi = ordered(as_pair(h));
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-      if (is_nan16(l[i]) || is_nan16(h[i])) l[i] = h[i] = 0x7fc0;
-    uint32_t* out = reinterpret_cast<uint32_t*>(ranges) + at * HD;
-    const int d2 = HD == 128 ? lane : (lane >> 4) * 8 + (col >> 1);
-    if (HD == 128 || !(col & 1)) {
-      out[d2] = __builtin_bit_cast(uint32_t, l);
-      out[HD / 2 + d2] = __builtin_bit_cast(uint32_t, h);
+      if (is_nan16(lo[i]) || is_nan16(hi[i])) lo[i] = hi[i] = 0x7fc0;
+  }
+}
+
+// A wave has `rows` consecutive rows of a KV head; for each page that one of them is the first of its sequence's in, it reads the
+// page's K whole: lane 16g + c has hd/4 dimensions of tokens c, 16 + c, 32 + c, 48 + c, and ends with two dimensions of all
+// tokens.  The next page's K is on its way meanwhile.
+//   84,000 prompt tokens of 8 KV heads of 128 dims: 15.5 us, 3.5 TB/s: HBM, after a chain of offsets, table and page.  Comparing
+// keys as 16-bit integers and exchanging them between lanes, 830 instructions a page instead of 450, took 17; several heads
+// to a wave 14.4 for 13.7 when the append has left the keys in the caches.
+template <int HD>
+__global__ __launch_bounds__(256) void k_kvq_ranges(KvqCache c, KvqBatch bt, uint16_t* ranges, int rows) {
+  constexpr int NP = HD / 8;
+  __shared__ __attribute__((aligned(16))) uint32_t lds[4][4 * kTurnGroup<NP>];
+  const int lane = threadIdx.x & 63;
+  const int in_block = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = blockIdx.x * 4 + in_block;
+  const int g = wave / c.n_kv, kh = wave - g * c.n_kv, base = g * rows;
+  if (base >= bt.n_rows) return;
+  const RowPlace place = wave_places(c, bt, base, rows);
+  uint64_t todo = __ballot(place.state == 1 && (place.t == 0 || place.i == 0));
+  PageK<HD> next;
+  size_t at = 0;
+  int held = 0;  // tokens of the page below the context, or more than 64
+  auto load = [&] {
+    const int src = __ffsll(static_cast<unsigned long long>(todo)) - 1;
+    at = static_cast<size_t>(__builtin_amdgcn_readlane(place.page, src)) * c.n_kv + kh;
+    held = __builtin_amdgcn_readlane(place.t + place.left, src);
+    next.template load<false>(c.blocks + at * kvq_block_bytes(HD));  // the append has just written there
+  };
+  if (todo) load();
+  while (todo) {
+    todo &= todo - 1;
+    const PageK<HD> pk = next;
+    const size_t now = at;
+    const int below = held;
+    if (todo) load();
+    s16x2 lo, hi;
+    // the four scales of the lane's tokens within 2^-23 .. 2^8, as fits_half has it
+    const bool fits = !(((pk.s + 0x18181818u) ^ 0x80808080u) & 0xe0e0e0e0u);
+    if (below >= kKvqPage && __all(fits)) page_range<HD, true>(pk, below, lds[in_block], lo, hi);
+    else page_range<HD, false>(pk, below, lds[in_block], lo, hi);
+    uint32_t* out = reinterpret_cast<uint32_t*>(ranges) + now * HD;
+    if (HD == 128 || !(lane & 8)) {
+      const int d2 = (lane >> 4) * NP + (lane & (NP - 1));
+      out[d2] = as_word(lo);
+      out[HD / 2 + d2] = as_word(hi);
     }
   }
 }
@@ -714,9 +749,9 @@ hipError_t launch_kvq_fit(const KvqFitArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_kvq_ranges(const KvqCache& c, const KvqBatch& b, uint16_t* ranges, hipStream_t s) {
-  // rows of a wave: 64 where that leaves 2,048 waves, as few as one where there are few rows
+  // As many rows to a wave, of 64, as leave 2,048 waves: one token each of 64 sequences (4 KV heads) 3.4 us, 64 rows to a wave 71.
   int rows = 64;
-  while (rows > 1 && static_cast<int64_t>(b.n_rows) * c.n_kv / rows < 2048) rows /= 2;
+  while (rows > 1 && (static_cast<int64_t>(b.n_rows) + rows - 1) / rows * c.n_kv < 2048) rows /= 2;
   const int64_t waves = (static_cast<int64_t>(b.n_rows) + rows - 1) / rows * c.n_kv;
   const dim3 grid(static_cast<uint32_t>((waves + 3) / 4));
   if (c.hd == 128) launch_kernel((k_kvq_ranges<128>), grid, dim3(256), 0, s, c, b, ranges, rows);

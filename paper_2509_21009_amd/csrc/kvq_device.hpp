@@ -79,6 +79,40 @@ __device__ __forceinline__ int wave_find_seq(const KvqBatch& bt, int row) {
   }
 }
 
+// row_place for the wave's lanes: rows base .. base + rows - 1 (64 at most).  Offsets, contexts of up to 64 sequences from the first
+// row's on are a lane's each, where the rows look theirs up: two or three reads that wait for each other in place of row_place's
+// search through memory.  Up to 64 sequences are all there.
+__device__ __forceinline__ RowPlace wave_places(const KvqCache& c, const KvqBatch& bt, int base, int rows) {
+  const int lane = threadIdx.x & 63, row = base + lane;
+  const bool mine = lane < rows;
+  if (!bt.row_off) return mine ? row_place(c, bt, row) : RowPlace{};
+  const int lo = bt.n_seqs <= 64 ? 0 : wave_find_seq(bt, base);
+  if (lo < 0) return RowPlace{};
+  const int b0 = min(lo + lane, bt.n_seqs - 1), start = bt.row_off[b0];
+  const KvqSeq s0 = kvq_seq(bt, b0);
+  const int end = __builtin_amdgcn_readlane(bt.row_off[b0 + 1], 63);
+  if (end < base + rows && lo + 63 < bt.n_seqs - 1) return mine ? row_place(c, bt, row) : RowPlace{};
+  int s = 0;  // the last whose first row is not past it
+#pragma unroll
+  for (int step = 32; step >= 1; step >>= 1)
+    if (__shfl(start, s + step, 64) <= row && lo + s + step < bt.n_seqs) s += step;
+  const int i = row - __shfl(s0.r0, s, 64), n = __shfl(s0.n, s, 64), ctx = __shfl(s0.ctx, s, 64);
+  const bool ok = __shfl(static_cast<int>(s0.ok), s, 64);
+  RowPlace p{};
+  if (!mine || row >= bt.n_rows || i < 0 || i >= n) return p;
+  const int pos = ctx - n + i;
+  p.i = i;
+  p.state = !ok ? 3 : pos < 0 ? 2 : 1;
+  if (p.state == 1) {
+    const int id = table_of(bt, lo + s)[pos / kKvqPage];
+    p.state = kvq_page_ok(c, id) ? 1 : 3;
+    p.t = pos % kKvqPage;
+    p.left = ctx - pos;
+    p.page = p.state == 1 ? id : 0;
+  }
+  return p;
+}
+
 // ---- tensors ---------------------------------------------------------------------------
 
 template <bool BF16>

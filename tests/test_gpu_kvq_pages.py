@@ -194,6 +194,35 @@ def test_ranges_of_odd_keys(hd):
     assert np.isnan(ref).any() and np.array_equal(got, ref, equal_nan=True)
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("n_kv", [1, 3, 8])
+def test_ranges_of_whole_pages_of_every_magnitude(n_kv, hd):
+    """Whole pages whose scales lie within fp16's exact range, at its ends and past them, and pages with a NaN, an infinity."""
+    s = Setup(n_kv, n_kv, hd, [64 * 24, 64 * 3 + 5], [64 * 24, 64 * 3 + 5], "f32", seed=n_kv + hd)
+    for p, e in enumerate([-30, -25, -24, -23, -22, -21, -20, -10, -3, 0, 3, 6, 7, 8, 9, 10, 11, 12, 20, 100]):
+        x = s.k[64 * p:64 * p + 64]
+        x.clamp_(-3.0, 3.0).mul_(2.0 ** e)
+    s.k[64 * 20 + 11, 0, 7], s.k[64 * 21, n_kv - 1, hd - 1], s.k[64 * 22 + 63, 0, 40] = float("nan"), float("inf"), float("-inf")
+    s.k[64 * 23:64 * 24] = 0.0
+    s.fill()
+    got = _f64(s.cache.update_ranges(s.batch(), s.cache.new_ranges()))
+    assert np.array_equal(got, _plain_ranges(s, s.held(), np.zeros(got.shape), s.rows), equal_nan=True)
+
+
+def test_ranges_of_many_rows_and_heads():
+    """Waves with 64 rows and several heads; sequences of every length side by side, some without rows."""
+    rng = np.random.default_rng(2)
+    ctx = rng.integers(0, 400, 300)
+    rows = np.where(rng.random(300) < 0.3, 0, np.minimum(ctx, rng.integers(0, 500, 300)))
+    for n_kv, hd in ((8, 64), (3, 128)):
+        s = Setup(n_kv, n_kv, hd, ctx.tolist(), rows.tolist(), "bf16", seed=n_kv).fill()
+        start = torch.randn((s.cache.n_pages, n_kv, 2, hd), device=DEV).to(torch.bfloat16)
+        got = s.cache.update_ranges(s.batch(), start.clone())
+        assert np.array_equal(_f64(got), _plain_ranges(s, s.held(), _f64(start), s.rows))
+        got = s.cache.update_ranges(s.batch(n_rows=int(rows.sum()) + 900, max_rows=500), start.clone())
+        assert np.array_equal(_f64(got), _plain_ranges(s, s.held(), _f64(start), s.rows))
+
+
 def test_ranges_of_bad_batches_are_left_alone():
     s = Setup(2, 2, 64, [70, 70, 70, 70], None, seed=6).fill()
     start = torch.randn((s.cache.n_pages, 2, 2, 64), device=DEV).to(torch.bfloat16)
