@@ -595,36 +595,30 @@ __device__ __forceinline__ int row_pages(const KvqBatch& bt, int row) {
   return s.ok ? max(0, s.ctx - s.n + i + kKvqPage) >> 6 : 0;  // none before the first token
 }
 
-// A wave has the list of a row and KV head, E of its up to 64 E pages in each lane.  The least key that is picked is found bit
-// by bit from the highest in which the keys differ: so many keys are at or above a value as a ballot has bits.
+// A wave has the list of a row and KV head, E of its up to 64 E pages in each lane, loaded while the row is looked up.  The
+// least key that is picked is found bit by bit from the highest: so many keys are at or above a value as a ballot has bits.
 template <int E>
 __global__ __launch_bounds__(256) void k_kvq_pick(KvqPickArgs a) {
   const int lane = threadIdx.x & 63;
-  const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row = static_cast<int>(unit / a.n_kv);
+  const int unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = unit / a.n_kv;
   if (row >= a.batch.n_rows) return;
+  float x[E];
+  const float* scores = a.scores + static_cast<size_t>(unit) * a.columns;
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[e] = scores[min(64 * e + lane, a.columns - 1)];
   const int m = row_pages(a.batch, row);
   if (m < 0) return;
-  int32_t* out = a.picks + unit * a.n;
+  int32_t* out = a.picks + static_cast<size_t>(unit) * a.n;
   if (m <= a.n) {
     for (int i = lane; i < a.n; i += 64) out[i] = i < m ? i : -1;
     return;
   }
-  const float* scores = a.scores + unit * a.columns;
   const int from = a.first, to = m - a.last, want = a.n - a.first - a.last;  // `want` of pages from .. to - 1
-  uint32_t key[E], top = 0, low = 0xffffffffu;
+  uint32_t key[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     const int p = 64 * e + lane;
-    const bool in = p >= from && p < to;
-    key[e] = in ? pick_key(scores[p]) : 0;
-    top = max(top, key[e]);
-    low = min(low, in ? key[e] : 0xffffffffu);
-  }
-#pragma unroll
-  for (int x = 32; x >= 1; x >>= 1) {
-    top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), x, 64)));
-    low = min(low, static_cast<uint32_t>(__shfl_xor(static_cast<int>(low), x, 64)));
+    key[e] = p >= from && p < to ? pick_key(x[e]) : 0;
   }
   auto count = [&](uint32_t t) {
     int k = 0;
@@ -632,12 +626,10 @@ __global__ __launch_bounds__(256) void k_kvq_pick(KvqPickArgs a) {
     for (int e = 0; e < E; ++e) k += lanes(__ballot(key[e] >= t));
     return k;
   };
-  // The largest t with `want` keys at or above it; where the count meets `want` before, it is far enough.
-  uint32_t least = top;
-  if (top != low) {
-    int bit = 31 - __clz(top ^ low);
-    least = top & ~((2u << bit) - 1);
-    for (; bit >= 0; --bit) {
+  // The largest value with `want` keys at or above it; where the count meets `want` before, it is far enough.
+  uint32_t least = want > 0 ? 0 : 0xffffffffu;
+  if (want > 0) {
+    for (int bit = 31; bit >= 0; --bit) {
       const int k = count(least | 1u << bit);
       if (k >= want) least |= 1u << bit;
       if (k == want) break;
@@ -670,7 +662,7 @@ __global__ __launch_bounds__(kPickThreads) void k_kvq_pick_long(KvqPickArgs a) {
   __shared__ int waves[2][kPickThreads / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t unit = blockIdx.x;
-  const int row = static_cast<int>(unit / a.n_kv);
+  const int row = static_cast<int>(blockIdx.x) / a.n_kv;
   const int m = row_pages(a.batch, row);
   if (m < 0) return;
   int32_t* out = a.picks + unit * a.n;

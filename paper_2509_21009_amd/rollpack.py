@@ -740,6 +740,10 @@ class Engine:
                                        temperature, P0, R0, eta, eta_r)
 
 
+def _pick_pages(cache: RpKvqCache, *args) -> None:  # called as the cache's other calls are
+    rp_kvq_pick_pages(*args)
+
+
 class KvqBatch:
     """The batch of a KvqCache call (rp_kvq_batch): its device arrays, kept alive, and their bounds."""
 
@@ -885,13 +889,14 @@ class KvqCache:
 
     def _per_list(self, t, batch: KvqBatch, dtype, name: str) -> int:
         """A contiguous tensor [n_rows, n_kv_heads, ..] of a batch; its last dimension."""
-        if t.dtype != dtype or t.device != self.device or t.dim() != 3 or not t.is_contiguous() or \
-                t.shape[:2] != (batch.struct.n_rows, self.n_kv_heads):
+        dims = t.shape
+        if t.dtype != dtype or t.device != self.device or len(dims) != 3 or dims[0] != batch.struct.n_rows or \
+                dims[1] != self.n_kv_heads or not t.is_contiguous():
             raise ValueError(f"{name} are a contiguous {dtype} tensor [{batch.struct.n_rows}, {self.n_kv_heads}, n] on {self.device}, "
-                             f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-        if t.shape[2] >= 1 << 31:
+                             f"got {t.dtype} {tuple(dims)} on {t.device}")
+        if dims[2] >= 1 << 31:
             raise ValueError(f"{name} have too long a last dimension")
-        return t.shape[2]
+        return dims[2]
 
     def update_ranges(self, batch: KvqBatch, ranges):
         """The smallest and largest key of each dimension, KV head and page, for the pages that the batch's rows are in,
@@ -917,15 +922,14 @@ class KvqCache:
     def pick_pages(self, batch: KvqBatch, scores, n_picks: int, first: int = 1, last: int = 1, out=None):
         """[n_rows, n_kv_heads, n_picks] int32: the pages to attend to, ascending, then -1.  All that the row sees, or its first
         `first`, its last `last`, and of the others those of the highest scores (ties: the lower page)."""
-        for name, x in (("n_picks", n_picks), ("first", first), ("last", last)):
-            if not 0 <= x < 1 << 31:  # ctypes would pass its lower half
-                raise ValueError(f"{name} must be between 0 and 2^31 - 1, got {x}")
+        if not (0 <= n_picks < 1 << 31 and 0 <= first < 1 << 31 and 0 <= last < 1 << 31):  # ctypes would pass a lower half
+            raise ValueError(f"n_picks, first and last must be between 0 and 2^31 - 1, got {n_picks}, {first}, {last}")
         columns = self._per_list(scores, batch, self.torch.float32, "scores")
         if out is None:
             out = self.torch.empty((batch.struct.n_rows, self.n_kv_heads, n_picks), dtype=self.torch.int32, device=self.device)
         elif self._per_list(out, batch, self.torch.int32, "picks") != n_picks:
             raise ValueError(f"out has lists of {out.shape[2]} pages, not {n_picks}")
-        self._call(lambda cache, *args: rp_kvq_pick_pages(*args), batch, self.n_kv_heads, scores.data_ptr(), columns, first, last,
+        self._call(_pick_pages, batch, self.n_kv_heads, scores.data_ptr(), columns, first, last,
                    n_picks, out.data_ptr())
         return out
 
