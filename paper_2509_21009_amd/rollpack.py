@@ -999,8 +999,8 @@ class KvqPages:
         if not (0 <= n_rows <= 1 << 24 and 0 <= max_rows <= n_rows and 0 <= max_context <= self.max_context):
             raise ValueError(f"n_rows must be between 0 and 2^24, max_rows between 0 and n_rows, max_context between 0 and "
                              f"{self.max_context}, got {n_rows}, {max_rows}, {max_context}")
-        off = torch.empty(n_seqs + 1, **self._ints)
-        positions, slots = torch.empty(n_rows, **self._ints), torch.empty(n_rows, **self._ints)
+        # one allocation for the three: each would cost the call 1.4 us
+        off, positions, slots = torch.empty(n_seqs + 1 + 2 * n_rows, **self._ints).split_with_sizes((n_seqs + 1, n_rows, n_rows))
         at = off.data_ptr()
         if torch.cuda.current_device() == self.device.index:
             rp_kvq_fit_pages(self.struct, lengths.data_ptr(), n_rows, at, positions.data_ptr(), slots.data_ptr(),
