@@ -1,12 +1,19 @@
 """The 4-bit cache's page calls without a GPU: their refusals, what needs no launch, and their plain forms."""
+import ctypes
 import os
+import re
+import subprocess
 
 import numpy as np
 import pytest
 
 from oracle import kvq_pages as op
+from paper_2509_21009_amd import build
 from paper_2509_21009_amd import rollpack as rp
 from tests.test_kvq_cpu import BAD_BATCHES, BAD_CACHES, BAD_TENSORS, OVERLAPS, PTR, _batch, _cache, _host_cache, _refused, _tensor
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+PLAN = os.path.join(ROOT, "tests", "cpp", "kvq_pages_plan.cpp")
 
 
 @pytest.fixture(scope="module")
@@ -156,6 +163,54 @@ def test_pools_live_in_gpu_memory_and_within_their_limits(lib):
     for args in ((4, 2, 64), (0, 2, 64), ((1 << 24) + 1, 2, 64), (4, -1, 64), (4, (1 << 20) + 1, 64), (4, 2, -1), (4, 2, (1 << 30) + 1), (2 ** 32 + 4, 2, 64)):
         with pytest.raises(ValueError):
             rp.KvqPages(*args, device="cpu")
+
+
+# ---- which kernel takes a call -------------------------------------------------------
+
+def test_plan_under_sanitizers(tmp_path):
+    exe = tmp_path / "kvq_pages_plan"
+    subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all", f"-I{build.CSRC}", PLAN,
+                    "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0 and "plan tests passed" in r.stdout, r.stderr
+
+
+def test_gpu_tests_reach_every_kernel(tmp_path):
+    """The calls of tests/test_gpu_kvq_pages.py that are there for a form of a kernel are of that form."""
+    so = tmp_path / "plan.so"
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", f"-I{build.CSRC}", PLAN, "-o", str(so)], check=True)
+    lib = ctypes.CDLL(str(so))
+
+    def plan(n_q, n_kv, hd, bf16, n_rows, max_rows, columns, n):
+        out = (ctypes.c_int * 6)()
+        lib.kvq_pages_plan_of(n_q, n_kv, hd, bf16, n_rows, max_rows, columns, n, out)
+        return tuple(out)
+
+    for bf16 in (1, 0):  # test_attend_picked_split_and_whole: items, waves, shared
+        assert plan(28, 4, 128, bf16, 1, 1, 313, 313)[3:] == (64, 4, 0) and plan(4, 2, 64, bf16, 2, 1, 141, 90)[3:] == (23, 4, 0)
+        assert plan(28, 4, 128, bf16, 210, 70, 47, 9)[3:] == (1, 4, 1) and plan(6, 3, 64, bf16, 80, 1, 12, 20)[3:] == (1, 8, 0)
+        assert plan(6, 3, 64, bf16, 80, 2, 12, 20)[3:] == (1, 8, 1) and plan(7, 1, 128, bf16, 60, 4, 40, 40)[3:] == (8, 4, 1)
+        # test_scores_of_many_rows: rows, tiles, shared
+        assert plan(14, 2, 64, bf16, 1700, 1700, 15, 1)[:3] == (2, 2, 1) and plan(28, 4, 128, bf16, 3000, 3000, 100, 1)[:3] == (16, 2, 1)
+        assert plan(28, 4, 128, bf16, 3000, 3000, 1024, 1)[:3] == (32, 4 if bf16 else 2, 1)
+        assert plan(28, 4, 128, bf16, 6, 1, 17, 1)[:3] == (1, 1, 0)
+
+
+@pytest.mark.skipif(not os.path.exists(build.HIPCC), reason="no hipcc")
+@pytest.mark.parametrize("source,least,limits", [
+    ("k_kvq_picked.hip", 16, (("attend_pickedILi128ELb0ELi4E", 168), ("attend_pickedILi64ELb0ELi4E", 128), ("attend_pickedILi128ELb1ELi8E", 256))),
+    ("k_kvq_pages.hip", 18, (("k_kvq_scoresILi128ELb0ELi1ELb0E", 128), ("k_kvq_scoresILi128ELb0ELi4ELb1E", 256), ("k_kvq_scoresILi128ELb1ELi2ELb1E", 256),
+                             ("k_kvq_rangesILi128E", 128)))])
+def test_registers_and_scratch(source, least, limits):
+    """No kernel spills, and the waves of a SIMD are those that the launch bounds and plans count with."""
+    asm = subprocess.run([build.HIPCC, *build.COMMON, *build.DEVICE, "--cuda-device-only", "-S", os.path.join(build.CSRC, source), "-o", "-"],
+                         check=True, capture_output=True, text=True, timeout=300).stdout
+    info = {m.group(1): (int(m.group(2)), int(m.group(3))) for m in
+            re.finditer(r"^(_Z\w+):.*?; TotalNumVgprs: (\d+).*?; ScratchSize: (\d+)", asm, flags=re.S | re.M)}
+    assert len(info) >= least and not [k for k, (_, scratch) in info.items() if scratch]
+    for name, most in limits:
+        found = [v for k, (v, _) in info.items() if name in k]
+        assert found and max(found) <= most, (name, found)
 
 
 # ---- the plain forms -----------------------------------------------------------------
