@@ -473,8 +473,8 @@ __device__ __forceinline__ uint32_t scales_below(uint32_t s, int t, int end) {
 // A page with NaN blocks: their scales become 2^-127, which the zero probability of a key out of sight clears (as NaN it
 // would not), and the lane's outputs turn NaN if its column sees the token.  A lane's outputs all lie in one block of 32
 // dimensions.
-template <int HD>
-__device__ __forceinline__ void nan_values(PageV<HD>& pg, const char* block, int tok0, int lim, f32x4_t (&o)[HD / 16]) {
+template <int HD, int NO = HD / 16>
+__device__ __forceinline__ void nan_values(PageV<HD>& pg, const char* block, int tok0, int lim, f32x4_t (&o)[NO]) {
   const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
   for (int u = 0; u < 4; ++u)
@@ -486,7 +486,7 @@ __device__ __forceinline__ void nan_values(PageV<HD>& pg, const char* block, int
     bad |= tok0 + t <= lim && static_cast<unsigned char>(block[kvq_v_scale(t, g * HD / 128, HD)]) == 255;
   if (bad) {
 #pragma unroll
-    for (int i = 0; i < HD / 16; ++i) o[i] += __builtin_nanf("");
+    for (int i = 0; i < NO; ++i) o[i] += __builtin_nanf("");
   }
 }
 

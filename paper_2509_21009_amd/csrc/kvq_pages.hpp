@@ -95,11 +95,12 @@ struct PickedPlan {
   int shared = 0;  // rows of a sequence may read the same pages, which the caches then keep
 };
 
-//   A wave takes 1 us a page, and the start and end of a block 6; a split's second launch and partial outputs take 4.5 and
-// more.  7 query heads to each of 4 KV heads of 128 dims, us, whole with four waves | with eight | split: lists of 64 pages of 1 row (4
+// A wave takes 1 us a page, and the start and end of a block 6; a split's second launch and partial outputs take 4.5 and more.
+// 7 query heads to each of 4 KV heads of 128 dims, us, whole with four waves | with eight | split: lists of 64 pages of 1 row (4
 // blocks) 21.5 | 18.8 | 9.4, of 8 rows 28 | 22 | 12.3, of 16 rows 29 | 22 | 16.3; of 32 pages of 4 rows 13.4 | 12.0 | 9.8, of 16 rows 16.9 | 14.7 | 12.9,
 // of 32 rows 17.6 | 15.7 | 17.0; of 16 pages of 8 rows 10.6 | 10.4 | 10.3; of 96 of 32 rows 42.6 | 34.1 | 28.7, of 64 rows 50.7 | 43.9 | 47.7; of 32
-// of 96 rows (384 blocks) 25.0 | 31.8 | 33.
+// of 96 rows (384 blocks) 25.0 | 31.8 | 33.  Many rows that share pages, with two waves | four: 200 of 8 pages 12.1 | 13.1, 512 of 32 53.8 |
+// 53.5, 1,500 of 32 125 | 130; rows of their own of 48 pages (512 blocks) 50 | 45.
 //   Pages that one row alone reads go past the caches; of 512 rows of 14,000 keys with 32 pages each 61 us with plain loads, 70
 // so; of 64 rows of their own 43 so, 51 with plain loads (40/8 heads, 48 pages).
 inline PickedPlan picked_plan(const KvqCache& c, const KvqBatch& b, int n, int n_q) {
@@ -111,6 +112,7 @@ inline PickedPlan picked_plan(const KvqCache& c, const KvqBatch& b, int n, int n
   p.shared = kvq_max_rows(b) > 1;
   if (blocks <= 128 && n >= 32 && 2 * n >= blocks) p.items = static_cast<int>(std::min<int64_t>(kvq_items(n, kKvqTileItems, 4), 512 / blocks));
   else if (blocks <= 256 && n > 16) p.waves = 8;
+  else if (blocks >= 512 && p.shared) p.waves = 2;
   return p;
 }
 

@@ -57,7 +57,7 @@ int main() {
     const int per = (n + p.items - 1) / p.items;
     assert(p.items >= 1 && p.items <= kKvqTileItems && per * p.items >= n && (p.items == 1 || (per >= 4 && p.waves == 4)));
     assert(p.items == 1 || picked_blocks(c, b, p) * p.items <= 512);
-    assert(p.waves == 4 || p.waves == 8);
+    assert(p.waves == 4 || p.waves == 8 || (p.waves == 2 && p.shared));
     assert((p.items > 1) == (kvq_picked_bytes(c, b, n, n_q) > 0));
     assert(kvq_picked_bytes(c, b, n, n_q) <= size_t{512} * 16 * (c.hd + 2) * 4);
     const bool bf16 = rng() % 2;
@@ -71,6 +71,6 @@ int main() {
     ++waves[p.waves];
     ++tiles[s.tiles];
   }
-  assert(split > 1000 && waves[4] > 1000 && waves[8] > 1000 && tiles[1] > 1000 && tiles[2] > 1000 && tiles[4] > 1000);
+  assert(split > 1000 && waves[2] > 1000 && waves[4] > 1000 && waves[8] > 1000 && tiles[1] > 1000 && tiles[2] > 1000 && tiles[4] > 1000);
   std::puts("page plan tests passed");
 }

@@ -460,6 +460,8 @@ def test_attend_picked(n_q, n_kv, hd, dtype, style):
     (6, 3, 64, [700, 64, 1] * 26 + [300, 5], None, 20),      # eight waves
     (6, 3, 64, [700, 2] * 40, [2, 0] * 40, 20),              # and rows that share pages
     (7, 1, 128, [2500, 130, 60] * 5, [4, 4, 4] * 5, 40),     # split, rows that share pages
+    (40, 2, 64, [900] * 3, [70] * 3, 9),     # two waves, more than 16 heads
+    (9, 1, 128, [900, 5] * 3, [250, 5] * 3, 4),
 ])
 def test_attend_picked_split_and_whole(n_q, n_kv, hd, ctx, rows, n, dtype):
     s = Setup(n_q, n_kv, hd, ctx, rows, dtype, seed=n).fill()

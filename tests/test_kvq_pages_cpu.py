@@ -188,8 +188,9 @@ def test_gpu_tests_reach_every_kernel(tmp_path):
 
     for bf16 in (1, 0):  # test_attend_picked_split_and_whole: items, waves, shared
         assert plan(28, 4, 128, bf16, 1, 1, 313, 313)[3:] == (64, 4, 0) and plan(4, 2, 64, bf16, 2, 1, 141, 90)[3:] == (23, 4, 0)
-        assert plan(28, 4, 128, bf16, 210, 70, 47, 9)[3:] == (1, 4, 1) and plan(6, 3, 64, bf16, 80, 1, 12, 20)[3:] == (1, 8, 0)
+        assert plan(28, 4, 128, bf16, 210, 70, 47, 9)[3:] == (1, 2, 1) and plan(6, 3, 64, bf16, 80, 1, 12, 20)[3:] == (1, 8, 0)
         assert plan(6, 3, 64, bf16, 80, 2, 12, 20)[3:] == (1, 8, 1) and plan(7, 1, 128, bf16, 60, 4, 40, 40)[3:] == (8, 4, 1)
+        assert plan(40, 2, 64, bf16, 210, 70, 47, 9)[3:] == (1, 2, 1)
         # test_scores_of_many_rows: rows, tiles, shared
         assert plan(14, 2, 64, bf16, 1700, 1700, 15, 1)[:3] == (2, 2, 1) and plan(28, 4, 128, bf16, 3000, 3000, 100, 1)[:3] == (16, 2, 1)
         assert plan(28, 4, 128, bf16, 3000, 3000, 1024, 1)[:3] == (32, 4 if bf16 else 2, 1)
@@ -198,7 +199,8 @@ def test_gpu_tests_reach_every_kernel(tmp_path):
 
 @pytest.mark.skipif(not os.path.exists(build.HIPCC), reason="no hipcc")
 @pytest.mark.parametrize("source,least,limits", [
-    ("k_kvq_picked.hip", 16, (("attend_pickedILi128ELb0ELi4E", 168), ("attend_pickedILi64ELb0ELi4E", 128), ("attend_pickedILi128ELb1ELi8E", 256))),
+    ("k_kvq_picked.hip", 16, (("attend_pickedILi128ELb0ELi4ELb0ELb1E", 128), ("attend_pickedILi128ELb0ELi2ELb1ELb1E", 128), ("attend_pickedILi128ELb0ELi4ELb0ELb0E", 168),
+                              ("attend_pickedILi64ELb0ELi4E", 128), ("attend_pickedILi128ELb1ELi8E", 256))),
     ("k_kvq_pages.hip", 18, (("k_kvq_scoresILi128ELb0ELi1ELb0E", 128), ("k_kvq_scoresILi128ELb0ELi4ELb1E", 256), ("k_kvq_scoresILi128ELb1ELi2ELb1E", 256),
                              ("k_kvq_rangesILi128E", 128)))])
 def test_registers_and_scratch(source, least, limits):
