@@ -678,7 +678,8 @@ rp_status rp_kvq_attend(const rp_kvq_cache* cache, const rp_kvq_batch* batch, in
  *   rp_kvq_page_scores  a bound of every page's scores for each query
  *   rp_kvq_pick_pages   the pages to attend to
  *   rp_kvq_attend_picked  attention over them
- * all on the GPU, with nothing for the host to wait for. */
+ * all on the GPU, with nothing for the host to wait for.  They launch kernels on hip_stream and return, as the calls above, and
+ * with their rules for graphs, devices and host structures. */
 
 /* A pool of pages and what its sequences hold, in caller-owned device memory that the
  * calls keep up to date; one call at a time.  Before the first call the caller writes
@@ -718,6 +719,8 @@ typedef struct rp_kvq_pool {
  *   positions    out [n_rows]: of each row, -1 behind the last
  *   slots        out [n_rows]: 64 * page + position mod 64, -1 behind the last
  *   n_rows       0 .. 2^24, the most new tokens of all sequences (a padded batch)
+ * The outputs overlap neither each other nor the pool nor lengths.  The batch of the new tokens has the pool's contexts and
+ * page_table, these row_offsets and n_rows, until the next call.
  * An error that only the device can see goes to state[1]; the call then changes nothing else of
  * the pool and has no rows: 1 too few free pages (state[3]: how many are missing), 2 a length
  * outside 0 .. max_context, 3 more than n_rows new tokens, 4 a state that no calls have made.
@@ -740,7 +743,8 @@ rp_status rp_kvq_key_ranges(const rp_kvq_cache* cache, const rp_kvq_batch* batch
  *   score = max_h sum_d max(q[h, d], 0) largest[d] + min(q[h, d], 0) smallest[d],
  * over the G = n_q_heads / n_kv_heads heads, in fp32, and minus infinity for pages past the one of
  * the row's position.  A NaN among them makes it NaN, as does a page id outside the cache; all
- * scores of a row are NaN where its sequence is out of the batch's bounds.
+ * scores of a row are NaN where its sequence is out of the batch's bounds.  An infinite q[h, d] makes the head's
+ * sums infinite or NaN.
  *   ranges     as rp_kvq_key_ranges has written them; the cache's blocks are not read
  *   q          [n_rows, n_q_heads, head_dim]
  *   scores     device [n_rows, n_kv_heads, n_columns] fp32; rows of no sequence are left as they are

@@ -90,7 +90,7 @@ __global__ __launch_bounds__(256) void k_kvq_append(KvqCache c, KvqBatch bt, Kvq
   const int wave = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = wave / c.n_kv, kh = wave - g * c.n_kv, base = g * rows;
   if (base >= bt.n_rows) return;
-  const RowPlace place = lane < rows ? row_place(c, bt, base + lane) : RowPlace{};
+  const RowPlace place = lane < rows ? row_place(c, bt, base + lane) : RowPlace{0, 0, 0};
   for (int it = 0; it < rows / RowStep<HD>::RPS; it += U) {
     float kf[U][8], vf[U][8];
 #pragma unroll
@@ -128,7 +128,7 @@ __global__ __launch_bounds__(256) void k_kvq_read(KvqCache c, KvqBatch bt, KvqTe
   const int wave = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = wave / c.n_kv, kh = wave - g * c.n_kv, base = g * rows;
   if (base >= bt.n_rows) return;
-  const RowPlace place = lane < rows ? row_place(c, bt, base + lane) : RowPlace{};
+  const RowPlace place = lane < rows ? row_place(c, bt, base + lane) : RowPlace{0, 0, 0};
   for (int it = 0; it < rows / RowStep<HD>::RPS; it += U) {
     uint32_t kw[U], vw[U], kb[U], vb[U];
 #pragma unroll

@@ -21,9 +21,13 @@ typedef short s16x2 __attribute__((ext_vector_type(2)));
 // each other's inverse, and what is given back is handed out again first.
 //   k_kvq_fit, one block: checks, sums over the sequences, offsets, contexts, pages given back.  Then the rows (in the
 // same launch where they are few): a row's page is new or in the table, and the first row of a new page enters it there.
+//   Bound by reads that wait for each other: state, context and length; the pages given back; the rows' pages.  64 sequences 4.5 us,
+// 512 that give back 2,600 pages 6.3, the rows' launch 6.0 for 162,000 rows, 7.4 for 590,000 (4.7 MB).
 
 constexpr int kFitThreads = 1024;
-constexpr int kFitRows1 = 8192;  // rows that the first launch takes, four to a thread at a time
+// Rows that the first launch takes, four to a thread at a time.  In it | in one of their own, us, with a call without rows: 512
+// sequences of 4 tokens 11.0 | 13.5, of 8 13.2 | 13.9, of 12 15.4 | 13.9, of 64 44 | 14.0; 16 of 500 14.3 | 13.1.
+constexpr int kFitRows1 = 4096;
 
 // The last of lo .. hi whose start is not past j, of starts that do not descend.
 template <typename F>
@@ -334,7 +338,7 @@ __global__ __launch_bounds__(256) void k_kvq_ranges(KvqCache c, KvqBatch bt, uin
   const int in_block = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = blockIdx.x * 4 + in_block;
   const int g = wave / c.n_kv, kh = wave - g * c.n_kv, base = g * rows;
   if (base >= bt.n_rows) return;
-  const RowPlace place = wave_places(c, bt, base, rows);
+  const PagePlace place = wave_places(c, bt, base, rows);
   uint64_t todo = __ballot(place.state == 1 && (place.t == 0 || place.i == 0));
   PageK<HD> next;
   size_t at = 0;

@@ -29,11 +29,14 @@ __device__ __forceinline__ const int32_t* table_of(const KvqBatch& bt, int b) {
 
 struct RowPlace {
   int state, t, page;  // state: 0 nothing to do, 1 a position of the cache, 2 before the sequence's first token, 3 bad
-  int i, left;         // which of its sequence's rows; with state 1, tokens from its own to the context's end
+};
+struct PagePlace : RowPlace {
+  int i, left;  // which of its sequence's rows; with state 1, tokens from its own to the context's end
 };
 
-__device__ __forceinline__ RowPlace row_place(const KvqCache& c, const KvqBatch& bt, int row) {
-  RowPlace p{0, 0, 0, 0, 0};
+template <typename Place = RowPlace>
+__device__ __forceinline__ Place row_place(const KvqCache& c, const KvqBatch& bt, int row) {
+  Place p{};
   if (row >= bt.n_rows) return p;
   int b = row;
   if (bt.row_off) {  // the last sequence whose first row is not past it
@@ -48,7 +51,6 @@ __device__ __forceinline__ RowPlace row_place(const KvqCache& c, const KvqBatch&
   const KvqSeq s = kvq_seq(bt, b);
   const int i = row - s.r0, pos = s.ctx - s.n + i;
   if (i < 0 || i >= s.n) return p;  // past max_rows, or offsets that do not ascend
-  p.i = i;
   if (!s.ok) {
     p.state = 3;
   } else if (pos < 0) {
@@ -57,8 +59,11 @@ __device__ __forceinline__ RowPlace row_place(const KvqCache& c, const KvqBatch&
     const int id = table_of(bt, b)[pos / kKvqPage];
     p.state = kvq_page_ok(c, id) ? 1 : 3;
     p.t = pos % kKvqPage;
-    p.left = s.ctx - pos;
     p.page = p.state == 1 ? id : 0;
+  }
+  if constexpr (std::is_same_v<Place, PagePlace>) {
+    p.i = i;
+    p.left = s.ctx - pos;
   }
   return p;
 }
@@ -82,23 +87,23 @@ __device__ __forceinline__ int wave_find_seq(const KvqBatch& bt, int row) {
 // row_place for the wave's lanes: rows base .. base + rows - 1 (64 at most).  Offsets, contexts of up to 64 sequences from the first
 // row's on are a lane's each, where the rows look theirs up: two or three reads that wait for each other in place of row_place's
 // search through memory.  Up to 64 sequences are all there.
-__device__ __forceinline__ RowPlace wave_places(const KvqCache& c, const KvqBatch& bt, int base, int rows) {
+__device__ __forceinline__ PagePlace wave_places(const KvqCache& c, const KvqBatch& bt, int base, int rows) {
   const int lane = threadIdx.x & 63, row = base + lane;
   const bool mine = lane < rows;
-  if (!bt.row_off) return mine ? row_place(c, bt, row) : RowPlace{};
+  if (!bt.row_off) return mine ? row_place<PagePlace>(c, bt, row) : PagePlace{};
   const int lo = bt.n_seqs <= 64 ? 0 : wave_find_seq(bt, base);
-  if (lo < 0) return RowPlace{};
+  if (lo < 0) return PagePlace{};
   const int b0 = min(lo + lane, bt.n_seqs - 1), start = bt.row_off[b0];
   const KvqSeq s0 = kvq_seq(bt, b0);
   const int end = __builtin_amdgcn_readlane(bt.row_off[b0 + 1], 63);
-  if (end < base + rows && lo + 63 < bt.n_seqs - 1) return mine ? row_place(c, bt, row) : RowPlace{};
+  if (end < base + rows && lo + 63 < bt.n_seqs - 1) return mine ? row_place<PagePlace>(c, bt, row) : PagePlace{};
   int s = 0;  // the last whose first row is not past it
 #pragma unroll
   for (int step = 32; step >= 1; step >>= 1)
     if (__shfl(start, s + step, 64) <= row && lo + s + step < bt.n_seqs) s += step;
   const int i = row - __shfl(s0.r0, s, 64), n = __shfl(s0.n, s, 64), ctx = __shfl(s0.ctx, s, 64);
   const bool ok = __shfl(static_cast<int>(s0.ok), s, 64);
-  RowPlace p{};
+  PagePlace p{};
   if (!mine || row >= bt.n_rows || i < 0 || i >= n) return p;
   const int pos = ctx - n + i;
   p.i = i;

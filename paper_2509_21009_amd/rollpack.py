@@ -896,6 +896,8 @@ class KvqCache:
                              f"got {t.dtype} {tuple(dims)} on {t.device}")
         if dims[2] >= 1 << 31:
             raise ValueError(f"{name} have too long a last dimension")
+        if t.requires_grad and self.torch.is_grad_enabled():
+            raise ValueError("the 4-bit cache passes no gradient back: detach its tensors, or call it under torch.no_grad()")
         return dims[2]
 
     def update_ranges(self, batch: KvqBatch, ranges):
@@ -961,6 +963,13 @@ class KvqPages:
     free_pages [n_pages] and state [4], int32 tensors that fit() keeps up to date on torch's current stream.
 
     One pool serves the caches of all layers.  fit() can be captured into a graph; its replays read the lengths then there.
+    A decode step of a layer, for queries q and the new tokens' k and v:
+
+        batch, positions, slots = pages.fit(lengths, n_rows, max_rows=1)
+        cache.append(batch, k, v)
+        cache.update_ranges(batch, ranges)
+        picks = cache.pick_pages(batch, cache.page_scores(batch, q, ranges), 64)
+        out = cache.attend_picked(batch, q, picks)
     """
 
     def __init__(self, n_pages: int, n_seqs: int, max_context: int, device="cuda"):
@@ -988,7 +997,8 @@ class KvqPages:
         """Give each sequence the pages of its new length (int32 tensor [n_seqs]), take back those of what it no longer has.
         Returns (batch, positions, slots) of the up to n_rows new tokens: the batch for a KvqCache's calls until the next fit,
         each row's position, and 64 * page + position % 64, -1 in padded rows (int32 tensors).
-        n_rows bounds the new tokens of all sequences, max_rows those of one (n_rows), max_context the lengths (the pool's).
+        n_rows bounds the new tokens of all sequences, max_rows those of one (n_rows; 1 for a decode step, whose calls are faster
+        for knowing it), max_context the lengths (the pool's).
         What does not fit shows in state[1] (status()): then nothing changed and there are no rows."""
         torch, n_seqs = self.torch, self.n_seqs
         if lengths.dtype != torch.int32 or lengths.device != self.device or lengths.shape != (n_seqs,) or not lengths.is_contiguous():

@@ -76,6 +76,19 @@ def test_pool_follows_lengths(n_seqs, max_context, steps, seed):
     assert p.gpu.status()["free_pages"] == p.gpu.n_pages
 
 
+def test_pool_of_very_many_sequences():
+    """Sums over tiles of 1,024 sequences and over many of them to a thread."""
+    n = 70001
+    p = Pools(2 * n, n, 70, 1)
+    rng = np.random.default_rng(4)
+    for most in (3, 70, 66):
+        to = rng.integers(0, most + 1, n)
+        p.fit(to.tolist(), int(np.maximum(to - np.array(p.plain.contexts), 0).sum()))
+    p.fit([70] * n, n)  # more rows than room for them
+    assert p.gpu.status()["error"] == 3
+    p.fit([0] * n, 0)
+
+
 def test_a_call_and_its_taking_back_leave_the_pool_as_it_was():
     rng = np.random.default_rng(3)
     p = Pools(300, 40, 600, 1)

@@ -138,7 +138,9 @@ def test_tensors_that_need_gradients_are_refused(lib):
     b = c.batch(torch.ones(3, dtype=torch.int32), torch.zeros((3, 1), dtype=torch.int32))
     q = torch.zeros(3, 4, 64).requires_grad_()
     picks = torch.zeros((3, 2, 1), dtype=torch.int32)
-    for call in (lambda: c.page_scores(b, q, c.new_ranges()), lambda: c.attend_picked(b, q, picks), lambda: c.attend_picked(b, q.detach(), picks, out=q)):
+    scores = torch.zeros(3, 2, 1).requires_grad_()
+    for call in (lambda: c.page_scores(b, q, c.new_ranges()), lambda: c.attend_picked(b, q, picks), lambda: c.attend_picked(b, q.detach(), picks, out=q),
+                 lambda: c.page_scores(b, q.detach(), c.new_ranges(), out=scores), lambda: c.pick_pages(b, scores, 1, first=0)):
         with pytest.raises(ValueError, match="gradient"):
             call()
 
