@@ -193,6 +193,12 @@ def test_gpu_tests_reach_every_kernel(tmp_path):
         assert plan(28, 4, 128, bf16, 210, 70, 47, 9)[3:] == (1, 2, 1) and plan(6, 3, 64, bf16, 80, 1, 12, 20)[3:] == (1, 8, 0)
         assert plan(6, 3, 64, bf16, 80, 2, 12, 20)[3:] == (1, 8, 1) and plan(7, 1, 128, bf16, 60, 4, 40, 40)[3:] == (8, 4, 1)
         assert plan(40, 2, 64, bf16, 210, 70, 47, 9)[3:] == (1, 2, 1)
+        # tests/test_gpu_kvq_picked_softmax.py's forms
+        for (n_q, n_kv, hd), n_rows, most, pages, want in (
+                ((7, 1, 128), 14, 9, 16, (1, 4, 1)), ((32, 2, 128), 13, 9, 15, (1, 4, 1)), ((10, 2, 64), 80, 1, 22, (1, 8, 0)),
+                ((8, 1, 128), 150, 1, 22, (1, 8, 0)), ((28, 4, 128), 160, 100, 11, (1, 2, 1)), ((14, 2, 64), 300, 200, 11, (1, 2, 1)),
+                ((7, 1, 128), 1, 1, 79, (20, 4, 0)), ((14, 2, 64), 3, 2, 68, (17, 4, 1))):
+            assert plan(n_q, n_kv, hd, bf16, n_rows, most, pages, pages)[3:] == want
         # test_scores_of_many_rows: rows, tiles, shared
         assert plan(14, 2, 64, bf16, 1700, 1700, 15, 1)[:3] == (2, 2, 1) and plan(28, 4, 128, bf16, 3000, 3000, 100, 1)[:3] == (16, 2, 1)
         assert plan(28, 4, 128, bf16, 3000, 3000, 1024, 1)[:3] == (32, 4 if bf16 else 2, 1)
