@@ -684,14 +684,14 @@ rp_status rp_kvq_attend(const rp_kvq_cache* cache, const rp_kvq_batch* batch, in
 /* A pool of pages and what its sequences hold, in caller-owned device memory that the
  * calls keep up to date; one call at a time.  Before the first call the caller writes
  * free_pages (every page once, in any order: the last ones are taken first), zeros to
- * contexts, and {n_pages, 0, 0, 0} to state.
+ * contexts and workspace, and {n_pages, 0, 0, 0} to state.
  *   page_table   [n_seqs] rows of table_stride entries, as an rp_kvq_batch has it; entries past a
  *                sequence's pages are left as they are
  *   contexts     [n_seqs] tokens of each sequence
  *   free_pages   [n_pages] the free ones are the first state[0]
  *   state        [4]: free pages; the last call's error (0, or below), its rows, and how many
  *                pages it was short of
- *   workspace    [n_seqs + 1], the calls' own
+ *   workspace    [n_seqs + 1, at least 1088], the calls' own
  *   n_seqs       0 .. 2^20
  *   n_pages      1 .. 2^24
  *   max_context  most tokens of a sequence, 0 .. 2^30; at most 64 * table_stride */

@@ -19,15 +19,21 @@ typedef short s16x2 __attribute__((ext_vector_type(2)));
 // have .. want - 1.  Counted over the sequences in order and each one's pages in order, of R given back the j-th becomes
 // entry n_free + R - 1 - j of the list, and the k-th needed is entry n_free + R - 1 - k: a call and the one that takes it back are
 // each other's inverse, and what is given back is handed out again first.
-//   k_kvq_fit, one block: checks, sums over the sequences, offsets, contexts, pages given back.  Then the rows (in the
-// same launch where they are few): a row's page is new or in the table, and the first row of a new page enters it there.
-//   Bound by reads that wait for each other: state, context and length; the pages given back; the rows' pages.  64 sequences 4.5 us,
-// 512 that give back 2,600 pages 6.3, the rows' launch 6.0 for 162,000 rows, 7.4 for 590,000 (4.7 MB).
-
+//   k_kvq_fit: checks, sums over the sequences, offsets, contexts, pages given back, and the rows: a row's page is new or in the
+// table, and the first row of a new page enters it there.  Every block of a launch does the sums for itself, and has a part of the
+// pages given back and of the rows.  What the blocks start from, contexts and the count of free pages, is written by the last one to
+// have read it, whichever that is: nothing waits.  Nothing else that is read is written: pages are taken from below n_free and given
+// back above it, a new page that was just given back is looked up where its last owner's table has it, and the table's new entries lie
+// behind those of the sequence's old pages.
+//   More sequences than a block has threads: one block, and the rows in a launch of their own, k_kvq_fit_rows.
+//   Bound by reads that wait for each other (state, context and length; the pages given back; the rows' pages), and by what 16 waves
+// issue for the sums.  A call and its taking back, us: 64 sequences 8.3; 512 of 162,000 tokens that turn into as many others, both
+// ways, 15; 1,024 prompts of 590,000 tokens (4.7 MB written) 20.6.  With the rows in a second launch the last two took 24.
 constexpr int kFitThreads = 1024;
-// Rows that the first launch takes, four to a thread at a time.  In it | in one of their own, us, with a call without rows: 512
-// sequences of 4 tokens 11.0 | 13.5, of 8 13.2 | 13.9, of 12 15.4 | 13.9, of 64 44 | 14.0; 16 of 500 14.3 | 13.1.
-constexpr int kFitRows1 = 4096;
+// Rows of a block, up to 256 blocks; then these have more.  In blocks of 1,024 | one block, us, with a call without rows: 512 sequences
+// of 4 tokens 10.8 | 9.9, of 8 10.6 | 12.1, of 64 10.4 | 32; 16 of 500 9.8 | 13.0.  Blocks of 1,024 | 256 blocks: 590,000 rows 27.6 | 20.6.
+constexpr int kFitBlock = 1024;
+constexpr int kFitUnroll = 4;
 
 // The last of lo .. hi whose start is not past j, of starts that do not descend.
 template <typename F>
@@ -39,33 +45,59 @@ __device__ __forceinline__ int last_from(int lo, int hi, int j, F start) {
   return lo;
 }
 
-// Row r, of a sequence whose rows are off .. end - 1 and that needs pages from the first_need-th on: its position and slot, and
-// the page's entry where it is the first of a new one.  top: entries of the list with those given back, from whose end pages are
-// taken.
-struct FitRow {
-  int pos, id;
-  bool enters;  // its page into the table
-};
-__device__ __forceinline__ FitRow fit_row(const KvqFitArgs& a, int r, int b, int len, int off, int end, int first_need, int top) {
-  const int first = len - (end - off), pos = first + (r - off), page = pos / kKvqPage, have = kvq_pages(first);
-  const bool fresh = page >= have;
-  const int32_t* from = fresh ? a.pool.free_pages + (top - 1 - (first_need + page - have)) : a.pool.page_table + b * a.pool.table_stride + page;
-  return {pos, *from, fresh && pos % kKvqPage == 0};
-}
-__device__ __forceinline__ void fit_store(const KvqFitArgs& a, int r, int b, const FitRow& f) {
-  if (f.enters) a.pool.page_table[b * a.pool.table_stride + f.pos / kKvqPage] = f.id;
-  a.position[r] = f.pos;
-  a.slot[r] = f.id * kKvqPage + f.pos % kKvqPage;
+// The same for a j of the wave's, in n <= 1024 starts in LDS, from 0: 16 to a lane, then these 16.
+__device__ __forceinline__ int wave_last(const int* start, int n, int j) {
+  const int lane = threadIdx.x & 63;
+  const int at = 16 * (__builtin_popcountll(__ballot(16 * lane < n && start[min(16 * lane, n)] <= j)) - 1);
+  return at + __builtin_popcountll(__ballot(lane < 16 && at + lane < n && start[min(at + lane, n)] <= j)) - 1;
 }
 
-__global__ __launch_bounds__(kFitThreads) void k_kvq_fit(KvqFitArgs a, int with_rows) {
+// Row r, of sequence b whose rows are off .. end - 1: its position and page, which is new or in the table.
+struct FitRow {
+  int b, pos, page, need;  // need: of a new page its number among all needed ones, the sequence's from first_need on
+  bool fresh;
+};
+__device__ __forceinline__ FitRow fit_row(int r, int b, int len, int off, int end, int first_need) {
+  const int first = len - (end - off), pos = first + (r - off), page = pos / kKvqPage, have = kvq_pages(first);
+  return {b, pos, page, first_need + page - have, page >= have};
+}
+__device__ __forceinline__ int32_t* fit_entry(const KvqPool& p, int64_t b, int page) { return p.page_table + b * p.table_stride + page; }
+__device__ __forceinline__ void fit_store(const KvqFitArgs& a, int r, const FitRow& f, int id) {
+  if (f.fresh && f.pos % kKvqPage == 0) *fit_entry(a.pool, f.b, f.page) = id;
+  a.position[r] = f.pos;
+  a.slot[r] = id * kKvqPage + f.pos % kKvqPage;
+}
+
+// Sums over the lanes of a row of 16 up to each.
+__device__ __forceinline__ int row_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  return x + __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+}
+
+// Counts this block; true for the last of the launch, which leaves the counts at 0.  Sixteen counts, 256 bytes apart, whose last ones
+// count once more: 20.6 us for 256 blocks where one count took 22.8, 15.2 for 158 where it took 16.4.
+__device__ __forceinline__ bool fit_arrives(int32_t* counts) {
+  auto last_of = [](int32_t* count, int of) {
+    if (__hip_atomic_fetch_add(count, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != of - 1) return false;
+    __hip_atomic_store(count, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return true;
+  };
+  const int blocks = gridDim.x, group = blockIdx.x % kFitCounts;
+  return last_of(counts + kFitCountStride * (1 + group), (blocks - group + kFitCounts - 1) / kFitCounts) && last_of(counts, min(blocks, kFitCounts));
+}
+
+__global__ __launch_bounds__(kFitThreads) void k_kvq_fit(KvqFitArgs a, int with_rows, int block_rows) {
   constexpr int kWaves = kFitThreads / 64;
-  __shared__ int64_t sums[kWaves][3];
+  __shared__ bool last_block;
+  __shared__ int64_t sums[3][kWaves];
   __shared__ int scan[kWaves][3], flags[kWaves];
   __shared__ int start[3][kFitThreads + 1], length_of[kFitThreads];  // of a tile's sequences: pages needed, given back, rows before
   const KvqPool& pool = a.pool;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = pool.n_seqs;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wave_u = __builtin_amdgcn_readfirstlane(wave), n = pool.n_seqs;
   const int n_free = pool.state[0];
+  const bool alone = gridDim.x == 1;
 
   // What all sequences need, give back and add, in 64 bits; anything out of bounds.
   int64_t all[3] = {0, 0, 0};
@@ -84,22 +116,26 @@ __global__ __launch_bounds__(kFitThreads) void k_kvq_fit(KvqFitArgs a, int with_
     all[2] += max(0, len - old);
   }
   const uint64_t any_len = __ballot(bad_len), any_pool = __ballot(bad_pool);
+  int upto[3];  // over the wave's lanes up to this one, below 2^31 where nothing fails
 #pragma unroll
   for (int i = 0; i < 3; ++i) {  // at most 2^10 sequences of 2^30 to a thread: halves of 20 bits, whose sums fit
-    const int low = wave_scan(static_cast<int>(all[i] & 0xfffff)), high = wave_scan(static_cast<int>(all[i] >> 20));
-    if (lane == 63) sums[wave][i] = (static_cast<int64_t>(high) << 20) + low;
+    const int low = wave_scan(static_cast<int>(all[i] & 0xfffff));
+    const int high = __ballot(all[i] >> 20 != 0) ? wave_scan(static_cast<int>(all[i] >> 20)) : 0;
+    upto[i] = static_cast<int>(static_cast<uint32_t>(low) + (static_cast<uint32_t>(high) << 20));
+    if (lane == 63) sums[i][wave] = (static_cast<int64_t>(high) << 20) + low;
   }
   if (lane == 0) flags[wave] = (any_len ? 1 : 0) | (any_pool ? 2 : 0);
   __syncthreads();
-  int64_t need = 0, back = 0, rows = 0;
-  int flag = n_free < 0 || n_free > pool.n_pages ? 2 : 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    need += sums[w][0];
-    back += sums[w][1];
-    rows += sums[w][2];
-    flag |= flags[w];
-  }
+  // The waves' sums, 16 lanes for each of the three: up to this wave's, and all.
+  const int64_t of_wave = lane < 3 * kWaves ? sums[lane / kWaves][lane % kWaves] : 0;
+  const int low = row_scan(static_cast<int>(of_wave & 0xffffff)), high = row_scan(static_cast<int>(of_wave >> 24));
+  auto sum_to = [&](int i, int w) {
+    const int at = i * kWaves + w;
+    return (static_cast<int64_t>(__builtin_amdgcn_readlane(high, at)) << 24) + __builtin_amdgcn_readlane(low, at);
+  };
+  const int64_t need = sum_to(0, kWaves - 1), back = sum_to(1, kWaves - 1), rows = sum_to(2, kWaves - 1);
+  const int seen = lane < kWaves ? flags[lane] : 0;
+  const int flag = (n_free < 0 || n_free > pool.n_pages || __ballot(seen & 2) ? 2 : 0) | (__ballot(seen & 1) ? 1 : 0);
   const int64_t short_of = need - back - n_free;
   const int error = (flag & 2) || n_free + back > pool.n_pages ? kFitPool : (flag & 1) ? kFitLength : short_of > 0 ? kFitPages
                     : rows > a.n_rows ? kFitRows : kFitOk;
@@ -112,46 +148,57 @@ __global__ __launch_bounds__(kFitThreads) void k_kvq_fit(KvqFitArgs a, int with_
       old = pool.context[b];
       len = a.length[b];
     }
-    int x[3] = {0, 0, 0}, mine[3], total[3];
-    if (b < n && !failed) {
-      const int have = kvq_pages(old), want = kvq_pages(len);
-      x[0] = max(0, want - have);
-      x[1] = max(0, have - want);
-      x[2] = max(0, len - old);
+    int mine[3], total[3];  // before this sequence in the tile, and all of the tile
+    if (n <= kFitThreads) {
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        total[i] = failed ? 0 : static_cast<int>(sum_to(i, kWaves - 1));
+        mine[i] = failed ? 0 : upto[i] - static_cast<int>(all[i]) + (wave_u > 0 ? static_cast<int>(sum_to(i, wave_u - 1)) : 0);
+      }
+    } else {
+      int x[3] = {0, 0, 0};
+      if (b < n && !failed) {
+        const int have = kvq_pages(old), want = kvq_pages(len);
+        x[0] = max(0, want - have);
+        x[1] = max(0, have - want);
+        x[2] = max(0, len - old);
+      }
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        mine[i] = wave_scan(x[i]);
+        if (lane == 63) scan[wave][i] = mine[i];
+        mine[i] -= x[i];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        const int before = wave_scan(lane < kWaves ? scan[lane][i] : 0);
+        total[i] = __builtin_amdgcn_readlane(before, 63);
+        mine[i] += wave_u > 0 ? __builtin_amdgcn_readlane(before, wave_u - 1) : 0;
+      }
     }
 #pragma unroll
-    for (int i = 0; i < 3; ++i) {
-      mine[i] = wave_scan(x[i]);
-      if (lane == 63) scan[wave][i] = mine[i];
-      mine[i] -= x[i];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 3; ++i) {
-      const int before = wave_scan(lane < kWaves ? scan[lane][i] : 0);
-      total[i] = __builtin_amdgcn_readlane(before, 63);
-      mine[i] += wave > 0 ? __builtin_amdgcn_readlane(before, wave - 1) : 0;
-      start[i][tid] = mine[i];
-    }
+    for (int i = 0; i < 3; ++i) start[i][tid] = mine[i];
     length_of[tid] = len;
     if (b < n) {
-      a.row_off[b] = carry[2] + mine[2];
-      pool.first_need[b] = carry[0] + mine[0];
-      if (!failed) pool.context[b] = len;
+      if (blockIdx.x == 0) a.row_off[b] = carry[2] + mine[2];
+      if (!with_rows) pool.workspace[b] = carry[0] + mine[0];
+      if (alone && !failed) pool.context[b] = len;
     }
     __syncthreads();
-    for (int j0 = tid; j0 < total[1]; j0 += 4 * kFitThreads) {  // pages given back, four at a time
+    const int stride = kFitThreads * static_cast<int>(gridDim.x);
+    for (int j0 = blockIdx.x * kFitThreads + tid; j0 < total[1]; j0 += 4 * stride) {  // pages given back, four at a time
       int page[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int j = j0 + k * kFitThreads;
+        const int j = j0 + k * stride;
         if (j >= total[1]) continue;
         const int s = last_from(0, here - 1, j, [&](int i) { return start[1][i]; });
         page[k] = pool.page_table[(b0 + s) * pool.table_stride + kvq_pages(length_of[s]) + (j - start[1][s])];
       }
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int j = j0 + k * kFitThreads;
+        const int j = j0 + k * stride;
         if (j < total[1]) pool.free_pages[top - 1 - (carry[1] + j)] = page[k];
       }
     }
@@ -159,34 +206,72 @@ __global__ __launch_bounds__(kFitThreads) void k_kvq_fit(KvqFitArgs a, int with_
     for (int i = 0; i < 3; ++i) carry[i] += total[i];
     __syncthreads();
   }
+  if (!alone) {
+    asm volatile("" ::"v"(n_free), "v"(old), "v"(len) : "memory");  // this block's reads of the state are in registers
+    __syncthreads();
+    if (tid == 0) last_block = fit_arrives(pool.workspace);
+  }
+  if (blockIdx.x == 0 && tid == 0) a.row_off[n] = carry[2];
+  if (with_rows) {  // all sequences are in LDS
+    if (tid == 0) start[2][n] = carry[2];
+    __syncthreads();
+    const int given = failed ? 0 : static_cast<int>(back), end = min(a.n_rows, static_cast<int>(blockIdx.x + 1) * block_rows);
+    const int held = min(end, carry[2]);
+    for (int r0 = blockIdx.x * block_rows + 64 * wave_u; r0 < end; r0 += kFitUnroll * kFitThreads) {
+      FitRow f[kFitUnroll];
+      int id[kFitUnroll];
+#pragma unroll
+      for (int k = 0; k < kFitUnroll; ++k) {  // 64 rows of a wave
+        const int first = r0 + k * kFitThreads, last = min(first + 63, held - 1), r = min(first + lane, last);
+        if (first >= held) continue;
+        const int lo = wave_last(start[2], n, first), hi = __builtin_amdgcn_readfirstlane(start[2][lo + 1]) > last ? lo : wave_last(start[2], n, last);
+        const int32_t* from;
+        if (lo == hi) {  // of one sequence: most of what follows is the wave's; pages given back are two at most
+          auto one = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+          f[k] = fit_row(r, lo, one(length_of[lo]), one(start[2][lo]), one(start[2][lo + 1]), one(start[0][lo]));
+          from = fit_entry(pool, lo, f[k].page);
+          if (f[k].fresh) from = pool.free_pages + (n_free - 1 - (f[k].need - given));
+          const bool again = f[k].fresh && f[k].need < given;
+          if (const uint64_t who = __ballot(again)) {
+            const int k1 = __builtin_amdgcn_readlane(f[k].need, __builtin_ctzll(who)), k2 = __builtin_amdgcn_readlane(f[k].need, 63 - __builtin_clzll(who));
+            auto entry = [&](int i) {
+              const int s = wave_last(start[1], n, i);
+              return fit_entry(pool, s, kvq_pages(one(length_of[s])) + (i - one(start[1][s])));
+            };
+            const int32_t *e1 = entry(k1), *e2 = k1 == k2 ? e1 : entry(k2);
+            if (again) from = f[k].need == k1 ? e1 : e2;
+          }
+        } else {
+          const int b = last_from(lo, hi, r, [&](int i) { return start[2][i]; });
+          f[k] = fit_row(r, b, length_of[b], start[2][b], start[2][b + 1], start[0][b]);
+          from = fit_entry(pool, b, f[k].page);
+          if (f[k].fresh && f[k].need >= given) from = pool.free_pages + (n_free - 1 - (f[k].need - given));
+          else if (f[k].fresh) {
+            const int s = last_from(0, n - 1, f[k].need, [&](int i) { return start[1][i]; });
+            from = fit_entry(pool, s, kvq_pages(length_of[s]) + (f[k].need - start[1][s]));
+          }
+        }
+        id[k] = *from;
+      }
+#pragma unroll
+      for (int k = 0; k < kFitUnroll; ++k) {
+        const int r = r0 + k * kFitThreads + lane;
+        if (r < held) fit_store(a, r, f[k], id[k]);
+        else if (r < end) a.position[r] = a.slot[r] = -1;
+      }
+    }
+  }
+  if (!alone) {
+    __syncthreads();
+    if (!last_block) return;
+    if (tid < n && !failed) pool.context[tid] = len;
+  }
   if (tid == 0) {
-    a.row_off[n] = carry[2];
-    pool.first_need[n] = top;
+    if (!with_rows) pool.workspace[n] = top;
     pool.state[1] = error;
     pool.state[2] = carry[2];
     pool.state[3] = error == kFitPages ? static_cast<int>(min(short_of, int64_t{0x7fffffff})) : 0;
     if (!failed) pool.state[0] = top - carry[0];
-  }
-  if (!with_rows) return;
-  // The rows, of sequences that are all in LDS.
-  if (tid == 0) start[2][n] = carry[2];
-  __syncthreads();
-  for (int r0 = tid; r0 < a.n_rows; r0 += 4 * kFitThreads) {
-    FitRow f[4];
-    int b[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int r = r0 + k * kFitThreads;
-      if (r >= carry[2]) continue;
-      b[k] = last_from(0, n - 1, r, [&](int i) { return start[2][i]; });
-      f[k] = fit_row(a, r, b[k], length_of[b[k]], start[2][b[k]], start[2][b[k] + 1], start[0][b[k]], top);
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int r = r0 + k * kFitThreads;
-      if (r < carry[2]) fit_store(a, r, b[k], f[k]);
-      else if (r < a.n_rows) a.position[r] = a.slot[r] = -1;
-    }
   }
 }
 
@@ -199,15 +284,15 @@ __global__ __launch_bounds__(256) void k_kvq_fit_rows(KvqFitArgs a) {
   KvqBatch bt;
   bt.n_seqs = n;
   bt.row_off = a.row_off;
-  const int total = a.row_off[n], top = a.pool.first_need[n], last = min(r0 + 255, a.n_rows - 1);
+  const int total = a.row_off[n], top = a.pool.workspace[n], last = min(r0 + 255, a.n_rows - 1);
   const int lo = wave_find_seq(bt, r0);  // -1: all behind the last
   int hi = wave_find_seq(bt, last);
   FitRow f[4];
-  int b[4];
+  int id[4];
   if (lo >= 0) {
     if (hi < 0) hi = n - 1;
     const int mine = min(lo + lane, n - 1);
-    const int off = a.row_off[mine], end = a.row_off[mine + 1], len = a.pool.context[mine], need = a.pool.first_need[mine];
+    const int off = a.row_off[mine], end = a.row_off[mine + 1], len = a.pool.context[mine], need = a.pool.workspace[mine];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const int r = r0 + k * 64 + lane;
@@ -216,19 +301,19 @@ __global__ __launch_bounds__(256) void k_kvq_fit_rows(KvqFitArgs a) {
 #pragma unroll
         for (int step = 32; step >= 1; step >>= 1)
           if (__shfl(off, s + step, 64) <= r && lo + s + step <= hi) s += step;
-        b[k] = lo + s;
         const int l = __shfl(len, s, 64), o = __shfl(off, s, 64), e = __shfl(end, s, 64), d = __shfl(need, s, 64);
-        if (r < total) f[k] = fit_row(a, r, b[k], l, o, e, d, top);
+        f[k] = fit_row(r, lo + s, l, o, e, d);
       } else if (r < total) {
-        b[k] = last_from(lo, hi, r, [&](int i) { return a.row_off[i]; });
-        f[k] = fit_row(a, r, b[k], a.pool.context[b[k]], a.row_off[b[k]], a.row_off[b[k] + 1], a.pool.first_need[b[k]], top);
+        const int b = last_from(lo, hi, r, [&](int i) { return a.row_off[i]; });
+        f[k] = fit_row(r, b, a.pool.context[b], a.row_off[b], a.row_off[b + 1], a.pool.workspace[b]);
       }
+      if (r < total) id[k] = *(f[k].fresh ? a.pool.free_pages + (top - 1 - f[k].need) : fit_entry(a.pool, f[k].b, f[k].page));
     }
   }
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const int r = r0 + k * 64 + lane;
-    if (r < total) fit_store(a, r, b[k], f[k]);
+    if (r < total) fit_store(a, r, f[k], id[k]);
     else if (r < a.n_rows) a.position[r] = a.slot[r] = -1;
   }
 }
@@ -758,8 +843,10 @@ __global__ __launch_bounds__(kPickThreads) void k_kvq_pick_long(KvqPickArgs a) {
 }  // namespace
 
 hipError_t launch_kvq_fit(const KvqFitArgs& a, hipStream_t s) {
-  const int with_rows = a.n_rows <= kFitRows1 && a.pool.n_seqs <= kFitThreads;
-  launch_kernel(k_kvq_fit, dim3(1), dim3(kFitThreads), 0, s, a, with_rows);
+  const int with_rows = a.pool.n_seqs <= kFitThreads;
+  const int rows = std::max(kFitBlock, (a.n_rows + 255) / 256);  // of a block
+  const int blocks = with_rows ? std::max(1, (a.n_rows + rows - 1) / rows) : 1;
+  launch_kernel(k_kvq_fit, dim3(static_cast<uint32_t>(blocks)), dim3(kFitThreads), 0, s, a, with_rows, rows);
   if (!with_rows && a.n_rows > 0) launch_kernel(k_kvq_fit_rows, dim3(static_cast<uint32_t>((a.n_rows + 1023) / 1024)), dim3(256), 0, s, a);
   return hipGetLastError();
 }

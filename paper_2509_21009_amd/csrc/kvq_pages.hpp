@@ -21,9 +21,11 @@ struct KvqPool {
   int32_t* context = nullptr;   // [n_seqs]
   int32_t* free_pages = nullptr;  // [n_pages]
   int32_t* state = nullptr;     // [4]: n_free, error, rows of the last call, pages it was short of
-  int32_t* first_need = nullptr;  // [n_seqs] workspace: pages that the sequences before took
+  int32_t* workspace = nullptr;  // [max(n_seqs + 1, kFitWorkspace)]: pages that the sequences before need, or counts of blocks
   int n_seqs = 0, n_pages = 0, max_context = 0;
 };
+constexpr int kFitCounts = 16, kFitCountStride = 64, kFitWorkspace = kFitCountStride * (1 + kFitCounts);
+static_assert(kFitWorkspace == 1088, "rp_kvq_pool's least workspace");
 enum KvqFitError { kFitOk = 0, kFitPages = 1, kFitLength = 2, kFitRows = 3, kFitPool = 4 };
 
 struct KvqFitArgs {

@@ -615,7 +615,7 @@ rp_status rp_kvq_fit_pages(const rp_kvq_pool* pool, const int32_t* lengths, int3
     a.pool.context = pool->contexts;
     a.pool.free_pages = pool->free_pages;
     a.pool.state = pool->state;
-    a.pool.first_need = pool->workspace;
+    a.pool.workspace = pool->workspace;
     a.pool.n_seqs = pool->n_seqs;
     a.pool.n_pages = static_cast<int>(pool->n_pages);
     a.pool.max_context = pool->max_context;

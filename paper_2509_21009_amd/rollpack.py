@@ -983,7 +983,7 @@ class KvqPages:
         self.page_table = torch.zeros((n_seqs, max(1, -(-max_context // 64))), **self._ints)
         self.contexts = torch.zeros(n_seqs, **self._ints)
         self.free_pages = torch.arange(n_pages - 1, -1, -1, **self._ints)  # page 0 goes first
-        self.state, self._workspace = torch.zeros(4, **self._ints), torch.zeros(n_seqs + 1, **self._ints)
+        self.state, self._workspace = torch.zeros(4, **self._ints), torch.zeros(max(n_seqs + 1, 1088), **self._ints)
         self.state[0] = n_pages
         self.device = self._ints["device"] = self.state.device
         if self.device.type != "cuda":

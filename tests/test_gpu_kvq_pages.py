@@ -61,7 +61,8 @@ class Pools:
     (1025, 129, 4, 7), (2500, 90, 4, 8), (7, 33000, 5, 9),
 ])
 def test_pool_follows_lengths(n_seqs, max_context, steps, seed):
-    """Sequences come, grow, shrink, stay and go, in any mix; more than 4,096 rows take a launch of their own."""
+    """Sequences come, grow, shrink, stay and go, in any mix; up to 1,024 rows are one block's, and those of more than 1,024
+    sequences a launch of their own."""
     rng = np.random.default_rng(seed)
     p = Pools(n_seqs * op.pages(max_context), n_seqs, max_context, seed)
     now = np.zeros(n_seqs, np.int64)
@@ -87,6 +88,50 @@ def test_pool_of_very_many_sequences():
     p.fit([70] * n, n)  # more rows than room for them
     assert p.gpu.status()["error"] == 3
     p.fit([0] * n, 0)
+
+
+@pytest.mark.parametrize("n_seqs,max_context", [(1, 500_000), (3, 150_000), (300, 1500), (1000, 400), (1024, 300)])
+def test_rows_of_many_blocks(n_seqs, max_context):
+    """Up to 256 blocks, of 1,024 rows and more, share a call; pages that it takes back serve it; and a call of padded rows, one that
+    fails and one that changes nothing leave the blocks' counts ready for the next."""
+    rng = np.random.default_rng(n_seqs)
+    p = Pools(n_seqs * op.pages(max_context) * 2 // 3 + 1, n_seqs, max_context, 5)
+    half = rng.permutation(n_seqs) < (n_seqs + 1) // 2
+    a = np.where(half, rng.integers(max_context // 2, max_context + 1, n_seqs), 1) if n_seqs > 1 else np.array([max_context // 2])
+    b = np.where(half, 30, a[::-1] // 2 + 65) if n_seqs > 1 else np.array([max_context * 3 // 5])
+    for to in (a, b, a):
+        p.fit(to.tolist(), int(np.maximum(to - np.array(p.plain.contexts), 0).sum()) + 1500)
+        assert p.gpu.status()["error"] == 0
+    p.fit(a.tolist(), 5000)                    # nothing to do
+    p.fit(np.full(n_seqs, max_context).tolist(), 300_000)   # too few pages
+    assert p.gpu.status()["error"] == 1
+    p.fit((a - 1).tolist(), 70_000)
+    p.fit(np.zeros(n_seqs, int).tolist(), 2000)
+    p.fit(b.tolist(), 400_000)
+    assert p.gpu.status()["error"] == 0
+
+
+def test_rows_of_many_blocks_in_a_graph():
+    """Replays with other lengths, the pool used eagerly in between."""
+    p, lengths = Pools(900, 40, 2000, 6), _ints(np.zeros(40))
+    rng = np.random.default_rng(8)
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        p.gpu.fit(lengths, 30_000)
+    torch.cuda.current_stream().wait_stream(stream)
+    with torch.cuda.graph(graph):
+        batch, positions, slots = p.gpu.fit(lengths, 30_000)
+    for i in range(6):
+        to = rng.integers(0, 1100, 40)
+        lengths.copy_(_ints(to))
+        graph.replay()
+        error, off, pos, slot = p.plain.fit(to.tolist(), 30_000)
+        assert p.check_state()["error"] == error == 0
+        assert np.array_equal(batch.row_offsets.cpu().numpy(), off)
+        assert np.array_equal(positions.cpu().numpy(), pos) and np.array_equal(slots.cpu().numpy(), slot)
+        if i % 2:
+            p.fit((to + 1).tolist(), [40, 3000][i // 2 % 2])
 
 
 def test_a_call_and_its_taking_back_leave_the_pool_as_it_was():
@@ -155,6 +200,10 @@ def test_no_sequences():
     batch, positions, slots = p.fit(_ints([]), 5)
     assert batch.row_offsets.tolist() == [0] and positions.tolist() == slots.tolist() == [-1] * 5
     assert p.status()["error"] == 0 and p.status()["free_pages"] == 3
+    for n_rows in (0, 70_000, 2000):
+        batch, positions, slots = p.fit(_ints([]), n_rows)
+        assert batch.row_offsets.tolist() == [0] and bool((positions == -1).all()) and bool((slots == -1).all())
+        assert p.status() == {"free_pages": 3, "error": 0, "message": rp().KVQ_FIT_ERRORS[0], "rows": 0, "missing_pages": 0}
 
 
 # ---- ranges --------------------------------------------------------------------------
