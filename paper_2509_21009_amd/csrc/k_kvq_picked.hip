@@ -152,7 +152,7 @@ __device__ __forceinline__ void narrow_values(const PageV<HD>& pg, const float (
 // room for fewer waves: 64 rows of 48 pages 45 | 43 us).
 //   HBM bounds decoding: one token each of 64 sequences, 48 pages each (8 KV heads of 128, 214 MB) 39 us, 5.5 TB/s.  The vector ALU
 // bounds many rows, whose pages come from the caches: 512 rows of 32 pages (4 KV heads) 53 us, 11 TB/s, 77% of the cycles
-// vector instructions, 250 a page, half of them conversions from 4 bits, and 30% products, of which 7 columns of 16 are heads.
+// vector instructions, 298 a page, nearly half of them conversions from 4 bits, and 30% products, of which 7 columns of 16 are heads.
 // NARROW took this from 61 us.
 template <int HD, bool F32, int NW, bool KEEP, bool NARROW>
 __global__ __launch_bounds__(64 * NW, F32 ? 2 : NARROW ? 4 : 3) void k_kvq_attend_picked(KvqPickedArgs a, PickedPlan plan) {

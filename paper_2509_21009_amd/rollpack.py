@@ -1012,13 +1012,12 @@ class KvqPages:
         # one allocation for the three: each would cost the call 1.4 us
         off, positions, slots = torch.empty(n_seqs + 1 + 2 * n_rows, **self._ints).split_with_sizes((n_seqs + 1, n_rows, n_rows))
         at = off.data_ptr()
+        args = self.struct, lengths.data_ptr(), n_rows, at, at + 4 * (n_seqs + 1), at + 4 * (n_seqs + 1 + n_rows)
         if torch.cuda.current_device() == self.device.index:
-            rp_kvq_fit_pages(self.struct, lengths.data_ptr(), n_rows, at, positions.data_ptr(), slots.data_ptr(),
-                             self._raw_stream(self.device.index))
+            rp_kvq_fit_pages(*args, self._raw_stream(self.device.index))
         else:
             with torch.cuda.device(self.device):
-                rp_kvq_fit_pages(self.struct, lengths.data_ptr(), n_rows, at, positions.data_ptr(), slots.data_ptr(),
-                                 self._raw_stream(self.device.index))
+                rp_kvq_fit_pages(*args, self._raw_stream(self.device.index))
         b = RpKvqBatch(n_seqs, n_rows, max_rows, max_context, at, self._contexts_at, self._table_at, self._table_stride)
         return KvqBatch(b, (self.contexts, self.page_table, off)), positions, slots
 
