@@ -678,7 +678,8 @@ rp_status rp_kvq_attend(const rp_kvq_cache* cache, const rp_kvq_batch* batch, in
  *   rp_kvq_page_scores  a bound of every page's scores for each query
  *   rp_kvq_pick_pages   the pages to attend to
  *   rp_kvq_attend_picked  attention over them
- * all on the GPU, with nothing for the host to wait for.  They launch kernels on hip_stream and return, as the calls above, and
+ * all on the GPU, with nothing for the host to wait for.  Scores, picks and attention take less than 2^22 rows times KV heads
+ * at a time.  They launch kernels on hip_stream and return, as the calls above, and
  * with their rules for graphs, devices and host structures. */
 
 /* A pool of pages and what its sequences hold, in caller-owned device memory that the
@@ -691,7 +692,7 @@ rp_status rp_kvq_attend(const rp_kvq_cache* cache, const rp_kvq_batch* batch, in
  *   free_pages   [n_pages] the free ones are the first state[0]
  *   state        [4]: free pages; the last call's error (0, or below), its rows, and how many
  *                pages it was short of
- *   workspace    [n_seqs + 1, at least 1088], the calls' own
+ *   workspace    [n_seqs + 1089], the calls' own
  *   n_seqs       0 .. 2^20
  *   n_pages      1 .. 2^24
  *   max_context  most tokens of a sequence, 0 .. 2^30; at most 64 * table_stride */
@@ -734,7 +735,8 @@ rp_status rp_kvq_fit_pages(const rp_kvq_pool* pool, const int32_t* lengths, int3
  * decode steps).  Exact.  A dimension with a NaN key has NaN for both.
  *   ranges  device [n_pages, n_kv_heads, 2, head_dim] bf16, smallest first, 16-byte aligned;
  *           other pages' are left as they are
- * Where no key is appended (rp_kvq_batch) no range is written.  No two sequences may have the same
+ * Where no key is appended (rp_kvq_batch) no range is written; of a page whose last tokens were taken back the
+ * ranges still cover these, and bound what is left, until tokens are appended to it again.  No two sequences may have the same
  * page where rows are.  Errors: RP_ERR_INVALID_ARG, RP_ERR_HIP. */
 rp_status rp_kvq_key_ranges(const rp_kvq_cache* cache, const rp_kvq_batch* batch, void* ranges, void* hip_stream);
 

@@ -182,7 +182,7 @@ __global__ __launch_bounds__(kFitThreads) void k_kvq_fit(KvqFitArgs a, int with_
     length_of[tid] = len;
     if (b < n) {
       if (blockIdx.x == 0) a.row_off[b] = carry[2] + mine[2];
-      if (!with_rows) pool.workspace[b] = carry[0] + mine[0];
+      if (!with_rows) pool.first_need()[b] = carry[0] + mine[0];
       if (alone && !failed) pool.context[b] = len;
     }
     __syncthreads();
@@ -267,7 +267,7 @@ __global__ __launch_bounds__(kFitThreads) void k_kvq_fit(KvqFitArgs a, int with_
     if (tid < n && !failed) pool.context[tid] = len;
   }
   if (tid == 0) {
-    if (!with_rows) pool.workspace[n] = top;
+    if (!with_rows) pool.first_need()[n] = top;
     pool.state[1] = error;
     pool.state[2] = carry[2];
     pool.state[3] = error == kFitPages ? static_cast<int>(min(short_of, int64_t{0x7fffffff})) : 0;
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(256) void k_kvq_fit_rows(KvqFitArgs a) {
   KvqBatch bt;
   bt.n_seqs = n;
   bt.row_off = a.row_off;
-  const int total = a.row_off[n], top = a.pool.workspace[n], last = min(r0 + 255, a.n_rows - 1);
+  const int total = a.row_off[n], top = a.pool.first_need()[n], last = min(r0 + 255, a.n_rows - 1);
   const int lo = wave_find_seq(bt, r0);  // -1: all behind the last
   int hi = wave_find_seq(bt, last);
   FitRow f[4];
@@ -292,7 +292,7 @@ __global__ __launch_bounds__(256) void k_kvq_fit_rows(KvqFitArgs a) {
   if (lo >= 0) {
     if (hi < 0) hi = n - 1;
     const int mine = min(lo + lane, n - 1);
-    const int off = a.row_off[mine], end = a.row_off[mine + 1], len = a.pool.context[mine], need = a.pool.workspace[mine];
+    const int off = a.row_off[mine], end = a.row_off[mine + 1], len = a.pool.context[mine], need = a.pool.first_need()[mine];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const int r = r0 + k * 64 + lane;
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(256) void k_kvq_fit_rows(KvqFitArgs a) {
         f[k] = fit_row(r, lo + s, l, o, e, d);
       } else if (r < total) {
         const int b = last_from(lo, hi, r, [&](int i) { return a.row_off[i]; });
-        f[k] = fit_row(r, b, a.pool.context[b], a.row_off[b], a.row_off[b + 1], a.pool.workspace[b]);
+        f[k] = fit_row(r, b, a.pool.context[b], a.row_off[b], a.row_off[b + 1], a.pool.first_need()[b]);
       }
       if (r < total) id[k] = *(f[k].fresh ? a.pool.free_pages + (top - 1 - f[k].need) : fit_entry(a.pool, f[k].b, f[k].page));
     }

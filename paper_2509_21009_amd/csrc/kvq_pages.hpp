@@ -15,17 +15,22 @@ namespace rollpack {
 
 // ---- pages handed out ------------------------------------------------------------------
 
+constexpr int kFitCounts = 16, kFitCountStride = 64, kFitWorkspace = kFitCountStride * (1 + kFitCounts);
+static_assert(kFitWorkspace == 1088, "rp_kvq_pool's workspace");
+
 // The pool (device memory): a list of free pages whose entries from n_free on are of no page, the sequences' contexts and tables.
 struct KvqPool {
   int32_t* page_table = nullptr; int64_t table_stride = 0;
   int32_t* context = nullptr;   // [n_seqs]
   int32_t* free_pages = nullptr;  // [n_pages]
   int32_t* state = nullptr;     // [4]: n_free, error, rows of the last call, pages it was short of
-  int32_t* workspace = nullptr;  // [max(n_seqs + 1, kFitWorkspace)]: pages that the sequences before need, or counts of blocks
+  int32_t* workspace = nullptr;  // [kFitWorkspace]: counts of blocks, 0 between calls; [n_seqs + 1]: first_need
   int n_seqs = 0, n_pages = 0, max_context = 0;
+#ifdef __HIPCC__
+  __host__ __device__
+#endif
+  int32_t* first_need() const { return workspace + kFitWorkspace; }  // pages that the sequences before need
 };
-constexpr int kFitCounts = 16, kFitCountStride = 64, kFitWorkspace = kFitCountStride * (1 + kFitCounts);
-static_assert(kFitWorkspace == 1088, "rp_kvq_pool's least workspace");
 enum KvqFitError { kFitOk = 0, kFitPages = 1, kFitLength = 2, kFitRows = 3, kFitPool = 4 };
 
 struct KvqFitArgs {

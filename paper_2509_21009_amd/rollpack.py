@@ -885,6 +885,8 @@ class KvqCache:
                 ranges.shape != (self.n_pages, self.n_kv_heads, 2, self.head_dim):
             raise ValueError(f"ranges are a contiguous bfloat16 tensor [{self.n_pages}, {self.n_kv_heads}, 2, {self.head_dim}] on "
                              f"{self.device}, got {ranges.dtype} {tuple(ranges.shape)} on {ranges.device}")
+        if ranges.requires_grad and self.torch.is_grad_enabled():
+            raise ValueError("the 4-bit cache passes no gradient back: detach its tensors, or call it under torch.no_grad()")
         return ranges.data_ptr()
 
     def _per_list(self, t, batch: KvqBatch, dtype, name: str) -> int:
@@ -902,7 +904,8 @@ class KvqCache:
 
     def update_ranges(self, batch: KvqBatch, ranges):
         """The smallest and largest key of each dimension, KV head and page, for the pages that the batch's rows are in,
-        after append: into `ranges` (new_ranges()), which is returned."""
+        after append: into `ranges` (new_ranges()), which is returned.  Where tokens were taken back, ranges cover them until the
+        page's next append."""
         self._call(rp_kvq_key_ranges, batch, self._ranges(ranges))
         return ranges
 
@@ -983,7 +986,7 @@ class KvqPages:
         self.page_table = torch.zeros((n_seqs, max(1, -(-max_context // 64))), **self._ints)
         self.contexts = torch.zeros(n_seqs, **self._ints)
         self.free_pages = torch.arange(n_pages - 1, -1, -1, **self._ints)  # page 0 goes first
-        self.state, self._workspace = torch.zeros(4, **self._ints), torch.zeros(max(n_seqs + 1, 1088), **self._ints)
+        self.state, self._workspace = torch.zeros(4, **self._ints), torch.zeros(n_seqs + 1089, **self._ints)
         self.state[0] = n_pages
         self.device = self._ints["device"] = self.state.device
         if self.device.type != "cuda":

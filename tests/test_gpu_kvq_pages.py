@@ -784,3 +784,44 @@ def test_refusals_on_the_device():
     for args in ((_ints([1]), 1), (_ints([1, 1]).long(), 2), (_ints([1, 1]).cpu(), 2), (_ints([1, 1]), -1), (_ints([1, 1]), 2 ** 24 + 1)):
         with pytest.raises(ValueError):
             p.fit(*args)
+
+
+def test_tensors_that_need_a_gradient_are_refused():
+    s = Setup(4, 2, 64, [100], None, "bf16").fill()
+    b, c = s.batch(), s.cache
+    ranges, picks, q = c.new_ranges(), torch.zeros((1, 2, 2), dtype=torch.int32, device=DEV), s.q.clone().requires_grad_()
+    scores = torch.zeros((1, 2, 2), device=DEV)
+    for call in (lambda: c.update_ranges(b, ranges.clone().requires_grad_()), lambda: c.page_scores(b, q, ranges), lambda: c.attend_picked(b, q, picks),
+                 lambda: c.page_scores(b, s.q, ranges.clone().requires_grad_()), lambda: c.pick_pages(b, scores.clone().requires_grad_(), 2)):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+        with torch.no_grad():
+            call()
+
+
+def test_ranges_of_a_page_whose_last_tokens_were_taken_back():
+    """Bounds of what is left; exact again with the next token."""
+    d = Decode(7, n=1)
+    q, k, v = d.tensors(100)
+    d.step(_ints([100]), 100, q, k, v)
+    d.pages.fit(_ints([70]), 0)
+    held = okvq.held(_f64(k))[:70]
+    table = d.pages.page_table[0, :2].cpu().numpy()
+    lo, hi = (_f64(d.ranges)[table][:, :, i] for i in (0, 1))                   # [pages, n_kv, hd]
+    for p, t in ((0, slice(0, 64)), (1, slice(64, 70))):
+        assert (lo[p] <= held[t].min(0)).all() and (hi[p] >= held[t].max(0)).all()
+    q2, k2, v2 = d.tensors(1)
+    d.step(_ints([71]), 1, q2, k2, v2)
+    held = np.concatenate([held, okvq.held(_f64(k2))])[64:]
+    got = _f64(d.ranges)[table[1]]
+    assert np.array_equal(got[:, 0], held.min(0)) and np.array_equal(got[:, 1], held.max(0))
+
+
+def test_a_workspace_that_another_pool_used():
+    """Of more than 1,024 sequences it keeps sums, of fewer what counts blocks, each in its own part."""
+    a, b = Pools(3000, 1500, 128, 1), Pools(900, 100, 700, 2)
+    b.gpu.struct.workspace = a.gpu.struct.workspace
+    rng = np.random.default_rng(3)
+    for _ in range(3):
+        a.fit(rng.integers(0, 129, 1500).tolist(), 200_000)
+        b.fit(rng.integers(0, 500, 100).tolist(), 60_000)
