@@ -516,20 +516,15 @@ __device__ __forceinline__ void split_signs(Eight<true>& q, bf16x8_t (&above)[3]
   }
 }
 
-// A block's four waves have 16 PT pages each of one KV head, for up to `rows` consecutive rows.  Queries are the 16 rows
-// of 16x16x32 products, 2 hd long, the ranges of 16 pages the 16 columns.  The G heads of a row take `seg` of the 16, a power of
-// two, the last head again in what is left of them, so that lane 16g + c gets four heads' scores of page c or whole rows':
-// their maximum is mostly the lane's own (with the heads in the columns, the maximum over lanes took 2,000 rows 51 us for 33).
-//   KEEP: rows of a sequence read the same ranges, a wave those of 32 or 64 pages for many rows.  Else they are read once, past
-// the caches, whole pages to an instruction, which LDS turns into operands: 64 rows of 6,000 to 33,000 keys (8 KV heads of 128)
-// 22 us, 3.7 TB/s, from HBM; read as operands, 64 bytes of a page to an instruction, 27.7 (24.5 with plain loads).  A wave's
-// way there is context and table, ranges, product: three reads that wait for each other; four heads of a page to a block took
-// 26 us, 32 pages to a wave 25.
-template <int HD, bool F32, int PT, bool KEEP>
-__global__ __launch_bounds__(256, KEEP || F32 ? 2 : 4) void k_kvq_scores(KvqScoreArgs a, int rows) {
+// Rows of a sequence read the same ranges: a block's four waves have 16 PT pages each of one KV head, for up to `rows` consecutive
+// rows.  Queries are the 16 rows of 16x16x32 products, 2 hd long, the ranges of 16 pages the 16 columns.  The G heads of a row take
+// `seg` of the 16, a power of two, the last head again in what is left of them, so that lane 16g + c gets four heads' scores of page
+// c or whole rows': their maximum is mostly the lane's own (with the heads in the columns, the maximum over lanes took 2,000 rows
+// 51 us for 33).
+template <int HD, bool F32, int PT>
+__global__ __launch_bounds__(256, 2) void k_kvq_scores(KvqScoreArgs a, int rows) {
   constexpr int NJ = HD / 32, NQ = F32 ? 3 : 1;
-  constexpr int NPC = HD / 4, NI = NPC / 4;  // 16-byte pieces of a page's ranges; loads of 16 pages
-  __shared__ u32x4 turn[KEEP ? 1 : 4][KEEP ? 1 : 16 * NPC];
+  constexpr int NPC = HD / 4;  // 16-byte pieces of a page's ranges
   const KvqBatch& bt = a.batch;
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -563,32 +558,11 @@ __global__ __launch_bounds__(256, KEEP || F32 ? 2 : 4) void k_kvq_scores(KvqScor
       if (p0 + 16 * t > seen) continue;
       const int use = ok[t] && p0 + 16 * t + c <= seen ? id[t] : 0;  // others read what page 0 has
       const u32x4* ranges = reinterpret_cast<const u32x4*>(a.ranges);
-      if constexpr (KEEP) {
-        const u32x4* at = ranges + (static_cast<size_t>(use) * n_kv + kh) * NPC + 2 * g;
+      const u32x4* at = ranges + (static_cast<size_t>(use) * n_kv + kh) * NPC + 2 * g;
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {  // a line of 128 bytes is four lanes' two pieces
-          lo[t][j] = __builtin_bit_cast(bf16x8_t, at[8 * (j >> 1) + (j & 1)]);
-          hi[t][j] = __builtin_bit_cast(bf16x8_t, at[NPC / 2 + 8 * (j >> 1) + (j & 1)]);
-        }
-      } else {
-        u32x4 x[NI];
-#pragma unroll
-        for (int k = 0; k < NI; ++k) {
-          const size_t page = __shfl(use, k * (64 / NPC) + lane / NPC, 64);
-          x[k] = load_page<true>(ranges + (page * n_kv + kh) * NPC + lane % NPC);
-        }
-#pragma unroll
-        for (int k = 0; k < NI; ++k) {
-          const int page = k * (64 / NPC) + lane / NPC;
-          turn[wave][page * NPC + (lane % NPC ^ page)] = x[k];
-        }
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          const int piece = 8 * (j >> 1) + 2 * g + (j & 1);
-          lo[t][j] = __builtin_bit_cast(bf16x8_t, turn[wave][c * NPC + (piece ^ c)]);
-          hi[t][j] = __builtin_bit_cast(bf16x8_t, turn[wave][c * NPC + ((piece + NPC / 2) ^ c)]);
-        }
+      for (int j = 0; j < NJ; ++j) {  // a line of 128 bytes is four lanes' two pieces
+        lo[t][j] = __builtin_bit_cast(bf16x8_t, at[8 * (j >> 1) + (j & 1)]);
+        hi[t][j] = __builtin_bit_cast(bf16x8_t, at[NPC / 2 + 8 * (j >> 1) + (j & 1)]);
       }
     }
     // The scores of the mine-th of these rows for the lane's pages: those that it does not see have minus infinity.
@@ -660,6 +634,95 @@ __global__ __launch_bounds__(256, KEEP || F32 ? 2 : 4) void k_kvq_scores(KvqScor
     }
     r += n;
   }
+}
+
+// A row whose sequence has no other: its ranges are read once, past the caches.  A wave has 16 PT pages, a lane's each in one read of the
+// table, and walks them 16 at a time, the next ones on their way: whole pages to an instruction, which LDS turns into operands.
+// The heads are the 16 rows of the products, the last one again where there are fewer; MANY: more, taken in turn for each 16 pages.
+//   64 rows of 6,000 to 33,000 keys (8 KV heads of 128) 17.4 us, 4.7 TB/s: HBM, after context and table; with operands instead of whole
+// pages, 64 bytes to an instruction, 27.7; with MANY's loop for all heads 17.9.
+template <int HD, bool F32, int PT, bool MANY>
+__global__ __launch_bounds__(256, F32 ? 2 : 3) void k_kvq_scores_walk(KvqScoreArgs a) {
+  constexpr int NJ = HD / 32, NQ = F32 ? 3 : 1, NPC = HD / 4, NI = NPC / 4;
+  __shared__ u32x4 turn[4][16 * NPC];
+  const KvqBatch& bt = a.batch;
+  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n_kv = a.cache.n_kv, G = a.n_q / n_kv, row = blockIdx.x / n_kv, kh = blockIdx.x - row * n_kv;
+  const int p0 = (blockIdx.y * 4 + wave) * 16 * PT, most = kvq_pages(bt.max_context) - 1;
+  if (p0 >= a.columns) return;
+  const int b = wave_find_seq(bt, row);
+  if (b < 0) return;
+  const int id = most >= 0 ? table_of(bt, b)[min(p0 + lane, most)] : -1;
+  const KvqSeq sq = kvq_seq(bt, b);
+  const int i = row - sq.r0;
+  if (i < 0 || i >= sq.n) return;
+  const int seen = sq.ok ? (sq.ctx - sq.n + i) >> 6 : -1;
+  const bool ok = kvq_page_ok(a.cache, id);
+  float mine = 0.f;
+  if (p0 <= seen) {
+    const int use = ok && p0 + lane <= seen ? id : 0;
+    const u32x4* ranges = reinterpret_cast<const u32x4*>(a.ranges);
+    u32x4 x[2][NI];
+    auto load = [&](int t) {
+#pragma unroll
+      for (int k = 0; k < NI; ++k) {
+        const size_t page = __shfl(use, 16 * t + k * (64 / NPC) + lane / NPC, 64);
+        x[t & 1][k] = load_page<true>(ranges + (page * n_kv + kh) * NPC + lane % NPC);
+      }
+    };
+    Eight<F32> q[NJ];
+    bf16x8_t above[NJ][NQ], below[NJ][NQ];
+    auto queries = [&](int h0) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) q[j].load(a.q, row, kh * G + min(h0 + c, G - 1), 64 * (j >> 1) + 16 * g + 8 * (j & 1));
+    };
+    auto operands = [&]() {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) split_signs(q[j], above[j], below[j]);
+    };
+    queries(0);
+    load(0);
+    operands();
+#pragma unroll
+    for (int t = 0; t < PT; ++t) {
+      if (p0 + 16 * t > seen) break;
+      if (t + 1 < PT && p0 + 16 * t + 16 <= seen) load(t + 1);
+#pragma unroll
+      for (int k = 0; k < NI; ++k) {
+        const int page = k * (64 / NPC) + lane / NPC;
+        turn[wave][page * NPC + (lane % NPC ^ page)] = x[t & 1][k];
+      }
+      __builtin_amdgcn_wave_barrier();
+      float best = 0.f;
+      for (int h0 = 0; h0 < (MANY ? G : 1); h0 += 16) {
+        if (MANY && t + h0 > 0) {  // else they are there
+          queries(h0);
+          operands();
+        }
+        f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          const int piece = 8 * (j >> 1) + 2 * g + (j & 1);
+          const bf16x8_t lo = __builtin_bit_cast(bf16x8_t, turn[wave][c * NPC + (piece ^ c)]);
+          const bf16x8_t hi = __builtin_bit_cast(bf16x8_t, turn[wave][c * NPC + ((piece + NPC / 2) ^ c)]);
+#pragma unroll
+          for (int m = 0; m < NQ; ++m) {
+            acc = mfma16x16x32(above[j][m], hi, acc);
+            acc = mfma16x16x32(below[j][m], lo, acc);
+          }
+        }
+        const float x = larger_of_32(larger_of_16(larger(larger(larger(acc[0], acc[1]), acc[2]), acc[3])));
+        best = h0 ? larger(best, x) : x;
+      }
+      __builtin_amdgcn_wave_barrier();
+      if (g == t) mine = best;
+    }
+  }
+  const int p = p0 + lane;
+  if (!ok || !sq.ok) mine = __builtin_nanf("");
+  if (sq.ok && p > seen) mine = -INFINITY;
+  if (lane < 16 * PT && p < a.columns) a.scores[(static_cast<size_t>(row) * n_kv + kh) * a.columns + p] = mine;
 }
 
 // ---- picks -------------------------------------------------------------------------------
@@ -864,13 +927,22 @@ hipError_t launch_kvq_ranges(const KvqCache& c, const KvqBatch& b, uint16_t* ran
 
 hipError_t launch_kvq_scores(const KvqScoreArgs& a, hipStream_t s) {
   const ScorePlan p = score_plan(a.cache, a.batch, a.columns, a.q.bf16);
+  const bool bf16 = a.q.bf16, wide = a.cache.hd == 128;
+  if (!p.shared) {
+    const bool many = a.n_q > 16 * a.cache.n_kv;
+    const int tiles = many ? 1 : p.tiles;
+    const dim3 grid(static_cast<uint32_t>(a.batch.n_rows) * a.cache.n_kv, static_cast<uint32_t>((a.columns + 64 * tiles - 1) / (64 * tiles)));
+#define RP_WALK(HD, BF16, PT, MANY) \
+  if (wide == (HD == 128) && bf16 == BF16 && tiles == PT && many == MANY) launch_kernel((k_kvq_scores_walk<HD, !BF16, PT, MANY>), grid, dim3(256), 0, s, a);
+#define RP_WALKS(HD, BF16) RP_WALK(HD, BF16, 1, false) RP_WALK(HD, BF16, 4, false) RP_WALK(HD, BF16, 1, true)
+    RP_WALKS(128, true) RP_WALKS(128, false) RP_WALKS(64, true) RP_WALKS(64, false)
+#undef RP_WALKS
+#undef RP_WALK
+    return hipGetLastError();
+  }
   const dim3 grid(static_cast<uint32_t>(p.groups * a.cache.n_kv), static_cast<uint32_t>((a.columns + 64 * p.tiles - 1) / (64 * p.tiles)));
-#define RP_SCORES(HD, BF16, PT, KEEP)                                                                                \
-  if (a.cache.hd == HD && static_cast<bool>(a.q.bf16) == BF16 && p.tiles == PT && static_cast<bool>(p.shared) == KEEP) \
-    launch_kernel((k_kvq_scores<HD, !BF16, PT, KEEP>), grid, dim3(256), 0, s, a, p.rows);
-#define RP_SCORES_HD(HD) RP_SCORES(HD, true, 1, false) RP_SCORES(HD, false, 1, false) RP_SCORES(HD, true, 2, true) RP_SCORES(HD, false, 2, true) RP_SCORES(HD, true, 4, true)
-  RP_SCORES_HD(128) RP_SCORES_HD(64)
-#undef RP_SCORES_HD
+#define RP_SCORES(HD, BF16, PT) if (wide == (HD == 128) && bf16 == BF16 && p.tiles == PT) launch_kernel((k_kvq_scores<HD, !BF16, PT>), grid, dim3(256), 0, s, a, p.rows);
+  RP_SCORES(128, true, 2) RP_SCORES(128, false, 2) RP_SCORES(128, true, 4) RP_SCORES(64, true, 2) RP_SCORES(64, false, 2) RP_SCORES(64, true, 4)
 #undef RP_SCORES
   return hipGetLastError();
 }

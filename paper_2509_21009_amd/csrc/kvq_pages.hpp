@@ -53,9 +53,13 @@ struct KvqScoreArgs {
   int n_q = 0, columns = 0;
 };
 
-// How a call of scores is cut: `rows` consecutive rows and 16 `tiles` pages to a wave, more rows the more waves there are.
+// How a call of scores is cut where rows share ranges: `rows` consecutive rows and 16 `tiles` pages to a wave, more rows the more
+// waves there are.
 // 28/4 heads of 128, us, tiles/rows: 512 rows of 14,000 keys 1/1 42, 2/4 12.8, 2/8 10.0, 2/16 10.5, 4/16 14.2; 2,000 of 30,000
 // 2/8 58, 2/16 52, 4/8 52, 4/32 33, 4/64 42; 9 rows each of 64 sequences in fp32 2/1 23, 2/4 16.7, 2/16 20.5.
+//   Where each row is its sequence's only one a wave has 16 pages of it, or 64 once that leaves many waves: us, 16 | 64, 1 row of
+// 30,000 keys 2.7 | 4.6, 32 of 20,000 to 30,000 7.2 | 7.9; 64 in fp32 12.4 | 11.1, 96 of up to 9,000 with 8 KV heads 8.6 | 8.3, 64 of up to
+// 33,000 18.4 | 17.4.
 struct ScorePlan {
   int rows = 1, tiles = 1;
   int64_t groups = 0;  // of rows
@@ -68,6 +72,8 @@ inline ScorePlan score_plan(const KvqCache& c, const KvqBatch& b, int columns, b
   if (p.shared) {
     p.tiles = bf16 && waves(32, 4) >= 1600 ? 4 : 2;
     while (p.rows < 32 && waves(2 * p.rows, p.tiles) >= 1600) p.rows *= 2;
+  } else if (waves(1, 1) >= 6144) {
+    p.tiles = 4;
   }
   p.groups = (static_cast<int64_t>(b.n_rows) + p.rows - 1) / p.rows;
   return p;

@@ -63,7 +63,7 @@ int main() {
     const bool bf16 = rng() % 2;
     const ScorePlan s = score_plan(c, b, columns, bf16);
     assert(s.rows >= 1 && s.groups * s.rows >= n_rows && (s.groups - 1) * s.rows < n_rows);
-    assert(s.shared ? s.tiles == 2 || (s.tiles == 4 && bf16) : s.tiles == 1 && s.rows == 1);
+    assert(s.shared ? s.tiles == 2 || (s.tiles == 4 && bf16) : (s.tiles == 1 || s.tiles == 4) && s.rows == 1);
     // a grid: 2^32 threads in the first dimension, 65,535 blocks in the second
     assert(s.groups * c.n_kv * 256 < (int64_t{1} << 32) && (columns + 64 * s.tiles - 1) / (64 * s.tiles) < 65536);
     if (picked_blocks(c, b, p) < (int64_t{1} << 22)) assert(picked_blocks(c, b, p) * 64 * p.waves < (int64_t{1} << 32));

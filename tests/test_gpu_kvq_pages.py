@@ -337,6 +337,28 @@ def test_scores(n_q, n_kv, hd, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("room", [10, 1000])
+@pytest.mark.parametrize("n_q,n_kv,hd", [(2, 2, 64), (28, 4, 128), (17, 1, 128), (40, 1, 64), (16, 1, 128)])
+def test_scores_of_long_sequences(n_q, n_kv, hd, room, dtype):
+    """One row each, of contexts that end inside, at and behind 16, 64 and 256 pages; columns past all of them, and rows of no sequence
+    (so many that a wave has 64 pages); a page id outside the cache makes its own score NaN."""
+    s = Setup(n_q, n_kv, hd, [4096, 4097, 1024, 1025, 6200, 16385, 1, 3000], None, dtype, seed=n_q).fill()
+    ranges = s.cache.update_ranges(s.batch(s.ctx), s.cache.new_ranges())
+    out = torch.full((room, n_kv, 300), 7.0, device=DEV)
+    q = torch.full((room, n_q, hd), float("nan"), device=DEV, dtype=s.dt)
+    q[:8] = s.q
+    b = s.cache.batch(_ints(s.ctx), s.dev_table, row_offsets=_ints(range(9)), n_rows=room, max_rows=1)
+    s.cache.page_scores(b, q, ranges, out=out)
+    _check_scores(out[:8], s, s.held(), _f64(s.q))
+    assert (out[8:] == 7.0).all()
+    want = out.clone()
+    s.dev_table[4, 70], want[4, :, 70] = s.cache.n_pages, float("nan")
+    s.dev_table[5, 3], want[5, :, 3] = -1, float("nan")
+    s.cache.page_scores(b, q, ranges, out=out)
+    assert torch.equal(out.nan_to_num(nan=9e30), want.nan_to_num(nan=9e30))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n_q,n_kv,hd,room,columns", [(14, 2, 64, 1700, 15), (28, 4, 128, 3000, 100), (28, 4, 128, 3000, 1024), (40, 1, 64, 5000, 200)])
 def test_scores_of_many_rows(n_q, n_kv, hd, room, columns, dtype):
     """Bounds under which a wave has several rows and 32 or 64 pages, whatever the sequences: short ones and long ones side by side,

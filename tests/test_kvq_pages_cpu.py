@@ -203,13 +203,16 @@ def test_gpu_tests_reach_every_kernel(tmp_path):
         assert plan(14, 2, 64, bf16, 1700, 1700, 15, 1)[:3] == (2, 2, 1) and plan(28, 4, 128, bf16, 3000, 3000, 100, 1)[:3] == (16, 2, 1)
         assert plan(28, 4, 128, bf16, 3000, 3000, 1024, 1)[:3] == (32, 4 if bf16 else 2, 1)
         assert plan(28, 4, 128, bf16, 6, 1, 17, 1)[:3] == (1, 1, 0)
+        # test_scores_of_long_sequences
+        for n_q, n_kv, hd in ((2, 2, 64), (28, 4, 128), (16, 1, 128)):
+            assert plan(n_q, n_kv, hd, bf16, 10, 1, 300, 1)[:3] == (1, 1, 0) and plan(n_q, n_kv, hd, bf16, 1000, 1, 300, 1)[:3] == (1, 4, 0)
 
 
 @pytest.mark.skipif(not os.path.exists(build.HIPCC), reason="no hipcc")
 @pytest.mark.parametrize("source,least,limits", [
     ("k_kvq_picked.hip", 16, (("attend_pickedILi128ELb0ELi4ELb0ELb1E", 128), ("attend_pickedILi128ELb0ELi2ELb1ELb1E", 128), ("attend_pickedILi128ELb0ELi4ELb0ELb0E", 168),
                               ("attend_pickedILi64ELb0ELi4E", 128), ("attend_pickedILi128ELb1ELi8E", 256))),
-    ("k_kvq_pages.hip", 18, (("k_kvq_scoresILi128ELb0ELi1ELb0E", 128), ("k_kvq_scoresILi128ELb0ELi4ELb1E", 256), ("k_kvq_scoresILi128ELb1ELi2ELb1E", 256),
+    ("k_kvq_pages.hip", 18, (("scores_walkILi128ELb0E", 168), ("scores_walkILi128ELb1E", 256), ("k_kvq_scoresILi128ELb0ELi4E", 256), ("k_kvq_scoresILi128ELb1ELi2E", 256),
                              ("k_kvq_rangesILi128E", 128)))])
 def test_registers_and_scratch(source, least, limits):
     """No kernel spills, and the waves of a SIMD are those that the launch bounds and plans count with."""
