@@ -412,7 +412,7 @@ __device__ __forceinline__ void page_range(const PageK<HD>& pk, int held, uint32
 // A wave has `rows` consecutive rows of a KV head; for each page that one of them is the first of its sequence's in, it reads the
 // page's K whole: lane 16g + c has hd/4 dimensions of tokens c, 16 + c, 32 + c, 48 + c, and ends with two dimensions of all
 // tokens.  The next page's K is on its way meanwhile.
-//   84,000 prompt tokens of 8 KV heads of 128 dims: 15.5 us, 3.5 TB/s: HBM, after a chain of offsets, table and page.  Comparing
+//   84,000 prompt tokens of 8 KV heads of 128 dims: 14 us, 3.7 TB/s: HBM, after a chain of offsets, table and page.  Comparing
 // keys as 16-bit integers and exchanging them between lanes, 830 instructions a page instead of 450, took 17; several heads
 // to a wave 14.4 for 13.7 when the append has left the keys in the caches.
 template <int HD>
