@@ -721,13 +721,21 @@ typedef struct rp_kvq_pool {
  *   slots        out [n_rows]: 64 * page + position mod 64, -1 behind the last
  *   n_rows       0 .. 2^24, the most new tokens of all sequences (a padded batch)
  * The outputs overlap neither each other nor the pool nor lengths.  The batch of the new tokens has the pool's contexts and
- * page_table, these row_offsets and n_rows, until the next call.
+ * page_table, these row_offsets and n_rows, until the next call; its max_rows and max_context are n_rows and the pool's, or any
+ * that hold (rp_kvq_fit_pages_within sees to it): a row past them would have its page, and no key there.
  * An error that only the device can see goes to state[1]; the call then changes nothing else of
  * the pool and has no rows: 1 too few free pages (state[3]: how many are missing), 2 a length
  * outside 0 .. max_context, 3 more than n_rows new tokens, 4 a state that no calls have made.
  * Returned errors: RP_ERR_INVALID_ARG, RP_ERR_HIP. */
 rp_status rp_kvq_fit_pages(const rp_kvq_pool* pool, const int32_t* lengths, int32_t n_rows, int32_t* row_offsets,
                            int32_t* positions, int32_t* slots, void* hip_stream);
+
+/* rp_kvq_fit_pages for a batch that says more of its sequences (a decode step, section 2.2: a row of each): lengths go up to
+ * max_context, 0 .. the pool's, which error 2 then goes by, and a sequence has up to max_rows new tokens, 0 .. n_rows; error 5: one
+ * has more.  The batch of the new tokens has these bounds. */
+rp_status rp_kvq_fit_pages_within(const rp_kvq_pool* pool, const int32_t* lengths, int32_t n_rows, int32_t max_rows,
+                                  int32_t max_context, int32_t* row_offsets, int32_t* positions, int32_t* slots,
+                                  void* hip_stream);
 
 /* The ranges of the pages that the batch's rows are in, after rp_kvq_append of these rows:
  * for each KV head and dimension the smallest and the largest of the keys that the cache

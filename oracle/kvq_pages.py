@@ -23,8 +23,10 @@ class Pool:
         self.contexts = [0] * n_seqs
         self.missing = 0
 
-    def fit(self, lengths, n_rows: int):
+    def fit(self, lengths, n_rows: int, max_rows=None, max_context=None):
         """(error, row offsets, positions, slots); with an error nothing changes and there are no rows."""
+        max_rows = n_rows if max_rows is None else max_rows
+        max_context = self.max_context if max_context is None else max_context
         lengths = [int(x) for x in lengths]
         old = self.contexts
         need = sum(max(0, pages(n) - pages(c)) for n, c in zip(lengths, old))
@@ -32,12 +34,14 @@ class Pool:
         rows = sum(max(0, n - c) for n, c in zip(lengths, old))
         self.missing = 0
         error = 0
-        if any(not 0 <= n <= self.max_context for n in lengths):
+        if any(not 0 <= n <= max_context for n in lengths):
             error = 2
         elif need > back + len(self.free):
             error, self.missing = 1, need - back - len(self.free)
         elif rows > n_rows:
             error = 3
+        elif any(n - c > max_rows for n, c in zip(lengths, old)):
+            error = 5
         if error:
             return error, np.zeros(len(lengths) + 1, np.int32), np.full(n_rows, -1, np.int32), np.full(n_rows, -1, np.int32)
         returned = []

@@ -101,12 +101,12 @@ __global__ __launch_bounds__(kFitThreads) void k_kvq_fit(KvqFitArgs a, int with_
 
   // What all sequences need, give back and add, in 64 bits; anything out of bounds.
   int64_t all[3] = {0, 0, 0};
-  bool bad_len = false, bad_pool = false;
+  bool bad_len = false, bad_pool = false, bad_rows = false;
   int old = 0, len = 0;  // the thread's last sequence, its only one where there are no more than threads
   for (int b = tid; b < n; b += kFitThreads) {
     old = pool.context[b];
     len = a.length[b];
-    const bool bl = len < 0 || len > pool.max_context, bp = old < 0 || old > pool.max_context;
+    const bool bl = len < 0 || len > a.max_context, bp = old < 0 || old > pool.max_context;
     bad_len |= bl;
     bad_pool |= bp;
     if (bl || bp) continue;
@@ -114,8 +114,9 @@ __global__ __launch_bounds__(kFitThreads) void k_kvq_fit(KvqFitArgs a, int with_
     all[0] += max(0, want - have);
     all[1] += max(0, have - want);
     all[2] += max(0, len - old);
+    bad_rows |= len - old > a.max_rows;
   }
-  const uint64_t any_len = __ballot(bad_len), any_pool = __ballot(bad_pool);
+  const uint64_t any_len = __ballot(bad_len), any_pool = __ballot(bad_pool), any_rows = __ballot(bad_rows);
   int upto[3];  // over the wave's lanes up to this one, below 2^31 where nothing fails
 #pragma unroll
   for (int i = 0; i < 3; ++i) {  // at most 2^10 sequences of 2^30 to a thread: halves of 20 bits, whose sums fit
@@ -124,7 +125,7 @@ __global__ __launch_bounds__(kFitThreads) void k_kvq_fit(KvqFitArgs a, int with_
     upto[i] = static_cast<int>(static_cast<uint32_t>(low) + (static_cast<uint32_t>(high) << 20));
     if (lane == 63) sums[i][wave] = (static_cast<int64_t>(high) << 20) + low;
   }
-  if (lane == 0) flags[wave] = (any_len ? 1 : 0) | (any_pool ? 2 : 0);
+  if (lane == 0) flags[wave] = (any_len ? 1 : 0) | (any_pool ? 2 : 0) | (any_rows ? 4 : 0);
   __syncthreads();
   // The waves' sums, 16 lanes for each of the three: up to this wave's, and all.
   const int64_t of_wave = lane < 3 * kWaves ? sums[lane / kWaves][lane % kWaves] : 0;
@@ -135,10 +136,10 @@ __global__ __launch_bounds__(kFitThreads) void k_kvq_fit(KvqFitArgs a, int with_
   };
   const int64_t need = sum_to(0, kWaves - 1), back = sum_to(1, kWaves - 1), rows = sum_to(2, kWaves - 1);
   const int seen = lane < kWaves ? flags[lane] : 0;
-  const int flag = (n_free < 0 || n_free > pool.n_pages || __ballot(seen & 2) ? 2 : 0) | (__ballot(seen & 1) ? 1 : 0);
+  const int flag = (n_free < 0 || n_free > pool.n_pages || __ballot(seen & 2) ? 2 : 0) | (__ballot(seen & 1) ? 1 : 0) | (__ballot(seen & 4) ? 4 : 0);
   const int64_t short_of = need - back - n_free;
   const int error = (flag & 2) || n_free + back > pool.n_pages ? kFitPool : (flag & 1) ? kFitLength : short_of > 0 ? kFitPages
-                    : rows > a.n_rows ? kFitRows : kFitOk;
+                    : rows > a.n_rows ? kFitRows : (flag & 4) ? kFitSeqRows : kFitOk;
   const bool failed = error != kFitOk;  // nothing changes: no rows
   const int top = n_free + static_cast<int>(failed ? 0 : back);
   int carry[3] = {0, 0, 0};

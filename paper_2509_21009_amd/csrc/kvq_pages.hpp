@@ -31,7 +31,7 @@ struct KvqPool {
 #endif
   int32_t* first_need() const { return workspace + kFitWorkspace; }  // pages that the sequences before need
 };
-enum KvqFitError { kFitOk = 0, kFitPages = 1, kFitLength = 2, kFitRows = 3, kFitPool = 4 };
+enum KvqFitError { kFitOk = 0, kFitPages = 1, kFitLength = 2, kFitRows = 3, kFitPool = 4, kFitSeqRows = 5 };
 
 struct KvqFitArgs {
   KvqPool pool;
@@ -40,6 +40,7 @@ struct KvqFitArgs {
   int32_t* position = nullptr;      // [n_rows]
   int32_t* slot = nullptr;          // [n_rows]
   int n_rows = 0;
+  int max_rows = 0, max_context = 0;  // of a sequence, in the batch that the call makes
 };
 
 // ---- ranges, scores, picks ---------------------------------------------------------------

@@ -588,6 +588,11 @@ rp_status rp_kvq_attend(const rp_kvq_cache* cache, const rp_kvq_batch* batch, in
 
 rp_status rp_kvq_fit_pages(const rp_kvq_pool* pool, const int32_t* lengths, int32_t n_rows, int32_t* row_offsets,
                            int32_t* positions, int32_t* slots, void* hip_stream) {
+  return rp_kvq_fit_pages_within(pool, lengths, n_rows, n_rows, pool ? pool->max_context : 0, row_offsets, positions, slots, hip_stream);
+}
+
+rp_status rp_kvq_fit_pages_within(const rp_kvq_pool* pool, const int32_t* lengths, int32_t n_rows, int32_t max_rows, int32_t max_context,
+                                  int32_t* row_offsets, int32_t* positions, int32_t* slots, void* hip_stream) {
   return guarded([&] {
     kvq_require(pool, "null pool");
     kvq_require(pool->n_seqs >= 0 && pool->n_seqs <= (1 << 20), "0 <= n_seqs <= 2^20");
@@ -596,6 +601,8 @@ rp_status rp_kvq_fit_pages(const rp_kvq_pool* pool, const int32_t* lengths, int3
     kvq_require(pool->table_stride >= 1 && pool->table_stride <= (int64_t{1} << 32), "1 <= table_stride <= 2^32");
     kvq_require(pool->max_context <= pool->table_stride * rollpack::kKvqPage, "max_context is past the page table's rows");
     kvq_require(n_rows >= 0 && n_rows <= (1 << 24), "0 <= n_rows <= 2^24");
+    kvq_require(max_rows >= 0 && max_rows <= n_rows, "0 <= max_rows <= n_rows");
+    kvq_require(max_context >= 0 && max_context <= pool->max_context, "max_context is past the pool's");
     if (pool->n_seqs > 0) {
       kvq_require_ints(pool->page_table, "page_table must be device memory of 32-bit numbers");
       kvq_require_ints(pool->contexts, "contexts must be device memory of 32-bit numbers");
@@ -624,6 +631,8 @@ rp_status rp_kvq_fit_pages(const rp_kvq_pool* pool, const int32_t* lengths, int3
     a.position = positions;
     a.slot = slots;
     a.n_rows = n_rows;
+    a.max_rows = max_rows;
+    a.max_context = max_context;
     kvq_launched(rollpack::launch_kvq_fit(a, kvq_stream(hip_stream)), "rp_kvq_fit_pages");
   });
 }

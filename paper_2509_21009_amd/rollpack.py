@@ -107,7 +107,7 @@ class RpKvqPool(ctypes.Structure):
 
 
 KVQ_FIT_ERRORS = ("none", "too few free pages", "a length outside 0 .. max_context", "more new tokens than n_rows",
-                  "a state that no calls have made")
+                  "a state that no calls have made", "more than max_rows new tokens of a sequence")
 
 
 class RollpackError(RuntimeError):
@@ -177,6 +177,7 @@ SIGNATURES = {
     "rp_kvq_attend_workspace": (ctypes.c_int, [_KC, _KB, ctypes.c_int32, _SZP]),
     "rp_kvq_attend": (ctypes.c_int, [_KC, _KB, ctypes.c_int32, ctypes.c_float, _KT, _KT, _P, ctypes.c_size_t, _P]),
     "rp_kvq_fit_pages": (ctypes.c_int, [_KP, _P, ctypes.c_int32, _P, _P, _P, _P]),
+    "rp_kvq_fit_pages_within": (ctypes.c_int, [_KP, _P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _P, _P, _P, _P]),
     "rp_kvq_key_ranges": (ctypes.c_int, [_KC, _KB, _P, _P]),
     "rp_kvq_page_scores": (ctypes.c_int, [_KC, _KB, ctypes.c_int32, _KT, _P, _P, ctypes.c_int32, _P]),
     "rp_kvq_pick_pages": (ctypes.c_int, [_KB, ctypes.c_int32, _P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
@@ -549,6 +550,12 @@ def rp_kvq_attend(cache: RpKvqCache, batch: RpKvqBatch, n_q_heads: int, scale: f
 def rp_kvq_fit_pages(pool: RpKvqPool, lengths_ptr: int, n_rows: int, row_offsets_ptr: int, positions_ptr: int,
                      slots_ptr: int, stream_ptr: int) -> None:
     _check(load_library().rp_kvq_fit_pages(pool, lengths_ptr, n_rows, row_offsets_ptr, positions_ptr, slots_ptr, stream_ptr))
+
+
+def rp_kvq_fit_pages_within(pool: RpKvqPool, lengths_ptr: int, n_rows: int, max_rows: int, max_context: int, row_offsets_ptr: int,
+                            positions_ptr: int, slots_ptr: int, stream_ptr: int) -> None:
+    _check(load_library().rp_kvq_fit_pages_within(pool, lengths_ptr, n_rows, max_rows, max_context, row_offsets_ptr, positions_ptr,
+                                                  slots_ptr, stream_ptr))
 
 
 def rp_kvq_key_ranges(cache: RpKvqCache, batch: RpKvqBatch, ranges_ptr: int, stream_ptr: int) -> None:
@@ -1005,7 +1012,7 @@ class KvqPages:
         each row's position, and 64 * page + position % 64, -1 in padded rows (int32 tensors).
         n_rows bounds the new tokens of all sequences, max_rows those of one (n_rows; 1 for a decode step, whose calls are faster
         for knowing it), max_context the lengths (the pool's).
-        What does not fit shows in state[1] (status()): then nothing changed and there are no rows."""
+        What does not fit, these bounds among it, shows in state[1] (status()): then nothing changed and there are no rows."""
         torch, n_seqs = self.torch, self.n_seqs
         if lengths.dtype != torch.int32 or lengths.device != self.device or lengths.shape != (n_seqs,) or not lengths.is_contiguous():
             raise ValueError(f"lengths are a contiguous int32 tensor [{n_seqs}] on {self.device}, got {lengths.dtype} "
@@ -1018,8 +1025,8 @@ class KvqPages:
         # one allocation for the three: each would cost the call 1.4 us
         off, positions, slots = torch.empty(n_seqs + 1 + 2 * n_rows, **self._ints).split_with_sizes((n_seqs + 1, n_rows, n_rows))
         at = off.data_ptr()
-        args = self.struct, lengths.data_ptr(), n_rows, at, at + 4 * (n_seqs + 1), at + 4 * (n_seqs + 1 + n_rows)
-        fit, index = load_library().rp_kvq_fit_pages, self.device.index
+        args = self.struct, lengths.data_ptr(), n_rows, max_rows, max_context, at, at + 4 * (n_seqs + 1), at + 4 * (n_seqs + 1 + n_rows)
+        fit, index = load_library().rp_kvq_fit_pages_within, self.device.index
         if self._current_device() == index:
             status = fit(*args, self._raw_stream(index))
         else:

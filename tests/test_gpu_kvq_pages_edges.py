@@ -1,0 +1,122 @@
+"""The 4-bit cache's page calls on the GPU where their bounds end (oracle/kvq_pages.py)."""
+import numpy as np
+import pytest
+
+from tests.gpu_helpers import rp
+from tests.test_gpu_kvq_pages import DEV, Decode, Pools, _ints
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+# ---- bounds of the batch that fit makes ----------------------------------------------
+
+class Bounded(Pools):
+    def fit(self, lengths, n_rows, **bounds):
+        """Both pools, with the same bounds; the GPU's is looked at as a whole."""
+        table = self.gpu.page_table.clone()
+        batch, positions, slots = self.gpu.fit(_ints(np.asarray(lengths)), n_rows, **bounds)
+        error, off, pos, slot = self.plain.fit(lengths, n_rows, **bounds)
+        st = self.check_state()
+        assert (st["error"], st["missing_pages"], st["rows"]) == (error, self.plain.missing, off[-1])
+        assert st["message"] == rp().KVQ_FIT_ERRORS[error]
+        assert np.array_equal(batch.row_offsets.cpu().numpy(), off)
+        assert np.array_equal(positions.cpu().numpy(), pos) and np.array_equal(slots.cpu().numpy(), slot)
+        assert not error or torch.equal(self.gpu.page_table, table)
+        assert (batch.struct.max_rows, batch.struct.max_context) == (bounds.get("max_rows", n_rows), bounds.get("max_context", self.gpu.max_context))
+        return error
+
+
+def test_a_sequence_with_more_rows_than_max_rows_changes_nothing():
+    p = Bounded(9, 3, 640, 4)
+    assert p.fit([10, 5, 0], 16) == 0
+    assert p.fit([11, 7, 0], 16, max_rows=1) == 5
+    assert p.fit([11, 6, 64], 100, max_rows=1) == 5     # a prompt in a step of single tokens
+    assert p.fit([11, 6, 1], 100, max_rows=0) == 5
+    assert p.fit([11, 6, 1], 100, max_rows=1) == 0
+    assert p.fit([0, 70, 1], 100, max_rows=64) == 0
+    assert p.fit([0, 135, 66], 200, max_rows=64) == 5
+    assert p.fit([0, 135, 66], 200, max_rows=65) == 0
+    assert p.fit([0, 130, 0], 5, max_rows=0) == 0       # taking back needs none
+
+
+def test_a_length_above_the_calls_max_context_changes_nothing():
+    p = Bounded(12, 3, 640, 4)
+    assert p.fit([10, 5, 0], 16, max_context=10) == 0
+    assert p.fit([11, 5, 0], 16, max_context=10) == 2
+    assert p.fit([10, 5, 0], 16, max_context=9) == 2    # one that has no new token
+    assert p.fit([9, 5, 3], 16, max_context=9) == 0     # a longer one that shrinks is within
+    assert p.fit([0, 0, 1], 16, max_context=0) == 2
+    assert p.fit([0, 0, 0], 16, max_context=0) == 0
+    assert p.fit([640, 0, 0], 640, max_context=640) == 0
+
+
+def test_which_error_is_told():
+    """A length out of range, too few pages, too many rows, too many of a sequence: the first of these."""
+    p = Bounded(4, 2, 640, 1)
+    assert p.fit([3, 3], 6) == 0
+    assert p.fit([301, 9], 4, max_rows=1, max_context=300) == 2
+    assert p.fit([300, 9], 4, max_rows=1, max_context=300) == 1
+    assert p.fit([100, 9], 4, max_rows=1, max_context=300) == 3
+    assert p.fit([100, 9], 103, max_rows=96, max_context=300) == 5
+    assert p.fit([100, 9], 103, max_rows=97, max_context=300) == 0
+
+
+@pytest.mark.parametrize("n", [64, 65, 1024, 1025, 3000])
+def test_bounds_of_any_one_sequence(n):
+    """The first, one in the middle and the last; up to 1,024 sequences and more, one block and many."""
+    p = Bounded(2 * n, n, 128, 2)
+    now = np.random.default_rng(n).integers(0, 64, n)
+    assert p.fit(now.tolist(), 64 * n) == 0
+    for b in (0, n // 2, n - 1):
+        for room in (3 * n, 70_000):
+            to = now + 1
+            to[b] += 1
+            assert p.fit(to.tolist(), room, max_rows=1) == 5
+            to[b] = 101
+            assert p.fit(to.tolist(), room, max_rows=101, max_context=100) == 2
+    assert p.fit((now + 1).tolist(), n, max_rows=1, max_context=64) == 0
+
+
+def test_rows_past_the_bounds_reach_no_cache():
+    """A prompt in a step of single tokens: nothing of the pool, the cache or the ranges changes, and the same lengths under bounds that
+    hold attend to what was appended."""
+    d = Decode(11)
+    q, k, v = d.tensors(94)
+    d.step(_ints([30, 0, 0, 64, 0]), 94, q, k, v)
+    kept = [t.clone() for t in (d.cache.blocks, d.ranges, d.pages.contexts, d.pages.page_table, d.pages.free_pages)]
+    lengths = [31, 0, 2, 65, 0]
+    q, k, v = d.tensors(6)
+    batch, positions, slots = d.pages.fit(_ints(lengths), 6, max_rows=1)
+    assert d.pages.status()["error"] == 5 and (positions == -1).all() and (slots == -1).all()
+    d.cache.append(batch, k, v)
+    d.cache.update_ranges(batch, d.ranges)
+    for a, b in zip((d.cache.blocks, d.ranges, d.pages.contexts, d.pages.page_table, d.pages.free_pages), kept):
+        assert torch.equal(a, b)
+    out, picks, scores, positions, slots = d.step(_ints(lengths), 6, q, k, v)
+    assert torch.isfinite(out[:4]).all() and positions.tolist() == [30, 0, 1, 64, -1, -1]
+
+
+def test_bounds_in_a_graph():
+    """Replays read the lengths that are there: those past the bounds change nothing, those within are served."""
+    p, lengths = Bounded(40, 8, 300, 3), _ints(np.zeros(8))
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        p.gpu.fit(lengths, 8, max_rows=1, max_context=200)
+    torch.cuda.current_stream().wait_stream(stream)
+    with torch.cuda.graph(graph):
+        batch, positions, slots = p.gpu.fit(lengths, 8, max_rows=1, max_context=200)
+    assert p.fit([70, 1, 199, 0, 5, 6, 200, 8], 500) == 0
+    now = np.array(p.plain.contexts)
+    for grow, error in (([1, 1, 1, 1, 1, 1, 0, 1], 0), ([0, 0, 1, 0, 0, 0, 0, 0], 2), ([2, 0, 0, 0, 0, 0, 0, 0], 5), ([1, 0, 0, 2, 1, 0, -3, 0], 5),
+                        ([1, 0, 0, 1, 1, 0, -3, 0], 0)):
+        to = (now + np.array(grow)).tolist()
+        lengths.copy_(_ints(to))
+        graph.replay()
+        want, off, pos, slot = p.plain.fit(to, 8, 1, 200)
+        assert p.check_state()["error"] == want == error
+        assert np.array_equal(batch.row_offsets.cpu().numpy(), off)
+        assert np.array_equal(positions.cpu().numpy(), pos) and np.array_equal(slots.cpu().numpy(), slot)
+        now = np.array(p.plain.contexts)
