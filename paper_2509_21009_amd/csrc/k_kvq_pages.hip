@@ -534,15 +534,10 @@ __global__ __launch_bounds__(256, 2) void k_kvq_scores(KvqScoreArgs a, int rows)
   const int group = blockIdx.x / n_kv, kh = blockIdx.x - group * n_kv;
   const int p0 = (blockIdx.y * 4 + wave) * 16 * PT;
   if (p0 >= a.columns) return;
-  const int last_row = min((group + 1) * rows, bt.n_rows), most = kvq_pages(bt.max_context) - 1;
+  const int last_row = min((group + 1) * rows, bt.n_rows);
   for (int r = group * rows; r < last_row;) {
     const int b = wave_find_seq(bt, r);
     if (b < 0) return;
-    // entries of the table beside the context; those past it may be anything
-    int id[PT];
-    const int32_t* pt = table_of(bt, b);
-#pragma unroll
-    for (int t = 0; t < PT; ++t) id[t] = most >= 0 ? pt[min(p0 + 16 * t + c, most)] : -1;
     const KvqSeq sq = kvq_seq(bt, b);
     const int i = r - sq.r0;
     if (i < 0 || i >= sq.n) {  // past max_rows
@@ -550,14 +545,21 @@ __global__ __launch_bounds__(256, 2) void k_kvq_scores(KvqScoreArgs a, int rows)
       continue;
     }
     const int n = min(last_row, sq.r0 + sq.n) - r, first = sq.ctx - sq.n + i;  // rows, the first one's position
-    const int seen = sq.ok ? (first + n - 1) >> 6 : -1;                           // the last page that some row sees
+    const int seen = kvq_row_sees(sq, i + n - 1);                                 // the last page that some row sees
+    int id[PT];
+    const int32_t* pt = table_of(bt, b);
+#pragma unroll
+    for (int t = 0; t < PT; ++t) {
+      const int entry = kvq_seen_entry(p0 + 16 * t + c, seen);
+      id[t] = entry >= 0 ? pt[entry] : -1;
+    }
     bf16x8_t hi[PT][NJ], lo[PT][NJ];
     bool ok[PT];  // the lane's page is in the cache
 #pragma unroll
     for (int t = 0; t < PT; ++t) {
       ok[t] = kvq_page_ok(a.cache, id[t]);
       if (p0 + 16 * t > seen) continue;
-      const int use = ok[t] && p0 + 16 * t + c <= seen ? id[t] : 0;  // others read what page 0 has
+      const int use = ok[t] ? id[t] : 0;  // others read what page 0 has
       const u32x4* ranges = reinterpret_cast<const u32x4*>(a.ranges);
       const u32x4* at = ranges + (static_cast<size_t>(use) * n_kv + kh) * NPC + 2 * g;
 #pragma unroll
@@ -650,19 +652,19 @@ __global__ __launch_bounds__(256, F32 ? 2 : 3) void k_kvq_scores_walk(KvqScoreAr
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n_kv = a.cache.n_kv, G = a.n_q / n_kv, row = blockIdx.x / n_kv, kh = blockIdx.x - row * n_kv;
-  const int p0 = (blockIdx.y * 4 + wave) * 16 * PT, most = kvq_pages(bt.max_context) - 1;
+  const int p0 = (blockIdx.y * 4 + wave) * 16 * PT;
   if (p0 >= a.columns) return;
   const int b = wave_find_seq(bt, row);
   if (b < 0) return;
-  const int id = most >= 0 ? table_of(bt, b)[min(p0 + lane, most)] : -1;
   const KvqSeq sq = kvq_seq(bt, b);
   const int i = row - sq.r0;
   if (i < 0 || i >= sq.n) return;
-  const int seen = sq.ok ? (sq.ctx - sq.n + i) >> 6 : -1;
+  const int seen = kvq_row_sees(sq, i), entry = kvq_seen_entry(p0 + lane, seen);
+  const int id = entry >= 0 ? table_of(bt, b)[entry] : -1;
   const bool ok = kvq_page_ok(a.cache, id);
   float mine = 0.f;
   if (p0 <= seen) {
-    const int use = ok && p0 + lane <= seen ? id : 0;
+    const int use = ok ? id : 0;
     const u32x4* ranges = reinterpret_cast<const u32x4*>(a.ranges);
     u32x4 x[2][NI];
     auto load = [&](int t) {

@@ -54,6 +54,12 @@ struct KvqScoreArgs {
   int n_q = 0, columns = 0;
 };
 
+// The last page that row i of a sequence sees; below 0: none, or its sequence is out of the batch's bounds.
+RP_HD int kvq_row_sees(const KvqSeq& s, int i) { return s.ok ? (s.ctx - s.n + i) >> 6 : -1; }
+// The entry of the page table that page p's id is read from, where rows see pages 0 .. `seen`: -1, none, past them.  What the table has
+// behind a sequence's context is not read.
+RP_HD int kvq_seen_entry(int p, int seen) { return p <= seen ? p : -1; }
+
 // How a call of scores is cut where rows share ranges: `rows` consecutive rows and 16 `tiles` pages to a wave, more rows the more
 // waves there are.
 // 28/4 heads of 128, us, tiles/rows: 512 rows of 14,000 keys 1/1 42, 2/4 12.8, 2/8 10.0, 2/16 10.5, 4/16 14.2; 2,000 of 30,000

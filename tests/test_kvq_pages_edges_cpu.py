@@ -1,12 +1,17 @@
-"""The 4-bit cache's page calls without a GPU: the bounds of a batch that a pool hands out."""
+"""The 4-bit cache's page calls without a GPU: the bounds of a batch that a pool hands out, what is read of a page table."""
 import os
+import re
+import subprocess
 
 import pytest
 
 from oracle import kvq_pages as op
+from paper_2509_21009_amd import build
 from paper_2509_21009_amd import rollpack as rp
 from tests.test_kvq_cpu import PTR, _refused
 from tests.test_kvq_pages_cpu import _pool
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture(scope="module")
@@ -38,3 +43,17 @@ def test_plain_pool_bounds():
         before = list(p.contexts)
         got = p.fit(lengths, n_rows, max_rows, max_context)
         assert got[0] == error and p.contexts == (before if error else lengths) and (not error or got[1].tolist() == [0] * 4)
+
+
+# ---- the page table ------------------------------------------------------------------
+
+def test_scores_read_no_entry_past_a_context(tmp_path):
+    exe = tmp_path / "kvq_pages_table"
+    subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all", f"-I{build.CSRC}",
+                    os.path.join(ROOT, "tests", "cpp", "kvq_pages_table.cpp"), "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0 and "table tests passed" in r.stdout, r.stderr
+    # and the kernels take their entries from there alone
+    text = open(os.path.join(build.CSRC, "k_kvq_pages.hip")).read()
+    text = text[text.index("// ---- scores"):text.index("// ---- picks")]
+    assert text.count("kvq_seen_entry(") == 2 and re.findall(r"(?:\bpt|table_of\(bt, b\))\[(.*?)\]", text) == ["entry", "entry"]
