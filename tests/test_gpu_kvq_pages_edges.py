@@ -1,9 +1,13 @@
-"""The 4-bit cache's page calls on the GPU where their bounds end (oracle/kvq_pages.py)."""
+"""The 4-bit cache's page calls on the GPU where their bounds end, and every form of the scores of pages and of
+attention over picked ones (oracle/kvq_pages.py).  Tolerances are those of tests/test_gpu_kvq_pages.py and tests/test_gpu_kvq_softmax.py.
+"""
 import numpy as np
 import pytest
 
+from tests import test_gpu_kvq_picked_softmax as softmax
 from tests.gpu_helpers import rp
-from tests.test_gpu_kvq_pages import DEV, Decode, Pools, _ints
+from tests.kvq_page_forms import CALLS, HARD, SCORES
+from tests.test_gpu_kvq_pages import DEV, Decode, Pools, Setup, _check_picked, _check_scores, _f64, _ints, _lists
 
 pytestmark = pytest.mark.gpu
 
@@ -120,3 +124,73 @@ def test_bounds_in_a_graph():
         assert np.array_equal(batch.row_offsets.cpu().numpy(), off)
         assert np.array_equal(positions.cpu().numpy(), pos) and np.array_equal(slots.cpu().numpy(), slot)
         now = np.array(p.plain.contexts)
+
+
+# ---- every form of scores, and of attention over picked pages --------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("call", SCORES)
+def test_every_form_of_page_scores(call, dtype):
+    n_q, n_kv, hd, ctx, rows, room, columns = SCORES[call]
+    s = Setup(n_q, n_kv, hd, ctx, rows, dtype, seed=hd + columns).fill()
+    ranges, n = s.cache.update_ranges(s.batch(s.ctx), s.cache.new_ranges()), sum(s.rows)
+    q = torch.full((room, n_q, hd), float("nan"), device=DEV, dtype=s.dt)
+    q[:n] = s.q
+    out = torch.full((room, n_kv, columns), 7.0, device=DEV)
+    s.cache.page_scores(s.batch(n_rows=room, max_rows=1 if rows is None else room), q, ranges, out=out)
+    _check_scores(out[:n], s, s.held(), _f64(s.q))
+    assert (out[n:] == 7.0).all()
+    table = s.dev_table.clone()
+    s.dev_table[torch.arange(s.table.shape[1], device=DEV) >= torch.tensor([-(-c // 64) for c in ctx], device=DEV)[:, None]] = 2 ** 31 - 1
+    again = torch.full_like(out, 7.0)  # what the table has behind a context does not count
+    s.cache.page_scores(s.batch(n_rows=room, max_rows=1 if rows is None else room), q, ranges, out=again)
+    s.dev_table.copy_(table)
+    assert torch.equal(again, out)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("call", CALLS)
+def test_every_form_of_attend_picked(call, dtype):
+    n_q, n_kv, hd, ctx, rows, n = CALLS[call]
+    s = Setup(n_q, n_kv, hd, ctx, rows, dtype, seed=n + hd).fill()
+    rng = np.random.default_rng(n)
+    for style in ("picks", "any"):
+        picks = _lists(s, n, rng, style)
+        out = torch.full_like(s.q, 9.0)
+        assert s.cache.attend_picked(s.batch(), s.q, torch.from_numpy(picks).to(DEV), out=out) is out
+        _check_picked(s, out, picks)
+
+
+@pytest.mark.parametrize("form", HARD)
+def test_eight_waves_where_the_softmax_is_hard(form, monkeypatch):
+    monkeypatch.setitem(softmax.FORMS, form, HARD[form])
+    softmax.test_weights_far_below_the_largest(form)
+    softmax.test_maxima_that_move(form)
+    softmax.test_values_beyond_half_precision_after_a_move(form)
+    softmax.test_strong_keys_everywhere(form)
+    softmax.test_large_scores_and_values_near_the_end_of_the_range(form)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("call", ["eight-wide-128", "eight-wide-64-rows", "eight-17-heads", "eight-narrow-128-rows"])
+def test_eight_waves_of_bad_pages_and_empty_lists(call, dtype):
+    """Ids outside the cache and NaN keys make their row and KV head NaN where they are listed; lists without a page that the row sees give
+    zeros, rows of no sequence are left as they are."""
+    n_q, n_kv, hd, ctx, rows, n = CALLS[call]
+    s = Setup(n_q, n_kv, hd, ctx, rows, dtype, seed=3)
+    s.k[ctx[0] + 70, 0, 5] = float("nan")                # of the second sequence, page 1
+    s.fill()
+    picks = _lists(s, n, np.random.default_rng(5))
+    first = np.concatenate([[0], np.cumsum(s.rows)])[:-1]
+    picks[first[0], 0] = [0, 3, 5] + [-1] * (n - 3)      # page 3 is lost
+    picks[first[1], 0] = [0, 1, 2] + [-1] * (n - 3)
+    picks[first[3], 0] = [-1] * (n - 2) + [11, 2 ** 31 - 1]  # of 700 tokens: pages 0 .. 10
+    s.dev_table[0, 3] = s.cache.n_pages
+    room = sum(s.rows) + 3
+    q = torch.cat([s.q, s.q[:3]])
+    out = torch.full_like(q, 5.0)
+    all_picks = torch.from_numpy(np.concatenate([picks, picks[:3]])).to(DEV)
+    s.cache.attend_picked(s.batch(n_rows=room), q, all_picks, out=out)
+    assert torch.isnan(out[first[0]]).all() and torch.isnan(out[first[1]]).all() and (out[first[3]] == 0).all()
+    assert (out[sum(s.rows):] == 5.0).all()
+    _check_picked(s, out, picks, seqs=[2, 4, 5])

@@ -1,4 +1,6 @@
-"""The 4-bit cache's page calls without a GPU: the bounds of a batch that a pool hands out, what is read of a page table."""
+"""The 4-bit cache's page calls without a GPU: the bounds of a batch that a pool hands out, what is read of a page table, and
+which kernel takes a call."""
+import ctypes
 import os
 import re
 import subprocess
@@ -8,6 +10,7 @@ import pytest
 from oracle import kvq_pages as op
 from paper_2509_21009_amd import build
 from paper_2509_21009_amd import rollpack as rp
+from tests.kvq_page_forms import CALLS, HARD, SCORES
 from tests.test_kvq_cpu import PTR, _refused
 from tests.test_kvq_pages_cpu import _pool
 
@@ -57,3 +60,47 @@ def test_scores_read_no_entry_past_a_context(tmp_path):
     text = open(os.path.join(build.CSRC, "k_kvq_pages.hip")).read()
     text = text[text.index("// ---- scores"):text.index("// ---- picks")]
     assert text.count("kvq_seen_entry(") == 2 and re.findall(r"(?:\bpt|table_of\(bt, b\))\[(.*?)\]", text) == ["entry", "entry"]
+
+
+# ---- which kernel takes a call -------------------------------------------------------
+
+@pytest.fixture(scope="module")
+def forms(tmp_path_factory):
+    so = tmp_path_factory.mktemp("forms") / "forms.so"
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", f"-I{build.CSRC}", os.path.join(ROOT, "tests", "cpp", "kvq_page_forms.cpp"),
+                    "-o", str(so)], check=True)
+    return ctypes.CDLL(str(so))
+
+
+def test_gpu_tests_reach_every_form_of_attention(forms):
+    """Every form that some call has is one of tests/kvq_page_forms.py's, for both head dimensions (and both types, which
+    do not count here); each of these has the form that its name says."""
+    reached = {64: set(), 128: set()}
+    for name, (n_q, n_kv, hd, ctx, rows, n) in {**CALLS, **{"hard " + k: (*v, -(-max(v[3]) // 64)) for k, v in HARD.items()}}.items():
+        f = forms.kvq_picked_form_of(n_q, n_kv, hd, sum(rows or [1] * len(ctx)), max(rows or [1]), n)
+        said = name.split()[-1].split("-")
+        assert f >> 3 == {"eight": 8, "four": 4, "two": 2, "split": 4}[said[0]] and bool(f & 4) == (said[0] == "split"), name
+        assert bool(f & 2) == (n_q // n_kv > 8) and bool(f & 1) == (rows is not None and max(rows) > 1), name
+        reached[hd].add(f)
+    for hd in (64, 128):
+        seen = (ctypes.c_ubyte * 128)()
+        forms.kvq_picked_forms(hd, seen)
+        assert {i for i in range(128) if seen[i]} <= reached[hd]
+        assert len(reached[hd]) == 14
+
+
+def test_gpu_tests_reach_every_form_of_scores(forms):
+    """The same; here the type counts."""
+    for hd in (64, 128):
+        for bf16 in (0, 1):
+            reached = set()
+            for name, (n_q, n_kv, hd_, ctx, rows, room, columns) in SCORES.items():
+                if hd_ == hd:
+                    f = forms.kvq_score_form_of(n_q, n_kv, hd, bf16, room, 1 if rows is None else room, columns)
+                    said = name.split("-")
+                    assert f & 3 == (1 if said[0] == "rows" else 2 if said[1] == "heads" else 0), name
+                    assert f >> 2 == (1 if said[1] == "heads" else int(said[1]) // 16 if said[0] == "walk" or bf16 else 2), name
+                    reached.add(f)
+            seen = (ctypes.c_ubyte * 64)()
+            forms.kvq_score_forms(hd, bf16, seen)
+            assert {i for i in range(64) if seen[i]} <= reached and len(reached) == 4 + bf16
