@@ -748,11 +748,13 @@ rp_status rp_kvq_fit_pages_within(const rp_kvq_pool* pool, const int32_t* length
  * page where rows are.  Errors: RP_ERR_INVALID_ARG, RP_ERR_HIP. */
 rp_status rp_kvq_key_ranges(const rp_kvq_cache* cache, const rp_kvq_batch* batch, void* ranges, void* hip_stream);
 
-/* For each row, KV head and page a score that no key of the page exceeds for any of the KV
+/* For each row, KV head and page a score that bounds q . k of the page's keys for each of the KV
  * head's query heads (a decode step's cheap look at a long context, section 2.2):
  *   score = max_h sum_d max(q[h, d], 0) largest[d] + min(q[h, d], 0) smallest[d],
- * over the G = n_q_heads / n_kv_heads heads, in fp32, and minus infinity for pages past the one of
- * the row's position.  A NaN among them makes it NaN, as does a page id outside the cache; all
+ * over the G = n_q_heads / n_kv_heads heads, and minus infinity for pages past the one of
+ * the row's position.  The sum is formed in fp32, off by up to (2 head_dim + 2) 2^-23 of its terms' magnitudes with queries
+ * in bf16, (6 head_dim + 2) 2^-23 with fp32 ones: a key that takes the range's end in every dimension may exceed the score by that
+ * much, and no key by more.  A NaN among them makes it NaN, as does a page id outside the cache; all
  * scores of a row are NaN where its sequence is out of the batch's bounds.  An infinite q[h, d] makes the head's
  * sums infinite or NaN.
  *   ranges     as rp_kvq_key_ranges has written them; the cache's blocks are not read

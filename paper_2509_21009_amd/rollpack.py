@@ -921,7 +921,7 @@ class KvqCache:
 
     def page_scores(self, batch: KvqBatch, q, ranges, out=None):
         """[n_rows, n_kv_heads, pages] float32: for each page that a row sees, what no q . k with a key of it exceeds, for any
-        of the KV head's query heads; minus infinity past them.  pages: those of the batch's max_context, or of `out`."""
+        of the KV head's query heads, by more than the rounding of a sum in fp32; minus infinity past them.  pages: those of the batch's max_context, or of `out`."""
         if q.dim() != 3:
             raise ValueError("q is [n_rows, n_q_heads, head_dim]")
         n, heads = batch.struct.n_rows, q.shape[1]

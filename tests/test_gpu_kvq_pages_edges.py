@@ -4,10 +4,11 @@ attention over picked ones (oracle/kvq_pages.py).  Tolerances are those of tests
 import numpy as np
 import pytest
 
+from oracle import kvq_pages as op
 from tests import test_gpu_kvq_picked_softmax as softmax
 from tests.gpu_helpers import rp
 from tests.kvq_page_forms import CALLS, HARD, SCORES
-from tests.test_gpu_kvq_pages import DEV, Decode, Pools, Setup, _check_picked, _check_scores, _f64, _ints, _lists
+from tests.test_gpu_kvq_pages import DEV, Decode, Pools, Setup, _check_picked, _check_scores, _f64, _ints, _lists, _score_bar
 
 pytestmark = pytest.mark.gpu
 
@@ -124,6 +125,32 @@ def test_bounds_in_a_graph():
         assert np.array_equal(batch.row_offsets.cpu().numpy(), off)
         assert np.array_equal(positions.cpu().numpy(), pos) and np.array_equal(slots.cpu().numpy(), slot)
         now = np.array(p.plain.contexts)
+
+
+# ---- scores as a bound -----------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n_q,n_kv,hd", [(28, 4, 128), (14, 2, 64), (17, 1, 128), (2, 2, 64)])
+def test_scores_bound_keys_up_to_their_rounding(n_q, n_kv, hd, dtype):
+    """No key's q . k exceeds its page's score by more than the error of the score's sum; a page of one token has that token's."""
+    for rows in ([9, 2, 1, 3], [1, 1, 1, 1]):
+        s = Setup(n_q, n_kv, hd, [500, 65, 1, 129 + 2], rows, dtype, seed=8 + rows[0]).fill()
+        ranges = s.cache.update_ranges(s.batch(s.ctx), s.cache.new_ranges())
+        got, q, at, alone = _f64(s.cache.page_scores(s.batch(), s.q, ranges)), _f64(s.q), 0, 0
+        for b, (c, n) in enumerate(zip(s.ctx, s.rows)):
+            k = s.held()[b][0]
+            _, mag = op.page_scores(q[at:at + n], op.key_ranges(k), np.arange(c - n, c), got.shape[2])
+            bar = _score_bar(None, mag, hd, dtype)
+            dot = np.einsum("nhgd,thd->nhgt", q[at:at + n].reshape(n, n_kv, -1, hd), k).max(2)
+            for i in range(n):
+                for p in range((c - n + i) // 64 + 1):
+                    top = dot[i, :, p * 64:min(c, (p + 1) * 64)].max(-1)  # of all of the page's keys, those behind the row among them
+                    assert (got[at + i, :, p] >= top - bar[i, :, p]).all()
+                    if min(c, (p + 1) * 64) - p * 64 == 1:
+                        assert (np.abs(got[at + i, :, p] - top) <= bar[i, :, p]).all()
+                        alone += 1
+            at += n
+        assert alone >= 2
 
 
 # ---- every form of scores, and of attention over picked pages --------------------------
