@@ -4,6 +4,7 @@ attention over picked ones (oracle/kvq_pages.py).  Tolerances are those of tests
 import numpy as np
 import pytest
 
+from oracle import kvq as okvq
 from oracle import kvq_pages as op
 from tests import test_gpu_kvq_picked_softmax as softmax
 from tests.gpu_helpers import rp
@@ -196,6 +197,40 @@ def test_eight_waves_where_the_softmax_is_hard(form, monkeypatch):
     softmax.test_values_beyond_half_precision_after_a_move(form)
     softmax.test_strong_keys_everywhere(form)
     softmax.test_large_scores_and_values_near_the_end_of_the_range(form)
+
+
+@pytest.mark.parametrize("form", ["four", "four-64", "wide", "wide-64", "two", "eight-128", "eight-wide-128", "eight-wide-64-rows"])
+def test_small_weights_beside_the_keys_of_their_lane(form, monkeypatch):
+    """Strong keys with a value of zero in all pages, as softmax.test_strong_keys_everywhere has them, but only where they share no lane's
+    sum with what the output is made of: 4 of each 16 tokens of a page are a lane's, with up to eight query heads of half a page.  A weight
+    below 2^-14 of fp16's is off by 2^-25 where its lane's N <= 16 keys sum to 2^-9 at least, by N 2^-25 <= 2^-21 < 2^-11 2^-9 of
+    them together; where they do not, each is off by 2^-11 of itself alone.  The sum of a row's weights has the same errors (another
+    2^-11 of the output)."""
+    if form in HARD:
+        monkeypatch.setitem(softmax.FORMS, form, HARD[form])
+    for nats in (12.0, 18.0, 27.0):
+        s = softmax._setup(form, "bf16", 48)
+        narrow = s.n_q // s.n_kv <= 8
+        lane = lambda t: (t % 16) // 4 + 4 * ((t % 64) // 32 if narrow else 0) + 8 * (t // 64)  # noqa: E731
+        strong = lambda t: (t % 16) // 4 == 1  # noqa: E731
+        pos = np.concatenate([np.arange(c) for c in s.ctx])
+        s.v[torch.from_numpy(strong(pos)).to(DEV)] = 0
+        softmax._aim(s, [np.where(strong(np.arange(c)), 32, 0) for c in s.ctx], nats).fill()
+        out, q, at, g = _f64(softmax._attend(s)), _f64(s.q), 0, s.n_q // s.n_kv
+        held = s.held()
+        for b, (c, n) in enumerate(zip(s.ctx, s.rows)):
+            k, v = held[b]
+            ref, mag, top = okvq.attend(q[at:at + n], k, v, np.arange(c - n, c), s.hd ** -0.5)
+            bar = softmax._bar(ref, mag, top, c, s.hd, "bf16", np.abs(v).max()) + 2.0 ** -11 * mag
+            mine = lane(np.arange(c))[:, None] == np.arange(8 * (-(-c // 64)))
+            for h in range(s.n_q):
+                z = np.where(np.arange(c)[None] <= np.arange(c - n, c)[:, None], q[at:at + n, h] @ k[:, h // g].T * s.hd ** -0.5, -np.inf)
+                p = np.exp(z - z.max(1, keepdims=True))
+                p /= p.sum(1, keepdims=True)
+                most = np.where(mine[:, :, None], np.abs(v[:, None, h // g]), 0.0).max(0)  # of a lane's keys
+                bar[:, h] += 2.0 ** -11 * (p @ mine) @ most
+            assert (np.abs(out[at:at + n] - ref) <= bar).all(), (b, c, n, nats)
+            at += n
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
