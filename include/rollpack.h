@@ -679,7 +679,8 @@ rp_status rp_kvq_attend(const rp_kvq_cache* cache, const rp_kvq_batch* batch, in
  *   rp_kvq_pick_pages   the pages to attend to
  *   rp_kvq_attend_picked  attention over them
  * all on the GPU, with nothing for the host to wait for.  Scores, picks and attention take less than 2^22 rows times KV heads
- * at a time.  They launch kernels on hip_stream and return, as the calls above, and
+ * at a time: a larger batch is cut between sequences, each part with the arrays from its first sequence on and offsets that
+ * count from that one's first row.  They launch kernels on hip_stream and return, as the calls above, and
  * with their rules for graphs, devices and host structures. */
 
 /* A pool of pages and what its sequences hold, in caller-owned device memory that the

@@ -128,6 +128,35 @@ def test_bounds_in_a_graph():
         now = np.array(p.plain.contexts)
 
 
+# ---- a batch in parts ------------------------------------------------------------------
+
+@pytest.mark.parametrize("cuts", [[0, 2, 5], [0, 1, 3, 4, 5]])
+def test_a_batch_cut_between_sequences(cuts):
+    """Prompts of a pool, whose scores, picks and attention take more rows than a call may have: parts of the batch give what it gives."""
+    d = Decode(13)
+    before = [30, 0, 64, 129, 0]
+    d.step(_ints(before), 223, *(first := d.tensors(223)))
+    d.k, d.v = ([x[a:b] for a, b in ((0, 30), (30, 30), (30, 94), (94, 223), (223, 223))] for x in (okvq.held(_f64(t)) for t in first[1:]))
+    lengths = [31, 700, 64, 300, 5]
+    rows = np.maximum(np.array(lengths) - np.array(before), 0)
+    q, k, v = d.tensors(int(rows.sum()))
+    batch, _, _ = d.pages.fit(_ints(lengths), len(q))
+    d.cache.append(batch, k, v)
+    d.cache.update_ranges(batch, d.ranges)
+    scores = d.cache.page_scores(batch, q, d.ranges)
+    picks = d.cache.pick_pages(batch, scores, 4)
+    at, out = np.concatenate([[0], np.cumsum(rows)]), torch.full_like(q, 9.0)
+    for a, b in zip(cuts, cuts[1:]):
+        part = slice(int(at[a]), int(at[b]))
+        offsets = batch.row_offsets[a:b + 1] - batch.row_offsets[a]
+        n = part.stop - part.start
+        cut = d.cache.batch(d.pages.contexts[a:b], d.pages.page_table[a:b], row_offsets=offsets, n_rows=n, max_rows=int(rows[a:b].max()))
+        assert torch.equal(d.cache.page_scores(cut, q[part], d.ranges), scores[part])
+        assert torch.equal(d.cache.pick_pages(cut, scores[part], 4), picks[part])
+        d.cache.attend_picked(cut, q[part], picks[part], out=out[part])
+    d.check(before, lengths, q, k, v, out, picks, scores)
+
+
 # ---- scores as a bound -----------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
