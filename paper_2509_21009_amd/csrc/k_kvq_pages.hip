@@ -752,8 +752,8 @@ __device__ __forceinline__ int row_pages(const KvqBatch& bt, int row) {
 
 // A wave has the list of a row and KV head, E of its up to 64 E pages in each lane, loaded while the row is looked up.  The
 // least key that is picked is found bit by bit from the highest: so many keys are at or above a value as a ballot has bits, or (E
-// from 8 on) as the lanes count.  256 lists of up to 71 pages 3.6 us, 2,048 of 219 pages 5.8, 512 of up to 516 10: 32 bits
-// where scores tie, about half of them where not, each a wave's wait for its count.
+// from 8 on) as the lanes count.  256 lists of up to 71 pages 3.6 us, 2,048 of 219 pages 5.8, 512 of up to 516
+// 7.8 to 10.4: 32 bits where scores tie, about half of them where not, each a wave's wait for its count.
 template <int E>
 __global__ __launch_bounds__(256) void k_kvq_pick(KvqPickArgs a) {
   const int lane = threadIdx.x & 63;
