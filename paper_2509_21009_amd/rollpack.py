@@ -752,8 +752,11 @@ class KvqBatch:
 
     def __init__(self, struct: RpKvqBatch, tensors):
         self.struct, self.tensors = struct, tensors
-        self.contexts, self.page_table, self.row_offsets = tensors
         self.device = tensors[0].device
+
+    contexts = property(lambda self: self.tensors[0])
+    page_table = property(lambda self: self.tensors[1])
+    row_offsets = property(lambda self: self.tensors[2])
 
 
 class KvqCache:

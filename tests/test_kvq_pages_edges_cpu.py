@@ -11,7 +11,7 @@ from oracle import kvq_pages as op
 from paper_2509_21009_amd import build
 from paper_2509_21009_amd import rollpack as rp
 from tests.kvq_page_forms import CALLS, HARD, SCORES
-from tests.test_kvq_cpu import PTR, _refused
+from tests.test_kvq_cpu import PTR, _host_cache, _refused
 from tests.test_kvq_pages_cpu import _pool
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -46,6 +46,19 @@ def test_plain_pool_bounds():
         before = list(p.contexts)
         got = p.fit(lengths, n_rows, max_rows, max_context)
         assert got[0] == error and p.contexts == (before if error else lengths) and (not error or got[1].tolist() == [0] * 4)
+
+
+def test_a_batch_keeps_the_arrays_that_it_is_given(lib):
+    """All three, as its makers give them, or those that a structure made elsewhere points to."""
+    torch = pytest.importorskip("torch")
+    c = _host_cache(torch)
+    ctx, table, off = torch.ones(3, dtype=torch.int32), torch.zeros((3, 1), dtype=torch.int32), torch.arange(4, dtype=torch.int32)
+    b = c.batch(ctx, table, row_offsets=off, n_rows=3)
+    assert b.contexts is ctx and b.page_table is table and b.row_offsets is off
+    assert c.batch(ctx, table).row_offsets is None
+    for kept in ((ctx,), (ctx, table)):
+        again = rp.KvqBatch(b.struct, kept)
+        assert again.tensors is kept and again.device == ctx.device and again.contexts is ctx
 
 
 # ---- the page table ------------------------------------------------------------------
